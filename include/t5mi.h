@@ -336,6 +336,74 @@ int t5_encdec_loss_and_grad(const t5_encdec_cfg* cfg, const int32_t* enc_tokens,
                             const t5_encdec_grads* grads, int accumulate, void* workspace,
                             size_t workspace_bytes, void* stream);
 
+/* Operators at the vocabulary ends of a stack (paper Sec. 4 models as plain stacks), for training a model from a
+ * teacher and for callers that build their own ends.
+ *
+ * Token embedding with a scale:  x[t, :] = scale * table[tokens[t], :], rounded once.  tokens: device int32 [n_tokens],
+ * ids clamped into [0, vocab) as in a stack; table [vocab, d_model] and x [n_tokens, d_model] of dtype.
+ * Errors: NULL with n_tokens > 0 -> T5_ERR_NULL; n_tokens < 0, vocab or d_model < 1, scale not finite -> T5_ERR_SHAPE;
+ * n_tokens > 2^24, vocab > 2^22, d_model > 2^16, unknown dtype -> T5_ERR_UNSUPPORTED.  n_tokens == 0 is a no-op. */
+typedef struct {
+  int64_t n_tokens;
+  int32_t vocab, d_model;
+  int32_t dtype; /* T5_F32 or T5_BF16: table, x and dx */
+  float scale;   /* 1 in T5; sqrt(d_model) in models whose table is also their output matrix */
+} t5_embed_cfg;
+int t5_embed_fwd(const t5_embed_cfg* cfg, const int32_t* tokens, const void* table, void* x, void* stream);
+
+/* Its gradient:  dtable[v, :] (+)= scale * sum over { t : tokens[t] = v } of dx[t, :], float32 [vocab, d_model].
+ * Positions are sorted by id and summed in an order that depends on tokens alone: the same bits every time.
+ * accumulate == 0 writes every row (rows of ids that do not occur: zeros); accumulate != 0 adds to the rows of ids that
+ * occur and touches no other.  n_tokens == 0 writes zeros, or nothing.
+ * Errors: as t5_embed_fwd; small workspace -> T5_ERR_WORKSPACE. */
+size_t t5_embed_bwd_workspace_bytes(const t5_embed_cfg* cfg);
+int t5_embed_bwd(const t5_embed_cfg* cfg, const int32_t* tokens, const void* dx, float* dtable, int accumulate,
+                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* The top_k largest logits of each row, descending, equal ones by ascending id: what a teacher hands to
+ * t5_distill_loss_and_grad.  logits: rows of vocab elements of dtype, ld elements apart; values: float32 [rows, top_k]
+ * (the logits themselves, exactly); ids: int32 [rows, top_k].  -0 and +0 are equal; NaN counts as larger than +inf
+ * and comes back as NaN.  Elements between vocab and ld are not read.  rows == 0 is a no-op.
+ * Errors: NULL with rows > 0 -> T5_ERR_NULL; rows < 0, vocab < 2, ld < vocab, top_k < 1 or > vocab -> T5_ERR_SHAPE;
+ * rows > 2^24, vocab > 2^22, ld > 2^32, top_k > 256, unknown dtype -> T5_ERR_UNSUPPORTED; small workspace ->
+ * T5_ERR_WORKSPACE. */
+typedef struct {
+  int64_t rows, ld;
+  int32_t vocab, top_k;
+  int32_t dtype;
+} t5_top_logits_cfg;
+size_t t5_top_logits_workspace_bytes(const t5_top_logits_cfg* cfg);
+int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* values, int32_t* ids, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/* Distillation from a teacher's top logits: loss of a student's logits x, forward and gradient in one call.  Per row,
+ * with the teacher's entries (teacher_logits t_k, teacher_ids id_k), k < top_k, of which those with an id in
+ * [0, vocab) count (give the others -1; their t_k is not used):
+ *   p = softmax_k(t_k / T)        over the entries that count;   log q_v = x_v / T - lse(x / T)
+ *   row = (1 - a) (lse(x) - x[target]) + z_loss lse(x)^2 + a T^2 sum_k p_k (log p_k - log q[id_k])
+ * with T = temperature, a = soft_weight.  An id may occur more than once (its probabilities add up).  A t_k of -inf is
+ * an entry of probability 0; NaN and +inf give NaN.  A row of which no entry is left has no soft term.
+ * targets: device int32 [rows]; rows whose target is outside [0, vocab) carry no loss of any kind and get a zero
+ * gradient, whatever their logits and entries hold (-1 for padding).  targets == NULL (soft_weight 1 only): every row counts.
+ * loss: one float32, the mean over the rows that count (0 if there are none); row_loss: float32 [rows] (nullable);
+ * dlogits: gradient of loss, rows ld elements apart, elements between vocab and ld left alone; it may be logits itself,
+ * or NULL: then the loss alone is computed.  Logits of -inf are allowed (their gradient is that of q = 0; an entry of
+ * positive probability there makes the loss +inf); a row of nothing but -inf gives NaN.  Sums are float32.
+ * Errors: as t5_top_logits; loss NULL, or targets NULL with soft_weight != 1 -> T5_ERR_NULL; temperature <= 0 or not
+ * finite (nor its inverse), soft_weight outside [0, 1], z_loss < 0 or not finite -> T5_ERR_SHAPE.  rows == 0 writes 0. */
+typedef struct {
+  int64_t rows, ld;
+  int32_t vocab, top_k;
+  int32_t dtype;
+  float temperature;
+  float soft_weight;
+  float z_loss;
+} t5_distill_cfg;
+size_t t5_distill_workspace_bytes(const t5_distill_cfg* cfg);
+int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, const int32_t* targets,
+                             const float* teacher_logits, const int32_t* teacher_ids, float* loss, float* row_loss,
+                             void* dlogits, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Adafactor (the optimizer of the T5 models of paper Sec. 4) with factored second moments and
  * update clipping, no momentum, no weight decay, for one [rows, cols] float32 tensor:
  *   beta2 = 1 - step^-decay_pow;  Q = G*G + eps1

@@ -78,6 +78,19 @@ class _EncDecGrads(C.Structure):
                 ("dec_cross", C.POINTER(_CrossGrads)), ("dec_final_scale", C.c_void_p), ("logits_w", C.c_void_p)]
 
 
+class _EmbedCfg(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64), ("vocab", C.c_int32), ("d_model", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class _TopCfg(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("ld", C.c_int64), ("vocab", C.c_int32), ("top_k", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _DistillCfg(C.Structure):
+    _fields_ = _TopCfg._fields_ + [("temperature", C.c_float), ("soft_weight", C.c_float), ("z_loss", C.c_float)]
+
+
 class _AfTensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("v_row", C.c_void_p), ("v_col", C.c_void_p),
                 ("v_full", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("factored", C.c_int32),
@@ -153,6 +166,20 @@ def lib() -> C.CDLL:
     L.adafactor_multi_workspace_bytes.argtypes = [C.POINTER(_AfTensor), i32]
     L.adafactor_step_multi.restype = i32
     L.adafactor_step_multi.argtypes = [C.POINTER(_AfTensor), i32, C.POINTER(_AfCfg), vp, sz, vp]
+    L.t5_embed_fwd.restype = i32
+    L.t5_embed_fwd.argtypes = [C.POINTER(_EmbedCfg), vp, vp, vp, vp]
+    L.t5_embed_bwd_workspace_bytes.restype = sz
+    L.t5_embed_bwd_workspace_bytes.argtypes = [C.POINTER(_EmbedCfg)]
+    L.t5_embed_bwd.restype = i32
+    L.t5_embed_bwd.argtypes = [C.POINTER(_EmbedCfg), vp, vp, vp, i32, vp, sz, vp]
+    L.t5_top_logits_workspace_bytes.restype = sz
+    L.t5_top_logits_workspace_bytes.argtypes = [C.POINTER(_TopCfg)]
+    L.t5_top_logits.restype = i32
+    L.t5_top_logits.argtypes = [C.POINTER(_TopCfg), vp, vp, vp, vp, sz, vp]
+    L.t5_distill_workspace_bytes.restype = sz
+    L.t5_distill_workspace_bytes.argtypes = [C.POINTER(_DistillCfg)]
+    L.t5_distill_loss_and_grad.restype = i32
+    L.t5_distill_loss_and_grad.argtypes = [C.POINTER(_DistillCfg), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.t5_gemm_bf16.restype = i32
     L.t5_gemm_bf16.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, vp]
     L.t5_wgrad_overlap_enable.restype = i32
@@ -666,6 +693,142 @@ def adafactor_step_multi(tensors, *, step, lr, decay_pow=0.8, eps1=1e-30, eps2=1
     rc = lib().adafactor_step_multi(arr, len(tensors), C.byref(cfg), _ptr(workspace), workspace.numel(), _stream())
     if rc:
         raise T5Error(rc, "adafactor_step_multi")
+
+
+def _elem_type(t, name):
+    """T5_F32 or T5_BF16 of a tensor that may have either type."""
+    if t.dtype == torch.bfloat16:
+        return T5_BF16
+    if t.dtype != torch.float32:
+        raise ValueError(f"{name}: need float32 or bfloat16, got {t.dtype}")
+    return T5_F32
+
+
+def _check_on(device, t, dtype, numel, name):
+    _check_tensor(t, dtype, numel, name)
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, other arguments on {device}")
+
+
+def _check_rows(t, name):
+    """Rows of a matrix whose elements are contiguous; (rows, columns, row stride)."""
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name}: need a 2-D cuda tensor with contiguous rows that do not overlap, got {tuple(t.shape)} "
+                         f"with strides {t.stride()} on {t.device}")
+    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _call(fn, what, device, *args):
+    """One library call on the current stream of the tensors' device."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream())
+    else:
+        rc = fn(*args, _stream())
+    if rc:
+        raise T5Error(rc, what)
+
+
+def t5_embed_fwd(tokens, table, scale=1.0, x=None):
+    """x[..., :] = scale * table[tokens[...], :]; tokens int32 of any shape, table [vocab, d_model].  Returns x."""
+    ty = _elem_type(table, "table")
+    vocab, d = table.shape
+    _check_tensor(table, table.dtype, vocab * d, "table")
+    n = tokens.numel()
+    _check_on(table.device, tokens, torch.int32, n, "tokens")
+    if x is None:
+        x = torch.empty(*tokens.shape, d, dtype=table.dtype, device=table.device)
+    else:
+        _check_on(table.device, x, table.dtype, n * d, "x")
+    cfg = _EmbedCfg(n, vocab, d, ty, scale)
+    _call(lib().t5_embed_fwd, "t5_embed_fwd", table.device, C.byref(cfg), tokens.data_ptr(), table.data_ptr(), x.data_ptr())
+    return x
+
+
+def t5_embed_bwd(tokens, dx, vocab, scale=1.0, dtable=None, accumulate=False, workspace=None):
+    """dtable[v, :] (+)= scale * sum of dx[t, :] over tokens[t] == v, float32 [vocab, d_model].  Returns dtable."""
+    ty = _elem_type(dx, "dx")
+    n, d = tokens.numel(), dx.shape[-1]
+    _check_tensor(dx, dx.dtype, n * d, "dx")
+    _check_on(dx.device, tokens, torch.int32, n, "tokens")
+    if dtable is None:
+        dtable = (torch.zeros if accumulate else torch.empty)(vocab, d, dtype=torch.float32, device=dx.device)
+    else:
+        _check_on(dx.device, dtable, torch.float32, vocab * d, "dtable")
+    cfg = _EmbedCfg(n, vocab, d, ty, scale)
+    if workspace is None:
+        workspace = _byte_buffer(lib().t5_embed_bwd_workspace_bytes(C.byref(cfg)), dx.device)
+    else:
+        _check_on(dx.device, workspace, torch.uint8, workspace.numel(), "workspace")
+    _call(lib().t5_embed_bwd, "t5_embed_bwd", dx.device, C.byref(cfg), tokens.data_ptr(), dx.data_ptr(), dtable.data_ptr(),
+          int(bool(accumulate)), workspace.data_ptr(), workspace.numel())
+    return dtable
+
+
+def t5_top_logits(logits, top_k, values=None, ids=None, workspace=None):
+    """(values float32, ids int32), both [rows, top_k]: the largest logits of each row, descending, equal ones by ascending
+    id.  logits [rows, vocab] may be a view of rows with a longer stride."""
+    ty = _elem_type(logits, "logits")
+    rows, vocab, ld = _check_rows(logits, "logits")
+    dev = logits.device
+    if values is None:
+        values = torch.empty(rows, top_k, dtype=torch.float32, device=dev)
+    else:
+        _check_on(dev, values, torch.float32, rows * top_k, "values")
+    if ids is None:
+        ids = torch.empty(rows, top_k, dtype=torch.int32, device=dev)
+    else:
+        _check_on(dev, ids, torch.int32, rows * top_k, "ids")
+    cfg = _TopCfg(rows, ld, vocab, top_k, ty)
+    if workspace is None:
+        workspace = _byte_buffer(lib().t5_top_logits_workspace_bytes(C.byref(cfg)), dev)
+    else:
+        _check_on(dev, workspace, torch.uint8, workspace.numel(), "workspace")
+    _call(lib().t5_top_logits, "t5_top_logits", dev, C.byref(cfg), logits.data_ptr(), values.data_ptr(), ids.data_ptr(),
+          workspace.data_ptr(), workspace.numel())
+    return values, ids
+
+
+def t5_distill_loss_and_grad(logits, targets, teacher_logits, teacher_ids, temperature=1.0, soft_weight=1.0, z_loss=0.0,
+                             want_grads=True, loss=None, row_loss=None, dlogits=None, workspace=None):
+    """Loss of logits [rows, vocab] (rows may have a longer stride) against a teacher's top logits and ids [rows, top_k] and
+    int32 targets [rows] (None: every row counts, soft targets alone).  dlogits may be the logits themselves; by default
+    it is a new tensor of the same strides.  Returns (loss of one float32, row losses float32, dlogits or None)."""
+    ty = _elem_type(logits, "logits")
+    rows, vocab, ld = _check_rows(logits, "logits")
+    dev = logits.device
+    if teacher_ids.dim() != 2:
+        raise ValueError(f"teacher_ids: need [rows, top_k], got {tuple(teacher_ids.shape)}")
+    k = teacher_ids.shape[1]
+    _check_on(dev, teacher_ids, torch.int32, rows * k, "teacher_ids")
+    _check_on(dev, teacher_logits, torch.float32, rows * k, "teacher_logits")
+    if targets is not None:
+        _check_on(dev, targets, torch.int32, rows, "targets")
+    if loss is None:
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+    else:
+        _check_on(dev, loss, torch.float32, 1, "loss")
+    if row_loss is None:
+        row_loss = torch.empty(rows, dtype=torch.float32, device=dev)
+    else:
+        _check_on(dev, row_loss, torch.float32, rows, "row_loss")
+    if not want_grads:
+        dlogits = None
+    elif dlogits is None:
+        dlogits = torch.empty(rows, ld, dtype=logits.dtype, device=dev)[:, :vocab]
+    elif dlogits.device != dev or dlogits.dtype != logits.dtype or _check_rows(dlogits, "dlogits") != (rows, vocab, ld):
+        raise ValueError(f"dlogits: need type, shape and row stride of logits, got {dlogits.dtype} {tuple(dlogits.shape)} "
+                         f"with strides {dlogits.stride()} on {dlogits.device}")
+    cfg = _DistillCfg(rows, ld, vocab, k, ty, temperature, soft_weight, z_loss)
+    if workspace is None:
+        workspace = _byte_buffer(lib().t5_distill_workspace_bytes(C.byref(cfg)), dev)
+    else:
+        _check_on(dev, workspace, torch.uint8, workspace.numel(), "workspace")
+    addr = lambda t: None if t is None else t.data_ptr()
+    _call(lib().t5_distill_loss_and_grad, "t5_distill_loss_and_grad", dev, C.byref(cfg), logits.data_ptr(), addr(targets),
+          teacher_logits.data_ptr(), teacher_ids.data_ptr(), loss.data_ptr(), row_loss.data_ptr(), addr(dlogits),
+          workspace.data_ptr(), workspace.numel())
+    return loss, row_loss, dlogits
 
 
 def t5_gemm_bf16(a: torch.Tensor, b: torch.Tensor, a_kc: bool, b_kc: bool, out: torch.Tensor | None = None):

@@ -275,6 +275,36 @@ hipError_t launch_xent_rows(void* logits, int type, const int32_t* targets, int6
 // *loss_out = sum(loss_rows) / max(*n_valid, 1), fixed summation order.
 hipError_t launch_loss_reduce(const float* loss_rows, int64_t rows, const float* n_valid, float* loss_out,
                               hipStream_t st);
+
+// ------------------------------------------------------------------ vocabulary ends as operators of their own
+// x[t, :] = scale * E[tok[t], :] (ids clamped into [0, vocab))
+hipError_t launch_embed_scaled_fwd(const int32_t* tokens, const void* E, void* x, int type, int64_t n, int d, int vocab,
+                                   float scale, hipStream_t st);
+// dE[v, :] (+)= scale * sum of dx[t, :] over tok[t] == v, positions sorted by id, the same bits every time
+size_t embed_sorted_ws_bytes(int64_t n, int vocab, int d);
+hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int type, float* dE, int64_t n, int d, int vocab,
+                                   float scale, int accumulate, void* ws, hipStream_t st);
+// The K (1..kTopMost) largest logits of each row [V], rows ld elements apart, descending, equal ones by ascending id.
+constexpr int kTopMost = 256;
+size_t top_logits_ws_bytes(int64_t rows, int V, int K, int type);
+hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, int64_t ld, int K, float* values,
+                             int32_t* ids, void* ws, hipStream_t st);
+// Distillation loss of rows [V], ld elements apart (see t5_distill_loss_and_grad).
+struct DistillArgs {
+  const int32_t* targets;  // null: every row counts, soft == 1
+  const float* teacher_logits;   // [rows, K]
+  const int32_t* teacher_ids;    // [rows, K]
+  const float* n_counted;
+  float* row_loss;
+  int64_t ld;
+  int32_t K, V;
+  float tau, inv_tau, soft, z_loss;
+};
+hipError_t launch_distill_count(const int32_t* targets, int64_t rows, int V, float* n_counted, hipStream_t st);
+// Row losses and, with out (the logits themselves, or a buffer of the same row stride), the gradient of the mean.
+hipError_t launch_distill_rows(const DistillArgs& a, const void* logits, void* out, int type, int64_t rows, hipStream_t st);
+hipError_t launch_distill_mean(const float* row_loss, int64_t rows, const float* n_counted, float* loss, hipStream_t st);
+
 // out = (accumulate ? out : 0) + alpha * in (float32);  out = alpha * in (storage type)
 hipError_t launch_axpy_f32(float* out, const float* in, float alpha, int n, int accumulate, hipStream_t st);
 hipError_t launch_scale_vec(void* out, const void* in, float alpha, int n, int type, hipStream_t st);

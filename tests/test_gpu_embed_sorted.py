@@ -1,0 +1,100 @@
+"""Scaled embedding and the gradient of its table by sorted tokens, against the float64 definitions."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import vocab_oracle as VO
+from vocab_util import STORE, U, dev, host, ints
+
+pytestmark = pytest.mark.gpu
+
+
+def _tokens(n, vocab, kind, rng):
+    if kind == "one":        # every position holds the same id
+        return np.full(n, vocab // 2)
+    if kind == "two":        # padding ids in front and behind, half of the positions
+        return np.where(rng.random(n) < 0.5, 0, vocab - 1)
+    if kind == "wild":       # ids outside the vocabulary on both sides
+        return rng.integers(-vocab, 2 * vocab, n)
+    if kind == "runs":       # runs of equal ids of every length from 1 on, in falling order of ids
+        ids = np.repeat(np.arange(vocab), 1 + np.arange(vocab) % 97)[:n]
+        return np.resize(ids, n)[::-1].copy()
+    return (vocab * rng.random(n) ** 3).astype(np.int64)  # skewed
+
+
+CASES = [(1, 1, 1, "skewed"), (1, 2, 8, "one"), (3, 5, 3, "wild"), (64, 256, 64, "skewed"), (65, 257, 72, "two"),
+         (777, 509, 67, "runs"), (2047, 128, 40, "one"), (2048, 300, 512, "wild"), (2049, 65536, 16, "skewed"),
+         (5000, 65537, 24, "skewed"), (9001, 1000, 520, "two"), (9000, 3, 264, "runs"), (20000, 32128, 768, "skewed"),
+         (70001, 4000, 33, "runs"), (600000, 70000, 8, "skewed")]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,d,kind", CASES)
+def test_lookup_and_gradient(n, vocab, d, kind, dtype):
+    import paper_2203_17189_amd as P
+    rng = np.random.default_rng(n + vocab + d)
+    tok = _tokens(n, vocab, kind, rng)
+    scale = float(np.float32(rng.choice([1.0, 0.37, d ** 0.5])))
+    table, dx = dev(rng.standard_normal((vocab, d)), dtype), dev(rng.standard_normal((n, d)), dtype)
+    tt = ints(tok)
+    x = P.t5_embed_fwd(tt, table, scale=scale)
+    want = VO.embed_fwd(tok, host(table), scale)
+    assert x.shape == (n, d) and x.dtype == table.dtype
+    assert np.all(np.abs(host(x) - want) <= (STORE[dtype] + U) * np.abs(want))  # a product and a rounding
+    g = P.t5_embed_bwd(tt, dx, vocab, scale=scale)
+    hdx = host(dx)
+    want, size = VO.embed_bwd(tok, hdx, vocab, scale), VO.embed_bwd(tok, np.abs(hdx), vocab, scale)
+    times = np.bincount(np.clip(tok, 0, vocab - 1), minlength=vocab)[:, None]
+    # float32: a sum of m terms is off by at most (m - 1) u of the sum of their sizes, the scale by one more rounding
+    tol = (times + 1) * U * size
+    assert np.all(np.abs(host(g) - want) <= tol)
+    again = P.t5_embed_bwd(tt, dx, vocab, scale=scale)
+    assert torch.equal(g, again)
+    old = dev(rng.standard_normal((vocab, d)))
+    acc = old.clone()
+    assert P.t5_embed_bwd(tt, dx, vocab, scale=scale, dtable=acc, accumulate=True) is acc
+    assert np.all(np.abs(host(acc) - (host(old) + want)) <= tol + 2 * U * (np.abs(host(old)) + size))
+    untouched = torch.from_numpy(times[:, 0] == 0).cuda()
+    assert torch.equal(acc[untouched], old[untouched])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_are_not_aligned(dtype):
+    import paper_2203_17189_amd as P
+    rng = np.random.default_rng(5)
+    n, vocab, d = 333, 100, 64
+    flat = dev(rng.standard_normal(vocab * d + 1), dtype)
+    table = flat[1:].view(vocab, d)  # contiguous, one element off every boundary
+    tok = rng.integers(0, vocab, n)
+    x = P.t5_embed_fwd(ints(tok), table, scale=2.0)
+    assert torch.equal(x, (table[ints(tok).long()] * 2))
+    dx = dev(rng.standard_normal(n * d + 1), dtype)[1:].view(n, d)
+    buf = torch.full((vocab * d + 2,), 7.0, device="cuda")
+    out = buf[1:-1].view(vocab, d)
+    P.t5_embed_bwd(ints(tok), dx, vocab, dtable=out)
+    assert torch.equal(out, P.t5_embed_bwd(ints(tok), dx.clone(), vocab))
+    assert float(buf[0]) == 7.0 and float(buf[-1]) == 7.0
+
+
+def test_empty_and_shapes():
+    import paper_2203_17189_amd as P
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    table = torch.ones(5, 8, device="cuda")
+    assert P.t5_embed_fwd(none, table).shape == (0, 8)
+    dx = torch.zeros(0, 8, device="cuda")
+    g = torch.full((5, 8), 3.0, device="cuda")
+    P.t5_embed_bwd(none, dx, 5, dtable=g, accumulate=True)
+    assert torch.equal(g, torch.full_like(g, 3.0))
+    P.t5_embed_bwd(none, dx, 5, dtable=g)
+    assert torch.equal(g, torch.zeros_like(g))
+    tok = torch.tensor([[1, 2], [3, 4]], dtype=torch.int32, device="cuda")
+    assert P.t5_embed_fwd(tok, table).shape == (2, 2, 8)
+
+
+def test_infinities_and_nans_stay_in_their_rows():
+    import paper_2203_17189_amd as P
+    tok = np.array([0, 1, 1, 2, 3])
+    dx = np.ones((5, 64))
+    dx[1, 3], dx[3, 5], dx[4, 7] = np.nan, np.inf, -np.inf
+    g = host(P.t5_embed_bwd(ints(tok), dev(dx), 6))
+    assert np.array_equal(g, VO.embed_bwd(tok, dx, 6), equal_nan=True)

@@ -1,0 +1,70 @@
+"""Top logits of each row: values and ids are exactly those of a stable descending sort."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import vocab_oracle as VO
+from vocab_util import dev, host, rows_with_gap
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(x, k, values, ids):
+    v, i = VO.top_logits(host(x), k)
+    assert ids.dtype == torch.int32 and values.dtype == torch.float32
+    assert np.array_equal(ids.cpu().numpy(), i)
+    assert np.array_equal(host(values), v, equal_nan=True)
+
+
+def _rows(rows, vocab, kind, rng):
+    if kind == "equal":      # nothing but ties
+        return np.full((rows, vocab), 1.5)
+    if kind == "coarse":     # a handful of values
+        return np.round(rng.standard_normal((rows, vocab)))
+    if kind == "rising":     # the largest side by side, at the end
+        return np.tile(np.arange(vocab) / 64.0, (rows, 1))
+    if kind == "falling":
+        return np.tile(-np.arange(vocab) / 64.0, (rows, 1))
+    if kind == "stripes":    # the largest all belong to the pieces of a few threads
+        x = rng.standard_normal((rows, vocab))
+        return np.where(np.arange(vocab) // 8 % 256 < 3, 50 + x, x)
+    if kind == "masked":     # all but a few are -inf; some rows have fewer finite values than are asked for
+        x = rng.standard_normal((rows, vocab))
+        x[rng.random((rows, vocab)) < 0.9] = -np.inf
+        x[0, 1:] = -np.inf
+        return x
+    if kind == "odd":        # every special value
+        x = rng.standard_normal((rows, vocab))
+        for val in (np.nan, np.inf, -np.inf, 0.0, -0.0, np.finfo(np.float32).min):
+            x[rng.random((rows, vocab)) < 0.1] = val
+        return x
+    return rng.standard_normal((rows, vocab)) * 3
+
+
+CASES = [(1, 2, 1), (3, 2, 2), (5, 17, 17), (2, 255, 100), (2, 256, 256), (3, 300, 256), (4, 1000, 8), (2, 2047, 64),
+         (3, 2048, 256), (2, 2049, 33), (5, 5000, 1), (40, 32128, 64), (2, 32128, 256), (1, 100003, 100), (3, 131072, 16),
+         (300, 509, 12)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["random", "equal", "coarse", "rising", "falling", "stripes", "masked", "odd"])
+@pytest.mark.parametrize("rows,vocab,k", CASES)
+def test_top(rows, vocab, k, kind, dtype):
+    import paper_2203_17189_amd as P
+    x = dev(_rows(rows, vocab, kind, np.random.default_rng(vocab + k)), dtype)
+    _check(x, k, *P.t5_top_logits(x, k))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,ld,shift", [(2048, 2056, 0), (2048, 2056, 8), (4000, 4001, 0), (4000, 4100, 3), (333, 1000, 1)])
+def test_rows_with_a_longer_stride(vocab, ld, shift, dtype):
+    import paper_2203_17189_amd as P
+    rng = np.random.default_rng(ld)
+    _, x = rows_with_gap(rng.standard_normal((9, vocab)), dtype, ld, shift, fill=float("inf"))
+    _check(x, 32, *P.t5_top_logits(x, 32))
+
+
+def test_empty():
+    import paper_2203_17189_amd as P
+    v, i = P.t5_top_logits(torch.zeros(0, 10, device="cuda"), 3)
+    assert v.shape == i.shape == (0, 3)
