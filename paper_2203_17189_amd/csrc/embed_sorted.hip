@@ -53,37 +53,40 @@ __global__ __launch_bounds__(256) void embed_scaled_fwd_kernel(const int32_t* __
   }
 }
 
-// Clears out[0, count) with this launch's workgroups from `first` on; the others sort meanwhile.
+// Clears out[0, count) with this launch's workgroups from `first` on, kFillEach floats each; the others sort meanwhile.
+constexpr int kFillEach = 1024 * 16;
 struct Fill {
-  float* out;     // null: nothing to clear
+  float* out;
   int64_t count;
-  int32_t first;  // workgroup of the launch at which the clearing ones start
+  int32_t first;
 };
 __device__ __forceinline__ void fill_zero(const Fill& f) {
-  const int64_t nb = gridDim.x - f.first, b = blockIdx.x - f.first;
-  const int64_t at = ((intptr_t)f.out >> 2) & 3, lead = at ? 4 - at : 0;  // elements in front of a 16-byte boundary
-  const int64_t pre = lead < f.count ? lead : f.count, quads = (f.count - pre) / 4;
+  const int b = blockIdx.x - f.first;
+  const int at = ((intptr_t)f.out >> 2) & 3;
+  const int64_t pre = at && f.count > 4 - at ? 4 - at : at ? f.count : 0;  // elements in front of a 16-byte boundary
+  const int64_t quads = (f.count - pre) / 4;
   f32x4* q = reinterpret_cast<f32x4*>(f.out + pre);
-  const int64_t each = (quads + nb - 1) / nb, q1 = (b + 1) * each < quads ? (b + 1) * each : quads;
-  for (int64_t i = b * each + threadIdx.x; i < q1; i += blockDim.x) st_stream(q + i, f32x4{0.f, 0.f, 0.f, 0.f});
-  if (b == 0 && threadIdx.x < pre) f.out[threadIdx.x] = 0.f;
+  const int64_t i0 = (int64_t)b * (kFillEach / 4) + threadIdx.x;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (i0 + j * 1024 < quads) q[i0 + j * 1024] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int64_t tail = pre + 4 * quads;
-  if (b == nb - 1 && threadIdx.x < f.count - tail) f.out[tail + threadIdx.x] = 0.f;
+  if (b == 0 && threadIdx.x < pre) f.out[threadIdx.x] = 0.f;
+  if (b == 0 && threadIdx.x < f.count - tail) f.out[tail + threadIdx.x] = 0.f;
 }
 
 // ------------------------------------------------------------------------------------------------
-// Stable sort of (id, position) by id: least significant digit first, `bits` bits a pass, two launches a pass.
-// Workgroup b owns positions [b * chunk, (b + 1) * chunk) of the pass's input.
+// Stable sort of (id, position) by id: least significant digit first, `bits` (at most 8) bits a pass, two launches a
+// pass.  Workgroup b owns keys [b * chunk, (b + 1) * chunk) of the pass's input, 1024 at a time.
 // ------------------------------------------------------------------------------------------------
-constexpr int kSortItems = 8;                 // keys of a thread at a time
-constexpr int kSortTile = 256 * kSortItems;   // keys of a workgroup at a time
-constexpr int kSortBlocks = 256;              // at most; a workgroup then loops over its chunk
+constexpr int kSortTile = 1024;
+constexpr int kSortBlocks = 256;  // at most; a workgroup then loops over its chunk
 
 struct SortPass {
   const int32_t* tok;  // first pass: ids as given; else null
   const u32x2* in;     // (id, position), sorted by the lower digits
   u32x2* out;
-  uint32_t* hist;      // [blocks][1 << bits]
+  uint32_t* hist;      // [blocks][256]
   int32_t n, vocab, chunk, blocks, shift, bits;
   Fill fill;
 };
@@ -93,195 +96,145 @@ __device__ __forceinline__ u32x2 sort_load(const SortPass& p, int i) {
   return p.in[i];
 }
 
-__global__ __launch_bounds__(256) void embed_sort_count_kernel(SortPass p) {
-  extern __shared__ uint32_t lds[];
+__global__ __launch_bounds__(1024) void embed_sort_count_kernel(SortPass p) {
+  __shared__ uint32_t cnt[256];
   if ((int)blockIdx.x >= p.blocks) {
     fill_zero(p.fill);
     return;
   }
-  const int bins = 1 << p.bits;
-  for (int i = threadIdx.x; i < bins; i += 256) lds[i] = 0;
+  const int tid = threadIdx.x;
+  if (tid < 256) cnt[tid] = 0;
   __syncthreads();
   const int i0 = blockIdx.x * p.chunk, i1 = min(i0 + p.chunk, p.n);
-  for (int i = i0 + (int)threadIdx.x; i < i1; i += 256)
-    atomicAdd(&lds[(sort_load(p, i).x >> p.shift) & (bins - 1)], 1u);  // whole numbers: the order does not matter
+  for (int i = i0 + tid; i < i1; i += 1024)
+    atomicAdd(&cnt[(sort_load(p, i).x >> p.shift) & ((1u << p.bits) - 1)], 1u);  // whole numbers: the order does not matter
   __syncthreads();
-  for (int i = threadIdx.x; i < bins; i += 256) p.hist[(size_t)blockIdx.x * bins + i] = lds[i];
+  if (tid < 256) p.hist[blockIdx.x * 256 + tid] = cnt[tid];
 }
 
 // base[d]: first place of digit d's keys of this workgroup = keys of smaller digits + keys of digit d of earlier
-// workgroups.  Then tile by tile: each wavefront ranks 512 consecutive keys among equal digits (64 at a time, with
-// ballots), the four wavefronts' counts are joined, and every key goes to its place.
-__global__ __launch_bounds__(256) void embed_sort_place_kernel(SortPass p) {
-  extern __shared__ uint32_t lds[];
+// workgroups.  Then 1024 keys at a time: each wavefront ranks its 64 among equal digits with ballots, the sixteen
+// wavefronts' counts are joined, and every key goes to its place.
+__global__ __launch_bounds__(1024) void embed_sort_place_kernel(SortPass p) {
+  __shared__ uint32_t cnt[16][256], base[256], all[4][256], before[4][256], wsum[4];
   if ((int)blockIdx.x >= p.blocks) {
     fill_zero(p.fill);
     return;
   }
-  const int bins = 1 << p.bits, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  uint32_t* base = lds;                 // [bins]
-  uint32_t* cnt = lds + bins + w * bins;  // this wavefront's, of [4][bins]
-  __shared__ uint32_t wsum[4];
-  // totals per digit, and the part of earlier workgroups
-  uint32_t carry = 0;
-  for (int d0 = 0; d0 < bins; d0 += 256) {
-    const int d = d0 + tid;
-    uint32_t total = 0, before = 0;
-    if (d < bins)
-      for (int b = 0; b < p.blocks; ++b) {
-        const uint32_t c = p.hist[(size_t)b * bins + d];
-        total += c;
-        before += b < (int)blockIdx.x ? c : 0;
-      }
-    uint32_t incl = total;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, d4 = tid & 255, part = tid >> 8;
+  const uint32_t mask = (1u << p.bits) - 1;
+  const int i0 = blockIdx.x * p.chunk, i1 = min(i0 + p.chunk, p.n);
+  u32x2 key = i0 + tid < i1 ? sort_load(p, i0 + tid) : u32x2{0, 0};
+  uint32_t total = 0, mine = 0;
+  for (int b = part; b < p.blocks; b += 32) {  // a quarter of the workgroups' counts each, eight in flight
+    uint32_t c[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[j] = b + 4 * j < p.blocks ? p.hist[(b + 4 * j) * 256 + d4] : 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      total += c[j];
+      mine += b + 4 * j < (int)blockIdx.x ? c[j] : 0;
+    }
+  }
+  all[part][d4] = total;
+  before[part][d4] = mine;
+  __syncthreads();
+  uint32_t incl = 0;
+  if (tid < 256) {
+    mine = before[0][tid] + before[1][tid] + before[2][tid] + before[3][tid];
+    incl = total = all[0][tid] + all[1][tid] + all[2][tid] + all[3][tid];
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
       const uint32_t o = __shfl_up(incl, off, 64);
       incl += lane >= off ? o : 0;
     }
     if (lane == 63) wsum[w] = incl;
-    __syncthreads();
-    uint32_t pre = carry, all = 0;
-    for (int q = 0; q < 4; ++q) {
-      pre += q < w ? wsum[q] : 0;
-      all += wsum[q];
-    }
-    if (d < bins) base[d] = pre + incl - total + before;
-    carry += all;
-    __syncthreads();
   }
-  const int i0 = blockIdx.x * p.chunk, i1 = min(i0 + p.chunk, p.n);
+  __syncthreads();
+  if (tid < 256) {
+    uint32_t at = incl - total + mine;
+    for (int q = 0; q < w; ++q) at += wsum[q];
+    base[tid] = at;
+  }
   for (int t0 = i0; t0 < i1; t0 += kSortTile) {
-    for (int i = lane; i < bins; i += 64) cnt[i] = 0;
-    u32x2 key[kSortItems];
-    uint32_t rank[kSortItems];
-    const int k0 = t0 + w * 64 * kSortItems + lane;
+    const bool on = t0 + tid < i1;
+    if (t0 > i0) key = on ? sort_load(p, t0 + tid) : u32x2{0, 0};
+    const uint32_t d = (key.x >> p.shift) & mask;
+    uint64_t same = __ballot(on);
+    for (int b = 0; b < p.bits; ++b) {
+      const uint64_t m = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? m : ~m;
+    }
+    const uint32_t below = (uint32_t)__popcll(same & ((1ull << lane) - 1));
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r) key[r] = k0 + r * 64 < i1 ? sort_load(p, k0 + r * 64) : u32x2{0, 0};
+    for (int i = 0; i < 4; ++i) cnt[w][i * 64 + lane] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (on && below == 0) cnt[w][d] = (uint32_t)__popcll(same);
+    __syncthreads();
+    if (tid < 256) {
+      uint32_t at = base[tid];
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r) {
-      const bool on = k0 + r * 64 < i1;
-      const uint32_t d = (key[r].x >> p.shift) & (bins - 1);
-      uint64_t same = __ballot(on);
-      for (int b = 0; b < p.bits; ++b) {
-        const uint64_t m = __ballot((d >> b) & 1);
-        same &= (d >> b) & 1 ? m : ~m;
+      for (int q = 0; q < 16; ++q) {
+        const uint32_t c = cnt[q][tid];
+        cnt[q][tid] = at;
+        at += c;
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the counts of the round before
-      if (on) {
-        const uint32_t old = cnt[d], below = (uint32_t)__popcll(same & ((1ull << lane) - 1));
-        rank[r] = old + below;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (below == 0) cnt[d] = old + (uint32_t)__popcll(same);
-      }
+      base[tid] = at;
     }
     __syncthreads();
-    for (int d = tid; d < bins; d += 256) {
-      uint32_t s = base[d];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t c = lds[bins + q * bins + d];
-        lds[bins + q * bins + d] = s;
-        s += c;
-      }
-      base[d] = s;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kSortItems; ++r)
-      if (k0 + r * 64 < i1) p.out[cnt[(key[r].x >> p.shift) & (bins - 1)] + rank[r]] = key[r];
+    if (on) p.out[cnt[w][d] + below] = key;
     __syncthreads();
   }
 }
 
 // ------------------------------------------------------------------------------------------------
-// The same sort by one workgroup, for n <= kOneSort and id and position in 32 bits together: keys in registers, one
-// exchange through LDS a pass.  The LDS of the counts is that of the exchange (64 KB in all).
+// The same order in one launch, for n <= kRankSort and id and position in 32 bits together: the place of a key is the
+// number of keys below it.  A workgroup places I keys, each held by 64 / I lanes of every wavefront; each of the sixteen
+// wavefronts compares them with a sixteenth of all keys, four keys a lane and LDS read, two instructions a comparison.
+// n^2 comparisons in all, bound by those reads: I is chosen for one workgroup per compute unit.
 // ------------------------------------------------------------------------------------------------
-constexpr int kOneRounds = 16, kOneSort = 1024 * kOneRounds;
+constexpr int kRankSort = 16384;
 
-__global__ __launch_bounds__(1024) void embed_sort_one_kernel(const int32_t* __restrict__ tok, u32x2* __restrict__ out, int n,
-                                                              int vocab, int pos_bits, int passes, int bits, Fill fill) {
-  __shared__ uint32_t lds[kOneSort];
+template <int I>
+__global__ __launch_bounds__(1024) void embed_sort_rank_kernel(const int32_t* __restrict__ tok, u32x2* __restrict__ out, int n,
+                                                               int vocab, int pos_bits, Fill fill) {
+  constexpr int G = 64 / I;
+  __shared__ uint32_t part[16][64];
+  __shared__ u32x4 keys[16][64];
   if ((int)blockIdx.x >= fill.first) {
     fill_zero(fill);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int rounds = (n + 1023) / 1024, k0 = w * 64 * rounds + lane;  // wavefront w: 64 * rounds consecutive keys
-  const uint32_t bins = 1u << bits;                                   // at most 256
-  uint32_t* cnt = lds + w * 256;
-  uint32_t* wsum = lds + 16 * 256;
-  uint32_t key[kOneRounds], place[kOneRounds];
+  auto key_at = [&](int i, int end) { return i < end ? clamp_id(tok[i], vocab) << pos_bits | (uint32_t)i : 0xFFFFFFFFu; };
+  const int i = blockIdx.x * I + lane % I;
+  const uint32_t mine = key_at(i, n);
+  const int each = (n + 15) / 16, j0 = w * each, j1 = min(j0 + each, n);
+  uint32_t below = 0;
+  for (int j = j0; j < j1; j += 256) {
+    u32x4 k;
 #pragma unroll
-  for (int r = 0; r < kOneRounds; ++r) {
-    const int i = k0 + r * 64;
-    key[r] = r < rounds && i < n ? clamp_id(tok[i], vocab) << pos_bits | (uint32_t)i : 0;
+    for (int q = 0; q < 4; ++q) k[q] = key_at(j + 4 * lane + q, j1);  // (what is beyond the end is below no key)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    keys[w][lane] = k;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int m = (min(256, j1 - j) + 4 * G - 1) / (4 * G);  // lanes' keys for each of the G groups of lanes
+    const u32x4* src = keys[w] + (lane / I) * m;
+#pragma unroll 8
+    for (int q = 0; q < m; ++q) {
+      const u32x4 o = src[q];
+      below += (o[0] < mine) + (o[1] < mine) + (o[2] < mine) + (o[3] < mine);
+    }
   }
-  for (int q = 0; q < passes; ++q) {
-    const int shift = pos_bits + q * bits;
-    for (int i = lane; i < 256; i += 64) cnt[i] = 0;
+  part[w][lane] = below;
+  __syncthreads();
+  if (tid >= I || i >= n) return;
+  below = 0;
 #pragma unroll
-    for (int r = 0; r < kOneRounds; ++r) {
-      if (r < rounds) {
-        const bool on = k0 + r * 64 < n;
-        const uint32_t d = (key[r] >> shift) & (bins - 1);
-        uint64_t same = __ballot(on);
-        for (int b = 0; b < bits; ++b) {
-          const uint64_t m = __ballot((d >> b) & 1);
-          same &= (d >> b) & 1 ? m : ~m;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the counts of the round before
-        if (on) {
-          const uint32_t old = cnt[d], below = (uint32_t)__popcll(same & ((1ull << lane) - 1));
-          place[r] = old + below;
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          if (below == 0) cnt[d] = old + (uint32_t)__popcll(same);
-        }
-      }
-    }
-    __syncthreads();
-    // places of digit d: after all smaller digits, then wavefront by wavefront
-    uint32_t total = 0, incl = 0;
-    if (tid < 256) {
+  for (int q = 0; q < 16; ++q)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) total += lds[i * 256 + tid];
-      incl = total;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t o = __shfl_up(incl, off, 64);
-        incl += lane >= off ? o : 0;
-      }
-      if (lane == 63) wsum[w] = incl;
-    }
-    __syncthreads();
-    if (tid < 256) {
-      uint32_t p = incl - total;
-      for (int i = 0; i < w; ++i) p += wsum[i];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t c = lds[i * 256 + tid];
-        lds[i * 256 + tid] = p;
-        p += c;
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kOneRounds; ++r)
-      if (r < rounds && k0 + r * 64 < n) place[r] += cnt[(key[r] >> shift) & (bins - 1)];
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kOneRounds; ++r)
-      if (r < rounds && k0 + r * 64 < n) lds[place[r]] = key[r];
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kOneRounds; ++r)
-      if (r < rounds && k0 + r * 64 < n) key[r] = lds[k0 + r * 64];
-    __syncthreads();
-  }
-#pragma unroll
-  for (int r = 0; r < kOneRounds; ++r)
-    if (r < rounds && k0 + r * 64 < n) out[k0 + r * 64] = u32x2{key[r] >> pos_bits, key[r] & ((1u << pos_bits) - 1)};
+    for (int g = 0; g < G; ++g) below += part[q][g * I + tid];
+  out[below] = u32x2{mine >> pos_bits, mine & ((1u << pos_bits) - 1)};
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -352,121 +305,184 @@ __global__ __launch_bounds__(256) void embed_tile_sum_kernel(SumArgs a) {
   flush((first && from_before) || (t1 < a.n && a.sorted[t1].x == cur));
 }
 
-// First index i in [lo, n) with sorted id > v, by one wavefront: 64 probes a step.
-__device__ __forceinline__ int wave_upper_bound(const u32x2* __restrict__ sorted, int lo, int n, uint32_t v) {
-  const int lane = threadIdx.x & 63;
-  int hi = n;  // the answer is in [lo, hi]
-  while (hi > lo) {
-    const int step = (hi - lo + 63) / 64;
-    const int i = lo + (lane + 1) * step - 1;  // last index of this lane's part
-    const int parts = __popcll(__ballot(i < hi && sorted[i < hi ? i : hi - 1].x <= v));  // whole parts below the answer
-    const int nlo = lo + parts * step;
-    hi = min(hi, nlo + step - 1);
-    lo = min(nlo, hi);
-  }
-  return lo;
-}
-
-// A workgroup per tile and 256 columns: if a run begins in the tile and reaches over its end, adds the run's parts, in
-// order within each wavefront's share of them, and writes the row.
-__global__ __launch_bounds__(256) void embed_join_kernel(SumArgs a) {
-  const int t = blockIdx.x, t0 = t * a.tile, t1 = min(t0 + a.tile, a.n);
-  const uint32_t last = a.sorted[t1 - 1].x;
-  if (t1 >= a.n || a.sorted[t1].x != last) return;
-  const bool whole = a.sorted[t0].x == last;
-  if (whole && t0 > 0 && a.sorted[t0 - 1].x == last) return;  // begins earlier
-  __shared__ float red[4][256];
+// A workgroup per tile and 64 * VEC columns: if a run begins in the tile and reaches over its end, adds the run's parts,
+// each of the eight wavefronts a share of them in order, and writes the row.
+template <int VEC>
+__global__ __launch_bounds__(512) void embed_join_kernel(SumArgs a) {
+  typedef typename Piece<float, VEC>::type F;
+  __shared__ F red[8][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int parts = (wave_upper_bound(a.sorted, t1, a.n, last) - 1) / a.tile - t + 1;  // part 0 here, part i in tile t + i
-  const int each = (parts + 3) / 4, p0 = w * each, p1 = min(p0 + each, parts);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  const int c0 = blockIdx.y * 256 + lane;
-  for (int p = p0; p < p1; p += 4) {
-    float v[4][4];
+  const int t = blockIdx.x, t0 = t * a.tile, t1 = min(t0 + a.tile, a.n);
+  auto id_at = [&](int64_t i) { return a.sorted[i < a.n ? i : a.n - 1].x; };
+  // (all of these loads are in flight together)
+  const uint32_t last = id_at(t1 - 1), next = id_at(t1), head = id_at(t0), prev = id_at(t0 > 0 ? t0 - 1 : 0);
+  uint32_t begin = id_at((int64_t)t1 + (int64_t)lane * a.tile);  // of tile t + 1 + lane
+  if (t1 >= a.n || next != last) return;
+  const bool whole = head == last;
+  if (whole && t0 > 0 && prev == last) return;  // the run begins earlier
+  // parts of the run: part 0 here, part i in tile t + i for as long as tiles begin with its id
+  int parts = 1;
+  for (int64_t first = t1;;) {
+    const uint64_t same = __ballot(first + (int64_t)lane * a.tile < a.n && begin == last);
+    parts += __popcll(same);
+    if (~same) break;
+    first += 64 * (int64_t)a.tile;
+    begin = id_at(first + (int64_t)lane * a.tile);
+  }
+  const int each = (parts + 7) / 8, p0 = w * each, p1 = min(p0 + each, parts);
+  const int c = (blockIdx.y * 64 + lane) * VEC;
+  const bool on = c < a.d;
+  const float* src = a.partial + (size_t)t * 2 * a.d + (on ? c : 0);
+  F s{};
+  for (int p = p0; p < p1; p += 8) {
+    F v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
       const int q = min(p + j, p1 - 1);
-      const float* src = a.partial + ((size_t)(t + q) * 2 + (q == 0 && !whole ? 1 : 0)) * a.d;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[j][k] = c0 + k * 64 < a.d ? src[c0 + k * 64] : 0.f;
+      v[j] = *reinterpret_cast<const F*>(src + (size_t)(2 * q + (q == 0 && !whole ? 1 : 0)) * a.d);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) s[k] += p + j < p1 ? v[j][k] : 0.f;
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) red[w][k * 64 + lane] = s[k];
-  __syncthreads();
-  const int c = blockIdx.y * 256 + threadIdx.x;
-  if (c >= a.d) return;
-  const float v = (red[0][threadIdx.x] + red[1][threadIdx.x]) + (red[2][threadIdx.x] + red[3][threadIdx.x]);
-  float* o = a.dE + (size_t)last * a.d + c;
-  *o = a.accumulate ? *o + v : v;
-}
-
-// ------------------------------------------------------------------------------------------------
-// Few tokens and a small table: one launch.  A workgroup owns kScanRows rows of the table and 64 columns, lists the
-// positions of its rows in order, shares the list among its 16 wavefronts (each with sums of its own in LDS), and adds
-// these up.
-// ------------------------------------------------------------------------------------------------
-constexpr int kScanRows = 8, kScanTokens = 4096;
-
-template <typename T>
-__global__ __launch_bounds__(1024) void embed_scan_sum_kernel(const int32_t* __restrict__ tok, const T* __restrict__ dx,
-                                                              float* __restrict__ dE, int n, int d, int vocab, float scale,
-                                                              int accumulate) {
-  __shared__ uint32_t list[kScanTokens];  // row << 16 | position
-  __shared__ float acc[16][kScanRows][64];
-  __shared__ uint32_t wcnt[16], seen[kScanRows];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const uint32_t v0 = blockIdx.x * kScanRows;
-  const int c = blockIdx.y * 64 + lane;
-  if (tid < kScanRows) seen[tid] = 0;
-#pragma unroll
-  for (int r = 0; r < kScanRows; ++r) acc[w][r][lane] = 0.f;
-  int found = 0;
-  for (int b = 0; b < n; b += 1024) {
-    const int i = b + tid;
-    const uint32_t r = i < n ? clamp_id(tok[i], vocab) - v0 : kScanRows;
-    const uint64_t hit = __ballot(r < (uint32_t)kScanRows);
-    if (lane == 0) wcnt[w] = (uint32_t)__popcll(hit);
-    __syncthreads();
-    int at = found;
-#pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      at += q < w ? wcnt[q] : 0;
-      found += wcnt[q];
-    }
-    if (r < (uint32_t)kScanRows) {
-      list[at + __popcll(hit & ((1ull << lane) - 1))] = r << 16 | (uint32_t)i;
-      seen[r] = 1;
-    }
-    __syncthreads();
-  }
-  const int each = (found + 15) / 16, l0 = w * each, l1 = min(l0 + each, found);
-  for (int l = l0; l < l1; l += 8) {
-    uint32_t e[8];
-    T v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = list[min(l + j, l1 - 1)];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = dx[(size_t)(e[j] & 0xFFFFu) * d + (c < d ? c : 0)];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (l + j < l1) acc[w][e[j] >> 16][lane] += to_f32(v[j]);
+      if (p + j < p1) s += v[j];
+  }
+  red[w][lane] = s;
+  __syncthreads();
+  if (w != 0 || !on) return;
+  for (int q = 1; q < 8 && q * each < parts; ++q) s += red[q][lane];
+  F* o = reinterpret_cast<F*>(a.dE + (size_t)last * a.d + c);
+  *o = a.accumulate ? *o + s : s;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Few tokens: one launch and no sort.  A wavefront per position looks for its id among all ids, held in LDS; if the
+// position is the first of its id it sums the rows of all of them in order.  Ids that occur more than kOwnerAlone times
+// are left to the whole workgroup, which shares their list out.  Behind these, workgroups that clear `zero_rows` rows of
+// the table each, all but those whose ids they find.
+// ------------------------------------------------------------------------------------------------
+constexpr int kOwnerTokens = 2048, kOwnerAlone = 16, kZeroRows = 512;
+
+struct OwnerArgs {
+  const int32_t* tok;
+  const void* dx;
+  float* dE;
+  int32_t n, d, vocab, zero_rows, accumulate, sum_blocks;
+  float scale;
+};
+
+// Sum over list[l0, l1) of the rows' VEC columns at dx, eight in flight.
+template <typename T, int VEC, typename F>
+__device__ __forceinline__ F sum_listed(const T* dx, int d, const uint16_t* list, int l0, int l1) {
+  typedef typename Piece<T, VEC>::type P;
+  F acc{};
+  for (int l = l0; l < l1; l += 8) {
+    P x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const P*>(dx + (size_t)list[min(l + j, l1 - 1)] * d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool in = l + j < l1;
+      if constexpr (VEC == 1) {
+        acc += in ? to_f32(x[j]) : 0.f;
+      } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) acc[k] += in ? to_f32(x[j][k]) : 0.f;
+      }
+    }
+  }
+  return acc;
+}
+
+template <typename T, int VEC>
+__global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
+  typedef typename Piece<float, VEC>::type F;
+  __shared__ uint32_t ids[kOwnerTokens];
+  __shared__ uint16_t list[kOwnerTokens], few[8][kOwnerAlone];
+  __shared__ F red[8][64];
+  __shared__ uint32_t many[8], n_many;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint64_t lower = (1ull << lane) - 1;
+  uint32_t id[kOwnerTokens / 512];
+#pragma unroll
+  for (int k = 0; k < kOwnerTokens / 512; ++k) id[k] = k * 512 + tid < a.n ? clamp_id(a.tok[k * 512 + tid], a.vocab) : ~0u;
+  if ((int)blockIdx.x >= a.sum_blocks) {
+    __shared__ uint8_t seen[kZeroRows];
+    const uint32_t v0 = (uint32_t)(blockIdx.x - a.sum_blocks) * a.zero_rows;
+    seen[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kOwnerTokens / 512; ++k)
+      if (id[k] - v0 < (uint32_t)a.zero_rows) seen[id[k] - v0] = 1;
+    __syncthreads();
+    for (int r = w; r < a.zero_rows && v0 + r < (uint32_t)a.vocab; r += 8) {
+      if (seen[r]) continue;
+      float* o = a.dE + (size_t)(v0 + r) * a.d;
+      for (int c = lane * VEC; c < a.d; c += 64 * VEC) *reinterpret_cast<F*>(o + c) = F{};
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kOwnerTokens / 512; ++k) ids[k * 512 + tid] = id[k];
+  if (tid == 0) n_many = 0;
+  __syncthreads();
+  auto put = [&](uint32_t v, int c, F s) {
+    F* o = reinterpret_cast<F*>(a.dE + (size_t)v * a.d + c);
+    *o = a.accumulate ? *o + s * a.scale : s * a.scale;
+  };
+  const int own = blockIdx.x * 8 + w;
+  if (own < a.n) {
+    const uint32_t v = ids[own];
+    bool first = true;
+    int m = 0;
+    for (int k = 0; k < a.n && first; k += 64) {
+      const uint64_t hit = __ballot(ids[k + lane] == v);  // (places behind the last id hold none)
+      if (k <= own) first = !(own - k < 64 ? hit & ((1ull << (own - k)) - 1) : hit);
+      const int at = m + __popcll(hit & lower);
+      if ((hit >> lane & 1) && at < kOwnerAlone) few[w][at] = (uint16_t)(k + lane);
+      m += __popcll(hit);
+    }
+    if (first && m > kOwnerAlone) {
+      if (lane == 0) many[atomicAdd(&n_many, 1u)] = v;
+    } else if (first) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      for (int c = lane * VEC; c < a.d; c += 64 * VEC) put(v, c, sum_listed<T, VEC, F>((const T*)a.dx + c, a.d, few[w], 0, m));
+    }
   }
   __syncthreads();
-  if (tid >= kScanRows * 64 || c >= d || v0 + w >= (uint32_t)vocab || (accumulate && !seen[w])) return;
-  float s = 0.f;
+  for (uint32_t h = 0; h < n_many; ++h) {
+    const uint32_t v = many[h];
+    // the list, a wavefront's 256 places of it at a time
+    int m = 0, mine = 0;
+    for (int k = 0; k < a.n; k += 64) {
+      if (k == w * 256) mine = m;
+      m += __popcll(__ballot(ids[k + lane] == v));
+    }
 #pragma unroll
-  for (int q = 0; q < 16; ++q) s += acc[q][w][lane];
-  float* o = dE + (size_t)(v0 + w) * d + c;
-  *o = accumulate ? *o + s * scale : s * scale;
+    for (int k = 0; k < 4; ++k) {
+      const int i = w * 256 + k * 64;
+      const uint64_t hit = __ballot(ids[i + lane] == v);
+      if (hit >> lane & 1) list[mine + __popcll(hit & lower)] = (uint16_t)(i + lane);
+      mine += __popcll(hit);
+    }
+    __syncthreads();
+    const int each = (m + 7) / 8, l0 = w * each, l1 = min(l0 + each, m);
+    for (int c0 = 0; c0 < a.d; c0 += 64 * VEC) {
+      const int c = c0 + lane * VEC;
+      red[w][lane] = sum_listed<T, VEC, F>((const T*)a.dx + (c < a.d ? c : 0), a.d, list, l0, l1);
+      __syncthreads();
+      if (w == 0 && c < a.d) {
+        F s = red[0][lane];
+#pragma unroll
+        for (int q = 1; q < 8; ++q) s += red[q][lane];
+        put(v, c, s);
+      }
+      __syncthreads();
+    }
+  }
 }
 
 struct SortPlan {
-  int bits_each, passes, blocks, chunk, pos_bits;  // pos_bits > 0: one workgroup sorts
+  int bits_each, passes, blocks, chunk;
+  int pos_bits;  // > 0: by rank, in one launch
 };
 int bits_of(int64_t v) {  // of the numbers 0 .. v, at least 1
   int b = 1;
@@ -475,26 +491,22 @@ int bits_of(int64_t v) {  // of the numbers 0 .. v, at least 1
 }
 SortPlan sort_plan(int64_t n, int vocab) {
   SortPlan s;
-  const int bits = bits_of(vocab - 1);
-  s.pos_bits = 0;
-  s.blocks = 1;
-  s.chunk = 0;
-  const int pos_bits = bits_of(n > 0 ? n - 1 : 0);
-  if (n <= kOneSort && bits + pos_bits <= 32) {
-    s.pos_bits = pos_bits;
-    s.passes = ceil_div(bits, 8);
-    s.bits_each = ceil_div(bits, s.passes);
-    return s;
-  }
-  // ids of up to 16 bits take one or two passes of at most 8 bits, longer ones (22 bits at most) two of at most 11
-  s.passes = bits <= 8 ? 1 : 2;
+  const int bits = bits_of(vocab - 1), pos_bits = bits_of(std::max<int64_t>(n - 1, 0));
+  s.pos_bits = n <= kRankSort && bits + pos_bits <= 32 ? pos_bits : 0;
+  s.passes = ceil_div(bits, 8);
   s.bits_each = ceil_div(bits, s.passes);
-  s.blocks = (int)std::min<int64_t>(kSortBlocks, ceil_div(n, kSortTile));
-  s.chunk = ceil_div(n, (int64_t)s.blocks * kSortTile) * kSortTile;
+  s.chunk = std::max(1, ceil_div(n, (int64_t)kSortBlocks * kSortTile)) * kSortTile;
   s.blocks = ceil_div(n, s.chunk);
   return s;
 }
-int sum_tile(int64_t n) { return n <= 32768 ? 16 : n <= 65536 ? 32 : 64; }
+// Positions of a tile: as many as leave 2048 wavefronts and more, up to 64 (16 rows of 768 bf16 columns at 16384
+// tokens: 3072 wavefronts; 64 rows of 2048 columns at 32768: 4096)
+int sum_tile(int64_t n, int d) {
+  const int64_t slabs = ceil_div(d, 256);
+  int t = 64;
+  while (t > 16 && ceil_div(n, t) * slabs < 2048) t /= 2;
+  return t;
+}
 
 struct BwdWs {
   u32x2* buf[2];
@@ -511,9 +523,9 @@ size_t carve_bwd_ws(int64_t n, int vocab, int d, void* base, BwdWs* w) {
     return (void*)q;
   };
   w->buf[0] = (u32x2*)take((size_t)n * sizeof(u32x2));
-  w->buf[1] = (u32x2*)take(s.pos_bits ? 0 : (size_t)n * sizeof(u32x2));
-  w->hist = (uint32_t*)take(s.pos_bits ? 0 : ((size_t)s.blocks << s.bits_each) * 4);
-  w->partial = (float*)take((size_t)ceil_div(n, sum_tile(n)) * 2 * d * 4);
+  w->buf[1] = (u32x2*)take((size_t)n * sizeof(u32x2));
+  w->hist = (uint32_t*)take(s.pos_bits ? 0 : (size_t)s.blocks * 256 * 4);
+  w->partial = (float*)take((size_t)ceil_div(n, sum_tile(n, d)) * 2 * d * 4);
   return off;
 }
 
@@ -562,13 +574,20 @@ size_t embed_sorted_ws_bytes(int64_t n, int vocab, int d) {
 hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int type, float* dE, int64_t n, int d, int vocab,
                                    float scale, int accumulate, void* ws, hipStream_t st) {
   if (n <= 0 && accumulate) return hipSuccess;
-  // one launch where the workgroups of the scan are few (each reads all ids)
-  if (n <= kScanTokens && (int64_t)ceil_div(vocab, kScanRows) * ceil_div(d, 64) <= 1024) {
-    const dim3 grid((unsigned)ceil_div(vocab, kScanRows), (unsigned)ceil_div(d, 64));
-    if (type == IN_BF16)
-      embed_scan_sum_kernel<bf16><<<grid, 1024, 0, st>>>(tokens, (const bf16*)dx, dE, (int)n, d, vocab, scale, accumulate);
-    else
-      embed_scan_sum_kernel<float><<<grid, 1024, 0, st>>>(tokens, (const float*)dx, dE, (int)n, d, vocab, scale, accumulate);
+  const bool vec = d % 4 == 0 && (((uintptr_t)dx & (type == IN_BF16 ? 7 : 15)) | ((uintptr_t)dE & 15)) == 0;
+  if (n <= kOwnerTokens) {
+    OwnerArgs a;
+    a.tok = tokens; a.dx = dx; a.dE = dE; a.n = (int)n; a.d = d; a.vocab = vocab; a.accumulate = accumulate; a.scale = scale;
+    a.zero_rows = std::min(kZeroRows, std::max(1, 32768 / d));  // 128 KB of the table
+    a.sum_blocks = ceil_div(n, 8);
+    const unsigned grid = (unsigned)(a.sum_blocks + (accumulate ? 0 : ceil_div(vocab, a.zero_rows)));
+    if (type == IN_BF16) {
+      if (vec) embed_owner_sum_kernel<bf16, 4><<<grid, 512, 0, st>>>(a);
+      else embed_owner_sum_kernel<bf16, 1><<<grid, 512, 0, st>>>(a);
+    } else {
+      if (vec) embed_owner_sum_kernel<float, 4><<<grid, 512, 0, st>>>(a);
+      else embed_owner_sum_kernel<float, 1><<<grid, 512, 0, st>>>(a);
+    }
     return hipGetLastError();
   }
   const SortPlan s = sort_plan(n, vocab);
@@ -576,46 +595,47 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
   carve_bwd_ws(n, vocab, d, ws, &w);
   // rows of ids that do not occur: the whole table's gradient is cleared beside the sort, which leaves most of the
   // chip idle, in equal shares of its launches
+  const int rank_keys = n <= 4096 ? 16 : n <= 8192 ? 32 : 64;
+  const int sorters = s.pos_bits ? ceil_div(n, rank_keys) : s.blocks;  // workgroups of a launch that sort
   const int launches = s.pos_bits ? 1 : 2 * s.passes;
   const int64_t all = accumulate ? 0 : (int64_t)vocab * d, share = ((all + launches - 1) / launches + 3) / 4 * 4;
-  int turn = 0;
-  auto fill_next = [&](int first) {
-    Fill f;
-    const int64_t i0 = std::min(all, share * turn), i1 = std::min(all, share * (turn + 1));
-    f.out = dE + i0; f.count = i1 - i0; f.first = first;
-    ++turn;
-    return f;
-  };
-  auto fill_blocks = [&](const Fill& f, int threads) { return (int)std::min<int64_t>(2048 * 256 / threads, ceil_div(f.count, 64 * threads)); };
   const u32x2* sorted = w.buf[0];
+  SortPass p;
+  p.hist = w.hist;
+  p.n = (int)n; p.vocab = vocab; p.chunk = s.chunk; p.blocks = s.blocks; p.bits = s.bits_each;
+  int turn = 0;
+  auto blocks = [&]() {  // of the next launch, its share of the clearing among them
+    const int64_t i0 = std::min(all, share * turn), i1 = std::min(all, share * (turn + 1));
+    ++turn;
+    p.fill.out = dE + i0; p.fill.count = i1 - i0; p.fill.first = sorters;
+    return (unsigned)(sorters + ceil_div(p.fill.count, kFillEach));
+  };
   if (s.pos_bits) {
-    const Fill f = fill_next(1);
-    embed_sort_one_kernel<<<1 + fill_blocks(f, 1024), 1024, 0, st>>>(tokens, w.buf[0], (int)n, vocab, s.pos_bits, s.passes,
-                                                                     s.bits_each, f);
-  } else {
-    for (int q = 0; q < s.passes; ++q) {
-      SortPass p;
-      p.tok = q == 0 ? tokens : nullptr;
-      p.in = w.buf[(q + 1) & 1];
-      p.out = w.buf[q & 1];
-      p.hist = w.hist;
-      p.n = (int)n; p.vocab = vocab; p.chunk = s.chunk; p.blocks = s.blocks; p.shift = q * s.bits_each; p.bits = s.bits_each;
-      p.fill = fill_next(s.blocks);
-      embed_sort_count_kernel<<<s.blocks + fill_blocks(p.fill, 256), 256, 4u << s.bits_each, st>>>(p);
-      p.fill = fill_next(s.blocks);
-      embed_sort_place_kernel<<<s.blocks + fill_blocks(p.fill, 256), 256, 20u << s.bits_each, st>>>(p);
-      sorted = p.out;
-    }
+    const unsigned grid = blocks();
+    auto go = [&](auto kern) { kern<<<grid, 1024, 0, st>>>(tokens, w.buf[0], (int)n, vocab, s.pos_bits, p.fill); };
+    if (rank_keys == 16) go(embed_sort_rank_kernel<16>);
+    else if (rank_keys == 32) go(embed_sort_rank_kernel<32>);
+    else go(embed_sort_rank_kernel<64>);
   }
-  if (n == 0) return hipGetLastError();
+  for (int q = 0; q < s.passes && !s.pos_bits; ++q) {
+    p.tok = q == 0 ? tokens : nullptr;
+    p.in = w.buf[(q + 1) & 1];
+    p.out = w.buf[q & 1];
+    p.shift = q * s.bits_each;
+    embed_sort_count_kernel<<<blocks(), 1024, 0, st>>>(p);
+    embed_sort_place_kernel<<<blocks(), 1024, 0, st>>>(p);
+    sorted = p.out;
+  }
   SumArgs a;
   a.sorted = sorted; a.dx = dx; a.dE = dE; a.partial = w.partial;
-  a.n = (int)n; a.d = d; a.tile = sum_tile(n); a.tiles = ceil_div(n, a.tile); a.slabs = 0; a.accumulate = accumulate;
+  a.n = (int)n; a.d = d; a.tile = sum_tile(n, d); a.tiles = ceil_div(n, a.tile); a.slabs = 0; a.accumulate = accumulate;
   a.scale = scale;
-  const bool vec = d % 4 == 0 && (((uintptr_t)dx & (type == IN_BF16 ? 7 : 15)) | ((uintptr_t)dE & 15)) == 0;
   if (type == IN_BF16) launch_tile_sum<bf16>(a, vec, st);
   else launch_tile_sum<float>(a, vec, st);
-  if (a.tiles > 1) embed_join_kernel<<<dim3((unsigned)a.tiles, (unsigned)ceil_div(d, 256)), 256, 0, st>>>(a);
+  if (a.tiles > 1) {
+    if (vec) embed_join_kernel<4><<<dim3((unsigned)a.tiles, (unsigned)ceil_div(d, 256)), 512, 0, st>>>(a);
+    else embed_join_kernel<1><<<dim3((unsigned)a.tiles, (unsigned)ceil_div(d, 64)), 512, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 
