@@ -365,16 +365,13 @@ int t5_embed_bwd(const t5_embed_cfg* cfg, const int32_t* tokens, const void* dx,
  * (the logits themselves, exactly); ids: int32 [rows, top_k].  -0 and +0 are equal; NaN counts as larger than +inf
  * and comes back as NaN.  Elements between vocab and ld are not read.  rows == 0 is a no-op.
  * Errors: NULL with rows > 0 -> T5_ERR_NULL; rows < 0, vocab < 2, ld < vocab, top_k < 1 or > vocab -> T5_ERR_SHAPE;
- * rows > 2^24, vocab > 2^22, ld > 2^32, top_k > 256, unknown dtype -> T5_ERR_UNSUPPORTED; small workspace ->
- * T5_ERR_WORKSPACE. */
+ * rows > 2^24, vocab > 2^22, ld > 2^32, top_k > 256, unknown dtype -> T5_ERR_UNSUPPORTED. */
 typedef struct {
   int64_t rows, ld;
   int32_t vocab, top_k;
   int32_t dtype;
 } t5_top_logits_cfg;
-size_t t5_top_logits_workspace_bytes(const t5_top_logits_cfg* cfg);
-int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* values, int32_t* ids, void* workspace,
-                  size_t workspace_bytes, void* stream);
+int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* values, int32_t* ids, void* stream);
 
 /* Distillation from a teacher's top logits: loss of a student's logits x, forward and gradient in one call.  Per row,
  * with the teacher's entries (teacher_logits t_k, teacher_ids id_k), k < top_k, of which those with an id in
@@ -389,7 +386,8 @@ int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* value
  * dlogits: gradient of loss, rows ld elements apart, elements between vocab and ld left alone; it may be logits itself,
  * or NULL: then the loss alone is computed.  Logits of -inf are allowed (their gradient is that of q = 0; an entry of
  * positive probability there makes the loss +inf); a row of nothing but -inf gives NaN.  Sums are float32.
- * Errors: as t5_top_logits; loss NULL, or targets NULL with soft_weight != 1 -> T5_ERR_NULL; temperature <= 0 or not
+ * Errors: as t5_top_logits; small workspace -> T5_ERR_WORKSPACE; loss NULL, or targets NULL with soft_weight != 1 ->
+ * T5_ERR_NULL; temperature <= 0 or not
  * finite (nor its inverse), soft_weight outside [0, 1], z_loss < 0 or not finite -> T5_ERR_SHAPE.  rows == 0 writes 0. */
 typedef struct {
   int64_t rows, ld;

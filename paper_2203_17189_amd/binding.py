@@ -172,10 +172,8 @@ def lib() -> C.CDLL:
     L.t5_embed_bwd_workspace_bytes.argtypes = [C.POINTER(_EmbedCfg)]
     L.t5_embed_bwd.restype = i32
     L.t5_embed_bwd.argtypes = [C.POINTER(_EmbedCfg), vp, vp, vp, i32, vp, sz, vp]
-    L.t5_top_logits_workspace_bytes.restype = sz
-    L.t5_top_logits_workspace_bytes.argtypes = [C.POINTER(_TopCfg)]
     L.t5_top_logits.restype = i32
-    L.t5_top_logits.argtypes = [C.POINTER(_TopCfg), vp, vp, vp, vp, sz, vp]
+    L.t5_top_logits.argtypes = [C.POINTER(_TopCfg), vp, vp, vp, vp]
     L.t5_distill_workspace_bytes.restype = sz
     L.t5_distill_workspace_bytes.argtypes = [C.POINTER(_DistillCfg)]
     L.t5_distill_loss_and_grad.restype = i32
@@ -765,7 +763,7 @@ def t5_embed_bwd(tokens, dx, vocab, scale=1.0, dtable=None, accumulate=False, wo
     return dtable
 
 
-def t5_top_logits(logits, top_k, values=None, ids=None, workspace=None):
+def t5_top_logits(logits, top_k, values=None, ids=None):
     """(values float32, ids int32), both [rows, top_k]: the largest logits of each row, descending, equal ones by ascending
     id.  logits [rows, vocab] may be a view of rows with a longer stride."""
     ty = _elem_type(logits, "logits")
@@ -780,12 +778,7 @@ def t5_top_logits(logits, top_k, values=None, ids=None, workspace=None):
     else:
         _check_on(dev, ids, torch.int32, rows * top_k, "ids")
     cfg = _TopCfg(rows, ld, vocab, top_k, ty)
-    if workspace is None:
-        workspace = _byte_buffer(lib().t5_top_logits_workspace_bytes(C.byref(cfg)), dev)
-    else:
-        _check_on(dev, workspace, torch.uint8, workspace.numel(), "workspace")
-    _call(lib().t5_top_logits, "t5_top_logits", dev, C.byref(cfg), logits.data_ptr(), values.data_ptr(), ids.data_ptr(),
-          workspace.data_ptr(), workspace.numel())
+    _call(lib().t5_top_logits, "t5_top_logits", dev, C.byref(cfg), logits.data_ptr(), values.data_ptr(), ids.data_ptr())
     return values, ids
 
 

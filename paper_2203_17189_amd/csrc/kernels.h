@@ -286,9 +286,8 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
                                    float scale, int accumulate, void* ws, hipStream_t st);
 // The K (1..kTopMost) largest logits of each row [V], rows ld elements apart, descending, equal ones by ascending id.
 constexpr int kTopMost = 256;
-size_t top_logits_ws_bytes(int64_t rows, int V, int K, int type);
 hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, int64_t ld, int K, float* values,
-                             int32_t* ids, void* ws, hipStream_t st);
+                             int32_t* ids, hipStream_t st);
 // Distillation loss of rows [V], ld elements apart (see t5_distill_loss_and_grad).
 struct DistillArgs {
   const int32_t* targets;  // null: every row counts, soft == 1

@@ -84,22 +84,14 @@ int t5_embed_bwd(const t5_embed_cfg* cfg, const int32_t* tokens, const void* dx,
   return T5_OK;
 }
 
-size_t t5_top_logits_workspace_bytes(const t5_top_logits_cfg* cfg) {
-  int ty;
-  if (check_top(cfg, &ty) != T5_OK) return 0;
-  return std::max<size_t>(256, top_logits_ws_bytes(cfg->rows, cfg->vocab, cfg->top_k, ty));
-}
-
-int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* values, int32_t* ids, void* workspace,
-                  size_t workspace_bytes, void* stream) {
+int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* values, int32_t* ids, void* stream) {
   int ty;
   const int rc = check_top(cfg, &ty);
   if (rc != T5_OK) return rc;
   if (cfg->rows == 0) return T5_OK;
-  if (!logits || !values || !ids || !workspace) return T5_ERR_NULL;
-  if (workspace_bytes < t5_top_logits_workspace_bytes(cfg)) return T5_ERR_WORKSPACE;
+  if (!logits || !values || !ids) return T5_ERR_NULL;
   hipStream_t st = (hipStream_t)stream;
-  T5_STEP("top_logits", launch_top_logits(logits, ty, cfg->rows, cfg->vocab, cfg->ld, cfg->top_k, values, ids, workspace, st));
+  T5_STEP("top_logits", launch_top_logits(logits, ty, cfg->rows, cfg->vocab, cfg->ld, cfg->top_k, values, ids, st));
   return T5_OK;
 }
 

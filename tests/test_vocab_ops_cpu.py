@@ -60,8 +60,7 @@ def test_embed_nulls_empty_and_workspace():
 @pytest.mark.parametrize("kw,rc", ROWS_BAD, ids=str)
 def test_row_refusals(kw, rc):
     L, t, d = P.lib(), _top(**kw), _distill(**kw)
-    assert L.t5_top_logits(C.byref(t), D, D, D, D, 1 << 40, None) == rc
-    assert L.t5_top_logits_workspace_bytes(C.byref(t)) == 0
+    assert L.t5_top_logits(C.byref(t), D, D, D, None) == rc
     assert L.t5_distill_loss_and_grad(C.byref(d), D, D, D, D, D, D, D, D, 1 << 40, None) == rc
     assert L.t5_distill_workspace_bytes(C.byref(d)) == 0
 
@@ -75,14 +74,12 @@ def test_distill_refusals(kw, rc):
 
 def test_top_and_distill_nulls_and_workspace():
     L, t, d = P.lib(), _top(), _distill()
-    assert L.t5_top_logits(None, D, D, D, D, 1 << 40, None) == NULL
-    for i in range(4):
-        a = [D, D, D, D]
+    assert L.t5_top_logits(None, D, D, D, None) == NULL
+    for i in range(3):
+        a = [D, D, D]
         a[i] = None
-        assert L.t5_top_logits(C.byref(t), *a, 1 << 40, None) == NULL
-    need = L.t5_top_logits_workspace_bytes(C.byref(t))
-    assert need > 0 and L.t5_top_logits(C.byref(t), D, D, D, D, need - 1, None) == WORKSPACE
-    assert L.t5_top_logits(C.byref(_top(rows=0)), None, None, None, None, 0, None) == 0
+        assert L.t5_top_logits(C.byref(t), *a, None) == NULL
+    assert L.t5_top_logits(C.byref(_top(rows=0)), None, None, None, None) == 0
     assert L.t5_distill_loss_and_grad(None, D, D, D, D, D, D, D, D, 1 << 40, None) == NULL
     for i in (0, 1, 2, 3, 4, 7):  # row losses and the gradient may be absent; targets only with soft_weight 1
         a = [D] * 8
