@@ -3,26 +3,41 @@
 //   p = softmax_k(t_k / tau) over the entries with an id in [0, V),   log q_v = x_v / tau - lse(x / tau)
 //   row = (1 - a) (lse(x) - x_target) + z lse(x)^2 + a tau^2 sum_k p_k (log p_k - log q_{id_k})
 //   d row / d x_v = softmax(x)_v (1 - a + 2 z lse(x)) - (1 - a) [v = target] + a tau (q_v - sum_{k: id_k = v} p_k)
-// Bound by bytes: every logit is read once and its gradient written once.
+// Bound by bytes where the row stays in registers: every logit is read once and its gradient written once.  With two
+// softmaxes the exponentials (a quarter of the rate of other instructions) come close behind: exp(x - m) is the square or
+// the fourth power of exp((x - m) / tau) where tau is 2 or 4.
 #include "kernels.h"
+#include "vocab_rows.h"
 #include <algorithm>
 
 namespace t5mi {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kSelfCount = 1024;  // rows up to which every workgroup counts the targets itself
 
-template <int NW>
-__device__ __forceinline__ float block_max_of(float v, float* red) {
-  v = wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float m = red[0];
-#pragma unroll
-  for (int i = 1; i < NW; ++i) m = fmaxf(m, red[i]);
-  return m;
+// Which exponentials a row needs: one (tau = 1, or only one of the two softmaxes has weight), two of which the second is
+// the square or fourth power of the first, or two.
+enum { EXP_ONE = 0, EXP_SQUARE = 1, EXP_FOURTH = 2, EXP_TWO = 3 };
+
+bool distill_counts(const int32_t* targets, int64_t rows) { return targets && rows > kSelfCount; }
+
+struct Exps {
+  float a, b;  // exp(x - m) and exp((x - m) / tau); with EXP_ONE both are the one that is needed
+};
+template <int MODE>
+__device__ __forceinline__ Exps exps_of(float x, float c1, float mc1, float ct, float mct) {
+  Exps e;
+  e.b = __builtin_amdgcn_exp2f(fmaf(x, ct, -mct));
+  if (MODE == EXP_ONE) e.a = e.b;
+  if (MODE == EXP_SQUARE) e.a = e.b * e.b;
+  if (MODE == EXP_FOURTH) {
+    e.a = e.b * e.b;
+    e.a *= e.a;
+  }
+  if (MODE == EXP_TWO) e.a = __builtin_amdgcn_exp2f(fmaf(x, c1, -mc1));
+  return e;
 }
 
 // Counted rows, as a float, by one workgroup.
@@ -30,7 +45,7 @@ __global__ __launch_bounds__(1024) void distill_count_kernel(const int32_t* __re
                                                              float* __restrict__ n_counted) {
   __shared__ int red[16];
   int c = 0;
-  for (int64_t r = threadIdx.x; r < rows; r += 1024) c += !targets || (targets[r] >= 0 && targets[r] < V) ? 1 : 0;
+  for (int64_t r = threadIdx.x; r < rows; r += 1024) c += targets[r] >= 0 && targets[r] < V ? 1 : 0;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) c += __shfl_xor(c, off, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
@@ -42,113 +57,352 @@ __global__ __launch_bounds__(1024) void distill_count_kernel(const int32_t* __re
   }
 }
 
-// One workgroup per row; the row is read again for each pass.  `out` may be the logits themselves.
-template <typename T>
-__global__ __launch_bounds__(256) void distill_rows_kernel(DistillArgs a, const T* logits, T* out) {
-  __shared__ float red[4];
+// One workgroup of NT threads per row.  NV > 0: the row is at most NV 16-byte pieces a thread (and one element) and stays
+// in registers.  NV == 0: any length, eight pieces a thread at a time, each with the largest element and the sums so far,
+// and read a second time for the gradient.  `out` may be the logits themselves.
+template <typename T, int NT, int NV, int MODE, bool GRAD>
+__global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T* logits, T* out) {
+  constexpr int EPV = RowSplit<T>::EPV, NW = NT / 64, CH = NV ? NV : 8;
+  typedef typename RowVec<T>::type VT;
+  __shared__ float red_m[NW], red_t[NW], red_a[NW], red_b[NW], red_w[NW], red_kl[NW];
+  __shared__ int red_n[NW];
   __shared__ int s_id[256];
   __shared__ float s_p[256];
-  const int tid = threadIdx.x, V = a.V;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, V = a.V;
   const int64_t row = blockIdx.x;
   const T* x = logits + row * a.ld;
-  T* g = out ? out + row * a.ld : nullptr;
+  T* g = GRAD ? out + row * a.ld : nullptr;
+  const RowSplit<T> sp(x, V);
+  const u32x4* body = reinterpret_cast<const u32x4*>(x + sp.head);
+  u32x4* gbody = GRAD ? reinterpret_cast<u32x4*>(g + sp.head) : nullptr;
+  const int own = sp.single(tid, NT, V), last = sp.pieces - 1;
   const int tgt = a.targets ? a.targets[row] : -1;
-  const bool hard = tgt >= 0 && tgt < V, counted = !a.targets || hard;
-  if (!counted) {
+  const bool hard = tgt >= 0 && tgt < V;
+  // (the gradient's rows need not lie on 16-byte boundaries where the logits' rows do)
+  auto put_piece = [&](int p, u32x4 b) {
+    if (!a.apart) {
+      gbody[p] = b;
+    } else {
+      const VT o = __builtin_bit_cast(VT, b);
+#pragma unroll
+      for (int k = 0; k < EPV; ++k) g[sp.head + p * EPV + k] = o[k];
+    }
+  };
+  if (a.targets && !hard) {
     if (tid == 0) a.row_loss[row] = 0.f;
-    if (g)
-      for (int c = tid; c < V; c += 256) g[c] = from_f32<T>(0.f);
+    if (GRAD) {
+      if (own >= 0) g[own] = from_f32<T>(0.f);
+      for (int p = tid; p < sp.pieces; p += NT) put_piece(p, u32x4{0, 0, 0, 0});
+    }
     return;
   }
-  float m = -INFINITY;
-  for (int c = tid; c < V; c += 256) m = fmaxf(m, to_f32(x[c]));
-  m = block_max_of<4>(m, red);
-  const float c1 = kLog2e, ct = kLog2e * a.inv_tau;
-  float s1 = 0.f, stau = 0.f;
-  for (int c = tid; c < V; c += 256) {
-    const float d = to_f32(x[c]) - m;
-    s1 += __builtin_amdgcn_exp2f(d * c1);
-    stau += __builtin_amdgcn_exp2f(d * ct);
+  constexpr uint32_t kNegInf = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+  auto piece_at = [&](int p) {  // (-inf behind the end: exponentials of 0)
+    u32x4 r = last >= 0 ? body[min(p, last)] : u32x4{kNegInf, kNegInf, kNegInf, kNegInf};
+    return p <= last ? r : u32x4{kNegInf, kNegInf, kNegInf, kNegInf};
+  };
+  u32x4 raw[CH];
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) raw[i] = piece_at(i * NT + tid);
   }
-  s1 = block_sum<4>(s1, red);
-  stau = block_sum<4>(stau, red);
-  const float log_s1 = logf(s1), log_st = logf(stau), lse = m + log_s1;
-  // teacher: thread k holds entry k
-  int id = -1;
-  float t = -INFINITY, xk = 0.f;
-  if (tid < a.K) {
-    id = a.teacher_ids[row * a.K + tid];
-    if (id < 0 || id >= V) id = -1;
-    if (id >= 0) {
-      t = a.teacher_logits[row * a.K + tid];
-      xk = to_f32(x[id]);
+  const float xs = own >= 0 ? to_f32(x[own]) : -INFINITY;
+  // thread k holds the teacher's entry k, and k + NT where NT < K
+  constexpr int EK = (256 + NT - 1) / NT;
+  int id[EK];
+  float t[EK], xk[EK];
+#pragma unroll
+  for (int q = 0; q < EK; ++q) {
+    const int k = q * NT + tid;
+    id[q] = -1;
+    t[q] = -INFINITY;
+    xk[q] = 0.f;
+    if (k < a.K) {
+      id[q] = a.teacher_ids[row * a.K + k];
+      if (id[q] < 0 || id[q] >= V) id[q] = -1;
+      if (id[q] >= 0) {
+        t[q] = a.teacher_logits[row * a.K + k];
+        xk[q] = to_f32(x[id[q]]);
+      }
     }
   }
-  // (fmax passes a NaN over: it counts as +inf here and comes back in the sum)
-  const float tm = block_max_of<4>(t != t ? INFINITY : t, red);
-  const bool any = tm != -INFINITY;
-  const float w = id >= 0 && any ? __builtin_amdgcn_exp2f((t - tm) * ct) : 0.f;
-  const float total = block_sum<4>(w, red);
-  const float p = any ? w / total : 0.f;
-  const float log_p = (t - tm) * a.inv_tau - logf(total);
-  const float kl = block_sum<4>(id >= 0 && p != 0.f ? p * (log_p - ((xk - m) * a.inv_tau - log_st)) : 0.f, red);
-  s_id[tid] = id;
-  s_p[tid] = p;
   const float x_t = hard ? to_f32(x[tgt]) : 0.f;
-  if (tid == 0) {
+  int n_here = 0;
+  const bool self_count = GRAD && a.targets && !a.n_counted;
+  if (self_count)
+    for (int r = tid; r < (int)a.all_rows; r += NT) n_here += a.all_targets[r] >= 0 && a.all_targets[r] < V ? 1 : 0;
+  const float c1 = kLog2e, ct = a.exp_scale;
+  // ---- largest element of the row, largest entry of the teacher
+  float m = xs, s1 = 0.f, st = 0.f, tm = -INFINITY;
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const VT v = __builtin_bit_cast(VT, raw[i]);
+#pragma unroll
+      for (int k = 0; k < EPV; ++k) m = fmaxf(m, to_f32(v[k]));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  } else {
+    // the thread's own largest element so far, and sums relative to it
+    for (int p0 = 0; p0 <= last; p0 += NT * CH) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) raw[i] = piece_at(p0 + i * NT + tid);
+      float nm = m;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const VT v = __builtin_bit_cast(VT, raw[i]);
+#pragma unroll
+        for (int k = 0; k < EPV; ++k) nm = fmaxf(nm, to_f32(v[k]));
+      }
+      if (nm != -INFINITY) {
+        const Exps f = exps_of<MODE>(m, c1, nm * c1, ct, nm * ct);  // (m = -inf: 0)
+        s1 *= f.a;
+        st *= f.b;
+        m = nm;
+        const float mc1 = m * c1, mct = m * ct;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          const VT v = __builtin_bit_cast(VT, raw[i]);
+#pragma unroll
+          for (int k = 0; k < EPV; ++k) {
+            const Exps e = exps_of<MODE>(to_f32(v[k]), c1, mc1, ct, mct);
+            s1 += e.a;
+            st += e.b;
+          }
+        }
+      } else {
+        // nothing but -inf so far, or NaN: the sums would be 0, or NaN
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          const VT v = __builtin_bit_cast(VT, raw[i]);
+#pragma unroll
+          for (int k = 0; k < EPV; ++k)
+            if (to_f32(v[k]) != to_f32(v[k])) s1 = st = __builtin_nanf("");
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < EK; ++q) tm = fmaxf(tm, t[q] != t[q] ? INFINITY : t[q]);  // (fmax passes a NaN over: it comes back in the sum)
+  const float own_m = m;
+  m = wave_max(m);
+  tm = wave_max(tm);
+  if (self_count) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) n_here += __shfl_xor(n_here, off, 64);
+  }
+  if (NW > 1) {
+    if (lane == 0) {
+      red_m[w] = m;
+      red_t[w] = tm;
+      red_n[w] = n_here;
+    }
+    __syncthreads();
+    m = red_m[0];
+    tm = red_t[0];
+    n_here = red_n[0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) {
+      m = fmaxf(m, red_m[i]);
+      tm = fmaxf(tm, red_t[i]);
+      n_here += red_n[i];
+    }
+  }
+  const float mc1 = m * c1, mct = m * ct;
+  // ---- sums
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      asm volatile("" : "+v"(raw[i]), "+v"(s1), "+v"(st));  // piece i is not touched before piece i-1 is summed
+      const VT v = __builtin_bit_cast(VT, raw[i]);
+#pragma unroll
+      for (int k = 0; k < EPV; ++k) {
+        const Exps e = exps_of<MODE>(to_f32(v[k]), c1, mc1, ct, mct);
+        if (MODE != EXP_ONE) s1 += e.a;
+        st += e.b;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  } else if (own_m != -INFINITY) {
+    const Exps f = exps_of<MODE>(own_m, c1, mc1, ct, mct);
+    s1 *= f.a;
+    st *= f.b;
+  }
+  if (own >= 0 || m == -INFINITY) {  // (a row of nothing but -inf: NaN)
+    const Exps e = exps_of<MODE>(own >= 0 ? xs : m, c1, mc1, ct, mct);
+    s1 += e.a;
+    st += e.b;
+  }
+  const bool any = tm != -INFINITY;
+  float wk[EK], total = 0.f;
+#pragma unroll
+  for (int q = 0; q < EK; ++q) {
+    wk[q] = id[q] >= 0 && any ? __builtin_amdgcn_exp2f((t[q] - tm) * (kLog2e * a.inv_tau)) : 0.f;
+    total += wk[q];
+  }
+  if (MODE == EXP_ONE) s1 = st;
+  s1 = wave_sum(s1);
+  st = MODE == EXP_ONE ? s1 : wave_sum(st);
+  total = wave_sum(total);
+  if (NW > 1) {
+    if (lane == 0) {
+      red_a[w] = s1;
+      red_b[w] = st;
+      red_w[w] = total;
+    }
+    __syncthreads();
+    s1 = red_a[0];
+    st = red_b[0];
+    total = red_w[0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) {
+      s1 += red_a[i];
+      st += red_b[i];
+      total += red_w[i];
+    }
+  }
+  // (logarithms of softmax values are taken off the same rounded products mc as the exponentials)
+  const float log_s1 = logf(s1), log_st = logf(st);
+  const float lse = fmaf(mc1, kLn2, log_s1);
+  const float log_total = logf(total);
+  float kl = 0.f;
+#pragma unroll
+  for (int q = 0; q < EK; ++q) {
+    const float p = any ? wk[q] / total : 0.f;
+    if (id[q] >= 0 && p != 0.f)
+      kl += p * (((t[q] - tm) * a.inv_tau - log_total) - (fmaf(xk[q], ct, -mct) * kLn2 - log_st));
+    if (q * NT + tid < 256) {
+      s_id[q * NT + tid] = id[q];
+      s_p[q * NT + tid] = p;
+    }
+  }
+  kl = wave_sum(kl);
+  if (NW > 1 && lane == 0) red_kl[w] = kl;
+  auto write_loss = [&] {
+    if (tid != 0) return;
+    if (NW > 1)
+      for (int i = 1; i < NW; ++i) kl += red_kl[i];
     float r = a.z_loss * lse * lse;
     if (a.soft > 0.f) r += a.soft * a.tau * a.tau * kl;
-    if (a.soft < 1.f) r += (1.f - a.soft) * (log_s1 - (x_t - m));
+    if (a.soft < 1.f) r += (1.f - a.soft) * (log_s1 - fmaf(x_t, c1, -mc1) * kLn2);
     a.row_loss[row] = r;
+  };
+  if constexpr (!GRAD) {
+    if (NW > 1) __syncthreads();
+    write_loss();
+  } else {
+    // ---- gradient: the softmax parts of every element, then the elements of the target and of the entries again, whole
+    const float n = !a.targets ? (float)a.all_rows : self_count ? (float)n_here : *a.n_counted;
+    const float inv_n = 1.f / fmaxf(n, 1.f), h = 1.f - a.soft;
+    const float k1 = (h + 2.f * a.z_loss * lse) * inv_n / s1, kt = any ? a.soft * a.tau * inv_n / st : 0.f;
+    const float kp = a.soft * a.tau * inv_n, kone = k1 + kt;
+    auto grad = [&](float xv) {
+      const Exps e = exps_of<MODE>(xv, c1, mc1, ct, mct);
+      return MODE == EXP_ONE ? e.b * kone : fmaf(e.a, k1, e.b * kt);
+    };
+    auto store_piece = [&](u32x4 r, int p) {
+      const VT v = __builtin_bit_cast(VT, r);
+      VT o;
+#pragma unroll
+      for (int k = 0; k < EPV; ++k) o[k] = from_f32<T>(grad(to_f32(v[k])));
+      const u32x4 b = __builtin_bit_cast(u32x4, o);
+      if (p <= last) put_piece(p, b);
+      return b[3];
+    };
+    if constexpr (NV > 0) {
+      uint32_t chain = 0;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        asm volatile("" : "+v"(raw[i]), "+v"(chain));  // one piece at a time, as above
+        chain = store_piece(raw[i], i * NT + tid);
+      }
+    } else {
+      for (int p0 = 0; p0 <= last; p0 += NT * CH) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) raw[i] = piece_at(p0 + i * NT + tid);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) store_piece(raw[i], p0 + i * NT + tid);
+      }
+    }
+    if (own >= 0) g[own] = from_f32<T>(grad(xs));
+    __syncthreads();
+    write_loss();
+    auto whole = [&](int v, float xv) {
+      float ps = 0.f;
+      for (int k = 0; k < a.K; ++k) ps += s_id[k] == v ? s_p[k] : 0.f;
+      float r = grad(xv) - kp * ps;
+      if (v == tgt) r -= h * inv_n;
+      g[v] = from_f32<T>(r);
+    };
+#pragma unroll
+    for (int q = 0; q < EK; ++q)
+      if (id[q] >= 0) whole(id[q], xk[q]);
+    if (hard && tid == NT - 1) whole(tgt, x_t);
   }
-  if (!g) return;
-  const float inv_n = 1.f / fmaxf(*a.n_counted, 1.f);
-  const float h = 1.f - a.soft;
-  const float k1 = (h + 2.f * a.z_loss * lse) * inv_n / s1, ktau = any ? a.soft * a.tau * inv_n / stau : 0.f;
-  const float kp = a.soft * a.tau * inv_n;
-  auto grad = [&](float xv) {
-    const float d = xv - m;
-    return __builtin_amdgcn_exp2f(d * c1) * k1 + __builtin_amdgcn_exp2f(d * ct) * ktau;
-  };
-  __syncthreads();
-  for (int c = tid; c < V; c += 256) g[c] = from_f32<T>(grad(to_f32(x[c])));
-  __syncthreads();  // the entries' own elements are written again, whole
-  auto whole = [&](int v, float xv) {
-    float ps = 0.f;
-    for (int k = 0; k < a.K; ++k) ps += s_id[k] == v ? s_p[k] : 0.f;
-    float r = grad(xv) - kp * ps;
-    if (v == tgt) r -= h * inv_n;
-    g[v] = from_f32<T>(r);
-  };
-  if (id >= 0) whole(id, xk);
-  if (hard && tid == 0) whole(tgt, x_t);
 }
 
-__global__ __launch_bounds__(1024) void distill_mean_kernel(const float* __restrict__ row_loss, int64_t rows,
-                                                            const float* __restrict__ n_counted, float* __restrict__ loss) {
+__global__ __launch_bounds__(1024) void distill_mean_kernel(const float* __restrict__ row_loss, const int32_t* __restrict__ targets,
+                                                            int64_t rows, int V, float* __restrict__ loss) {
   __shared__ float red[16];
-  float s = 0.f;
-  for (int64_t r = threadIdx.x; r < rows; r += 1024) s += row_loss[r];
+  float s = 0.f, n = 0.f;  // (whole numbers below 2^24: exact)
+  for (int64_t r = threadIdx.x; r < rows; r += 1024) {
+    s += row_loss[r];
+    n += !targets || (targets[r] >= 0 && targets[r] < V) ? 1.f : 0.f;
+  }
   s = block_sum<16>(s, red);
-  if (threadIdx.x == 0) *loss = s / fmaxf(*n_counted, 1.f);
+  n = block_sum<16>(n, red);
+  if (threadIdx.x == 0) *loss = s / fmaxf(n, 1.f);
+}
+
+template <typename T, int MODE, bool GRAD>
+void rows_of_mode(const DistillArgs& a, const T* x, T* g, int64_t rows, hipStream_t st) {
+  const int pieces = ceil_div(a.V, 16 / (int)sizeof(T));
+  auto go = [&](auto kern, int nt) { kern<<<(unsigned)rows, nt, 0, st>>>(a, x, g); };
+  // a row in a workgroup's registers, 16 pieces a thread at most; few rows: more threads for each
+  if (pieces <= 256) go(distill_rows_kernel<T, 64, 4, MODE, GRAD>, 64);
+  else if (rows < 512 && pieces <= 4096) go(distill_rows_kernel<T, 1024, 4, MODE, GRAD>, 1024);
+  else if (pieces <= 1024) go(distill_rows_kernel<T, 256, 4, MODE, GRAD>, 256);
+  else if (pieces <= 4096) go(distill_rows_kernel<T, 256, 16, MODE, GRAD>, 256);
+  else if (pieces <= 16384) go(distill_rows_kernel<T, 1024, 16, MODE, GRAD>, 1024);
+  else go(distill_rows_kernel<T, 1024, 0, MODE, GRAD>, 1024);
+}
+
+template <typename T, bool GRAD>
+void rows_of_type(const DistillArgs& a, const T* x, T* g, int mode, int64_t rows, hipStream_t st) {
+  if (mode == EXP_ONE) rows_of_mode<T, EXP_ONE, GRAD>(a, x, g, rows, st);
+  else if (mode == EXP_SQUARE) rows_of_mode<T, EXP_SQUARE, GRAD>(a, x, g, rows, st);
+  else if (mode == EXP_FOURTH) rows_of_mode<T, EXP_FOURTH, GRAD>(a, x, g, rows, st);
+  else rows_of_mode<T, EXP_TWO, GRAD>(a, x, g, rows, st);
 }
 
 }  // namespace
 
 hipError_t launch_distill_count(const int32_t* targets, int64_t rows, int V, float* n_counted, hipStream_t st) {
+  if (!distill_counts(targets, rows)) return hipSuccess;
   distill_count_kernel<<<1, 1024, 0, st>>>(targets, rows, V, n_counted);
   return hipGetLastError();
 }
 
-hipError_t launch_distill_rows(const DistillArgs& a, const void* logits, void* out, int type, int64_t rows, hipStream_t st) {
+hipError_t launch_distill_rows(const DistillArgs& args, const void* logits, void* out, int type, int64_t rows, hipStream_t st) {
   if (rows <= 0) return hipSuccess;
-  if (type == IN_BF16) distill_rows_kernel<bf16><<<(unsigned)rows, 256, 0, st>>>(a, (const bf16*)logits, (bf16*)out);
-  else distill_rows_kernel<float><<<(unsigned)rows, 256, 0, st>>>(a, (const float*)logits, (float*)out);
+  DistillArgs a = args;
+  if (!distill_counts(a.all_targets, a.all_rows)) a.n_counted = nullptr;
+  const bool soft_only = a.soft == 1.f && a.z_loss == 0.f;
+  const int mode = a.tau == 1.f || a.soft == 0.f || soft_only ? EXP_ONE : a.tau == 2.f ? EXP_SQUARE : a.tau == 4.f ? EXP_FOURTH : EXP_TWO;
+  a.exp_scale = a.soft == 0.f ? kLog2e : kLog2e * a.inv_tau;
+  a.apart = out && (((uintptr_t)out ^ (uintptr_t)logits) & 15) != 0;
+  if (type == IN_BF16) {
+    if (out) rows_of_type<bf16, true>(a, (const bf16*)logits, (bf16*)out, mode, rows, st);
+    else rows_of_type<bf16, false>(a, (const bf16*)logits, nullptr, mode, rows, st);
+  } else {
+    if (out) rows_of_type<float, true>(a, (const float*)logits, (float*)out, mode, rows, st);
+    else rows_of_type<float, false>(a, (const float*)logits, nullptr, mode, rows, st);
+  }
   return hipGetLastError();
 }
 
-hipError_t launch_distill_mean(const float* row_loss, int64_t rows, const float* n_counted, float* loss, hipStream_t st) {
-  distill_mean_kernel<<<1, 1024, 0, st>>>(row_loss, rows, n_counted, loss);
+hipError_t launch_distill_mean(const float* row_loss, const int32_t* targets, int64_t rows, int V, float* loss, hipStream_t st) {
+  distill_mean_kernel<<<1, 1024, 0, st>>>(row_loss, targets, rows, V, loss);
   return hipGetLastError();
 }
 

@@ -288,21 +288,25 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
 constexpr int kTopMost = 256;
 hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, int64_t ld, int K, float* values,
                              int32_t* ids, hipStream_t st);
-// Distillation loss of rows [V], ld elements apart (see t5_distill_loss_and_grad).
+// Distillation loss of rows [V], ld elements apart (see t5_distill_loss_and_grad), all of a batch's or a part of them.
 struct DistillArgs {
-  const int32_t* targets;  // null: every row counts, soft == 1
+  const int32_t* targets;        // [rows]; null: every row counts, soft == 1
   const float* teacher_logits;   // [rows, K]
   const int32_t* teacher_ids;    // [rows, K]
-  const float* n_counted;
+  const int32_t* all_targets;    // of the whole batch: the mean's divisor
+  const float* n_counted;        // what launch_distill_count wrote
   float* row_loss;
-  int64_t ld;
+  int64_t ld, all_rows;
   int32_t K, V;
   float tau, inv_tau, soft, z_loss;
+  float exp_scale;  // the last two are set by launch_distill_rows
+  int32_t apart;
 };
+// Number of the batch's rows that count (nothing where launch_distill_rows does without).
 hipError_t launch_distill_count(const int32_t* targets, int64_t rows, int V, float* n_counted, hipStream_t st);
 // Row losses and, with out (the logits themselves, or a buffer of the same row stride), the gradient of the mean.
 hipError_t launch_distill_rows(const DistillArgs& a, const void* logits, void* out, int type, int64_t rows, hipStream_t st);
-hipError_t launch_distill_mean(const float* row_loss, int64_t rows, const float* n_counted, float* loss, hipStream_t st);
+hipError_t launch_distill_mean(const float* row_loss, const int32_t* targets, int64_t rows, int V, float* loss, hipStream_t st);
 
 // out = (accumulate ? out : 0) + alpha * in (float32);  out = alpha * in (storage type)
 hipError_t launch_axpy_f32(float* out, const float* in, float alpha, int n, int accumulate, hipStream_t st);

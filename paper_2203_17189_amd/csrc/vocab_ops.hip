@@ -116,12 +116,13 @@ int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, cons
   hipStream_t st = (hipStream_t)stream;
   DistillArgs a;
   a.targets = targets; a.teacher_logits = teacher_logits; a.teacher_ids = teacher_ids; a.n_counted = w.n_counted;
+  a.all_targets = targets; a.all_rows = cfg->rows;
   a.row_loss = row_loss ? row_loss : w.row_loss;
   a.ld = cfg->ld; a.K = cfg->top_k; a.V = cfg->vocab;
   a.tau = cfg->temperature; a.inv_tau = 1.f / cfg->temperature; a.soft = cfg->soft_weight; a.z_loss = cfg->z_loss;
-  T5_STEP("distill_count", launch_distill_count(targets, cfg->rows, cfg->vocab, w.n_counted, st));
+  if (dlogits) T5_STEP("distill_count", launch_distill_count(targets, cfg->rows, cfg->vocab, w.n_counted, st));
   T5_STEP("distill_rows", launch_distill_rows(a, logits, dlogits, ty, cfg->rows, st));
-  T5_STEP("distill_mean", launch_distill_mean(a.row_loss, cfg->rows, w.n_counted, loss, st));
+  T5_STEP("distill_mean", launch_distill_mean(a.row_loss, targets, cfg->rows, cfg->vocab, loss, st));
   return T5_OK;
 }
 
