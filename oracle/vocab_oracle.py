@@ -50,20 +50,23 @@ def distill_loss(logits, targets, t, ids, temperature=1.0, soft=1.0, z_loss=0.0,
     grad = np.zeros_like(x)
     p, has = teacher_probs(np.asarray(t, np.float64), ids, vocab, temperature)
     for r in np.flatnonzero(counted):
-        lse1, lse_t = _lse(x[r]), _lse(x[r] / temperature)
-        row[r] = z_loss * lse1 ** 2
+        m = x[r].max()
+        d = x[r] - m  # (relative to the largest: next to 1e38 the sum's logarithm would be lost)
+        log_s, log_st = _lse(d), _lse(d / temperature)
+        lse = m + log_s
+        row[r] = z_loss * lse ** 2 if z_loss else 0.0
         if soft < 1:
-            row[r] += (1 - soft) * (lse1 - x[r, targets[r]])
+            row[r] += (1 - soft) * (log_s - d[targets[r]])
         pos = p[r] > 0
         if soft > 0 and has[r]:
             at = ids[r][pos]
-            row[r] += soft * temperature ** 2 * np.sum(p[r][pos] * (np.log(p[r][pos]) - (x[r, at] / temperature - lse_t)))
+            row[r] += soft * temperature ** 2 * np.sum(p[r][pos] * (np.log(p[r][pos]) - (d[at] / temperature - log_st)))
         if want_grad:
-            g = np.exp(x[r] - lse1) * (1 - soft + 2 * z_loss * lse1)
+            g = np.exp(d - log_s) * (1 - soft + 2 * z_loss * lse)
             if soft < 1:
                 g[targets[r]] -= 1 - soft
             if has[r]:
-                g += soft * temperature * np.exp(x[r] / temperature - lse_t)
+                g += soft * temperature * np.exp(d / temperature - log_st)
                 np.add.at(g, ids[r][pos], -soft * temperature * p[r][pos])
             grad[r] = g / n
     return row.sum() / n, row, grad

@@ -14,7 +14,7 @@ namespace t5mi {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSelfCount = 1024;  // rows up to which every workgroup counts the targets itself
 
 // Which exponentials a row needs: one (tau = 1, or only one of the two softmaxes has weight), two of which the second is
@@ -27,16 +27,16 @@ struct Exps {
   float a, b;  // exp(x - m) and exp((x - m) / tau); with EXP_ONE both are the one that is needed
 };
 template <int MODE>
-__device__ __forceinline__ Exps exps_of(float x, float c1, float mc1, float ct, float mct) {
+__device__ __forceinline__ Exps exps_of(float d, float ct) {  // d = x - m <= 0
   Exps e;
-  e.b = __builtin_amdgcn_exp2f(fmaf(x, ct, -mct));
+  e.b = __builtin_amdgcn_exp2f(d * ct);
   if (MODE == EXP_ONE) e.a = e.b;
   if (MODE == EXP_SQUARE) e.a = e.b * e.b;
   if (MODE == EXP_FOURTH) {
     e.a = e.b * e.b;
     e.a *= e.a;
   }
-  if (MODE == EXP_TWO) e.a = __builtin_amdgcn_exp2f(fmaf(x, c1, -mc1));
+  if (MODE == EXP_TWO) e.a = __builtin_amdgcn_exp2f(d * kLog2e);
   return e;
 }
 
@@ -45,7 +45,8 @@ __global__ __launch_bounds__(1024) void distill_count_kernel(const int32_t* __re
                                                              float* __restrict__ n_counted) {
   __shared__ int red[16];
   int c = 0;
-  for (int64_t r = threadIdx.x; r < rows; r += 1024) c += targets[r] >= 0 && targets[r] < V ? 1 : 0;
+#pragma unroll 8
+  for (int r = threadIdx.x; r < (int)rows; r += 1024) c += targets[r] >= 0 && targets[r] < V ? 1 : 0;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) c += __shfl_xor(c, off, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
@@ -57,12 +58,17 @@ __global__ __launch_bounds__(1024) void distill_count_kernel(const int32_t* __re
   }
 }
 
-// One workgroup of NT threads per row.  NV > 0: the row is at most NV 16-byte pieces a thread (and one element) and stays
-// in registers.  NV == 0: any length, eight pieces a thread at a time, each with the largest element and the sums so far,
-// and read a second time for the gradient.  `out` may be the logits themselves.
-template <typename T, int NT, int NV, int MODE, bool GRAD>
+// The row, or part blockIdx.y of it (PART_*), is at most NV 16-byte pieces a thread, and one element, and stays in
+// registers.  PART_STATS leaves the part's largest element and sums of exponentials, PART_APPLY reads those of all parts.
+// `out` may be the logits themselves.
+enum { WHOLE_ROW = 0, PART_STATS = 1, PART_APPLY = 2 };
+struct PartStats {
+  float m, s1, st;
+};
+
+template <typename T, int NT, int NV, int MODE, int PHASE, bool GRAD>
 __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T* logits, T* out) {
-  constexpr int EPV = RowSplit<T>::EPV, NW = NT / 64, CH = NV ? NV : 8;
+  constexpr int EPV = RowSplit<T>::EPV, NW = NT / 64;
   typedef typename RowVec<T>::type VT;
   __shared__ float red_m[NW], red_t[NW], red_a[NW], red_b[NW], red_w[NW], red_kl[NW];
   __shared__ int red_n[NW];
@@ -75,7 +81,13 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   const RowSplit<T> sp(x, V);
   const u32x4* body = reinterpret_cast<const u32x4*>(x + sp.head);
   u32x4* gbody = GRAD ? reinterpret_cast<u32x4*>(g + sp.head) : nullptr;
-  const int own = sp.single(tid, NT, V), last = sp.pieces - 1;
+  // pieces [first, last] are this workgroup's, the elements around them the first part's
+  const int part = PHASE == WHOLE_ROW ? 0 : blockIdx.y, first = part * (NT * NV);
+  const int last = PHASE == WHOLE_ROW ? sp.pieces - 1 : min(sp.pieces, first + NT * NV) - 1;
+  const int own = part == 0 ? sp.single(tid, NT, V) : -1;
+  PartStats* stats = (PartStats*)a.partial + row * a.parts;
+  // logits of the entries and of the target, as they were before any part's gradient was written over them
+  float* picked = (float*)((PartStats*)a.partial + a.rows * a.parts) + row * (a.K + 1);
   const int tgt = a.targets ? a.targets[row] : -1;
   const bool hard = tgt >= 0 && tgt < V;
   // (the gradient's rows need not lie on 16-byte boundaries where the logits' rows do)
@@ -89,22 +101,23 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
     }
   };
   if (a.targets && !hard) {
-    if (tid == 0) a.row_loss[row] = 0.f;
+    if (PHASE == PART_STATS) return;
+    if (tid == 0 && part == 0) a.row_loss[row] = 0.f;
     if (GRAD) {
       if (own >= 0) g[own] = from_f32<T>(0.f);
-      for (int p = tid; p < sp.pieces; p += NT) put_piece(p, u32x4{0, 0, 0, 0});
+      for (int p = first + tid; p <= last; p += NT) put_piece(p, u32x4{0, 0, 0, 0});
     }
     return;
   }
   constexpr uint32_t kNegInf = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
   auto piece_at = [&](int p) {  // (-inf behind the end: exponentials of 0)
-    u32x4 r = last >= 0 ? body[min(p, last)] : u32x4{kNegInf, kNegInf, kNegInf, kNegInf};
+    u32x4 r = last >= first ? body[min(p, last)] : u32x4{kNegInf, kNegInf, kNegInf, kNegInf};
     return p <= last ? r : u32x4{kNegInf, kNegInf, kNegInf, kNegInf};
   };
-  u32x4 raw[CH];
-  if constexpr (NV > 0) {
+  u32x4 raw[NV];
+  if (PHASE != PART_APPLY || GRAD) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) raw[i] = piece_at(i * NT + tid);
+    for (int i = 0; i < NV; ++i) raw[i] = piece_at(first + i * NT + tid);
   }
   const float xs = own >= 0 ? to_f32(x[own]) : -INFINITY;
   // thread k holds the teacher's entry k, and k + NT where NT < K
@@ -117,69 +130,43 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
     id[q] = -1;
     t[q] = -INFINITY;
     xk[q] = 0.f;
-    if (k < a.K) {
+    if ((PHASE != PART_STATS || part == 0) && k < a.K) {
       id[q] = a.teacher_ids[row * a.K + k];
-      if (id[q] < 0 || id[q] >= V) id[q] = -1;
+      if (id[q] < 0 || id[q] >= V || a.soft == 0.f) id[q] = -1;
       if (id[q] >= 0) {
         t[q] = a.teacher_logits[row * a.K + k];
-        xk[q] = to_f32(x[id[q]]);
+        xk[q] = PHASE == PART_APPLY ? picked[k] : to_f32(x[id[q]]);
       }
     }
   }
-  const float x_t = hard ? to_f32(x[tgt]) : 0.f;
+  const float x_t = !hard ? 0.f : PHASE == PART_APPLY ? picked[a.K] : to_f32(x[tgt]);
+  if (PHASE == PART_STATS && part == 0) {
+#pragma unroll
+    for (int q = 0; q < EK; ++q)
+      if (id[q] >= 0) picked[q * NT + tid] = xk[q];
+    if (tid == 0) picked[a.K] = x_t;
+  }
   int n_here = 0;
-  const bool self_count = GRAD && a.targets && !a.n_counted;
+  const bool self_count = GRAD && PHASE != PART_STATS && a.targets && !a.n_counted;
   if (self_count)
     for (int r = tid; r < (int)a.all_rows; r += NT) n_here += a.all_targets[r] >= 0 && a.all_targets[r] < V ? 1 : 0;
-  const float c1 = kLog2e, ct = a.exp_scale;
+  const float ct = a.exp_scale;
   // ---- largest element of the row, largest entry of the teacher
-  float m = xs, s1 = 0.f, st = 0.f, tm = -INFINITY;
-  if constexpr (NV > 0) {
+  float m = -INFINITY, s1 = 0.f, st = 0.f, tm = -INFINITY;
+  if constexpr (PHASE == PART_APPLY) {
+    if (tid < a.parts) {
+      m = stats[tid].m;
+      s1 = stats[tid].s1;
+      st = stats[tid].st;
+    }
+  } else {
+    m = xs;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const VT v = __builtin_bit_cast(VT, raw[i]);
 #pragma unroll
       for (int k = 0; k < EPV; ++k) m = fmaxf(m, to_f32(v[k]));
       __builtin_amdgcn_sched_barrier(0);
-    }
-  } else {
-    // the thread's own largest element so far, and sums relative to it
-    for (int p0 = 0; p0 <= last; p0 += NT * CH) {
-#pragma unroll
-      for (int i = 0; i < CH; ++i) raw[i] = piece_at(p0 + i * NT + tid);
-      float nm = m;
-#pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        const VT v = __builtin_bit_cast(VT, raw[i]);
-#pragma unroll
-        for (int k = 0; k < EPV; ++k) nm = fmaxf(nm, to_f32(v[k]));
-      }
-      if (nm != -INFINITY) {
-        const Exps f = exps_of<MODE>(m, c1, nm * c1, ct, nm * ct);  // (m = -inf: 0)
-        s1 *= f.a;
-        st *= f.b;
-        m = nm;
-        const float mc1 = m * c1, mct = m * ct;
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-          const VT v = __builtin_bit_cast(VT, raw[i]);
-#pragma unroll
-          for (int k = 0; k < EPV; ++k) {
-            const Exps e = exps_of<MODE>(to_f32(v[k]), c1, mc1, ct, mct);
-            s1 += e.a;
-            st += e.b;
-          }
-        }
-      } else {
-        // nothing but -inf so far, or NaN: the sums would be 0, or NaN
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-          const VT v = __builtin_bit_cast(VT, raw[i]);
-#pragma unroll
-          for (int k = 0; k < EPV; ++k)
-            if (to_f32(v[k]) != to_f32(v[k])) s1 = st = __builtin_nanf("");
-        }
-      }
     }
   }
 #pragma unroll
@@ -208,28 +195,29 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
       n_here += red_n[i];
     }
   }
-  const float mc1 = m * c1, mct = m * ct;
+  // (a row of nothing but -inf comes to NaN, a part of that kind to 0)
+  const float m0 = PHASE == PART_STATS && m == -INFINITY ? 0.f : m;
   // ---- sums
-  if constexpr (NV > 0) {
+  if constexpr (PHASE == PART_APPLY) {
+    if (tid < a.parts) {
+      const Exps f = exps_of<MODE>(own_m - m0, ct);
+      s1 *= f.a;
+      st *= f.b;
+    }
+  } else {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
+    for (int i = 0; i < NV; ++i) {
       asm volatile("" : "+v"(raw[i]), "+v"(s1), "+v"(st));  // piece i is not touched before piece i-1 is summed
       const VT v = __builtin_bit_cast(VT, raw[i]);
 #pragma unroll
       for (int k = 0; k < EPV; ++k) {
-        const Exps e = exps_of<MODE>(to_f32(v[k]), c1, mc1, ct, mct);
+        const Exps e = exps_of<MODE>(to_f32(v[k]) - m0, ct);
         if (MODE != EXP_ONE) s1 += e.a;
         st += e.b;
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-  } else if (own_m != -INFINITY) {
-    const Exps f = exps_of<MODE>(own_m, c1, mc1, ct, mct);
-    s1 *= f.a;
-    st *= f.b;
-  }
-  if (own >= 0 || m == -INFINITY) {  // (a row of nothing but -inf: NaN)
-    const Exps e = exps_of<MODE>(own >= 0 ? xs : m, c1, mc1, ct, mct);
+    const Exps e = exps_of<MODE>(xs - m0, ct);  // (0 where the thread has no single element)
     s1 += e.a;
     st += e.b;
   }
@@ -261,16 +249,19 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
       total += red_w[i];
     }
   }
-  // (logarithms of softmax values are taken off the same rounded products mc as the exponentials)
+  if constexpr (PHASE == PART_STATS) {
+    if (tid == 0) stats[part] = PartStats{m, s1, st};
+    return;
+  }
   const float log_s1 = logf(s1), log_st = logf(st);
-  const float lse = fmaf(mc1, kLn2, log_s1);
+  const float lse = m + log_s1;
   const float log_total = logf(total);
   float kl = 0.f;
 #pragma unroll
   for (int q = 0; q < EK; ++q) {
     const float p = any ? wk[q] / total : 0.f;
     if (id[q] >= 0 && p != 0.f)
-      kl += p * (((t[q] - tm) * a.inv_tau - log_total) - (fmaf(xk[q], ct, -mct) * kLn2 - log_st));
+      kl += p * (((t[q] - tm) * a.inv_tau - log_total) - ((xk[q] - m) * a.inv_tau - log_st));
     if (q * NT + tid < 256) {
       s_id[q * NT + tid] = id[q];
       s_p[q * NT + tid] = p;
@@ -279,12 +270,12 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   kl = wave_sum(kl);
   if (NW > 1 && lane == 0) red_kl[w] = kl;
   auto write_loss = [&] {
-    if (tid != 0) return;
+    if (tid != 0 || part != 0) return;
     if (NW > 1)
       for (int i = 1; i < NW; ++i) kl += red_kl[i];
     float r = a.z_loss * lse * lse;
     if (a.soft > 0.f) r += a.soft * a.tau * a.tau * kl;
-    if (a.soft < 1.f) r += (1.f - a.soft) * (log_s1 - fmaf(x_t, c1, -mc1) * kLn2);
+    if (a.soft < 1.f) r += (1.f - a.soft) * (log_s1 - (x_t - m));
     a.row_loss[row] = r;
   };
   if constexpr (!GRAD) {
@@ -297,7 +288,7 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
     const float k1 = (h + 2.f * a.z_loss * lse) * inv_n / s1, kt = any ? a.soft * a.tau * inv_n / st : 0.f;
     const float kp = a.soft * a.tau * inv_n, kone = k1 + kt;
     auto grad = [&](float xv) {
-      const Exps e = exps_of<MODE>(xv, c1, mc1, ct, mct);
+      const Exps e = exps_of<MODE>(xv - m, ct);
       return MODE == EXP_ONE ? e.b * kone : fmaf(e.a, k1, e.b * kt);
     };
     auto store_piece = [&](u32x4 r, int p) {
@@ -309,25 +300,20 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
       if (p <= last) put_piece(p, b);
       return b[3];
     };
-    if constexpr (NV > 0) {
-      uint32_t chain = 0;
+    uint32_t chain = 0;
 #pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        asm volatile("" : "+v"(raw[i]), "+v"(chain));  // one piece at a time, as above
-        chain = store_piece(raw[i], i * NT + tid);
-      }
-    } else {
-      for (int p0 = 0; p0 <= last; p0 += NT * CH) {
-#pragma unroll
-        for (int i = 0; i < CH; ++i) raw[i] = piece_at(p0 + i * NT + tid);
-#pragma unroll
-        for (int i = 0; i < CH; ++i) store_piece(raw[i], p0 + i * NT + tid);
-      }
+    for (int i = 0; i < NV; ++i) {
+      asm volatile("" : "+v"(raw[i]), "+v"(chain));  // one piece at a time, as above
+      chain = store_piece(raw[i], first + i * NT + tid);
     }
     if (own >= 0) g[own] = from_f32<T>(grad(xs));
     __syncthreads();
     write_loss();
     auto whole = [&](int v, float xv) {
+      if constexpr (PHASE == PART_APPLY) {  // another part's
+        const int p = v - sp.head;
+        if (p < 0 || p >= sp.pieces * EPV ? part != 0 : p < first * EPV || p > last * EPV + EPV - 1) return;
+      }
       float ps = 0.f;
       for (int k = 0; k < a.K; ++k) ps += s_id[k] == v ? s_p[k] : 0.f;
       float r = grad(xv) - kp * ps;
@@ -345,7 +331,8 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float* __restr
                                                             int64_t rows, int V, float* __restrict__ loss) {
   __shared__ float red[16];
   float s = 0.f, n = 0.f;  // (whole numbers below 2^24: exact)
-  for (int64_t r = threadIdx.x; r < rows; r += 1024) {
+#pragma unroll 8
+  for (int r = threadIdx.x; r < (int)rows; r += 1024) {
     s += row_loss[r];
     n += !targets || (targets[r] >= 0 && targets[r] < V) ? 1.f : 0.f;
   }
@@ -354,17 +341,34 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float* __restr
   if (threadIdx.x == 0) *loss = s / fmaxf(n, 1.f);
 }
 
+constexpr int kPartPieces = 256 * 16;  // 64 KB of a row
+
+// Workgroups that share a row: 1, or parts of 64 KB for rows that do not fit one workgroup's registers, or that would
+// leave compute units without work.
+int row_parts(int64_t rows, int V, int type) {
+  const int pieces = ceil_div(V, type == IN_BF16 ? 8 : 4);
+  return pieces <= kPartPieces || (pieces <= 16384 && rows >= 256) ? 1 : ceil_div(pieces, kPartPieces);
+}
+
 template <typename T, int MODE, bool GRAD>
 void rows_of_mode(const DistillArgs& a, const T* x, T* g, int64_t rows, hipStream_t st) {
   const int pieces = ceil_div(a.V, 16 / (int)sizeof(T));
-  auto go = [&](auto kern, int nt) { kern<<<(unsigned)rows, nt, 0, st>>>(a, x, g); };
+  auto go = [&](auto kern, int nt) { kern<<<dim3((unsigned)rows, (unsigned)a.parts), nt, 0, st>>>(a, x, g); };
+  if (a.parts > 1) {
+    go(distill_rows_kernel<T, 256, 16, MODE, PART_STATS, GRAD>, 256);
+    if (GRAD) {
+      go(distill_rows_kernel<T, 256, 16, MODE, PART_APPLY, GRAD>, 256);
+    } else {
+      distill_rows_kernel<T, 256, 16, MODE, PART_APPLY, GRAD><<<(unsigned)rows, 256, 0, st>>>(a, x, g);
+    }
+    return;
+  }
   // a row in a workgroup's registers, 16 pieces a thread at most; few rows: more threads for each
-  if (pieces <= 256) go(distill_rows_kernel<T, 64, 4, MODE, GRAD>, 64);
-  else if (rows < 512 && pieces <= 4096) go(distill_rows_kernel<T, 1024, 4, MODE, GRAD>, 1024);
-  else if (pieces <= 1024) go(distill_rows_kernel<T, 256, 4, MODE, GRAD>, 256);
-  else if (pieces <= 4096) go(distill_rows_kernel<T, 256, 16, MODE, GRAD>, 256);
-  else if (pieces <= 16384) go(distill_rows_kernel<T, 1024, 16, MODE, GRAD>, 1024);
-  else go(distill_rows_kernel<T, 1024, 0, MODE, GRAD>, 1024);
+  if (pieces <= 256) go(distill_rows_kernel<T, 64, 4, MODE, WHOLE_ROW, GRAD>, 64);
+  else if (rows < 512 && pieces <= 4096) go(distill_rows_kernel<T, 1024, 4, MODE, WHOLE_ROW, GRAD>, 1024);
+  else if (pieces <= 1024) go(distill_rows_kernel<T, 256, 4, MODE, WHOLE_ROW, GRAD>, 256);
+  else if (pieces <= 4096) go(distill_rows_kernel<T, 256, 16, MODE, WHOLE_ROW, GRAD>, 256);
+  else go(distill_rows_kernel<T, 1024, 16, MODE, WHOLE_ROW, GRAD>, 1024);
 }
 
 template <typename T, bool GRAD>
@@ -376,6 +380,11 @@ void rows_of_type(const DistillArgs& a, const T* x, T* g, int mode, int64_t rows
 }
 
 }  // namespace
+
+size_t distill_ws_bytes(int64_t rows, int V, int K, int type) {
+  const int parts = row_parts(rows, V, type);
+  return parts > 1 ? (size_t)rows * (parts * sizeof(PartStats) + (K + 1) * 4) : 0;
+}
 
 hipError_t launch_distill_count(const int32_t* targets, int64_t rows, int V, float* n_counted, hipStream_t st) {
   if (!distill_counts(targets, rows)) return hipSuccess;
@@ -390,6 +399,8 @@ hipError_t launch_distill_rows(const DistillArgs& args, const void* logits, void
   const bool soft_only = a.soft == 1.f && a.z_loss == 0.f;
   const int mode = a.tau == 1.f || a.soft == 0.f || soft_only ? EXP_ONE : a.tau == 2.f ? EXP_SQUARE : a.tau == 4.f ? EXP_FOURTH : EXP_TWO;
   a.exp_scale = a.soft == 0.f ? kLog2e : kLog2e * a.inv_tau;
+  a.rows = rows;
+  a.parts = row_parts(rows, a.V, type);
   a.apart = out && (((uintptr_t)out ^ (uintptr_t)logits) & 15) != 0;
   if (type == IN_BF16) {
     if (out) rows_of_type<bf16, true>(a, (const bf16*)logits, (bf16*)out, mode, rows, st);

@@ -299,9 +299,12 @@ struct DistillArgs {
   int64_t ld, all_rows;
   int32_t K, V;
   float tau, inv_tau, soft, z_loss;
-  float exp_scale;  // the last two are set by launch_distill_rows
-  int32_t apart;
+  void* partial;  // distill_ws_bytes(rows, ...) bytes
+  float exp_scale;  // the last four are set by launch_distill_rows
+  int32_t apart, parts;
+  int64_t rows;
 };
+size_t distill_ws_bytes(int64_t rows, int V, int K, int type);
 // Number of the batch's rows that count (nothing where launch_distill_rows does without).
 hipError_t launch_distill_count(const int32_t* targets, int64_t rows, int V, float* n_counted, hipStream_t st);
 // Row losses and, with out (the logits themselves, or a buffer of the same row stride), the gradient of the mean.

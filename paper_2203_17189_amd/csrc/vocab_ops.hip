@@ -41,11 +41,13 @@ int check_distill(const t5_distill_cfg* c, int* ty) {
 
 struct DistillWs {
   float *n_counted, *row_loss;
+  void* partial;
 };
-size_t carve_distill(const t5_distill_cfg* c, void* base, DistillWs* w) {
+size_t carve_distill(const t5_distill_cfg* c, int ty, void* base, DistillWs* w) {
   Carver cv(base);
   w->n_counted = cv.take<float>(256);
   w->row_loss = cv.take<float>((size_t)c->rows * 4);
+  w->partial = cv.take(distill_ws_bytes(c->rows, c->vocab, c->top_k, ty));
   return cv.off;
 }
 
@@ -99,7 +101,7 @@ size_t t5_distill_workspace_bytes(const t5_distill_cfg* cfg) {
   int ty;
   DistillWs w;
   if (check_distill(cfg, &ty) != T5_OK) return 0;
-  return carve_distill(cfg, nullptr, &w);
+  return carve_distill(cfg, ty, nullptr, &w);
 }
 
 int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, const int32_t* targets,
@@ -112,11 +114,11 @@ int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, cons
   if (cfg->rows > 0 && (!logits || !teacher_logits || !teacher_ids || (!targets && cfg->soft_weight != 1.f)))
     return T5_ERR_NULL;
   DistillWs w;
-  if (workspace_bytes < carve_distill(cfg, workspace, &w)) return T5_ERR_WORKSPACE;
+  if (workspace_bytes < carve_distill(cfg, ty, workspace, &w)) return T5_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   DistillArgs a;
   a.targets = targets; a.teacher_logits = teacher_logits; a.teacher_ids = teacher_ids; a.n_counted = w.n_counted;
-  a.all_targets = targets; a.all_rows = cfg->rows;
+  a.all_targets = targets; a.all_rows = cfg->rows; a.partial = w.partial;
   a.row_loss = row_loss ? row_loss : w.row_loss;
   a.ld = cfg->ld; a.K = cfg->top_k; a.V = cfg->vocab;
   a.tau = cfg->temperature; a.inv_tau = 1.f / cfg->temperature; a.soft = cfg->soft_weight; a.z_loss = cfg->z_loss;

@@ -46,7 +46,7 @@ def check(P, x, tgt, t, ids, tau, soft, z, dtype, tx=None, out=None):
 
 
 CASES = [(1, 2, 1), (1, 7, 7), (4, 33, 8), (7, 256, 16), (9, 509, 8), (8, 2048, 64), (8, 2056, 256), (7, 4100, 100),
-         (16, 32128, 64), (8, 32776, 32), (8, 65537, 40), (7, 131072, 128), (300, 700, 5)]
+         (16, 32128, 64), (8, 32776, 32), (8, 65537, 40), (7, 131072, 128), (300, 700, 5), (260, 33001, 9), (1030, 40, 3), (513, 5000, 20)]
 MIX = [(1.0, 1.0, 0.0), (2.0, 0.5, 1e-4), (0.7, 0.9, 1e-2), (1.0, 0.0, 1e-3), (4.0, 1.0, 0.0)]
 
 
@@ -118,8 +118,32 @@ def test_masked_logits(vocab, dtype):
     loss, row, g = P.t5_distill_loss_and_grad(tx, ints(tgt), dev(t), ints(ids), soft_weight=0.5)
     assert float(row[8]) == np.inf and bool(torch.isfinite(g[8].float()).all()) and float(loss) == np.inf
     # with soft_weight 0 the teacher does not matter
-    loss, row, _ = P.t5_distill_loss_and_grad(tx, ints(tgt), dev(t), ints(ids), soft_weight=0.0)
-    assert np.isfinite(float(row[8]))
+    loss, row, g = P.t5_distill_loss_and_grad(tx, ints(tgt), dev(t * np.nan), ints(ids), soft_weight=0.0)
+    assert np.isfinite(float(row[8])) and bool(torch.isfinite(g.float()).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [509, 4096, 40000, 140000])
+def test_far_from_zero(vocab, dtype):
+    """Rows shifted far from 0, and rows of nothing but the type's lowest value (uniform: loss log V, gradient 1 / V)."""
+    import paper_2203_17189_amd as P
+    x, _, t, ids = make(6, vocab, 4, 21)
+    tgt = np.array([5, 6, 7, 8, 9, 10])
+    ids[:] = np.arange(4)
+    t[3, 2:] = t[3, 0]
+    x[1] += 3000.0
+    x[2] -= 3000.0
+    x[4] = float(torch.finfo(torch.bfloat16).min)
+    x[5] = float(torch.finfo(torch.bfloat16).max)
+    for tau, soft in ((1.0, 0.5), (0.5, 0.5), (2.0, 0.5), (2.0, 1.0), (1.0, 0.0)):
+        tx = dev(x, dtype)
+        _, row, g = P.t5_distill_loss_and_grad(tx, ints(tgt), dev(t), ints(ids), temperature=tau, soft_weight=soft)
+        hx, ht = host(tx), np.float32(t).astype(float)
+        _, wr, wg = VO.distill_loss(hx, tgt, ht, ids, tau, soft)
+        shifted = hx - hx.max(1, keepdims=True)   # the loss without z does not depend on the shift
+        rt, gt = distill_bounds(shifted, tgt, ht, ids, tau, soft, 0.0, dtype, wr, wg)
+        assert np.all(np.abs(host(row) - wr) <= rt), (tau, soft, np.abs(host(row) - wr) / rt)
+        assert np.all(np.abs(host(g) - wg) <= gt)
 
 
 @pytest.mark.parametrize("vocab", [100, 4096, 40000])
