@@ -75,19 +75,23 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   __shared__ int s_id[256];
   __shared__ float s_p[256];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, V = a.V;
-  const int64_t row = blockIdx.x;
+  // the parts of a row are neighbours: workgroups that start together read one stretch of memory, not one part of many
+  // rows a power of two apart
+  const int parts = PHASE == WHOLE_ROW || (PHASE == PART_APPLY && !GRAD) ? 1 : a.parts;
+  const uint32_t row = blockIdx.x / parts;
+  const int part = blockIdx.x - row * parts;
   const T* x = logits + row * a.ld;
   T* g = GRAD ? out + row * a.ld : nullptr;
   const RowSplit<T> sp(x, V);
   const u32x4* body = reinterpret_cast<const u32x4*>(x + sp.head);
   u32x4* gbody = GRAD ? reinterpret_cast<u32x4*>(g + sp.head) : nullptr;
   // pieces [first, last] are this workgroup's, the elements around them the first part's
-  const int part = PHASE == WHOLE_ROW ? 0 : blockIdx.y, first = part * (NT * NV);
+  const int first = part * (NT * NV);
   const int last = PHASE == WHOLE_ROW ? sp.pieces - 1 : min(sp.pieces, first + NT * NV) - 1;
   const int own = part == 0 ? sp.single(tid, NT, V) : -1;
-  PartStats* stats = (PartStats*)a.partial + row * a.parts;
+  PartStats* stats = (PartStats*)a.partial + (size_t)row * a.parts;
   // logits of the entries and of the target, as they were before any part's gradient was written over them
-  float* picked = (float*)((PartStats*)a.partial + a.rows * a.parts) + row * (a.K + 1);
+  float* picked = (float*)((PartStats*)a.partial + a.rows * a.parts) + (size_t)row * (a.K + 1);
   const int tgt = a.targets ? a.targets[row] : -1;
   const bool hard = tgt >= 0 && tgt < V;
   // (the gradient's rows need not lie on 16-byte boundaries where the logits' rows do)
@@ -131,10 +135,10 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
     t[q] = -INFINITY;
     xk[q] = 0.f;
     if ((PHASE != PART_STATS || part == 0) && k < a.K) {
-      id[q] = a.teacher_ids[row * a.K + k];
+      id[q] = a.teacher_ids[(size_t)row * a.K + k];
       if (id[q] < 0 || id[q] >= V || a.soft == 0.f) id[q] = -1;
       if (id[q] >= 0) {
-        t[q] = a.teacher_logits[row * a.K + k];
+        t[q] = a.teacher_logits[(size_t)row * a.K + k];
         xk[q] = PHASE == PART_APPLY ? picked[k] : to_f32(x[id[q]]);
       }
     }
@@ -154,11 +158,7 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   // ---- largest element of the row, largest entry of the teacher
   float m = -INFINITY, s1 = 0.f, st = 0.f, tm = -INFINITY;
   if constexpr (PHASE == PART_APPLY) {
-    if (tid < a.parts) {
-      m = stats[tid].m;
-      s1 = stats[tid].s1;
-      st = stats[tid].st;
-    }
+    for (int j = tid; j < a.parts; j += NT) m = fmaxf(m, stats[j].m);
   } else {
     m = xs;
 #pragma unroll
@@ -171,7 +171,6 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   }
 #pragma unroll
   for (int q = 0; q < EK; ++q) tm = fmaxf(tm, t[q] != t[q] ? INFINITY : t[q]);  // (fmax passes a NaN over: it comes back in the sum)
-  const float own_m = m;
   m = wave_max(m);
   tm = wave_max(tm);
   if (self_count) {
@@ -199,10 +198,10 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   const float m0 = PHASE == PART_STATS && m == -INFINITY ? 0.f : m;
   // ---- sums
   if constexpr (PHASE == PART_APPLY) {
-    if (tid < a.parts) {
-      const Exps f = exps_of<MODE>(own_m - m0, ct);
-      s1 *= f.a;
-      st *= f.b;
+    for (int j = tid; j < a.parts; j += NT) {
+      const Exps f = exps_of<MODE>(stats[j].m - m, ct);
+      s1 = fmaf(stats[j].s1, f.a, s1);
+      st = fmaf(stats[j].st, f.b, st);
     }
   } else {
 #pragma unroll
@@ -341,25 +340,26 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float* __restr
   if (threadIdx.x == 0) *loss = s / fmaxf(n, 1.f);
 }
 
-constexpr int kPartPieces = 256 * 16;  // 64 KB of a row
+constexpr int kPartNV = 8;
+constexpr int kPartPieces = 256 * kPartNV;
 
 // Workgroups that share a row: 1, or parts of 64 KB for rows that do not fit one workgroup's registers, or that would
 // leave compute units without work.
 int row_parts(int64_t rows, int V, int type) {
   const int pieces = ceil_div(V, type == IN_BF16 ? 8 : 4);
-  return pieces <= kPartPieces || (pieces <= 16384 && rows >= 256) ? 1 : ceil_div(pieces, kPartPieces);
+  return pieces <= 4096 || (pieces <= 16384 && rows >= 256) ? 1 : ceil_div(pieces, kPartPieces);
 }
 
 template <typename T, int MODE, bool GRAD>
 void rows_of_mode(const DistillArgs& a, const T* x, T* g, int64_t rows, hipStream_t st) {
   const int pieces = ceil_div(a.V, 16 / (int)sizeof(T));
-  auto go = [&](auto kern, int nt) { kern<<<dim3((unsigned)rows, (unsigned)a.parts), nt, 0, st>>>(a, x, g); };
+  auto go = [&](auto kern, int nt) { kern<<<(unsigned)(rows * a.parts), nt, 0, st>>>(a, x, g); };
   if (a.parts > 1) {
-    go(distill_rows_kernel<T, 256, 16, MODE, PART_STATS, GRAD>, 256);
+    go(distill_rows_kernel<T, 256, kPartNV, MODE, PART_STATS, GRAD>, 256);
     if (GRAD) {
-      go(distill_rows_kernel<T, 256, 16, MODE, PART_APPLY, GRAD>, 256);
+      go(distill_rows_kernel<T, 256, kPartNV, MODE, PART_APPLY, GRAD>, 256);
     } else {
-      distill_rows_kernel<T, 256, 16, MODE, PART_APPLY, GRAD><<<(unsigned)rows, 256, 0, st>>>(a, x, g);
+      distill_rows_kernel<T, 256, kPartNV, MODE, PART_APPLY, GRAD><<<(unsigned)rows, 256, 0, st>>>(a, x, g);
     }
     return;
   }
@@ -368,6 +368,7 @@ void rows_of_mode(const DistillArgs& a, const T* x, T* g, int64_t rows, hipStrea
   else if (rows < 512 && pieces <= 4096) go(distill_rows_kernel<T, 1024, 4, MODE, WHOLE_ROW, GRAD>, 1024);
   else if (pieces <= 1024) go(distill_rows_kernel<T, 256, 4, MODE, WHOLE_ROW, GRAD>, 256);
   else if (pieces <= 4096) go(distill_rows_kernel<T, 256, 16, MODE, WHOLE_ROW, GRAD>, 256);
+  else if (pieces <= 8192) go(distill_rows_kernel<T, 512, 16, MODE, WHOLE_ROW, GRAD>, 512);
   else go(distill_rows_kernel<T, 1024, 16, MODE, WHOLE_ROW, GRAD>, 1024);
 }
 
@@ -401,6 +402,7 @@ hipError_t launch_distill_rows(const DistillArgs& args, const void* logits, void
   a.exp_scale = a.soft == 0.f ? kLog2e : kLog2e * a.inv_tau;
   a.rows = rows;
   a.parts = row_parts(rows, a.V, type);
+  if (rows * a.parts > INT32_MAX) return hipErrorInvalidValue;
   a.apart = out && (((uintptr_t)out ^ (uintptr_t)logits) & 15) != 0;
   if (type == IN_BF16) {
     if (out) rows_of_type<bf16, true>(a, (const bf16*)logits, (bf16*)out, mode, rows, st);
