@@ -402,6 +402,38 @@ int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, cons
                              const float* teacher_logits, const int32_t* teacher_ids, float* loss, float* row_loss,
                              void* dlogits, void* workspace, size_t workspace_bytes, void* stream);
 
+/* The same inside whole models.  The teacher's side: forward pass of a stack and the top_k largest logits of every
+ * position, values float32 and ids int32 [batch, seq, top_k] (decoder positions for the pair); the logits exist a chunk of
+ * tokens at a time, the workspace holds one layer's activations.  The configuration's dropout applies as everywhere: a
+ * teacher's has dropout_rate 0.
+ * The student's side: t5_stack_loss_and_grad with the loss of t5_distill_loss_and_grad in place of the cross-entropy,
+ * z_loss from the configuration, teacher_logits and teacher_ids [batch, seq, top_k].  The embedding gradient is the one
+ * of t5_embed_bwd (the same bits every time, whatever block.deterministic says).  All else as in the call it stands beside.
+ * Errors: as that call and t5_distill_loss_and_grad (top_k > vocab -> T5_ERR_SHAPE, > 256 -> T5_ERR_UNSUPPORTED). */
+typedef struct {
+  int32_t top_k;
+  float temperature;
+  float soft_weight;
+} t5_distill_opts;
+size_t t5_stack_top_logits_workspace_bytes(const t5_stack_cfg* cfg, int32_t top_k);
+int t5_stack_top_logits(const t5_stack_cfg* cfg, const int32_t* tokens, const t5_stack_weights* w, int32_t top_k,
+                        float* values, int32_t* ids, void* workspace, size_t workspace_bytes, void* stream);
+size_t t5_encdec_top_logits_workspace_bytes(const t5_encdec_cfg* cfg, int32_t top_k);
+int t5_encdec_top_logits(const t5_encdec_cfg* cfg, const int32_t* enc_tokens, const int32_t* dec_tokens,
+                         const t5_encdec_weights* w, int32_t top_k, float* values, int32_t* ids, void* workspace,
+                         size_t workspace_bytes, void* stream);
+size_t t5_stack_distill_workspace_bytes(const t5_stack_cfg* cfg, const t5_distill_opts* opts);
+int t5_stack_distill_loss_and_grad(const t5_stack_cfg* cfg, const t5_distill_opts* opts, const int32_t* tokens,
+                                   const int32_t* targets, const float* teacher_logits, const int32_t* teacher_ids,
+                                   const t5_stack_weights* w, float* loss, const t5_stack_grads* grads, int accumulate,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+size_t t5_encdec_distill_workspace_bytes(const t5_encdec_cfg* cfg, const t5_distill_opts* opts);
+int t5_encdec_distill_loss_and_grad(const t5_encdec_cfg* cfg, const t5_distill_opts* opts, const int32_t* enc_tokens,
+                                    const int32_t* dec_tokens, const int32_t* targets, const float* teacher_logits,
+                                    const int32_t* teacher_ids, const t5_encdec_weights* w, float* loss,
+                                    const t5_encdec_grads* grads, int accumulate, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
 /* Adafactor (the optimizer of the T5 models of paper Sec. 4) with factored second moments and
  * update clipping, no momentum, no weight decay, for one [rows, cols] float32 tensor:
  *   beta2 = 1 - step^-decay_pow;  Q = G*G + eps1

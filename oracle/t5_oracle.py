@@ -535,12 +535,14 @@ def stack_loss(sc, tokens: np.ndarray, targets: np.ndarray, w: dict):
                       lse=lse, n=n, m_embed=m_embed, m_final=m_final)
 
 
-def stack_loss_grad(sc, w: dict, saved: dict) -> dict:
+def stack_loss_grad(sc, w: dict, saved: dict, dlogits=None) -> dict:
     """Gradient of stack_loss w.r.t. every weight: {"embedding", "rel_table" (summed over layers),
-    "final_scale", "logits_w" (untied), "layers": [block gradient dicts without rel_table]}."""
+    "final_scale", "logits_w" (untied), "layers": [block gradient dicts without rel_table]}.
+    dlogits: gradient over the logits, of another loss on them; by default that of the cross-entropy with z-loss."""
     cfg = sc.block
     flat = lambda t: t.reshape(-1, t.shape[-1])
-    dlogits = xent_zloss_grad(saved["logits"], saved["targets"], saved["lse"], sc.z_loss, saved["n"])
+    if dlogits is None:
+        dlogits = xent_zloss_grad(saved["logits"], saved["targets"], saved["lse"], sc.z_loss, saved["n"])
     g = {"layers": [None] * sc.n_layers, "embedding": np.zeros_like(w["embedding"])}
     if sc.tied_logits:
         s = cfg.d_model ** -0.5
@@ -603,11 +605,12 @@ def encdec_loss(ec, enc_tokens: np.ndarray, dec_tokens: np.ndarray, targets: np.
                       lse=lse, n=n, masks=(me_embed, me_final, md_embed, md_final))
 
 
-def encdec_loss_grad(ec, w: dict, saved: dict) -> dict:
-    """Gradient of encdec_loss w.r.t. every weight (same nesting as the weights)."""
+def encdec_loss_grad(ec, w: dict, saved: dict, dlogits=None) -> dict:
+    """Gradient of encdec_loss w.r.t. every weight (same nesting as the weights); dlogits as in stack_loss_grad."""
     e, d = ec.enc_block, ec.dec_block
     flat = lambda t: t.reshape(-1, t.shape[-1])
-    dlogits = xent_zloss_grad(saved["logits"], saved["targets"], saved["lse"], ec.z_loss, saved["n"])
+    if dlogits is None:
+        dlogits = xent_zloss_grad(saved["logits"], saved["targets"], saved["lse"], ec.z_loss, saved["n"])
     g = {"embedding": np.zeros_like(w["embedding"]), "enc_layers": [None] * ec.n_enc_layers,
          "dec_layers": [None] * ec.n_dec_layers}
     if ec.tied_logits:

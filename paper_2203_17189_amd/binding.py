@@ -91,6 +91,10 @@ class _DistillCfg(C.Structure):
     _fields_ = _TopCfg._fields_ + [("temperature", C.c_float), ("soft_weight", C.c_float), ("z_loss", C.c_float)]
 
 
+class _DistillOpts(C.Structure):
+    _fields_ = [("top_k", C.c_int32), ("temperature", C.c_float), ("soft_weight", C.c_float)]
+
+
 class _AfTensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("v_row", C.c_void_p), ("v_col", C.c_void_p),
                 ("v_full", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("factored", C.c_int32),
@@ -156,6 +160,24 @@ def lib() -> C.CDLL:
     L.t5_encdec_loss_and_grad.restype = i32
     L.t5_encdec_loss_and_grad.argtypes = [C.POINTER(_EncDecCfg), vp, vp, vp, C.POINTER(_EncDecWeights), vp,
                                           C.POINTER(_EncDecGrads), i32, vp, sz, vp]
+    L.t5_stack_top_logits_workspace_bytes.restype = sz
+    L.t5_stack_top_logits_workspace_bytes.argtypes = [C.POINTER(_StackCfg), C.c_int32]
+    L.t5_stack_top_logits.restype = i32
+    L.t5_stack_top_logits.argtypes = [C.POINTER(_StackCfg), vp, C.POINTER(_StackWeights), C.c_int32, vp, vp, vp, sz, vp]
+    L.t5_encdec_top_logits_workspace_bytes.restype = sz
+    L.t5_encdec_top_logits_workspace_bytes.argtypes = [C.POINTER(_EncDecCfg), C.c_int32]
+    L.t5_encdec_top_logits.restype = i32
+    L.t5_encdec_top_logits.argtypes = [C.POINTER(_EncDecCfg), vp, vp, C.POINTER(_EncDecWeights), C.c_int32, vp, vp, vp, sz, vp]
+    L.t5_stack_distill_workspace_bytes.restype = sz
+    L.t5_stack_distill_workspace_bytes.argtypes = [C.POINTER(_StackCfg), C.POINTER(_DistillOpts)]
+    L.t5_stack_distill_loss_and_grad.restype = i32
+    L.t5_stack_distill_loss_and_grad.argtypes = [C.POINTER(_StackCfg), C.POINTER(_DistillOpts), vp, vp, vp, vp,
+                                                 C.POINTER(_StackWeights), vp, C.POINTER(_StackGrads), i32, vp, sz, vp]
+    L.t5_encdec_distill_workspace_bytes.restype = sz
+    L.t5_encdec_distill_workspace_bytes.argtypes = [C.POINTER(_EncDecCfg), C.POINTER(_DistillOpts)]
+    L.t5_encdec_distill_loss_and_grad.restype = i32
+    L.t5_encdec_distill_loss_and_grad.argtypes = [C.POINTER(_EncDecCfg), C.POINTER(_DistillOpts), vp, vp, vp, vp, vp,
+                                                  C.POINTER(_EncDecWeights), vp, C.POINTER(_EncDecGrads), i32, vp, sz, vp]
     L.adafactor_workspace_bytes.restype = sz
     L.adafactor_workspace_bytes.argtypes = [i64, i64, i32]
     L.adafactor_step.restype = i32
@@ -448,17 +470,9 @@ def alloc_stack_grads(sc, weights) -> dict:
     return g
 
 
-def t5_stack_loss_and_grad(sc, tokens, targets, weights, grads=None, want_grads=True, accumulate=False,
-                           workspace=None, loss=None):
-    """Loss (and gradients) of a stack of blocks with embedding, final norm, logits and cross-entropy with
-    z-loss.  weights: {"embedding", "rel_table", "final_scale", "logits_w" (untied), "layers": [dict of the
-    block's tensors without rel_table, per layer]}.  Returns (loss tensor of one float32, grads or None)."""
+def _stack_weights_struct(sc, weights) -> _StackWeights:
     b = sc.block
-    cs = _stack_cfg_struct(sc)
     dt = _torch_dtype(b)
-    n_tok = b.batch * b.seq
-    _check_tensor(tokens, torch.int32, n_tok, "tokens")
-    _check_tensor(targets, torch.int32, n_tok, "targets")
     _check_tensor(weights["embedding"], dt, sc.vocab * b.d_model, "embedding")
     _check_tensor(weights["rel_table"], dt, b.num_buckets * b.n_heads, "rel_table")
     _check_tensor(weights["final_scale"], dt, b.d_model, "final_scale")
@@ -469,25 +483,42 @@ def t5_stack_loss_and_grad(sc, tokens, targets, weights, grads=None, want_grads=
     lw = (_Weights * sc.n_layers)()
     for l, d in enumerate(weights["layers"]):
         lw[l] = _weights_struct(b, dict(d, rel_table=weights["rel_table"]))
-    ws = _StackWeights(weights["embedding"].data_ptr(), weights["rel_table"].data_ptr(), lw,
-                       weights["final_scale"].data_ptr(),
-                       None if sc.tied_logits else weights["logits_w"].data_ptr())
+    return _StackWeights(weights["embedding"].data_ptr(), weights["rel_table"].data_ptr(), lw,
+                         weights["final_scale"].data_ptr(),
+                         None if sc.tied_logits else weights["logits_w"].data_ptr())
+
+
+def _stack_grads_struct(sc, weights, grads) -> _StackGrads:
+    b = sc.block
+    names = ["embedding", "rel_table", "final_scale"] + ([] if sc.tied_logits else ["logits_w"])
+    for nme in names:
+        _check_tensor(grads[nme], torch.float32, weights[nme].numel(), "grad " + nme)
+    lg = (_Grads * sc.n_layers)()
+    for l, d in enumerate(grads["layers"]):
+        for nme in _block_names(b, LAYER_WEIGHT_NAMES):
+            _check_tensor(d[nme], torch.float32, weights["layers"][l][nme].numel(), f"grad layer {l} {nme}")
+        lg[l] = _Grads(*[(_addr(d, nme) if nme != "rel_table" else grads["rel_table"].data_ptr())
+                         for nme in WEIGHT_NAMES])
+    return _StackGrads(grads["embedding"].data_ptr(), grads["rel_table"].data_ptr(), lg,
+                       grads["final_scale"].data_ptr(), None if sc.tied_logits else grads["logits_w"].data_ptr())
+
+
+def t5_stack_loss_and_grad(sc, tokens, targets, weights, grads=None, want_grads=True, accumulate=False,
+                           workspace=None, loss=None):
+    """Loss (and gradients) of a stack of blocks with embedding, final norm, logits and cross-entropy with
+    z-loss.  weights: {"embedding", "rel_table", "final_scale", "logits_w" (untied), "layers": [dict of the
+    block's tensors without rel_table, per layer]}.  Returns (loss tensor of one float32, grads or None)."""
+    b = sc.block
+    cs = _stack_cfg_struct(sc)
+    n_tok = b.batch * b.seq
+    _check_tensor(tokens, torch.int32, n_tok, "tokens")
+    _check_tensor(targets, torch.int32, n_tok, "targets")
+    ws = _stack_weights_struct(sc, weights)
     gs_ref = None
     if want_grads:
         if grads is None:
             grads = alloc_stack_grads(sc, weights)
-        names = ["embedding", "rel_table", "final_scale"] + ([] if sc.tied_logits else ["logits_w"])
-        for nme in names:
-            _check_tensor(grads[nme], torch.float32, weights[nme].numel(), "grad " + nme)
-        lg = (_Grads * sc.n_layers)()
-        for l, d in enumerate(grads["layers"]):
-            for nme in _block_names(b, LAYER_WEIGHT_NAMES):
-                _check_tensor(d[nme], torch.float32, weights["layers"][l][nme].numel(), f"grad layer {l} {nme}")
-            lg[l] = _Grads(*[(_addr(d, nme) if nme != "rel_table" else grads["rel_table"].data_ptr())
-                             for nme in WEIGHT_NAMES])
-        gs = _StackGrads(grads["embedding"].data_ptr(), grads["rel_table"].data_ptr(), lg,
-                         grads["final_scale"].data_ptr(), None if sc.tied_logits else grads["logits_w"].data_ptr())
-        gs_ref = C.byref(gs)
+        gs_ref = C.byref(_stack_grads_struct(sc, weights, grads))
     else:
         grads = None
     if loss is None:
@@ -498,6 +529,74 @@ def t5_stack_loss_and_grad(sc, tokens, targets, weights, grads=None, want_grads=
                                       int(bool(accumulate)), _ptr(workspace), workspace.numel(), _stream())
     if rc:
         raise T5Error(rc, "t5_stack_loss_and_grad")
+    return loss, grads
+
+
+def _top_outputs(batch, seq, top_k, device, values, ids):
+    if values is None:
+        values = torch.empty(batch, seq, top_k, dtype=torch.float32, device=device)
+    if ids is None:
+        ids = torch.empty(batch, seq, top_k, dtype=torch.int32, device=device)
+    _check_on(device, values, torch.float32, batch * seq * top_k, "values")
+    _check_on(device, ids, torch.int32, batch * seq * top_k, "ids")
+    return values, ids
+
+
+def _model_workspace(workspace, nbytes, device):
+    if workspace is None:
+        return _byte_buffer(nbytes, device)
+    _check_on(device, workspace, torch.uint8, workspace.numel(), "workspace")
+    return workspace
+
+
+def _teacher_entries(n_tok, teacher_logits, teacher_ids, device):
+    """Entries per position of a teacher's top logits [..., top_k]."""
+    k = teacher_ids.shape[-1]
+    _check_on(device, teacher_ids, torch.int32, n_tok * k, "teacher_ids")
+    _check_on(device, teacher_logits, torch.float32, n_tok * k, "teacher_logits")
+    return k
+
+
+def t5_stack_top_logits(sc, tokens, weights, top_k, values=None, ids=None, workspace=None):
+    """Forward pass of a stack; (values float32, ids int32), both [batch, seq, top_k]: the largest logits of every position,
+    descending, equal ones by ascending id."""
+    b, dev = sc.block, tokens.device
+    cs = _stack_cfg_struct(sc)
+    _check_tensor(tokens, torch.int32, b.batch * b.seq, "tokens")
+    ws = _stack_weights_struct(sc, weights)
+    nbytes = lib().t5_stack_top_logits_workspace_bytes(C.byref(cs), top_k)
+    if nbytes:  # (0: the call below says what is wrong)
+        values, ids = _top_outputs(b.batch, b.seq, top_k, dev, values, ids)
+    workspace = _model_workspace(workspace, nbytes, dev)
+    _call(lib().t5_stack_top_logits, "t5_stack_top_logits", dev, C.byref(cs), tokens.data_ptr(), C.byref(ws), top_k,
+          _ptr(values), _ptr(ids), workspace.data_ptr(), workspace.numel())
+    return values, ids
+
+
+def t5_stack_distill_loss_and_grad(sc, tokens, targets, teacher_logits, teacher_ids, weights, temperature=1.0,
+                                   soft_weight=1.0, grads=None, want_grads=True, accumulate=False, workspace=None, loss=None):
+    """t5_stack_loss_and_grad against a teacher's top logits (float32) and ids (int32), both [batch, seq, top_k], as
+    t5_stack_top_logits gives them.  Returns (loss tensor of one float32, grads or None)."""
+    b, dev = sc.block, tokens.device
+    cs = _stack_cfg_struct(sc)
+    n_tok = b.batch * b.seq
+    _check_tensor(tokens, torch.int32, n_tok, "tokens")
+    _check_on(dev, targets, torch.int32, n_tok, "targets")
+    opts = _DistillOpts(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev), temperature, soft_weight)
+    ws = _stack_weights_struct(sc, weights)
+    gs_ref = None
+    if want_grads:
+        if grads is None:
+            grads = alloc_stack_grads(sc, weights)
+        gs_ref = C.byref(_stack_grads_struct(sc, weights, grads))
+    else:
+        grads = None
+    if loss is None:
+        loss = torch.zeros(1, dtype=torch.float32, device=dev)
+    workspace = _model_workspace(workspace, lib().t5_stack_distill_workspace_bytes(C.byref(cs), C.byref(opts)), dev)
+    _call(lib().t5_stack_distill_loss_and_grad, "t5_stack_distill_loss_and_grad", dev, C.byref(cs), C.byref(opts),
+          tokens.data_ptr(), targets.data_ptr(), teacher_logits.data_ptr(), teacher_ids.data_ptr(), C.byref(ws),
+          loss.data_ptr(), gs_ref, int(bool(accumulate)), workspace.data_ptr(), workspace.numel())
     return loss, grads
 
 
@@ -525,18 +624,9 @@ def alloc_encdec_grads(ec, weights) -> dict:
     return g
 
 
-def t5_encdec_loss_and_grad(ec, enc_tokens, dec_tokens, targets, weights, grads=None, want_grads=True,
-                            accumulate=False, workspace=None, loss=None):
-    """Loss (and gradients) of the encoder-decoder model.  weights: {"embedding", "enc_rel_table",
-    "enc_layers": [block dicts without rel_table], "enc_final_scale", "dec_rel_table", "dec_layers": [block +
-    cross-attention dicts without rel_table], "dec_final_scale", "logits_w" (untied)}.
-    Returns (loss tensor of one float32, grads or None)."""
+def _encdec_weights_struct(ec, weights) -> _EncDecWeights:
     e, d = ec.enc_block, ec.dec_block
-    cs = _encdec_cfg_struct(ec)
     dt = _torch_dtype(d)
-    _check_tensor(enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
-    _check_tensor(dec_tokens, torch.int32, d.batch * d.seq, "dec_tokens")
-    _check_tensor(targets, torch.int32, d.batch * d.seq, "targets")
     _check_tensor(weights["embedding"], dt, ec.vocab * d.d_model, "embedding")
     for nme, cfgb in (("enc_rel_table", e), ("dec_rel_table", d)):
         _check_tensor(weights[nme], dt, cfgb.num_buckets * cfgb.n_heads, nme)
@@ -555,31 +645,50 @@ def t5_encdec_loss_and_grad(ec, enc_tokens, dec_tokens, targets, weights, grads=
         dlw[l] = _weights_struct(d, dict(lw, rel_table=weights["dec_rel_table"]))
         dxw[l] = _cross_weights_struct(d, lw)
     p = lambda t: t.data_ptr()
-    ws = _EncDecWeights(p(weights["embedding"]), p(weights["enc_rel_table"]), elw, p(weights["enc_final_scale"]),
-                        p(weights["dec_rel_table"]), dlw, dxw, p(weights["dec_final_scale"]),
-                        None if ec.tied_logits else p(weights["logits_w"]))
+    return _EncDecWeights(p(weights["embedding"]), p(weights["enc_rel_table"]), elw, p(weights["enc_final_scale"]),
+                          p(weights["dec_rel_table"]), dlw, dxw, p(weights["dec_final_scale"]),
+                          None if ec.tied_logits else p(weights["logits_w"]))
+
+
+def _encdec_grads_struct(ec, weights, grads) -> _EncDecGrads:
+    e, d = ec.enc_block, ec.dec_block
+    p = lambda t: t.data_ptr()
+    for nme in _ENCDEC_FLAT + (() if ec.tied_logits else ("logits_w",)):
+        _check_tensor(grads[nme], torch.float32, weights[nme].numel(), "grad " + nme)
+    elg = (_Grads * ec.n_enc_layers)()
+    for l, gd in enumerate(grads["enc_layers"]):
+        for nme in _block_names(e, LAYER_WEIGHT_NAMES):
+            _check_tensor(gd[nme], torch.float32, weights["enc_layers"][l][nme].numel(), f"grad enc {l} {nme}")
+        elg[l] = _Grads(*[(_addr(gd, nme) if nme != "rel_table" else p(grads["enc_rel_table"])) for nme in WEIGHT_NAMES])
+    dlg = (_Grads * ec.n_dec_layers)()
+    dxg = (_CrossGrads * ec.n_dec_layers)()
+    for l, gd in enumerate(grads["dec_layers"]):
+        for nme in _block_names(d, LAYER_WEIGHT_NAMES) + CROSS_WEIGHT_NAMES:
+            _check_tensor(gd[nme], torch.float32, weights["dec_layers"][l][nme].numel(), f"grad dec {l} {nme}")
+        dlg[l] = _Grads(*[(_addr(gd, nme) if nme != "rel_table" else p(grads["dec_rel_table"])) for nme in WEIGHT_NAMES])
+        dxg[l] = _CrossGrads(*[p(gd[nme]) for nme in CROSS_WEIGHT_NAMES])
+    return _EncDecGrads(p(grads["embedding"]), p(grads["enc_rel_table"]), elg, p(grads["enc_final_scale"]),
+                        p(grads["dec_rel_table"]), dlg, dxg, p(grads["dec_final_scale"]),
+                        None if ec.tied_logits else p(grads["logits_w"]))
+
+
+def t5_encdec_loss_and_grad(ec, enc_tokens, dec_tokens, targets, weights, grads=None, want_grads=True,
+                            accumulate=False, workspace=None, loss=None):
+    """Loss (and gradients) of the encoder-decoder model.  weights: {"embedding", "enc_rel_table",
+    "enc_layers": [block dicts without rel_table], "enc_final_scale", "dec_rel_table", "dec_layers": [block +
+    cross-attention dicts without rel_table], "dec_final_scale", "logits_w" (untied)}.
+    Returns (loss tensor of one float32, grads or None)."""
+    e, d = ec.enc_block, ec.dec_block
+    cs = _encdec_cfg_struct(ec)
+    _check_tensor(enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
+    _check_tensor(dec_tokens, torch.int32, d.batch * d.seq, "dec_tokens")
+    _check_tensor(targets, torch.int32, d.batch * d.seq, "targets")
+    ws = _encdec_weights_struct(ec, weights)
     gs_ref = None
     if want_grads:
         if grads is None:
             grads = alloc_encdec_grads(ec, weights)
-        for nme in _ENCDEC_FLAT + (() if ec.tied_logits else ("logits_w",)):
-            _check_tensor(grads[nme], torch.float32, weights[nme].numel(), "grad " + nme)
-        elg = (_Grads * ec.n_enc_layers)()
-        for l, gd in enumerate(grads["enc_layers"]):
-            for nme in _block_names(e, LAYER_WEIGHT_NAMES):
-                _check_tensor(gd[nme], torch.float32, weights["enc_layers"][l][nme].numel(), f"grad enc {l} {nme}")
-            elg[l] = _Grads(*[(_addr(gd, nme) if nme != "rel_table" else p(grads["enc_rel_table"])) for nme in WEIGHT_NAMES])
-        dlg = (_Grads * ec.n_dec_layers)()
-        dxg = (_CrossGrads * ec.n_dec_layers)()
-        for l, gd in enumerate(grads["dec_layers"]):
-            for nme in _block_names(d, LAYER_WEIGHT_NAMES) + CROSS_WEIGHT_NAMES:
-                _check_tensor(gd[nme], torch.float32, weights["dec_layers"][l][nme].numel(), f"grad dec {l} {nme}")
-            dlg[l] = _Grads(*[(_addr(gd, nme) if nme != "rel_table" else p(grads["dec_rel_table"])) for nme in WEIGHT_NAMES])
-            dxg[l] = _CrossGrads(*[p(gd[nme]) for nme in CROSS_WEIGHT_NAMES])
-        gs = _EncDecGrads(p(grads["embedding"]), p(grads["enc_rel_table"]), elg, p(grads["enc_final_scale"]),
-                          p(grads["dec_rel_table"]), dlg, dxg, p(grads["dec_final_scale"]),
-                          None if ec.tied_logits else p(grads["logits_w"]))
-        gs_ref = C.byref(gs)
+        gs_ref = C.byref(_encdec_grads_struct(ec, weights, grads))
     else:
         grads = None
     if loss is None:
@@ -591,6 +700,51 @@ def t5_encdec_loss_and_grad(ec, enc_tokens, dec_tokens, targets, weights, grads=
                                        _stream())
     if rc:
         raise T5Error(rc, "t5_encdec_loss_and_grad")
+    return loss, grads
+
+
+def t5_encdec_top_logits(ec, enc_tokens, dec_tokens, weights, top_k, values=None, ids=None, workspace=None):
+    """t5_stack_top_logits for the encoder-decoder model: the largest logits of every decoder position."""
+    e, d, dev = ec.enc_block, ec.dec_block, dec_tokens.device
+    cs = _encdec_cfg_struct(ec)
+    _check_tensor(enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
+    _check_tensor(dec_tokens, torch.int32, d.batch * d.seq, "dec_tokens")
+    ws = _encdec_weights_struct(ec, weights)
+    nbytes = lib().t5_encdec_top_logits_workspace_bytes(C.byref(cs), top_k)
+    if nbytes:  # (0: the call below says what is wrong)
+        values, ids = _top_outputs(d.batch, d.seq, top_k, dev, values, ids)
+    workspace = _model_workspace(workspace, nbytes, dev)
+    _call(lib().t5_encdec_top_logits, "t5_encdec_top_logits", dev, C.byref(cs), enc_tokens.data_ptr(),
+          dec_tokens.data_ptr(), C.byref(ws), top_k, _ptr(values), _ptr(ids), workspace.data_ptr(), workspace.numel())
+    return values, ids
+
+
+def t5_encdec_distill_loss_and_grad(ec, enc_tokens, dec_tokens, targets, teacher_logits, teacher_ids, weights,
+                                    temperature=1.0, soft_weight=1.0, grads=None, want_grads=True, accumulate=False,
+                                    workspace=None, loss=None):
+    """t5_encdec_loss_and_grad against a teacher's top logits and ids of the decoder positions, [batch, seq, top_k]."""
+    e, d, dev = ec.enc_block, ec.dec_block, dec_tokens.device
+    cs = _encdec_cfg_struct(ec)
+    n_tok = d.batch * d.seq
+    _check_tensor(dec_tokens, torch.int32, n_tok, "dec_tokens")
+    _check_on(dev, enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
+    _check_on(dev, targets, torch.int32, n_tok, "targets")
+    opts = _DistillOpts(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev), temperature, soft_weight)
+    ws = _encdec_weights_struct(ec, weights)
+    gs_ref = None
+    if want_grads:
+        if grads is None:
+            grads = alloc_encdec_grads(ec, weights)
+        gs_ref = C.byref(_encdec_grads_struct(ec, weights, grads))
+    else:
+        grads = None
+    if loss is None:
+        loss = torch.zeros(1, dtype=torch.float32, device=dev)
+    workspace = _model_workspace(workspace, lib().t5_encdec_distill_workspace_bytes(C.byref(cs), C.byref(opts)), dev)
+    _call(lib().t5_encdec_distill_loss_and_grad, "t5_encdec_distill_loss_and_grad", dev, C.byref(cs), C.byref(opts),
+          enc_tokens.data_ptr(), dec_tokens.data_ptr(), targets.data_ptr(), teacher_logits.data_ptr(),
+          teacher_ids.data_ptr(), C.byref(ws), loss.data_ptr(), gs_ref, int(bool(accumulate)), workspace.data_ptr(),
+          workspace.numel())
     return loss, grads
 
 

@@ -3,6 +3,7 @@
 // a single stack (decoder-only or encoder-style) and the encoder-decoder pair in which every decoder
 // layer cross-attends to the encoder's output.
 #include "block_host.h"
+#include "vocab_host.h"
 
 namespace {
 
@@ -61,8 +62,18 @@ bool wgrads_grouped_ok(const Dims& D, int L, bool remat) {
   return true;
 }
 
-void carve_layers(Carver& cv, Layers& s) {
+// forward_only: what layers_forward needs, with one stash for all layers
+void carve_layers(Carver& cv, Layers& s, bool forward_only = false) {
   const Dims& D = s.D;
+  if (forward_only) {
+    s.remat = true;
+    s.xs = cv.take((size_t)(s.L + 1) * s.xbytes());
+    s.stash_each = carve_stash(D, nullptr, nullptr);
+    s.stash = cv.take(s.stash_each);
+    s.diag = cv.take<float>((size_t)D.H * (2 * D.S - 1) * 4);
+    s.block_ws = cv.take(carve_fwd(D, nullptr, nullptr));
+    return;
+  }
   s.xs = cv.take((size_t)(s.L + 1) * s.xbytes());
   s.stash_each = carve_stash(D, nullptr, nullptr);
   s.stash = cv.take(s.stash_each * (s.remat ? 1 : s.L));
@@ -269,6 +280,11 @@ struct Head {
   void *nf = nullptr, *logits = nullptr, *wout_t = nullptr, *scale_s = nullptr;
   float *rf = nullptr, *loss_rows = nullptr, *n_valid = nullptr, *dnf = nullptr, *dg_tmp = nullptr,
         *dg_partial = nullptr;
+  // training from a teacher (opts set): its entries, [T, top_k], and room for the loss kernels and the sorted embedding gradient
+  const t5_distill_opts* opts = nullptr;
+  const float* teacher_logits = nullptr;
+  const int32_t* teacher_ids = nullptr;
+  void *distill_ws = nullptr, *embed_ws = nullptr;
   float* wg_partials = nullptr;  // float32, or reproducible mode: partial sums of the output-matrix gradient's k-slices
 };
 
@@ -285,17 +301,24 @@ void head_wgrad_gemm(const Head& h, const Dims& D, int tc, const void* nf_c, Gem
   e.aux0 = h.wg_partials;  // null unless carve_head took room for it
 }
 
-void carve_head(Carver& cv, Head& h, const Dims& D) {
+void carve_head(Carver& cv, Head& h, const Dims& D, bool forward_only = false) {
   h.nf = cv.take((size_t)D.T * D.d * D.es);
   h.logits = cv.take((size_t)h.chunk * h.V * D.es);
   h.wout_t = cv.take((size_t)h.V * D.d * D.es);
   h.scale_s = cv.take((size_t)D.d * D.es);
   h.rf = cv.take<float>(D.T * 4);
+  if (forward_only) return;
   h.loss_rows = cv.take<float>(D.T * 4);
   h.n_valid = cv.take<float>(256);
   h.dnf = cv.take<float>((size_t)D.T * D.d * 4);
   h.dg_tmp = cv.take<float>((size_t)D.d * 4);
   h.dg_partial = cv.take<float>((size_t)rmsnorm_bwd_partial_rows((int)D.T) * D.d * 4);
+  if (h.opts) {
+    // (fewer rows may be cut into more parts: the last chunk counts too)
+    const int64_t rest = D.T % h.chunk;
+    h.distill_ws = cv.take(std::max(distill_ws_bytes(h.chunk, h.V, h.opts->top_k, D.ty),
+                                    rest ? distill_ws_bytes(rest, h.V, h.opts->top_k, D.ty) : 0));
+  }
   h.wg_partials = nullptr;
   if (D.det && D.ty == IN_BF16) {
     GemmDesc g;
@@ -312,10 +335,15 @@ void carve_head(Carver& cv, Head& h, const Dims& D) {
   }
 }
 
-int head_loss_and_grad(const Head& h, const Dims& D, float rms_eps, const void* x_last, const int32_t* targets,
-                       float* loss, bool want_grads, int acc, void* dx_out, hipStream_t st) {
+// The MFMA GEMMs want the contraction index contiguous in both operands.  logits = nf W contracts over
+// d_model: E [V, d] has it contiguous, Wout [d, V] is transposed once per step.  dnf = dlogits W^T
+// contracts over the vocabulary: Wout has it contiguous, E is transposed once per step.
+bool head_mfma(const Head& h, const Dims& D) { return D.ty == IN_BF16 && D.d % 64 == 0 && h.V % 64 == 0; }
+
+// Final norm, and the output matrix as the GEMMs want it; *gf_out: the norm's scale as it was used.
+int head_norm(const Head& h, const Dims& D, float rms_eps, const void* x_last, bool want_grads, const void** gf_out,
+              hipStream_t st) {
   const int T = (int)D.T, ty = D.ty, V = h.V;
-  const size_t es = D.es;
   // tied logits: the factor d_model^-1/2 rides on the final norm's scale, nf' = RMSNorm(x; s gf) = s nf,
   // so logits = nf' E^T, dE += dlogits^T nf' and the norm backward returns d/d(s gf), scaled back below
   const float s_tied = h.tied ? 1.f / std::sqrt((float)D.d) : 1.f;
@@ -326,11 +354,7 @@ int head_loss_and_grad(const Head& h, const Dims& D, float rms_eps, const void* 
   }
   T5_STEP("rmsnorm_fwd", launch_rmsnorm_fwd(x_last, ty, gf, h.nf, ty, h.rf, T, D.d, rms_eps, st));
   T5_SUB(end_dropout(D, h.drop_site_final, h.nf, ty, st));  // the logits (and dW) see the dropped norm output
-  // The MFMA GEMMs want the contraction index contiguous in both operands.  logits = nf W contracts over
-  // d_model: E [V, d] has it contiguous, Wout [d, V] is transposed once per step.  dnf = dlogits W^T
-  // contracts over the vocabulary: Wout has it contiguous, E is transposed once per step.
-  const bool head_mfma = ty == IN_BF16 && D.d % 64 == 0 && V % 64 == 0;
-  if (head_mfma && (!h.tied || want_grads)) {
+  if (head_mfma(h, D) && (!h.tied || want_grads)) {
     PackJobs pj;
     std::memset(&pj, 0, sizeof(pj));
     if (h.tied) pj.j[0] = PackJob{{h.embedding, nullptr, nullptr}, 1, V, D.d, 0, h.wout_t};   // -> [d, V]
@@ -338,24 +362,52 @@ int head_loss_and_grad(const Head& h, const Dims& D, float rms_eps, const void* 
     pj.count = 1;
     T5_STEP("pack_logits_w", launch_pack_transpose_multi(pj, st));
   }
-  T5_STEP("xent_count", launch_xent_count(targets, D.T, V, h.n_valid, st));
+  *gf_out = gf;
+  return T5_OK;
+}
+
+// logits = nf W for the tc tokens whose norm outputs are at nf_c
+int head_logits(const Head& h, const Dims& D, int tc, const void* nf_c, hipStream_t st) {
+  const int ty = D.ty, V = h.V;
+  GemmDesc g;
+  if (h.tied) g = gemm1(tc, V, D.d, nf_c, D.d, 1, h.embedding, D.d, 1, ty);
+  else if (head_mfma(h, D)) g = gemm1(tc, V, D.d, nf_c, D.d, 1, h.wout_t, D.d, 1, ty);
+  else g = gemm1(tc, V, D.d, nf_c, D.d, 1, h.logits_w, V, 0, ty);
+  T5_STEP("gemm_logits", run_gemm(g, epi(EPI_STORE, h.logits, V, ty), st));
+  return T5_OK;
+}
+
+// The loss against a teacher of the logits of tokens [t0, t0 + tc), and its gradient over them.
+int head_distill_rows(const Head& h, const Dims& D, const int32_t* targets, int64_t t0, int tc, bool want_grads,
+                      hipStream_t st) {
+  DistillArgs a;
+  a.K = h.opts->top_k; a.V = h.V; a.ld = h.V;
+  a.targets = targets + t0; a.teacher_logits = h.teacher_logits + t0 * a.K; a.teacher_ids = h.teacher_ids + t0 * a.K;
+  a.all_targets = targets; a.all_rows = D.T; a.n_counted = h.n_valid; a.row_loss = h.loss_rows + t0; a.partial = h.distill_ws;
+  a.tau = h.opts->temperature; a.inv_tau = 1.f / a.tau; a.soft = h.opts->soft_weight; a.z_loss = h.z_loss;
+  T5_STEP("distill_rows", launch_distill_rows(a, h.logits, want_grads ? h.logits : nullptr, D.ty, tc, st));
+  return T5_OK;
+}
+
+int head_loss_and_grad(const Head& h, const Dims& D, float rms_eps, const void* x_last, const int32_t* targets,
+                       float* loss, bool want_grads, int acc, void* dx_out, hipStream_t st) {
+  const int T = (int)D.T, ty = D.ty, V = h.V;
+  const void* gf = nullptr;
+  T5_SUB(head_norm(h, D, rms_eps, x_last, want_grads, &gf, st));
+  if (h.opts) T5_STEP("distill_count", launch_distill_count(targets, D.T, V, h.n_valid, st));
+  else T5_STEP("xent_count", launch_xent_count(targets, D.T, V, h.n_valid, st));
   for (int64_t t0 = 0; t0 < D.T; t0 += h.chunk) {
     const int tc = (int)std::min<int64_t>(h.chunk, D.T - t0);
-    const void* nf_c = at((const void*)h.nf, (size_t)t0 * D.d, es);
-    {  // logits = nf W
-      GemmDesc g;
-      if (h.tied) g = gemm1(tc, V, D.d, nf_c, D.d, 1, h.embedding, D.d, 1, ty);
-      else if (head_mfma) g = gemm1(tc, V, D.d, nf_c, D.d, 1, h.wout_t, D.d, 1, ty);
-      else g = gemm1(tc, V, D.d, nf_c, D.d, 1, h.logits_w, V, 0, ty);
-      T5_STEP("gemm_logits", run_gemm(g, epi(EPI_STORE, h.logits, V, ty), st));
-    }
-    T5_STEP("xent_rows", launch_xent_rows(h.logits, ty, targets + t0, tc, V, V, h.z_loss, h.n_valid,
-                                          h.loss_rows + t0, want_grads ? 1 : 0, st));
+    const void* nf_c = at((const void*)h.nf, (size_t)t0 * D.d, D.es);
+    T5_SUB(head_logits(h, D, tc, nf_c, st));
+    if (h.opts) T5_SUB(head_distill_rows(h, D, targets, t0, tc, want_grads, st));
+    else T5_STEP("xent_rows", launch_xent_rows(h.logits, ty, targets + t0, tc, V, V, h.z_loss, h.n_valid,
+                                               h.loss_rows + t0, want_grads ? 1 : 0, st));
     if (!want_grads) continue;
     {  // dnf = dlogits W^T
       GemmDesc g;
       if (!h.tied) g = gemm1(tc, D.d, V, h.logits, V, 1, h.logits_w, V, 1, ty);
-      else if (head_mfma) g = gemm1(tc, D.d, V, h.logits, V, 1, h.wout_t, V, 1, ty);
+      else if (head_mfma(h, D)) g = gemm1(tc, D.d, V, h.logits, V, 1, h.wout_t, V, 1, ty);
       else g = gemm1(tc, D.d, V, h.logits, V, 1, h.embedding, D.d, 0, ty);
       T5_STEP("gemm_dnf", run_gemm(g, epi(EPI_STORE, h.dnf + (size_t)t0 * D.d, D.d, IN_F32), st));
     }
@@ -372,8 +424,10 @@ int head_loss_and_grad(const Head& h, const Dims& D, float rms_eps, const void* 
       }
     }
   }
-  T5_STEP("loss_reduce", launch_loss_reduce(h.loss_rows, D.T, h.n_valid, loss, st));
+  if (h.opts) T5_STEP("distill_mean", launch_distill_mean(h.loss_rows, targets, D.T, V, loss, st));
+  else T5_STEP("loss_reduce", launch_loss_reduce(h.loss_rows, D.T, h.n_valid, loss, st));
   if (!want_grads) return T5_OK;
+  const float s_tied = h.tied ? 1.f / std::sqrt((float)D.d) : 1.f;
   // gradient of the stack's last output through the final norm (no residual term)
   float* dg = h.tied ? h.dg_tmp : h.d_final_scale;
   T5_SUB(end_dropout(D, h.drop_site_final, h.dnf, IN_F32, st));
@@ -381,6 +435,29 @@ int head_loss_and_grad(const Head& h, const Dims& D, float rms_eps, const void* 
                                             ty == IN_F32 ? (float*)dx_out : nullptr, ty == IN_BF16 ? dx_out : nullptr,
                                             ty, dg, h.dg_partial, h.tied ? 0 : acc, T, D.d, st));
   if (h.tied) T5_STEP("axpy", launch_axpy_f32(h.d_final_scale, h.dg_tmp, s_tied, D.d, acc, st));
+  return T5_OK;
+}
+
+// Adds the gradient of the embedded tokens to the embedding's: sorted by token where a teacher trains the model, else as
+// the stack always has.
+int embed_gradient(const Head& h, const Dims& D, const int32_t* tokens, const void* dx0, float* d_embedding, hipStream_t st) {
+  if (h.opts)
+    T5_STEP("embed_bwd", launch_embed_sorted_bwd(tokens, dx0, D.ty, d_embedding, D.T, D.d, h.V, 1.f, 1, h.embed_ws, st));
+  else
+    T5_STEP("embed_bwd", launch_embed_bwd(tokens, dx0, D.ty, d_embedding, D.T, D.d, h.V, D.det, st));
+  return T5_OK;
+}
+
+// The K largest logits of every position.
+int head_top_logits(const Head& h, const Dims& D, float rms_eps, const void* x_last, int K, float* values, int32_t* ids,
+                    hipStream_t st) {
+  const void* gf = nullptr;
+  T5_SUB(head_norm(h, D, rms_eps, x_last, false, &gf, st));
+  for (int64_t t0 = 0; t0 < D.T; t0 += h.chunk) {
+    const int tc = (int)std::min<int64_t>(h.chunk, D.T - t0);
+    T5_SUB(head_logits(h, D, tc, at((const void*)h.nf, (size_t)t0 * D.d, D.es), st));
+    T5_STEP("top_logits", launch_top_logits(h.logits, D.ty, tc, h.V, h.V, K, values + t0 * K, ids + t0 * K, st));
+  }
   return T5_OK;
 }
 
@@ -415,11 +492,20 @@ int plan_stack(const t5_stack_cfg* c, StackPlan* p) {
   p->H.chunk = p->S.D.T < kLogitChunk ? (int)p->S.D.T : kLogitChunk;
   return T5_OK;
 }
-size_t carve_stack(StackPlan& p, void* base) {
+size_t carve_stack(StackPlan& p, void* base, bool forward_only = false) {
   Carver cv(base);
-  carve_layers(cv, p.S);
-  carve_head(cv, p.H, p.S.D);
+  carve_layers(cv, p.S, forward_only);
+  carve_head(cv, p.H, p.S.D, forward_only);
+  if (p.H.opts) p.H.embed_ws = cv.take(embed_sorted_ws_bytes(p.S.D.T, p.H.V, p.S.D.d));
   return cv.off;
+}
+int check_opts(const t5_distill_opts* o, int64_t rows, int vocab, float z_loss) {
+  if (!o) return T5_ERR_NULL;
+  t5_distill_cfg c;
+  c.rows = rows; c.ld = vocab; c.vocab = vocab; c.top_k = o->top_k; c.dtype = T5_F32;
+  c.temperature = o->temperature; c.soft_weight = o->soft_weight; c.z_loss = z_loss;
+  int ty;
+  return check_distill(&c, &ty);
 }
 
 // ---- encoder-decoder pair
@@ -451,35 +537,26 @@ int plan_encdec(const t5_encdec_cfg* c, EncDecPlan* p) {
   p->H.chunk = p->Dc.D.T < kLogitChunk ? (int)p->Dc.D.T : kLogitChunk;
   return T5_OK;
 }
-size_t carve_encdec(EncDecPlan& p, void* base) {
+size_t carve_encdec(EncDecPlan& p, void* base, bool forward_only = false) {
   Carver cv(base);
-  carve_layers(cv, p.E);
-  carve_layers(cv, p.Dc);
-  carve_head(cv, p.H, p.Dc.D);
+  carve_layers(cv, p.E, forward_only);
+  carve_layers(cv, p.Dc, forward_only);
+  carve_head(cv, p.H, p.Dc.D, forward_only);
   const Dims& E = p.E.D;
   p.enc_out = cv.take((size_t)E.T * E.d * E.es);
   p.enc_rf = cv.take<float>(E.T * 4);
+  if (forward_only) return cv.off;
+  if (p.H.opts) p.H.embed_ws = cv.take(std::max(embed_sorted_ws_bytes(E.T, p.H.V, E.d),
+                                                embed_sorted_ws_bytes(p.Dc.D.T, p.H.V, E.d)));
   p.denc = cv.take<float>((size_t)E.T * E.d * 4);
   p.enc_dg_partial = cv.take<float>((size_t)rmsnorm_bwd_partial_rows((int)E.T) * E.d * 4);
   return cv.off;
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t t5_stack_workspace_bytes(const t5_stack_cfg* cfg) {
-  StackPlan p;
-  if (plan_stack(cfg, &p) != T5_OK) return 0;
-  return carve_stack(p, nullptr);
-}
-
-int t5_stack_loss_and_grad(const t5_stack_cfg* cfg, const int32_t* tokens, const int32_t* targets,
-                           const t5_stack_weights* w, float* loss, const t5_stack_grads* grads, int accumulate,
-                           void* workspace, size_t workspace_bytes, void* stream) {
-  StackPlan p;
-  int rc = plan_stack(cfg, &p);
-  if (rc != T5_OK) return rc;
+// A training step of a planned stack (p.H.opts: against a teacher).
+int run_stack(StackPlan& p, const t5_stack_cfg* cfg, const int32_t* tokens, const int32_t* targets, const t5_stack_weights* w,
+              float* loss, const t5_stack_grads* grads, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc;
   if (!tokens || !targets || !w || !loss || !workspace) return T5_ERR_NULL;
   if (!w->embedding || !w->final_scale || (!p.H.tied && !w->logits_w)) return T5_ERR_NULL;
   if (grads && (!grads->embedding || !grads->final_scale || (!p.H.tied && !grads->logits_w))) return T5_ERR_NULL;
@@ -507,23 +584,34 @@ int t5_stack_loss_and_grad(const t5_stack_cfg* cfg, const int32_t* tokens, const
   void* dx0 = nullptr;
   T5_SUB(layers_backward(p.S, nullptr, nullptr, acc, &dx0, st));
   T5_SUB(end_dropout(D, DROP_EMBED, dx0, D.ty, st));
-  T5_STEP("embed_bwd", launch_embed_bwd(tokens, dx0, D.ty, grads->embedding, D.T, D.d, V, D.det, st));
+  T5_SUB(embed_gradient(p.H, D, tokens, dx0, grads->embedding, st));
   return T5_OK;
 }
 
-size_t t5_encdec_workspace_bytes(const t5_encdec_cfg* cfg) {
-  EncDecPlan p;
-  if (plan_encdec(cfg, &p) != T5_OK) return 0;
-  return carve_encdec(p, nullptr);
+// Both stacks' forward passes, up to the decoder's last output.
+int encdec_forward(const EncDecPlan& p, const t5_encdec_cfg* cfg, const int32_t* enc_tokens, const int32_t* dec_tokens,
+                   const t5_encdec_weights* w, hipStream_t st) {
+  const Dims& E = p.E.D;
+  const Dims& D = p.Dc.D;
+  const int ty = D.ty, V = p.H.V;
+  // encoder: embedding, layers, final norm -> enc_out
+  T5_STEP("embed_fwd", launch_embed_fwd(enc_tokens, w->embedding, p.E.x_of(0), ty, E.T, E.d, V, st));
+  T5_SUB(end_dropout(E, DROP_EMBED, p.E.x_of(0), ty, st));
+  T5_SUB(layers_forward(p.E, nullptr, st));
+  T5_STEP("rmsnorm_fwd", launch_rmsnorm_fwd(p.E.x_of(p.E.L), ty, w->enc_final_scale, p.enc_out, ty, p.enc_rf, (int)E.T,
+                                            E.d, cfg->enc_block.rms_eps, st));
+  T5_SUB(end_dropout(E, DROP_FINAL, p.enc_out, ty, st));
+  // decoder: embedding, layers cross-attending to enc_out, head
+  T5_STEP("embed_fwd", launch_embed_fwd(dec_tokens, w->embedding, p.Dc.x_of(0), ty, D.T, D.d, V, st));
+  T5_SUB(end_dropout(D, DROP_DEC_EMBED, p.Dc.x_of(0), ty, st));
+  T5_SUB(layers_forward(p.Dc, p.enc_out, st));
+  return T5_OK;
 }
 
-int t5_encdec_loss_and_grad(const t5_encdec_cfg* cfg, const int32_t* enc_tokens, const int32_t* dec_tokens,
-                            const int32_t* targets, const t5_encdec_weights* w, float* loss,
-                            const t5_encdec_grads* grads, int accumulate, void* workspace, size_t workspace_bytes,
-                            void* stream) {
-  EncDecPlan p;
-  int rc = plan_encdec(cfg, &p);
-  if (rc != T5_OK) return rc;
+int run_encdec(EncDecPlan& p, const t5_encdec_cfg* cfg, const int32_t* enc_tokens, const int32_t* dec_tokens,
+               const int32_t* targets, const t5_encdec_weights* w, float* loss, const t5_encdec_grads* grads, int accumulate,
+               void* workspace, size_t workspace_bytes, void* stream) {
+  int rc;
   if (!enc_tokens || !dec_tokens || !targets || !w || !loss || !workspace) return T5_ERR_NULL;
   if (!w->embedding || !w->enc_final_scale || !w->dec_final_scale || (!p.H.tied && !w->logits_w)) return T5_ERR_NULL;
   if (grads && (!grads->embedding || !grads->enc_final_scale || !grads->dec_final_scale ||
@@ -547,17 +635,7 @@ int t5_encdec_loss_and_grad(const t5_encdec_cfg* cfg, const int32_t* enc_tokens,
     p.H.d_logits_w = p.H.tied ? nullptr : grads->logits_w;
   }
 
-  // encoder: embedding, layers, final norm -> enc_out
-  T5_STEP("embed_fwd", launch_embed_fwd(enc_tokens, w->embedding, p.E.x_of(0), ty, E.T, E.d, V, st));
-  T5_SUB(end_dropout(E, DROP_EMBED, p.E.x_of(0), ty, st));
-  T5_SUB(layers_forward(p.E, nullptr, st));
-  T5_STEP("rmsnorm_fwd", launch_rmsnorm_fwd(p.E.x_of(p.E.L), ty, w->enc_final_scale, p.enc_out, ty, p.enc_rf, (int)E.T,
-                                            E.d, cfg->enc_block.rms_eps, st));
-  T5_SUB(end_dropout(E, DROP_FINAL, p.enc_out, ty, st));
-  // decoder: embedding, layers cross-attending to enc_out, head
-  T5_STEP("embed_fwd", launch_embed_fwd(dec_tokens, w->embedding, p.Dc.x_of(0), ty, D.T, D.d, V, st));
-  T5_SUB(end_dropout(D, DROP_DEC_EMBED, p.Dc.x_of(0), ty, st));
-  T5_SUB(layers_forward(p.Dc, p.enc_out, st));
+  T5_SUB(encdec_forward(p, cfg, enc_tokens, dec_tokens, w, st));
   if (grads && !acc) T5_SUB(zero_end_grads(grads->embedding, p.H.d_logits_w, V, D.d, st));
   T5_SUB(head_loss_and_grad(p.H, D, cfg->dec_block.rms_eps, p.Dc.x_of(p.Dc.L), targets, loss, grads != nullptr, acc,
                             p.Dc.dxa, st));
@@ -565,7 +643,7 @@ int t5_encdec_loss_and_grad(const t5_encdec_cfg* cfg, const int32_t* enc_tokens,
   void* dx0 = nullptr;
   T5_SUB(layers_backward(p.Dc, p.enc_out, p.denc, acc, &dx0, st));
   T5_SUB(end_dropout(D, DROP_DEC_EMBED, dx0, ty, st));
-  T5_STEP("embed_bwd", launch_embed_bwd(dec_tokens, dx0, ty, grads->embedding, D.T, D.d, V, D.det, st));
+  T5_SUB(embed_gradient(p.H, D, dec_tokens, dx0, grads->embedding, st));
   T5_SUB(end_dropout(E, DROP_FINAL, p.denc, IN_F32, st));
   // encoder: final norm backward (no residual term), layers, embedding
   T5_STEP("rmsnorm_bwd", launch_rmsnorm_bwd(p.E.x_of(p.E.L), ty, w->enc_final_scale, ty, p.enc_rf, p.denc, nullptr,
@@ -574,8 +652,138 @@ int t5_encdec_loss_and_grad(const t5_encdec_cfg* cfg, const int32_t* enc_tokens,
                                             p.enc_dg_partial, acc, (int)E.T, E.d, st));
   T5_SUB(layers_backward(p.E, nullptr, nullptr, acc, &dx0, st));
   T5_SUB(end_dropout(E, DROP_EMBED, dx0, ty, st));
-  T5_STEP("embed_bwd", launch_embed_bwd(enc_tokens, dx0, ty, grads->embedding, E.T, E.d, V, E.det, st));
+  T5_SUB(embed_gradient(p.H, E, enc_tokens, dx0, grads->embedding, st));
   return T5_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t t5_stack_workspace_bytes(const t5_stack_cfg* cfg) {
+  StackPlan p;
+  if (plan_stack(cfg, &p) != T5_OK) return 0;
+  return carve_stack(p, nullptr);
+}
+
+int t5_stack_loss_and_grad(const t5_stack_cfg* cfg, const int32_t* tokens, const int32_t* targets,
+                           const t5_stack_weights* w, float* loss, const t5_stack_grads* grads, int accumulate,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  StackPlan p;
+  const int rc = plan_stack(cfg, &p);
+  if (rc != T5_OK) return rc;
+  return run_stack(p, cfg, tokens, targets, w, loss, grads, accumulate, workspace, workspace_bytes, stream);
+}
+
+size_t t5_stack_distill_workspace_bytes(const t5_stack_cfg* cfg, const t5_distill_opts* opts) {
+  StackPlan p;
+  if (plan_stack(cfg, &p) != T5_OK || check_opts(opts, p.S.D.T, p.H.V, p.H.z_loss) != T5_OK) return 0;
+  p.H.opts = opts;
+  return carve_stack(p, nullptr);
+}
+
+int t5_stack_distill_loss_and_grad(const t5_stack_cfg* cfg, const t5_distill_opts* opts, const int32_t* tokens,
+                                   const int32_t* targets, const float* teacher_logits, const int32_t* teacher_ids,
+                                   const t5_stack_weights* w, float* loss, const t5_stack_grads* grads, int accumulate,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+  StackPlan p;
+  int rc = plan_stack(cfg, &p);
+  if (rc != T5_OK) return rc;
+  if ((rc = check_opts(opts, p.S.D.T, p.H.V, p.H.z_loss)) != T5_OK) return rc;
+  if (!teacher_logits || !teacher_ids) return T5_ERR_NULL;
+  p.H.opts = opts; p.H.teacher_logits = teacher_logits; p.H.teacher_ids = teacher_ids;
+  return run_stack(p, cfg, tokens, targets, w, loss, grads, accumulate, workspace, workspace_bytes, stream);
+}
+
+size_t t5_stack_top_logits_workspace_bytes(const t5_stack_cfg* cfg, int32_t top_k) {
+  StackPlan p;
+  if (plan_stack(cfg, &p) != T5_OK || check_rows(p.S.D.T, p.H.V, p.H.V, top_k) != T5_OK) return 0;
+  return carve_stack(p, nullptr, true);
+}
+
+int t5_stack_top_logits(const t5_stack_cfg* cfg, const int32_t* tokens, const t5_stack_weights* w, int32_t top_k,
+                        float* values, int32_t* ids, void* workspace, size_t workspace_bytes, void* stream) {
+  StackPlan p;
+  int rc = plan_stack(cfg, &p);
+  if (rc != T5_OK) return rc;
+  if ((rc = check_rows(p.S.D.T, p.H.V, p.H.V, top_k)) != T5_OK) return rc;
+  if (!tokens || !w || !values || !ids || !workspace) return T5_ERR_NULL;
+  if (!w->embedding || !w->final_scale || (!p.H.tied && !w->logits_w)) return T5_ERR_NULL;
+  rc = bind_layers(p.S, w->layers, nullptr, w->rel_table, nullptr, nullptr, nullptr, false);
+  if (rc != T5_OK) return rc;
+  if (workspace_bytes < carve_stack(p, nullptr, true)) return T5_ERR_WORKSPACE;
+  carve_stack(p, workspace, true);
+  hipStream_t st = (hipStream_t)stream;
+  const Dims& D = p.S.D;
+  p.H.embedding = w->embedding; p.H.final_scale = w->final_scale; p.H.logits_w = w->logits_w;
+  T5_STEP("embed_fwd", launch_embed_fwd(tokens, w->embedding, p.S.x_of(0), D.ty, D.T, D.d, p.H.V, st));
+  T5_SUB(end_dropout(D, DROP_EMBED, p.S.x_of(0), D.ty, st));
+  T5_SUB(layers_forward(p.S, nullptr, st));
+  return head_top_logits(p.H, D, cfg->block.rms_eps, p.S.x_of(p.S.L), top_k, values, ids, st);
+}
+
+size_t t5_encdec_workspace_bytes(const t5_encdec_cfg* cfg) {
+  EncDecPlan p;
+  if (plan_encdec(cfg, &p) != T5_OK) return 0;
+  return carve_encdec(p, nullptr);
+}
+
+int t5_encdec_loss_and_grad(const t5_encdec_cfg* cfg, const int32_t* enc_tokens, const int32_t* dec_tokens,
+                            const int32_t* targets, const t5_encdec_weights* w, float* loss,
+                            const t5_encdec_grads* grads, int accumulate, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  EncDecPlan p;
+  const int rc = plan_encdec(cfg, &p);
+  if (rc != T5_OK) return rc;
+  return run_encdec(p, cfg, enc_tokens, dec_tokens, targets, w, loss, grads, accumulate, workspace, workspace_bytes, stream);
+}
+
+size_t t5_encdec_distill_workspace_bytes(const t5_encdec_cfg* cfg, const t5_distill_opts* opts) {
+  EncDecPlan p;
+  if (plan_encdec(cfg, &p) != T5_OK || check_opts(opts, p.Dc.D.T, p.H.V, p.H.z_loss) != T5_OK) return 0;
+  p.H.opts = opts;
+  return carve_encdec(p, nullptr);
+}
+
+int t5_encdec_distill_loss_and_grad(const t5_encdec_cfg* cfg, const t5_distill_opts* opts, const int32_t* enc_tokens,
+                                    const int32_t* dec_tokens, const int32_t* targets, const float* teacher_logits,
+                                    const int32_t* teacher_ids, const t5_encdec_weights* w, float* loss,
+                                    const t5_encdec_grads* grads, int accumulate, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  EncDecPlan p;
+  int rc = plan_encdec(cfg, &p);
+  if (rc != T5_OK) return rc;
+  if ((rc = check_opts(opts, p.Dc.D.T, p.H.V, p.H.z_loss)) != T5_OK) return rc;
+  if (!teacher_logits || !teacher_ids) return T5_ERR_NULL;
+  p.H.opts = opts; p.H.teacher_logits = teacher_logits; p.H.teacher_ids = teacher_ids;
+  return run_encdec(p, cfg, enc_tokens, dec_tokens, targets, w, loss, grads, accumulate, workspace, workspace_bytes, stream);
+}
+
+size_t t5_encdec_top_logits_workspace_bytes(const t5_encdec_cfg* cfg, int32_t top_k) {
+  EncDecPlan p;
+  if (plan_encdec(cfg, &p) != T5_OK || check_rows(p.Dc.D.T, p.H.V, p.H.V, top_k) != T5_OK) return 0;
+  return carve_encdec(p, nullptr, true);
+}
+
+int t5_encdec_top_logits(const t5_encdec_cfg* cfg, const int32_t* enc_tokens, const int32_t* dec_tokens,
+                         const t5_encdec_weights* w, int32_t top_k, float* values, int32_t* ids, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  EncDecPlan p;
+  int rc = plan_encdec(cfg, &p);
+  if (rc != T5_OK) return rc;
+  if ((rc = check_rows(p.Dc.D.T, p.H.V, p.H.V, top_k)) != T5_OK) return rc;
+  if (!enc_tokens || !dec_tokens || !w || !values || !ids || !workspace) return T5_ERR_NULL;
+  if (!w->embedding || !w->enc_final_scale || !w->dec_final_scale || (!p.H.tied && !w->logits_w)) return T5_ERR_NULL;
+  rc = bind_layers(p.E, w->enc_layers, nullptr, w->enc_rel_table, nullptr, nullptr, nullptr, false);
+  if (rc != T5_OK) return rc;
+  rc = bind_layers(p.Dc, w->dec_layers, w->dec_cross, w->dec_rel_table, nullptr, nullptr, nullptr, false);
+  if (rc != T5_OK) return rc;
+  if (workspace_bytes < carve_encdec(p, nullptr, true)) return T5_ERR_WORKSPACE;
+  carve_encdec(p, workspace, true);
+  hipStream_t st = (hipStream_t)stream;
+  p.H.embedding = w->embedding; p.H.final_scale = w->dec_final_scale; p.H.logits_w = w->logits_w;
+  T5_SUB(encdec_forward(p, cfg, enc_tokens, dec_tokens, w, st));
+  return head_top_logits(p.H, p.Dc.D, cfg->dec_block.rms_eps, p.Dc.x_of(p.Dc.L), top_k, values, ids, st);
 }
 
 }  // extern "C"

@@ -1,41 +1,14 @@
 // C-ABI entry points of the operators at the vocabulary ends of a stack (see include/t5mi.h): scaled embedding and
 // its gradient, top logits, distillation loss.
 #include "block_host.h"
+#include "vocab_host.h"
 
 namespace {
-
-int elem_type(int32_t dtype, int* ty) {
-  if (dtype != T5_F32 && dtype != T5_BF16) return T5_ERR_UNSUPPORTED;
-  *ty = dtype == T5_BF16 ? IN_BF16 : IN_F32;
-  return T5_OK;
-}
 
 int check_embed(const t5_embed_cfg* c, int* ty) {
   if (!c) return T5_ERR_NULL;
   if (c->n_tokens < 0 || c->vocab < 1 || c->d_model < 1 || !std::isfinite(c->scale)) return T5_ERR_SHAPE;
   if (c->n_tokens > (1 << 24) || c->vocab > (1 << 22) || c->d_model > (1 << 16)) return T5_ERR_UNSUPPORTED;
-  return elem_type(c->dtype, ty);
-}
-
-int check_rows(int64_t rows, int32_t vocab, int64_t ld, int32_t top_k) {
-  if (rows < 0 || vocab < 2 || ld < vocab || top_k < 1 || top_k > vocab) return T5_ERR_SHAPE;
-  if (rows > (1 << 24) || vocab > (1 << 22) || ld > ((int64_t)1 << 32) || top_k > kTopMost) return T5_ERR_UNSUPPORTED;
-  return T5_OK;
-}
-
-int check_top(const t5_top_logits_cfg* c, int* ty) {
-  if (!c) return T5_ERR_NULL;
-  const int rc = check_rows(c->rows, c->vocab, c->ld, c->top_k);
-  return rc != T5_OK ? rc : elem_type(c->dtype, ty);
-}
-
-int check_distill(const t5_distill_cfg* c, int* ty) {
-  if (!c) return T5_ERR_NULL;
-  const int rc = check_rows(c->rows, c->vocab, c->ld, c->top_k);
-  if (rc != T5_OK) return rc;
-  if (!(c->temperature > 0.f) || !std::isfinite(c->temperature) || !std::isfinite(1.f / c->temperature) ||
-      !(c->soft_weight >= 0.f && c->soft_weight <= 1.f) || !(c->z_loss >= 0.f) || !std::isfinite(c->z_loss))
-    return T5_ERR_SHAPE;
   return elem_type(c->dtype, ty);
 }
 

@@ -101,3 +101,37 @@ def test_wrappers_refuse_host_tensors_types_and_shapes():
         P.t5_top_logits(f, 2)
     with pytest.raises(ValueError):
         P.t5_distill_loss_and_grad(f, None, f[:, :2], i.reshape(4, 1))
+
+
+def test_model_refusals():
+    import synth_inputs as SI
+    from dataclasses import replace
+    L = P.lib()
+    sc = SI.StackConfig("r", replace(SI.CONFIGS["c1_tiny_f32"], causal=True), n_layers=1, vocab=300)
+    ec = SI._encdec("r", 1, 2, 8, 8, 32, 2, 8, 48, 1, 1, 300)
+    cs, ce = B._stack_cfg_struct(sc), B._encdec_cfg_struct(ec)
+    ok = B._DistillOpts(8, 1.0, 0.5)
+    lw = (B._Weights * 1)(B._Weights(*[4096] * 10))
+    xw = (B._CrossWeights * 1)(B._CrossWeights(*[4096] * 5))
+    ws, we = B._StackWeights(4096, 4096, lw, 4096, 4096), B._EncDecWeights(4096, 4096, lw, 4096, 4096, lw, xw, 4096, 4096)
+    top_s = lambda k, tok=D, v=D, w=D, n=1 << 40, W=ws: L.t5_stack_top_logits(C.byref(cs), tok, C.byref(W), k, v, D, w, n, None)
+    top_e = lambda k, tok=D, v=D, w=D, n=1 << 40, W=we: L.t5_encdec_top_logits(C.byref(ce), tok, D, C.byref(W), k, v, D, w, n, None)
+    for top, q in ((top_s, lambda k: L.t5_stack_top_logits_workspace_bytes(C.byref(cs), k)),
+                   (top_e, lambda k: L.t5_encdec_top_logits_workspace_bytes(C.byref(ce), k))):
+        for k, rc in ((0, SHAPE), (301, SHAPE), (257, UNSUPPORTED)):
+            assert top(k) == rc and q(k) == 0
+        assert top(8, tok=None) == top(8, v=None) == top(8, w=None) == NULL
+        assert q(8) > 0 and top(8, n=q(8) - 1) == WORKSPACE
+    dis_s = lambda o, t=D, tl=D, n=1 << 40: L.t5_stack_distill_loss_and_grad(C.byref(cs), o and C.byref(o), D, t, tl, D, C.byref(ws), D, None, 0, D, n, None)
+    dis_e = lambda o, t=D, tl=D, n=1 << 40: L.t5_encdec_distill_loss_and_grad(C.byref(ce), o and C.byref(o), D, D, t, tl, D, C.byref(we), D, None, 0, D, n, None)
+    for dis, q in ((dis_s, lambda o: L.t5_stack_distill_workspace_bytes(C.byref(cs), o and C.byref(o))),
+                   (dis_e, lambda o: L.t5_encdec_distill_workspace_bytes(C.byref(ce), o and C.byref(o)))):
+        for o, rc in ((None, NULL), (B._DistillOpts(0, 1.0, 0.5), SHAPE), (B._DistillOpts(301, 1.0, 0.5), SHAPE),
+                      (B._DistillOpts(257, 1.0, 0.5), UNSUPPORTED), (B._DistillOpts(8, 0.0, 0.5), SHAPE),
+                      (B._DistillOpts(8, nan, 0.5), SHAPE), (B._DistillOpts(8, 1.0, 1.5), SHAPE)):
+            assert dis(o) == rc and q(o) == 0
+        assert dis(ok, t=None) == dis(ok, tl=None) == NULL
+        assert dis(ok, n=q(ok) - 1) == WORKSPACE
+        # the teacher's loss and the sorted embedding gradient need room of their own
+    assert L.t5_stack_distill_workspace_bytes(C.byref(cs), C.byref(ok)) > L.t5_stack_workspace_bytes(C.byref(cs))
+    assert L.t5_stack_top_logits_workspace_bytes(C.byref(cs), 8) < L.t5_stack_workspace_bytes(C.byref(cs))
