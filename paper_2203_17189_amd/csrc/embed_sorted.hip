@@ -356,16 +356,17 @@ __global__ __launch_bounds__(512) void embed_join_kernel(SumArgs a) {
 // ------------------------------------------------------------------------------------------------
 // Few tokens: one launch and no sort.  A wavefront per position looks for its id among all ids, held in LDS; if the
 // position is the first of its id it sums the rows of all of them in order.  Ids that occur more than kOwnerAlone times
-// are left to the whole workgroup, which shares their list out.  Behind these, workgroups that clear `zero_rows` rows of
-// the table each, all but those whose ids they find.
+// are left to the whole workgroup, which shares their list out.  `splits` workgroups of every eight positions take a part
+// of the columns each.  Behind these, workgroups that clear `zero_rows` rows of the table each, all but those whose ids
+// they find.
 // ------------------------------------------------------------------------------------------------
-constexpr int kOwnerTokens = 2048, kOwnerAlone = 16, kZeroRows = 512;
+constexpr int kOwnerTokens = 4096, kOwnerAlone = 48, kZeroRows = 512;
 
 struct OwnerArgs {
   const int32_t* tok;
   const void* dx;
   float* dE;
-  int32_t n, d, vocab, zero_rows, accumulate, sum_blocks;
+  int32_t n, d, vocab, zero_rows, accumulate, sum_blocks, splits, split_cols;
   float scale;
 };
 
@@ -399,6 +400,7 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
   __shared__ uint16_t list[kOwnerTokens], few[8][kOwnerAlone];
   __shared__ F red[8][64];
   __shared__ uint32_t many[8], n_many;
+  __shared__ int found[8];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint64_t lower = (1ull << lane) - 1;
   uint32_t id[kOwnerTokens / 512];
@@ -428,48 +430,72 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
     F* o = reinterpret_cast<F*>(a.dE + (size_t)v * a.d + c);
     *o = a.accumulate ? *o + s * a.scale : s * a.scale;
   };
-  const int own = blockIdx.x * 8 + w;
+  const int split = blockIdx.x % a.splits, own = blockIdx.x / a.splits * 8 + w;
+  const int c_begin = split * a.split_cols, c_end = min(c_begin + a.split_cols, a.d);
   if (own < a.n) {
     const uint32_t v = ids[own];
+    // 256 ids at a time (places behind the last id hold none): first those in front of the position, then all behind
+    const int start = own & ~255;
     bool first = true;
     int m = 0;
-    for (int k = 0; k < a.n && first; k += 64) {
-      const uint64_t hit = __ballot(ids[k + lane] == v);  // (places behind the last id hold none)
-      if (k <= own) first = !(own - k < 64 ? hit & ((1ull << (own - k)) - 1) : hit);
-      const int at = m + __popcll(hit & lower);
-      if ((hit >> lane & 1) && at < kOwnerAlone) few[w][at] = (uint16_t)(k + lane);
-      m += __popcll(hit);
+    uint64_t hit[4];
+    auto look = [&](int k) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) hit[j] = __ballot(ids[k + j * 64 + lane] == v);
+    };
+    for (int k = 0; k < start && first; k += 256) {
+      look(k);
+      first = !(hit[0] | hit[1] | hit[2] | hit[3]);
+    }
+    for (int k = start; k < a.n && first; k += 256) {
+      look(k);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (hit[j]) {
+          const int i = k + j * 64, at = m + __popcll(hit[j] & lower);
+          if ((hit[j] >> lane & 1) && at < kOwnerAlone) few[w][at] = (uint16_t)(i + lane);
+          if (m == 0 && i + __ffsll((long long)hit[j]) - 1 < own) first = false;
+          m += __popcll(hit[j]);
+        }
+      }
     }
     if (first && m > kOwnerAlone) {
       if (lane == 0) many[atomicAdd(&n_many, 1u)] = v;
     } else if (first) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      for (int c = lane * VEC; c < a.d; c += 64 * VEC) put(v, c, sum_listed<T, VEC, F>((const T*)a.dx + c, a.d, few[w], 0, m));
+      for (int c = c_begin + lane * VEC; c < c_end; c += 64 * VEC) put(v, c, sum_listed<T, VEC, F>((const T*)a.dx + c, a.d, few[w], 0, m));
     }
   }
   __syncthreads();
   for (uint32_t h = 0; h < n_many; ++h) {
     const uint32_t v = many[h];
-    // the list, a wavefront's 256 places of it at a time
-    int m = 0, mine = 0;
-    for (int k = 0; k < a.n; k += 64) {
-      if (k == w * 256) mine = m;
-      m += __popcll(__ballot(ids[k + lane] == v));
+    // the list, each wavefront an eighth of the ids
+    uint64_t hit[kOwnerTokens / 512];
+    int here = 0, mine = 0, m = 0;
+#pragma unroll
+    for (int k = 0; k < kOwnerTokens / 512; ++k) {
+      hit[k] = __ballot(ids[w * (kOwnerTokens / 8) + k * 64 + lane] == v);
+      here += __popcll(hit[k]);
+    }
+    if (lane == 0) found[w] = here;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      mine += q < w ? found[q] : 0;
+      m += found[q];
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = w * 256 + k * 64;
-      const uint64_t hit = __ballot(ids[i + lane] == v);
-      if (hit >> lane & 1) list[mine + __popcll(hit & lower)] = (uint16_t)(i + lane);
-      mine += __popcll(hit);
+    for (int k = 0; k < kOwnerTokens / 512; ++k) {
+      if (hit[k] >> lane & 1) list[mine + __popcll(hit[k] & lower)] = (uint16_t)(w * (kOwnerTokens / 8) + k * 64 + lane);
+      mine += __popcll(hit[k]);
     }
     __syncthreads();
     const int each = (m + 7) / 8, l0 = w * each, l1 = min(l0 + each, m);
-    for (int c0 = 0; c0 < a.d; c0 += 64 * VEC) {
+    for (int c0 = c_begin; c0 < c_end; c0 += 64 * VEC) {
       const int c = c0 + lane * VEC;
-      red[w][lane] = sum_listed<T, VEC, F>((const T*)a.dx + (c < a.d ? c : 0), a.d, list, l0, l1);
+      red[w][lane] = sum_listed<T, VEC, F>((const T*)a.dx + (c < c_end ? c : 0), a.d, list, l0, l1);
       __syncthreads();
-      if (w == 0 && c < a.d) {
+      if (w == 0 && c < c_end) {
         F s = red[0][lane];
 #pragma unroll
         for (int q = 1; q < 8; ++q) s += red[q][lane];
@@ -579,7 +605,11 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
     OwnerArgs a;
     a.tok = tokens; a.dx = dx; a.dE = dE; a.n = (int)n; a.d = d; a.vocab = vocab; a.accumulate = accumulate; a.scale = scale;
     a.zero_rows = std::min(kZeroRows, std::max(1, 32768 / d));  // 128 KB of the table
-    a.sum_blocks = ceil_div(n, 8);
+    // as many column parts as leave about a thousand workgroups
+    const int piece = vec ? 256 : 64, pieces = ceil_div(d, piece), groups = std::max(1, ceil_div(n, 8));
+    a.split_cols = ceil_div(pieces, std::max(1, std::min(pieces, 1024 / groups))) * piece;
+    a.splits = ceil_div(d, a.split_cols);
+    a.sum_blocks = n > 0 ? groups * a.splits : 0;
     const unsigned grid = (unsigned)(a.sum_blocks + (accumulate ? 0 : ceil_div(vocab, a.zero_rows)));
     if (type == IN_BF16) {
       if (vec) embed_owner_sum_kernel<bf16, 4><<<grid, 512, 0, st>>>(a);
