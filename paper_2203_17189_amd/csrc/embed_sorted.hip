@@ -66,10 +66,9 @@ __device__ __forceinline__ void fill_zero(const Fill& f) {
   const int64_t pre = at && f.count > 4 - at ? 4 - at : at ? f.count : 0;  // elements in front of a 16-byte boundary
   const int64_t quads = (f.count - pre) / 4;
   f32x4* q = reinterpret_cast<f32x4*>(f.out + pre);
-  const int64_t i0 = (int64_t)b * (kFillEach / 4) + threadIdx.x;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (i0 + j * 1024 < quads) q[i0 + j * 1024] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t i0 = (int64_t)b * (kFillEach / 4);
+  for (int j = threadIdx.x; j < kFillEach / 4; j += blockDim.x)
+    if (i0 + j < quads) q[i0 + j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int64_t tail = pre + 4 * quads;
   if (b == 0 && threadIdx.x < pre) f.out[threadIdx.x] = 0.f;
   if (b == 0 && threadIdx.x < f.count - tail) f.out[tail + threadIdx.x] = 0.f;
@@ -77,7 +76,9 @@ __device__ __forceinline__ void fill_zero(const Fill& f) {
 
 // ------------------------------------------------------------------------------------------------
 // Stable sort of (id, position) by id: least significant digit first, `bits` (at most 8) bits a pass, two launches a
-// pass.  Workgroup b owns keys [b * chunk, (b + 1) * chunk) of the pass's input, 1024 at a time.
+// pass.  Workgroup b owns keys [b * chunk, (b + 1) * chunk) of the pass's input, 1024 at a time.  (One launch less a pass,
+// each counting the next one's digits as it places its keys, costs more than it saves where an id is frequent: atomics on
+// few addresses, 36 -> 47 us with 30% padding among 40000.)
 // ------------------------------------------------------------------------------------------------
 constexpr int kSortTile = 1024;
 constexpr int kSortBlocks = 256;  // at most; a workgroup then loops over its chunk
@@ -188,53 +189,89 @@ __global__ __launch_bounds__(1024) void embed_sort_place_kernel(SortPass p) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// The same order in one launch, for n <= kRankSort and id and position in 32 bits together: the place of a key is the
-// number of keys below it.  A workgroup places I keys, each held by 64 / I lanes of every wavefront; each of the sixteen
-// wavefronts compares them with a sixteenth of all keys, four keys a lane and LDS read, two instructions a comparison.
-// n^2 comparisons in all, bound by those reads: I is chosen for one workgroup per compute unit.
+// The same order in two launches, for n <= kMergeSort and id and position in 32 bits together: blocks of 1024 keys are
+// sorted by a workgroup each, then the place of a key is its place in its block plus the number of smaller keys in every
+// other block, found by bisection in LDS, which holds all keys.
 // ------------------------------------------------------------------------------------------------
-constexpr int kRankSort = 16384;
+constexpr int kMergeSort = 16384;
 
-template <int I>
-__global__ __launch_bounds__(1024) void embed_sort_rank_kernel(const int32_t* __restrict__ tok, u32x2* __restrict__ out, int n,
-                                                               int vocab, int pos_bits, Fill fill) {
-  constexpr int G = 64 / I;
-  __shared__ uint32_t part[16][64];
-  __shared__ u32x4 keys[16][64];
+__global__ __launch_bounds__(1024) void embed_sort_block_kernel(const int32_t* __restrict__ tok, uint32_t* __restrict__ out,
+                                                                int n, int vocab, int pos_bits, int passes, int bits,
+                                                                Fill fill) {
+  __shared__ uint32_t cnt[16][256], base[256], wsum[4], keys[1024];
   if ((int)blockIdx.x >= fill.first) {
     fill_zero(fill);
     return;
   }
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  auto key_at = [&](int i, int end) { return i < end ? clamp_id(tok[i], vocab) << pos_bits | (uint32_t)i : 0xFFFFFFFFu; };
-  const int i = blockIdx.x * I + lane % I;
-  const uint32_t mine = key_at(i, n);
-  const int each = (n + 15) / 16, j0 = w * each, j1 = min(j0 + each, n);
-  uint32_t below = 0;
-  for (int j = j0; j < j1; j += 256) {
-    u32x4 k;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) k[q] = key_at(j + 4 * lane + q, j1);  // (what is beyond the end is below no key)
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    keys[w][lane] = k;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int m = (min(256, j1 - j) + 4 * G - 1) / (4 * G);  // lanes' keys for each of the G groups of lanes
-    const u32x4* src = keys[w] + (lane / I) * m;
-#pragma unroll 8
-    for (int q = 0; q < m; ++q) {
-      const u32x4 o = src[q];
-      below += (o[0] < mine) + (o[1] < mine) + (o[2] < mine) + (o[3] < mine);
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, i = blockIdx.x * 1024 + tid;
+  uint32_t key = i < n ? clamp_id(tok[i], vocab) << pos_bits | (uint32_t)i : 0xFFFFFFFFu;  // (the last block's end stays last)
+  for (int q = 0; q < passes; ++q) {
+    const uint32_t d = (key >> (pos_bits + q * bits)) & ((1u << bits) - 1);
+    uint64_t same = ~0ull;
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t m = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? m : ~m;
     }
+    const uint32_t below = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) cnt[w][j * 64 + lane] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (below == 0) cnt[w][d] = (uint32_t)__popcll(same);
+    __syncthreads();
+    uint32_t total = 0, incl = 0;
+    if (tid < 256) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const uint32_t c = cnt[j][tid];
+        cnt[j][tid] = total;
+        total += c;
+      }
+      incl = total;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t o = __shfl_up(incl, off, 64);
+        incl += lane >= off ? o : 0;
+      }
+      if (lane == 63) wsum[w] = incl;
+    }
+    __syncthreads();
+    if (tid < 256) {
+      uint32_t at = incl - total;
+      for (int j = 0; j < w; ++j) at += wsum[j];
+      base[tid] = at;
+    }
+    __syncthreads();
+    keys[base[d] + cnt[w][d] + below] = key;
+    __syncthreads();
+    key = keys[tid];
   }
-  part[w][lane] = below;
+  out[i] = key;
+}
+
+__global__ __launch_bounds__(256) void embed_sort_merge_kernel(const u32x4* __restrict__ in, u32x2* __restrict__ out, int n,
+                                                               int pos_bits, Fill fill) {
+  __shared__ uint32_t keys[kMergeSort];
+  if ((int)blockIdx.x >= fill.first) {
+    fill_zero(fill);
+    return;
+  }
+  const int tid = threadIdx.x, blocks = (n + 1023) / 1024;
+  for (int j = tid; j < blocks * 256; j += 256) reinterpret_cast<u32x4*>(keys)[j] = in[j];
   __syncthreads();
-  if (tid >= I || i >= n) return;
-  below = 0;
+  const int i = blockIdx.x * 256 + tid;
+  if (i >= n) return;
+  const uint32_t mine = keys[i];
+  uint32_t place = i & 1023;
+#pragma unroll 4
+  for (int b = 0; b < blocks; ++b) {
+    const uint32_t* k = keys + b * 1024;
+    uint32_t lo = 0;
 #pragma unroll
-  for (int q = 0; q < 16; ++q)
-#pragma unroll
-    for (int g = 0; g < G; ++g) below += part[q][g * I + tid];
-  out[below] = u32x2{mine >> pos_bits, mine & ((1u << pos_bits) - 1)};
+    for (int step = 512; step > 0; step >>= 1) lo += k[lo + step - 1] < mine ? step : 0;
+    lo += k[lo] < mine ? 1 : 0;  // (lo <= 1023)
+    place += b == i >> 10 ? 0 : lo;
+  }
+  out[place] = u32x2{mine >> pos_bits, mine & ((1u << pos_bits) - 1)};
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -248,7 +285,7 @@ struct SumArgs {
   const void* dx;
   float* dE;
   float* partial;  // [tiles][2][d]
-  int32_t n, d, tile, tiles, slabs, accumulate;
+  int32_t n, d, tile, tiles, slabs, join, accumulate;
   float scale;
 };
 
@@ -305,8 +342,8 @@ __global__ __launch_bounds__(256) void embed_tile_sum_kernel(SumArgs a) {
   flush((first && from_before) || (t1 < a.n && a.sorted[t1].x == cur));
 }
 
-// A workgroup per tile and 64 * VEC columns: if a run begins in the tile and reaches over its end, adds the run's parts,
-// each of the eight wavefronts a share of them in order, and writes the row.
+// A workgroup per tile and `join` pieces of 64 * VEC columns: if a run begins in the tile and reaches over its end, adds
+// the run's parts and writes the row.  The eight wavefronts take a piece each, or a share of a piece's parts, in order.
 template <int VEC>
 __global__ __launch_bounds__(512) void embed_join_kernel(SumArgs a) {
   typedef typename Piece<float, VEC>::type F;
@@ -329,9 +366,11 @@ __global__ __launch_bounds__(512) void embed_join_kernel(SumArgs a) {
     first += 64 * (int64_t)a.tile;
     begin = id_at(first + (int64_t)lane * a.tile);
   }
-  const int each = (parts + 7) / 8, p0 = w * each, p1 = min(p0 + each, parts);
-  const int c = (blockIdx.y * 64 + lane) * VEC;
-  const bool on = c < a.d;
+  const int slabs = min(a.join, a.slabs - (int)blockIdx.y * a.join);
+  const int shares = slabs == 1 ? 8 : slabs == 2 ? 4 : 2;
+  const int slab = w / shares, each = (parts + shares - 1) / shares, p0 = (w % shares) * each, p1 = min(p0 + each, parts);
+  const int c = ((blockIdx.y * a.join + slab) * 64 + lane) * VEC;
+  const bool on = slab < slabs && c < a.d;
   const float* src = a.partial + (size_t)t * 2 * a.d + (on ? c : 0);
   F s{};
   for (int p = p0; p < p1; p += 8) {
@@ -347,8 +386,8 @@ __global__ __launch_bounds__(512) void embed_join_kernel(SumArgs a) {
   }
   red[w][lane] = s;
   __syncthreads();
-  if (w != 0 || !on) return;
-  for (int q = 1; q < 8 && q * each < parts; ++q) s += red[q][lane];
+  if (w % shares != 0 || !on) return;
+  for (int q = 1; q < shares && q * each < parts; ++q) s += red[w + q][lane];
   F* o = reinterpret_cast<F*>(a.dE + (size_t)last * a.d + c);
   *o = a.accumulate ? *o + s : s;
 }
@@ -508,7 +547,7 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
 
 struct SortPlan {
   int bits_each, passes, blocks, chunk;
-  int pos_bits;  // > 0: by rank, in one launch
+  int pos_bits;  // > 0: blocks and a merge
 };
 int bits_of(int64_t v) {  // of the numbers 0 .. v, at least 1
   int b = 1;
@@ -518,19 +557,18 @@ int bits_of(int64_t v) {  // of the numbers 0 .. v, at least 1
 SortPlan sort_plan(int64_t n, int vocab) {
   SortPlan s;
   const int bits = bits_of(vocab - 1), pos_bits = bits_of(std::max<int64_t>(n - 1, 0));
-  s.pos_bits = n <= kRankSort && bits + pos_bits <= 32 ? pos_bits : 0;
+  s.pos_bits = n <= kMergeSort && bits + pos_bits <= 32 ? pos_bits : 0;
   s.passes = ceil_div(bits, 8);
   s.bits_each = ceil_div(bits, s.passes);
   s.chunk = std::max(1, ceil_div(n, (int64_t)kSortBlocks * kSortTile)) * kSortTile;
   s.blocks = ceil_div(n, s.chunk);
   return s;
 }
-// Positions of a tile: as many as leave 2048 wavefronts and more, up to 64 (16 rows of 768 bf16 columns at 16384
-// tokens: 3072 wavefronts; 64 rows of 2048 columns at 32768: 4096)
+// Positions of a tile: as many as leave 1024 wavefronts and more, up to 64 (60000 x 512: 54 us with 32, 51 with 64)
 int sum_tile(int64_t n, int d) {
   const int64_t slabs = ceil_div(d, 256);
   int t = 64;
-  while (t > 16 && ceil_div(n, t) * slabs < 2048) t /= 2;
+  while (t > 16 && ceil_div(n, t) * slabs < 1024) t /= 2;
   return t;
 }
 
@@ -549,7 +587,7 @@ size_t carve_bwd_ws(int64_t n, int vocab, int d, void* base, BwdWs* w) {
     return (void*)q;
   };
   w->buf[0] = (u32x2*)take((size_t)n * sizeof(u32x2));
-  w->buf[1] = (u32x2*)take((size_t)n * sizeof(u32x2));
+  w->buf[1] = (u32x2*)take((size_t)std::max<int64_t>(n, 1024) * sizeof(u32x2));
   w->hist = (uint32_t*)take(s.pos_bits ? 0 : (size_t)s.blocks * 256 * 4);
   w->partial = (float*)take((size_t)ceil_div(n, sum_tile(n, d)) * 2 * d * 4);
   return off;
@@ -625,35 +663,32 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
   carve_bwd_ws(n, vocab, d, ws, &w);
   // rows of ids that do not occur: the whole table's gradient is cleared beside the sort, which leaves most of the
   // chip idle, in equal shares of its launches
-  const int rank_keys = n <= 4096 ? 16 : n <= 8192 ? 32 : 64;
-  const int sorters = s.pos_bits ? ceil_div(n, rank_keys) : s.blocks;  // workgroups of a launch that sort
-  const int launches = s.pos_bits ? 1 : 2 * s.passes;
+  const int launches = s.pos_bits ? 2 : 2 * s.passes;
   const int64_t all = accumulate ? 0 : (int64_t)vocab * d, share = ((all + launches - 1) / launches + 3) / 4 * 4;
   const u32x2* sorted = w.buf[0];
   SortPass p;
   p.hist = w.hist;
   p.n = (int)n; p.vocab = vocab; p.chunk = s.chunk; p.blocks = s.blocks; p.bits = s.bits_each;
   int turn = 0;
-  auto blocks = [&]() {  // of the next launch, its share of the clearing among them
+  auto blocks = [&](int sorters) {  // of the next launch, its share of the clearing among them
     const int64_t i0 = std::min(all, share * turn), i1 = std::min(all, share * (turn + 1));
     ++turn;
     p.fill.out = dE + i0; p.fill.count = i1 - i0; p.fill.first = sorters;
     return (unsigned)(sorters + ceil_div(p.fill.count, kFillEach));
   };
   if (s.pos_bits) {
-    const unsigned grid = blocks();
-    auto go = [&](auto kern) { kern<<<grid, 1024, 0, st>>>(tokens, w.buf[0], (int)n, vocab, s.pos_bits, p.fill); };
-    if (rank_keys == 16) go(embed_sort_rank_kernel<16>);
-    else if (rank_keys == 32) go(embed_sort_rank_kernel<32>);
-    else go(embed_sort_rank_kernel<64>);
+    unsigned grid = blocks(s.blocks);
+    embed_sort_block_kernel<<<grid, 1024, 0, st>>>(tokens, (uint32_t*)w.buf[1], (int)n, vocab, s.pos_bits, s.passes, s.bits_each, p.fill);
+    grid = blocks(ceil_div(n, 256));
+    embed_sort_merge_kernel<<<grid, 256, 0, st>>>((const u32x4*)w.buf[1], w.buf[0], (int)n, s.pos_bits, p.fill);
   }
   for (int q = 0; q < s.passes && !s.pos_bits; ++q) {
     p.tok = q == 0 ? tokens : nullptr;
     p.in = w.buf[(q + 1) & 1];
     p.out = w.buf[q & 1];
     p.shift = q * s.bits_each;
-    embed_sort_count_kernel<<<blocks(), 1024, 0, st>>>(p);
-    embed_sort_place_kernel<<<blocks(), 1024, 0, st>>>(p);
+    embed_sort_count_kernel<<<blocks(s.blocks), 1024, 0, st>>>(p);
+    embed_sort_place_kernel<<<blocks(s.blocks), 1024, 0, st>>>(p);
     sorted = p.out;
   }
   SumArgs a;
@@ -663,8 +698,13 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
   if (type == IN_BF16) launch_tile_sum<bf16>(a, vec, st);
   else launch_tile_sum<float>(a, vec, st);
   if (a.tiles > 1) {
-    if (vec) embed_join_kernel<4><<<dim3((unsigned)a.tiles, (unsigned)ceil_div(d, 256)), 512, 0, st>>>(a);
-    else embed_join_kernel<1><<<dim3((unsigned)a.tiles, (unsigned)ceil_div(d, 64)), 512, 0, st>>>(a);
+    // most workgroups have nothing to do and cost 0.3 ns a wavefront: four pieces each where there are more than four
+    // (32768 x 2048: 111.5 us in all with one piece, 109.3 with four; 16384 x 768, a seventh of it padding: 39.0 and 41.1)
+    a.slabs = ceil_div(d, vec ? 256 : 64);
+    a.join = a.slabs > 4 ? 4 : 1;
+    const dim3 grid((unsigned)a.tiles, (unsigned)ceil_div(a.slabs, a.join));
+    if (vec) embed_join_kernel<4><<<grid, 512, 0, st>>>(a);
+    else embed_join_kernel<1><<<grid, 512, 0, st>>>(a);
   }
   return hipGetLastError();
 }
