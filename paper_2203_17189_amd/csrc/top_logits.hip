@@ -9,13 +9,13 @@
 #include "kernels.h"
 #include "vocab_rows.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace t5mi {
 
 namespace {
 
-constexpr int kCand = 2048;   // keys collected in LDS at most
-constexpr int kPieces = 16;   // 16-byte pieces of a thread in a chunk
+constexpr int kCand = 2048;  // keys collected in LDS at most
 
 // -0 counts as +0, NaN as larger than everything else.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -29,10 +29,34 @@ __device__ __forceinline__ float unordered(uint32_t o) {
 }
 __device__ __forceinline__ uint64_t make_key(float x, int id) { return (uint64_t)ordered(x) << 32 | (uint32_t)~id; }
 
+// Largest element of a 16-byte piece; a NaN stays.  (bf16 by its bits: from values the compiler forms bf16 maxima, four
+// instructions an element.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+template <typename T>
+__device__ __forceinline__ float piece_max(u32x4 r);
+template <>
+__device__ __forceinline__ float piece_max<float>(u32x4 r) {
+  const f32x4 v = __builtin_bit_cast(f32x4, r);
+  return __builtin_elementwise_maximum(max3(v[0], v[1], v[2]), v[3]);
+}
+template <>
+__device__ __forceinline__ float piece_max<bf16>(u32x4 r) {
+  float m = __builtin_bit_cast(float, r[0] << 16);
+  m = __builtin_elementwise_maximum(m, __builtin_bit_cast(float, r[0] & 0xFFFF0000u));
+#pragma unroll
+  for (int k = 1; k < 4; ++k)
+    m = max3(m, __builtin_bit_cast(float, r[k] << 16), __builtin_bit_cast(float, r[k] & 0xFFFF0000u));
+  return m;
+}
+
 template <int NT>
 struct TopShared {
+  static constexpr int kKeys = NT == 64 ? 1024 : kCand;
   alignas(16) uint32_t best[256];
-  alignas(16) uint64_t cand[kCand];
+  alignas(16) uint64_t cand[kKeys];
+  uint32_t places[NT];
   uint64_t floor;  // no smaller key is of interest
   uint32_t count, sum, level;
 };
@@ -53,12 +77,13 @@ __device__ __forceinline__ uint32_t block_total(TopShared<NT>& s, uint32_t n) {
 // Keeps the K largest of the C >= K keys in s.cand, in descending order, and raises s.floor to the K-th.
 template <int NT>
 __device__ __forceinline__ void keep_top(TopShared<NT>& s, int C, int K) {
-  constexpr int R = (kCand + NT - 1) / NT;
-  uint64_t key[R];
-  if (C > 512) {
+  const int tid = threadIdx.x;
+  constexpr int R = (TopShared<NT>::kKeys + NT - 1) / NT;
+  if (C > NT && C > 512) {
     // the K-th largest, from its highest bit down; the keys below it are dropped
+    uint64_t key[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) key[r] = r * NT + (int)threadIdx.x < C ? s.cand[r * NT + threadIdx.x] : 0;
+    for (int r = 0; r < R; ++r) key[r] = r * NT + tid < C ? s.cand[r * NT + tid] : 0;
     uint64_t t = 0;
     for (int bit = 63; bit >= 0; --bit) {
       const uint64_t probe = t | 1ull << bit;
@@ -67,7 +92,7 @@ __device__ __forceinline__ void keep_top(TopShared<NT>& s, int C, int K) {
       for (int r = 0; r < R; ++r) n += key[r] >= probe ? 1 : 0;
       if ((int)block_total(s, n) >= K) t = probe;
     }
-    if (threadIdx.x == 0) s.count = 0;
+    if (tid == 0) s.count = 0;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -75,83 +100,95 @@ __device__ __forceinline__ void keep_top(TopShared<NT>& s, int C, int K) {
     __syncthreads();
     C = K;
   }
-  // each key's place is the number of larger ones
-  constexpr int Q = (512 + NT - 1) / NT;
-  int place[Q];
-  const bool some = (int)(threadIdx.x & ~63u) < C, more = Q > 1 && C > NT;  // this wavefront holds keys; a second each
-#pragma unroll
-  for (int q = 0; q < Q; ++q) {
-    const int i = q * NT + threadIdx.x;
-    key[q] = i < C ? s.cand[i] : 0;
-    place[q] = 0;
-  }
-  if (threadIdx.x == 0 && C & 1) s.cand[C] = 0;  // (C < kCand here)
+  // each key's place is the number of larger ones; where keys are few, several threads count a part of the list each
+  const int keys = C <= 64 ? 64 : C <= 128 ? 128 : C <= 256 ? 256 : C <= 512 ? 512 : 1024;  // threads a part, C and more (or 2 NT)
+  const int parts = keys < NT ? NT / keys : 1, part = keys < NT ? tid / keys : 0, own = keys < NT ? tid % keys : tid;
+  if (tid == 0 && C & 1) s.cand[C] = 0;  // (C < kKeys here)
+  const bool two = C > NT;  // (C <= 2 NT: with NT = 64 there are no more than 128 keys)
+  const uint64_t k0 = own < C ? s.cand[own] : 0, k1 = two && NT + tid < C ? s.cand[NT + tid] : 0;
+  int place0 = 0, place1 = 0;
   __syncthreads();
   const u32x4* pair = reinterpret_cast<const u32x4*>(s.cand);
-  if (some) {
+  const int pairs = (C + 1) / 2, each = (pairs + parts - 1) / parts, j1 = min(pairs, (part + 1) * each);
+  if ((own & ~63) < C) {  // (this wavefront holds keys)
+    if (!two) {
 #pragma unroll 4
-    for (int j = 0; j < (C + 1) / 2; ++j) {
-      const u32x4 two = pair[j];
-      const uint64_t a = (uint64_t)two[1] << 32 | two[0], b = (uint64_t)two[3] << 32 | two[2];
-      place[0] += (a > key[0]) + (b > key[0]);
-      if (more) place[Q - 1] += (a > key[Q - 1]) + (b > key[Q - 1]);
+      for (int j = part * each; j < j1; ++j) {
+        const u32x4 o = pair[j];
+        place0 += (((uint64_t)o[1] << 32 | o[0]) > k0) + (((uint64_t)o[3] << 32 | o[2]) > k0);
+      }
+    } else {
+#pragma unroll 4
+      for (int j = 0; j < pairs; ++j) {
+        const u32x4 o = pair[j];
+        const uint64_t a = (uint64_t)o[1] << 32 | o[0], b = (uint64_t)o[3] << 32 | o[2];
+        place0 += (a > k0) + (b > k0);
+        place1 += (a > k1) + (b > k1);
+      }
     }
   }
+  s.places[tid] = place0;
   __syncthreads();
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-    if (q * NT + (int)threadIdx.x < C && place[q] < K) {
-      s.cand[place[q]] = key[q];
-      if (place[q] == K - 1) s.floor = key[q];
+  if (part == 0) {
+    for (int q = 1; q < parts; ++q) place0 += s.places[q * keys + own];
+    if (own < C && place0 < K) {
+      s.cand[place0] = k0;
+      if (place0 == K - 1) s.floor = k0;
     }
-  if (threadIdx.x == 0) s.count = K;
+    if (two && NT + tid < C && place1 < K) {
+      s.cand[place1] = k1;
+      if (place1 == K - 1) s.floor = k1;
+    }
+  }
+  if (tid == 0) s.count = K;
   __syncthreads();
 }
 
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void top_logits_kernel(const T* __restrict__ logits, int V, int64_t ld, int K,
-                                                        float* __restrict__ values, int32_t* __restrict__ ids) {
-  constexpr int EPV = RowSplit<T>::EPV;
+// NT threads a row, NP pieces of 16 bytes a thread in a chunk, or (ONE) of one element: rows too short to give every
+// thread a whole piece.
+template <typename T, int NT, int NP, bool ONE>
+__global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : 4) void top_logits_kernel(
+    const T* __restrict__ logits, int V, int64_t ld, int K, float* __restrict__ values, int32_t* __restrict__ ids) {
+  constexpr int EPV = ONE ? 1 : RowSplit<T>::EPV;
+  constexpr bool kAgain = NP > 4 && !ONE;  // pieces that matter are read again (from L2) instead of held
   typedef typename RowVec<T>::type VT;
   __shared__ TopShared<NT> s;
   const int tid = threadIdx.x;
   const int64_t row = blockIdx.x;
   const T* x = logits + row * ld;
   const RowSplit<T> sp(x, V);
-  const u32x4* body = reinterpret_cast<const u32x4*>(x + sp.head);
+  const int head = ONE ? 0 : sp.head, pieces = ONE ? V : sp.pieces, last = pieces - 1;
+  const u32x4* body = reinterpret_cast<const u32x4*>(x + head);
   if (tid == 0) {
     s.level = 0;
     s.count = 0;
   }
-  const int own = sp.single(tid, NT, V);
+  const int own = ONE ? -1 : sp.single(tid, NT, V);
   const float xs = own >= 0 ? to_f32(x[own]) : -INFINITY;
-  const int last = sp.pieces - 1;
   const int groups = K <= 32 ? 64 : K <= 64 ? 128 : 256;  // twice K bounds nearly as well as more, for fewer comparisons
   bool crowded = false;
-  for (int p0 = 0; p0 == 0 || p0 < sp.pieces; p0 += NT * kPieces) {
-    float top[kPieces];  // largest of each piece; the pieces themselves are read again (from L2) where they matter
-    {
-      u32x4 raw[kPieces];
+  uint32_t level = 0;  // value of the bound
+  for (int p0 = 0; p0 == 0 || p0 < pieces; p0 += NT * NP) {
+    float top[NP];  // largest of each piece
+    u32x4 raw[ONE ? 1 : NP];
+    if constexpr (ONE) {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) raw[i] = last >= 0 ? body[min(p0 + i * NT + tid, last)] : u32x4{0, 0, 0, 0};
+      for (int i = 0; i < NP; ++i) top[i] = to_f32(x[min(p0 + i * NT + tid, last)]);
+    } else {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const VT v = __builtin_bit_cast(VT, raw[i]);
-        float m = to_f32(v[0]);
+      for (int i = 0; i < NP; ++i) raw[i] = last >= 0 ? body[min(p0 + i * NT + tid, last)] : u32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int k = 1; k < EPV; ++k) m = __builtin_elementwise_maximum(m, to_f32(v[k]));  // (a NaN stays)
-        top[i] = m;
-      }
+      for (int i = 0; i < NP; ++i) top[i] = piece_max<T>(raw[i]);
     }
     const bool with_single = p0 == 0 && own >= 0;
     if (p0 == 0) {
       // the K-th largest of `groups` groups' largest values: the largest that at least K of them reach
       uint32_t g = with_single ? ordered(xs) : 0;
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i)
-        if (p0 + i * NT + tid < sp.pieces) g = max(g, ordered(top[i]));
+      for (int i = 0; i < NP; ++i)
+        if (i * NT + tid < pieces) g = max(g, ordered(top[i]));
       for (int off = 1; off < NT / groups; off <<= 1) g = max(g, (uint32_t)__shfl_xor(g, off, 64));
-      if (tid % (NT / groups) == 0) s.best[tid / (NT / groups)] = g;
+      if (NT <= groups || tid % (NT / groups) == 0) s.best[NT <= groups ? tid : tid / (NT / groups)] = g;
       __syncthreads();
       if (tid < groups) {
         const uint32_t mine = s.best[tid];
@@ -167,28 +204,50 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(const T* __restrict__ lo
       __syncthreads();
     }
     const uint64_t floor = p0 == 0 ? (uint64_t)s.level << 32 : s.floor;
-    const uint32_t level = (uint32_t)(floor >> 32);
-    auto offer = [&](float v, int id) {
-      const uint64_t k = make_key(v, id);
-      if (k >= floor) {
-        const uint32_t at = atomicAdd(&s.count, 1u);
-        if (at < kCand) s.cand[at] = k;
-      }
+    level = (uint32_t)(floor >> 32);
+    auto offer = [&](const float* v, int n, int id) {
+      uint32_t take = 0;
+#pragma unroll
+      for (int k = 0; k < n; ++k) take |= make_key(v[k], id + k) >= floor ? 1u << k : 0;
+      if (!take) return;
+      uint32_t at = atomicAdd(&s.count, (uint32_t)__popc(take));
+#pragma unroll
+      for (int k = 0; k < n; ++k)
+        if (take >> k & 1) {
+          if (at < (uint32_t)TopShared<NT>::kKeys) s.cand[at] = make_key(v[k], id + k);
+          ++at;
+        }
     };
-    if (with_single) offer(xs, own);
-    uint32_t reach = 0;
+    auto offer_piece = [&](u32x4 r, int p) {
+      const VT v = __builtin_bit_cast(VT, r);
+      float f[EPV];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) reach |= p0 + i * NT + tid < sp.pieces && ordered(top[i]) >= level ? 1u << i : 0;
-    while (reach) {
-      const int p = p0 + (__ffs(reach) - 1) * NT + tid;
-      reach &= reach - 1;
-      const VT v = __builtin_bit_cast(VT, body[p]);
+      for (int k = 0; k < EPV; ++k) f[k] = to_f32(v[k]);
+      offer(f, EPV, head + p * EPV);
+    };
+    if (with_single) offer(&xs, 1, own);
+    if constexpr (kAgain) {
+      uint32_t reach = 0;
 #pragma unroll
-      for (int k = 0; k < EPV; ++k) offer(to_f32(v[k]), sp.head + p * EPV + k);
+      for (int i = 0; i < NP; ++i) reach |= p0 + i * NT + tid < pieces && ordered(top[i]) >= level ? 1u << i : 0;
+      while (reach) {
+        const int p = p0 + (__ffs(reach) - 1) * NT + tid;
+        reach &= reach - 1;
+        offer_piece(body[p], p);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int p = p0 + i * NT + tid;
+        if (p < pieces && ordered(top[i]) >= level) {
+          if constexpr (ONE) offer(&top[i], 1, p);
+          else offer_piece(raw[i], p);
+        }
+      }
     }
     __syncthreads();
     const int C = (int)s.count;
-    if (C > kCand) {
+    if (C > TopShared<NT>::kKeys || (NT == 64 && C > 128)) {
       crowded = true;
       break;
     }
@@ -196,22 +255,56 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(const T* __restrict__ lo
     else __syncthreads();
   }
   if (crowded) {
-    // the row's K-th largest key, from its highest bit down; the row is read for each
-    auto each = [&](auto f) {
-      for (int c = tid; c < V; c += NT) f(make_key(to_f32(x[c]), c));
-    };
-    uint64_t t = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t probe = t | 1ull << bit;
-      uint32_t n = 0;
-      each([&](uint64_t k) { n += k >= probe ? 1 : 0; });
-      if ((int)block_total(s, n) >= K) t = probe;
+    // Mostly ties: if fewer than K elements exceed the bound's value, they and the first of those equal to it are the answer.
+    uint32_t more = 0, same = 0;
+    for (int c = tid; c < V; c += NT) {
+      const uint32_t o = ordered(to_f32(x[c]));
+      more += o > level;
+      same += o == level;
     }
+    more = block_total(s, more);
+    same = block_total(s, same);
     if (tid == 0) s.count = 0;
     __syncthreads();
-    each([&](uint64_t k) {
-      if (k >= t) s.cand[atomicAdd(&s.count, 1u) & (kCand - 1)] = k;  // K of them
-    });
+    if ((int)more < K && (int)(more + same) >= K) {
+      int need = K - (int)more;  // of those equal to the bound, in order of ids
+      for (int c0 = 0; c0 < V; c0 += NT) {
+        const int c = c0 + tid;
+        const uint64_t k = c < V ? make_key(to_f32(x[c]), c) : 0;
+        if ((uint32_t)(k >> 32) > level) s.cand[atomicAdd(&s.count, 1u)] = k;
+        if (need > 0) {
+          const uint64_t eq = __ballot(c < V && (uint32_t)(k >> 32) == level);
+          if ((tid & 63) == 0) s.places[tid >> 6] = (uint32_t)__popcll(eq);
+          __syncthreads();
+          int before = 0, all = 0;
+          for (int q = 0; q < NT / 64; ++q) {
+            before += q < tid >> 6 ? (int)s.places[q] : 0;
+            all += (int)s.places[q];
+          }
+          if ((eq >> (tid & 63) & 1) && before + __popcll(eq & ((1ull << (tid & 63)) - 1)) < need)
+            s.cand[atomicAdd(&s.count, 1u)] = k;
+          need -= all;
+          __syncthreads();
+        }
+      }
+    } else {
+      // the row's K-th largest key, from its highest bit down; the row is read for each
+      auto each = [&](auto f) {
+        for (int c = tid; c < V; c += NT) f(make_key(to_f32(x[c]), c));
+      };
+      uint64_t t = 0;
+      for (int bit = 63; bit >= 0; --bit) {
+        const uint64_t probe = t | 1ull << bit;
+        uint32_t n = 0;
+        each([&](uint64_t k) { n += k >= probe ? 1 : 0; });
+        if ((int)block_total(s, n) >= K) t = probe;
+      }
+      if (tid == 0) s.count = 0;
+      __syncthreads();
+      each([&](uint64_t k) {
+        if (k >= t) s.cand[atomicAdd(&s.count, 1u) & (TopShared<NT>::kKeys - 1)] = k;  // K of them
+      });
+    }
     __syncthreads();
     keep_top(s, K, K);
   }
@@ -227,16 +320,20 @@ __global__ __launch_bounds__(NT) void top_logits_kernel(const T* __restrict__ lo
 hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, int64_t ld, int K, float* values,
                              int32_t* ids, hipStream_t st) {
   if (rows <= 0) return hipSuccess;
-  // few rows: all of a compute unit's wavefronts on one; many: four workgroups of a compute unit overlap
-  const bool wide = rows < 512 && V >= 16384;
-  auto go = [&](auto kern, auto* p) { kern<<<(unsigned)rows, wide ? 1024 : 256, 0, st>>>(p, V, ld, K, values, ids); };
-  if (type == IN_BF16) {
-    if (wide) go(top_logits_kernel<bf16, 1024>, (const bf16*)logits);
-    else go(top_logits_kernel<bf16, 256>, (const bf16*)logits);
-  } else {
-    if (wide) go(top_logits_kernel<float, 1024>, (const float*)logits);
-    else go(top_logits_kernel<float, 256>, (const float*)logits);
-  }
+  const int pieces = ceil_div(V, type == IN_BF16 ? 8 : 4);
+  auto go = [&](auto kern, int nt, auto* p) { kern<<<(unsigned)rows, nt, 0, st>>>(p, V, ld, K, values, ids); };
+  auto of_type = [&](auto* p) {
+    typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type T;
+    // short rows: a wavefront, or a workgroup, that reads elements one by one; few rows: all of a compute unit's
+    // wavefronts on one; else workgroups of four wavefronts, more of them at a time on rows of up to 16 KB
+    if (V <= 1024 && K <= 32) go(top_logits_kernel<T, 64, 16, true>, 64, p);
+    else if (V <= 4096 && K > pieces / 8) go(top_logits_kernel<T, 256, 16, true>, 256, p);
+    else if (rows < 512 && V >= 16384) go(top_logits_kernel<T, 1024, 16, false>, 1024, p);
+    else if (pieces <= 1024) go(top_logits_kernel<T, 256, 4, false>, 256, p);
+    else go(top_logits_kernel<T, 256, 16, false>, 256, p);
+  };
+  if (type == IN_BF16) of_type((const bf16*)logits);
+  else of_type((const float*)logits);
   return hipGetLastError();
 }
 
