@@ -366,7 +366,9 @@ void rows_of_mode(const DistillArgs& a, const T* x, T* g, int64_t rows, hipStrea
   // a row in a workgroup's registers, 16 pieces a thread at most; few rows: more threads for each
   if (pieces <= 256) go(distill_rows_kernel<T, 64, 4, MODE, WHOLE_ROW, GRAD>, 64);
   else if (rows < 512 && pieces <= 4096) go(distill_rows_kernel<T, 1024, 4, MODE, WHOLE_ROW, GRAD>, 1024);
+  else if (pieces <= 512) go(distill_rows_kernel<T, 128, 4, MODE, WHOLE_ROW, GRAD>, 128);
   else if (pieces <= 1024) go(distill_rows_kernel<T, 256, 4, MODE, WHOLE_ROW, GRAD>, 256);
+  else if (pieces <= 2048) go(distill_rows_kernel<T, 256, 8, MODE, WHOLE_ROW, GRAD>, 256);
   else if (pieces <= 4096) go(distill_rows_kernel<T, 256, 16, MODE, WHOLE_ROW, GRAD>, 256);
   else if (pieces <= 8192) go(distill_rows_kernel<T, 512, 16, MODE, WHOLE_ROW, GRAD>, 512);
   else go(distill_rows_kernel<T, 1024, 16, MODE, WHOLE_ROW, GRAD>, 1024);

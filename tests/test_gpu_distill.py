@@ -69,6 +69,20 @@ def test_loss_and_gradient(rows, vocab, k, tau, soft, z, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,k,mix", [(520, 1600, 7, 0), (520, 1601, 100, 2), (513, 3500, 5, 1), (512, 9001, 33, 2), (512, 17003, 16, 1),
+                                              (256, 66001, 8, 4), (300, 131073, 3, 2)])
+def test_many_rows(rows, vocab, k, mix, dtype):
+    """Rows enough for workgroups that share a compute unit, of every size of theirs."""
+    import paper_2203_17189_amd as P
+    x, tgt, t, ids = make(rows, vocab, k, vocab)
+    tx = dev(x, dtype)
+    _, _, g = check(P, x, tgt, t, ids, *MIX[mix], dtype, tx=tx.clone())
+    tau, soft, z = MIX[mix]
+    P.t5_distill_loss_and_grad(tx, ints(tgt), dev(t), ints(ids), temperature=tau, soft_weight=soft, z_loss=z, dlogits=tx)
+    assert torch.equal(tx, g)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,vocab,k", [(5, 40, 3), (12, 5001, 20), (6, 33000, 64)])
 def test_without_targets(rows, vocab, k, dtype):
     import paper_2203_17189_amd as P

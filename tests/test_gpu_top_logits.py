@@ -64,6 +64,34 @@ def test_rows_with_a_longer_stride(vocab, ld, shift, dtype):
     _check(x, 32, *P.t5_top_logits(x, 32))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["random", "equal", "coarse", "stripes", "odd"])
+@pytest.mark.parametrize("rows,vocab,k", [(600, 100, 32), (600, 1024, 32), (600, 1025, 33), (700, 4096, 20), (700, 8200, 128), (513, 20000, 200)])
+def test_many_rows(rows, vocab, k, kind, dtype):
+    """Rows enough for workgroups that share a compute unit; long rows of the few-rows kernel are above."""
+    import paper_2203_17189_amd as P
+    x = dev(_rows(rows, vocab, kind, np.random.default_rng(vocab + k)), dtype)
+    values, ids = P.t5_top_logits(x, k)
+    some = np.r_[0:40, rows - 40:rows]
+    _check(x[torch.from_numpy(some).cuda()], k, values[torch.from_numpy(some).cuda()], ids[torch.from_numpy(some).cuda()])
+    v2, i2 = P.t5_top_logits(x.flip(0).contiguous(), k)
+    assert torch.equal(i2.flip(0), ids) and torch.equal(v2.flip(0).nan_to_num(9e9), values.nan_to_num(9e9))
+
+
+def test_thousands_of_ties_next_to_the_bound():
+    """A few values above, thousands equal to the K-th: the first of those, by id, in rows of one and of several chunks."""
+    import paper_2203_17189_amd as P
+    for vocab in (900, 4000, 33000, 200000):
+        for dtype in ("f32", "bf16"):
+            rng = np.random.default_rng(vocab)
+            x = np.where(rng.random((4, vocab)) < 0.7, 2.0, -1.0)
+            x[:, rng.permutation(vocab)[:20]] = 3.0 + np.arange(20) % 3
+            x[1] = np.where(np.arange(vocab) < vocab - 30, -np.inf, 0.0)
+            x[2, :] = -np.inf
+            for k in (20, 21, 31, 100):
+                _check(dev(x, dtype), k, *P.t5_top_logits(dev(x, dtype), k))
+
+
 def test_empty():
     import paper_2203_17189_amd as P
     v, i = P.t5_top_logits(torch.zeros(0, 10, device="cuda"), 3)
