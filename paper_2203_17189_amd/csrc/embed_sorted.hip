@@ -14,41 +14,73 @@ __device__ __forceinline__ uint32_t clamp_id(int32_t id, int vocab) {
   return (uint32_t)(id < 0 ? 0 : (id >= vocab ? vocab - 1 : id));
 }
 
-template <typename T, int N> struct Piece { typedef __attribute__((ext_vector_type(N))) T type; };
-template <typename T> struct Piece<T, 1> { typedef T type; };
+// N elements at an address that is a multiple of the element's size and need be of nothing more (the part loads and stores
+// them whole, wherever they lie).
+template <typename T, int N> struct Piece {
+  typedef __attribute__((ext_vector_type(N))) T vec;
+  typedef vec __attribute__((aligned(sizeof(T)))) type;
+};
+template <typename T> struct Piece<T, 1> { typedef T vec, type; };
+
+// VEC columns of a row of d >= VEC, as many as end with the row where the lane's own would reach beyond it: then the first
+// `shift` belong to the lane before and are read but not written.
+struct Cols {
+  int c, shift;
+  bool on;
+  __device__ __forceinline__ Cols(int at, int d, int vec) {
+    on = at < d;
+    c = on ? min(at, d - vec) : 0;
+    shift = on ? at - c : 0;
+  }
+};
+template <int VEC, typename F>
+__device__ __forceinline__ void put_cols(float* o, const Cols& q, F v, bool add) {
+  if constexpr (VEC == 1) {
+    *o = add ? *o + v : v;
+  } else if (q.shift == 0) {
+    typedef typename Piece<float, VEC>::type P;
+    *reinterpret_cast<P*>(o) = add ? *reinterpret_cast<P*>(o) + v : v;
+  } else {
+#pragma unroll
+    for (int k = 1; k < VEC; ++k)
+      if (k >= q.shift) o[k] = add ? o[k] + v[k] : v[k];
+  }
+}
 
 // ------------------------------------------------------------------------------------------------
-// Lookup.  A workgroup takes rows_per_block consecutive tokens, their rows cut into pieces of EPV elements (16 bytes
-// where rows allow it), four pieces per thread in flight.
+// Lookup.  A workgroup takes rows_per_block consecutive tokens, their rows cut into pieces of EPV elements, four pieces per
+// thread in flight.  A row's last piece ends with the row: it may share elements with the one before, which then get the
+// same values twice.
 // ------------------------------------------------------------------------------------------------
 template <typename T, int EPV>
 __global__ __launch_bounds__(256) void embed_scaled_fwd_kernel(const int32_t* __restrict__ tok, const T* __restrict__ E,
                                                                T* __restrict__ x, int64_t n, int d, int vocab,
                                                                float scale, int rows_per_block) {
   typedef typename Piece<T, EPV>::type P;
-  const uint32_t cpr = (uint32_t)d / EPV;
+  const uint32_t cpr = ((uint32_t)d + EPV - 1) / EPV;
   const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
   const uint32_t m = (uint32_t)(n - r0 < rows_per_block ? n - r0 : rows_per_block) * cpr;
   for (uint32_t t0 = threadIdx.x; t0 < m; t0 += 1024) {
-    P v[4];
+    typename Piece<T, EPV>::vec v[4];
+    uint32_t at[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const uint32_t t = t0 + 256 * u;
       if (t >= m) break;
-      const uint32_t r = t / cpr, c = t - r * cpr;
-      v[u] = reinterpret_cast<const P*>(E + (size_t)clamp_id(tok[r0 + r], vocab) * d)[c];
+      const uint32_t r = t / cpr, c = min((t - r * cpr) * EPV, (uint32_t)d - EPV);
+      at[u] = r * (uint32_t)d + c;
+      v[u] = *reinterpret_cast<const P*>(E + (size_t)clamp_id(tok[r0 + r], vocab) * d + c);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const uint32_t t = t0 + 256 * u;
-      if (t >= m) break;
+      if (t0 + 256 * u >= m) break;
       if constexpr (EPV == 1) {
         v[u] = from_f32<T>(to_f32(v[u]) * scale);
       } else {
 #pragma unroll
         for (int k = 0; k < EPV; ++k) v[u][k] = from_f32<T>(to_f32(v[u][k]) * scale);
       }
-      reinterpret_cast<P*>(x + (size_t)r0 * d)[t] = v[u];
+      *reinterpret_cast<P*>(x + (size_t)r0 * d + at[u]) = v[u];
     }
   }
 }
@@ -292,32 +324,26 @@ struct SumArgs {
 template <typename T, int VEC, int G>
 __global__ __launch_bounds__(256) void embed_tile_sum_kernel(SumArgs a) {
   typedef typename Piece<T, VEC>::type P;
-  typedef typename Piece<float, VEC>::type F;
+  typedef typename Piece<float, VEC>::vec F;
   uint32_t unit = blockIdx.x * (256 / G) + threadIdx.x / G;
   if (G == 64) unit = __builtin_amdgcn_readfirstlane(unit);
   const int t = unit / a.slabs;
   if (t >= a.tiles) return;
-  const int c = ((unit - t * a.slabs) * G + threadIdx.x % G) * VEC;
-  const bool on = c < a.d;
-  const T* dx = (const T*)a.dx + (on ? c : 0);
+  const Cols q(((unit - t * a.slabs) * G + threadIdx.x % G) * VEC, a.d, VEC);
+  const T* dx = (const T*)a.dx + q.c;
   const int t0 = t * a.tile, t1 = min(t0 + a.tile, a.n);
   uint32_t cur = a.sorted[t0].x;
   const bool from_before = t0 > 0 && a.sorted[t0 - 1].x == cur;
   bool first = true;
   F acc{};
   auto flush = [&](bool part) {
-    if (!on) return;
-    const F v = acc * a.scale;
-    if (part) {
-      *reinterpret_cast<F*>(a.partial + ((size_t)t * 2 + (first ? 0 : 1)) * a.d + c) = v;
-    } else {
-      F* o = reinterpret_cast<F*>(a.dE + (size_t)cur * a.d + c);
-      *o = a.accumulate ? *o + v : v;
-    }
+    if (!q.on) return;
+    if (part) put_cols<VEC, F>(a.partial + ((size_t)t * 2 + (first ? 0 : 1)) * a.d + q.c, q, acc * a.scale, false);
+    else put_cols<VEC, F>(a.dE + (size_t)cur * a.d + q.c, q, acc * a.scale, a.accumulate);
   };
   for (int i = t0; i < t1; i += 8) {
     u32x2 s[8];
-    P v[8];
+    typename Piece<T, VEC>::vec v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = a.sorted[min(i + j, t1 - 1)];
 #pragma unroll
@@ -346,7 +372,8 @@ __global__ __launch_bounds__(256) void embed_tile_sum_kernel(SumArgs a) {
 // the run's parts and writes the row.  The eight wavefronts take a piece each, or a share of a piece's parts, in order.
 template <int VEC>
 __global__ __launch_bounds__(512) void embed_join_kernel(SumArgs a) {
-  typedef typename Piece<float, VEC>::type F;
+  typedef typename Piece<float, VEC>::type P;
+  typedef typename Piece<float, VEC>::vec F;
   __shared__ F red[8][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int t = blockIdx.x, t0 = t * a.tile, t1 = min(t0 + a.tile, a.n);
@@ -369,16 +396,16 @@ __global__ __launch_bounds__(512) void embed_join_kernel(SumArgs a) {
   const int slabs = min(a.join, a.slabs - (int)blockIdx.y * a.join);
   const int shares = slabs == 1 ? 8 : slabs == 2 ? 4 : 2;
   const int slab = w / shares, each = (parts + shares - 1) / shares, p0 = (w % shares) * each, p1 = min(p0 + each, parts);
-  const int c = ((blockIdx.y * a.join + slab) * 64 + lane) * VEC;
-  const bool on = slab < slabs && c < a.d;
-  const float* src = a.partial + (size_t)t * 2 * a.d + (on ? c : 0);
+  const Cols cols(((blockIdx.y * a.join + slab) * 64 + lane) * VEC, a.d, VEC);
+  const bool on = slab < slabs && cols.on;
+  const float* src = a.partial + (size_t)t * 2 * a.d + cols.c;
   F s{};
   for (int p = p0; p < p1; p += 8) {
     F v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int q = min(p + j, p1 - 1);
-      v[j] = *reinterpret_cast<const F*>(src + (size_t)(2 * q + (q == 0 && !whole ? 1 : 0)) * a.d);
+      v[j] = *reinterpret_cast<const P*>(src + (size_t)(2 * q + (q == 0 && !whole ? 1 : 0)) * a.d);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -388,8 +415,7 @@ __global__ __launch_bounds__(512) void embed_join_kernel(SumArgs a) {
   __syncthreads();
   if (w % shares != 0 || !on) return;
   for (int q = 1; q < shares && q * each < parts; ++q) s += red[w + q][lane];
-  F* o = reinterpret_cast<F*>(a.dE + (size_t)last * a.d + c);
-  *o = a.accumulate ? *o + s : s;
+  put_cols<VEC, F>(a.dE + (size_t)last * a.d + cols.c, cols, s, a.accumulate);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -415,7 +441,7 @@ __device__ __forceinline__ F sum_listed(const T* dx, int d, const uint16_t* list
   typedef typename Piece<T, VEC>::type P;
   F acc{};
   for (int l = l0; l < l1; l += 8) {
-    P x[8];
+    typename Piece<T, VEC>::vec x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const P*>(dx + (size_t)list[min(l + j, l1 - 1)] * d);
 #pragma unroll
@@ -434,7 +460,7 @@ __device__ __forceinline__ F sum_listed(const T* dx, int d, const uint16_t* list
 
 template <typename T, int VEC>
 __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
-  typedef typename Piece<float, VEC>::type F;
+  typedef typename Piece<float, VEC>::vec F;
   __shared__ uint32_t ids[kOwnerTokens];
   __shared__ uint16_t list[kOwnerTokens], few[8][kOwnerAlone];
   __shared__ F red[8][64];
@@ -457,7 +483,10 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
     for (int r = w; r < a.zero_rows && v0 + r < (uint32_t)a.vocab; r += 8) {
       if (seen[r]) continue;
       float* o = a.dE + (size_t)(v0 + r) * a.d;
-      for (int c = lane * VEC; c < a.d; c += 64 * VEC) *reinterpret_cast<F*>(o + c) = F{};
+      for (int c = lane * VEC; c < a.d; c += 64 * VEC) {
+        const Cols q(c, a.d, VEC);
+        put_cols<VEC, F>(o + q.c, q, F{}, false);
+      }
     }
     return;
   }
@@ -465,10 +494,7 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
   for (int k = 0; k < kOwnerTokens / 512; ++k) ids[k * 512 + tid] = id[k];
   if (tid == 0) n_many = 0;
   __syncthreads();
-  auto put = [&](uint32_t v, int c, F s) {
-    F* o = reinterpret_cast<F*>(a.dE + (size_t)v * a.d + c);
-    *o = a.accumulate ? *o + s * a.scale : s * a.scale;
-  };
+  auto put = [&](uint32_t v, const Cols& q, F s) { put_cols<VEC, F>(a.dE + (size_t)v * a.d + q.c, q, s * a.scale, a.accumulate); };
   const int split = blockIdx.x % a.splits, own = blockIdx.x / a.splits * 8 + w;
   const int c_begin = split * a.split_cols, c_end = min(c_begin + a.split_cols, a.d);
   if (own < a.n) {
@@ -502,7 +528,10 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
       if (lane == 0) many[atomicAdd(&n_many, 1u)] = v;
     } else if (first) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      for (int c = c_begin + lane * VEC; c < c_end; c += 64 * VEC) put(v, c, sum_listed<T, VEC, F>((const T*)a.dx + c, a.d, few[w], 0, m));
+      for (int c = c_begin + lane * VEC; c < c_end; c += 64 * VEC) {
+        const Cols q(c, a.d, VEC);
+        put(v, q, sum_listed<T, VEC, F>((const T*)a.dx + q.c, a.d, few[w], 0, m));
+      }
     }
   }
   __syncthreads();
@@ -531,14 +560,14 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
     __syncthreads();
     const int each = (m + 7) / 8, l0 = w * each, l1 = min(l0 + each, m);
     for (int c0 = c_begin; c0 < c_end; c0 += 64 * VEC) {
-      const int c = c0 + lane * VEC;
-      red[w][lane] = sum_listed<T, VEC, F>((const T*)a.dx + (c < c_end ? c : 0), a.d, list, l0, l1);
+      const Cols q(c0 + lane * VEC, c_end, VEC);  // (a part ends with the row, or with whole pieces)
+      red[w][lane] = sum_listed<T, VEC, F>((const T*)a.dx + q.c, a.d, list, l0, l1);
       __syncthreads();
-      if (w == 0 && c < c_end) {
+      if (w == 0 && q.on) {
         F s = red[0][lane];
 #pragma unroll
-        for (int q = 1; q < 8; ++q) s += red[q][lane];
-        put(v, c, s);
+        for (int j = 1; j < 8; ++j) s += red[j][lane];
+        put(v, q, s);
       }
       __syncthreads();
     }
@@ -600,14 +629,11 @@ void launch_tile_sum(const SumArgs& a, bool vec, hipStream_t st) {
     b.slabs = ceil_div(a.d, G * vec_n);
     kern<<<(unsigned)ceil_div((int64_t)b.tiles * b.slabs, 256 / G), 256, 0, st>>>(b);
   };
-  // 64 lanes a tile where they have columns to hold, else 16 (a wavefront then takes four tiles)
-  if (vec) {
-    if (a.d > 128) go(embed_tile_sum_kernel<T, 4, 64>, 4, 64);
-    else go(embed_tile_sum_kernel<T, 4, 16>, 4, 16);
-  } else {
-    if (a.d > 32) go(embed_tile_sum_kernel<T, 1, 64>, 1, 64);
-    else go(embed_tile_sum_kernel<T, 1, 16>, 1, 16);
-  }
+  // 64 lanes a tile where they have columns to hold, else 32 or 16 (a wavefront then takes two or four tiles)
+  if (!vec) go(embed_tile_sum_kernel<T, 1, 16>, 1, 16);
+  else if (a.d > 128) go(embed_tile_sum_kernel<T, 4, 64>, 4, 64);
+  else if (a.d > 64) go(embed_tile_sum_kernel<T, 4, 32>, 4, 32);
+  else go(embed_tile_sum_kernel<T, 4, 16>, 4, 16);
 }
 
 }  // namespace
@@ -616,15 +642,14 @@ hipError_t launch_embed_scaled_fwd(const int32_t* tokens, const void* E, void* x
                                    float scale, hipStream_t st) {
   if (n <= 0) return hipSuccess;
   const int epv = type == IN_BF16 ? 8 : 4;
-  const bool vec = d % epv == 0 && (((uintptr_t)E | (uintptr_t)x) & 15) == 0;
-  const int cpr = vec ? d / epv : d;
-  const int rpb = std::max(1, 1024 / cpr);
+  const bool whole = d >= epv;
+  const int rpb = std::max(1, 1024 / (whole ? ceil_div(d, epv) : d));
   const unsigned grid = (unsigned)ceil_div(n, rpb);
   if (type == IN_BF16) {
-    if (vec) embed_scaled_fwd_kernel<bf16, 8><<<grid, 256, 0, st>>>(tokens, (const bf16*)E, (bf16*)x, n, d, vocab, scale, rpb);
+    if (whole) embed_scaled_fwd_kernel<bf16, 8><<<grid, 256, 0, st>>>(tokens, (const bf16*)E, (bf16*)x, n, d, vocab, scale, rpb);
     else embed_scaled_fwd_kernel<bf16, 1><<<grid, 256, 0, st>>>(tokens, (const bf16*)E, (bf16*)x, n, d, vocab, scale, rpb);
   } else {
-    if (vec) embed_scaled_fwd_kernel<float, 4><<<grid, 256, 0, st>>>(tokens, (const float*)E, (float*)x, n, d, vocab, scale, rpb);
+    if (whole) embed_scaled_fwd_kernel<float, 4><<<grid, 256, 0, st>>>(tokens, (const float*)E, (float*)x, n, d, vocab, scale, rpb);
     else embed_scaled_fwd_kernel<float, 1><<<grid, 256, 0, st>>>(tokens, (const float*)E, (float*)x, n, d, vocab, scale, rpb);
   }
   return hipGetLastError();
@@ -638,7 +663,7 @@ size_t embed_sorted_ws_bytes(int64_t n, int vocab, int d) {
 hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int type, float* dE, int64_t n, int d, int vocab,
                                    float scale, int accumulate, void* ws, hipStream_t st) {
   if (n <= 0 && accumulate) return hipSuccess;
-  const bool vec = d % 4 == 0 && (((uintptr_t)dx & (type == IN_BF16 ? 7 : 15)) | ((uintptr_t)dE & 15)) == 0;
+  const bool vec = d >= 4;
   if (n <= kOwnerTokens) {
     OwnerArgs a;
     a.tok = tokens; a.dx = dx; a.dE = dE; a.n = (int)n; a.d = d; a.vocab = vocab; a.accumulate = accumulate; a.scale = scale;
