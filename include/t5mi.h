@@ -352,18 +352,18 @@ typedef struct {
 int t5_embed_fwd(const t5_embed_cfg* cfg, const int32_t* tokens, const void* table, void* x, void* stream);
 
 /* Its gradient:  dtable[v, :] (+)= scale * sum over { t : tokens[t] = v } of dx[t, :], float32 [vocab, d_model].
- * Positions are sorted by id and summed in an order that depends on tokens alone: the same bits every time.
+ * Positions are sorted by id and summed in an order that depends on tokens and sizes alone: the same bits every time.
  * accumulate == 0 writes every row (rows of ids that do not occur: zeros); accumulate != 0 adds to the rows of ids that
  * occur and touches no other.  n_tokens == 0 writes zeros, or nothing.
- * Errors: as t5_embed_fwd; small workspace -> T5_ERR_WORKSPACE. */
+ * Errors: as t5_embed_fwd; workspace small, or not 256-byte aligned -> T5_ERR_WORKSPACE. */
 size_t t5_embed_bwd_workspace_bytes(const t5_embed_cfg* cfg);
 int t5_embed_bwd(const t5_embed_cfg* cfg, const int32_t* tokens, const void* dx, float* dtable, int accumulate,
                  void* workspace, size_t workspace_bytes, void* stream);
 
 /* The top_k largest logits of each row, descending, equal ones by ascending id: what a teacher hands to
  * t5_distill_loss_and_grad.  logits: rows of vocab elements of dtype, ld elements apart; values: float32 [rows, top_k]
- * (the logits themselves, exactly); ids: int32 [rows, top_k].  -0 and +0 are equal; NaN counts as larger than +inf
- * and comes back as NaN.  Elements between vocab and ld are not read.  rows == 0 is a no-op.
+ * (the logits themselves, exactly); ids: int32 [rows, top_k].  -0 and +0 are equal (and come back as +0); NaN counts as
+ * larger than +inf and comes back as NaN.  Elements between vocab and ld are not read.  rows == 0 is a no-op.
  * Errors: NULL with rows > 0 -> T5_ERR_NULL; rows < 0, vocab < 2, ld < vocab, top_k < 1 or > vocab -> T5_ERR_SHAPE;
  * rows > 2^24, vocab > 2^22, ld > 2^32, top_k > 256, unknown dtype -> T5_ERR_UNSUPPORTED. */
 typedef struct {
@@ -386,9 +386,9 @@ int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* value
  * dlogits: gradient of loss, rows ld elements apart, elements between vocab and ld left alone; it may be logits itself,
  * or NULL: then the loss alone is computed.  Logits of -inf are allowed (their gradient is that of q = 0; an entry of
  * positive probability there makes the loss +inf); a row of nothing but -inf gives NaN.  Sums are float32.
- * Errors: as t5_top_logits; small workspace -> T5_ERR_WORKSPACE; loss NULL, or targets NULL with soft_weight != 1 ->
- * T5_ERR_NULL; temperature <= 0 or not
- * finite (nor its inverse), soft_weight outside [0, 1], z_loss < 0 or not finite -> T5_ERR_SHAPE.  rows == 0 writes 0. */
+ * Errors: as t5_top_logits; workspace small, or not 256-byte aligned -> T5_ERR_WORKSPACE; loss NULL, or targets NULL
+ * with soft_weight != 1 -> T5_ERR_NULL; temperature <= 0 or not finite (nor its inverse), soft_weight outside [0, 1],
+ * z_loss < 0 or not finite -> T5_ERR_SHAPE.  rows == 0 writes 0. */
 typedef struct {
   int64_t rows, ld;
   int32_t vocab, top_k;
@@ -407,8 +407,9 @@ int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, cons
  * tokens at a time, the workspace holds one layer's activations.  The configuration's dropout applies as everywhere: a
  * teacher's has dropout_rate 0.
  * The student's side: t5_stack_loss_and_grad with the loss of t5_distill_loss_and_grad in place of the cross-entropy,
- * z_loss from the configuration, teacher_logits and teacher_ids [batch, seq, top_k].  The embedding gradient is the one
- * of t5_embed_bwd (the same bits every time, whatever block.deterministic says).  All else as in the call it stands beside.
+ * z_loss from the configuration, teacher_logits and teacher_ids [batch, seq, top_k].  The embedded tokens' gradient is
+ * added to the embedding's as by t5_embed_bwd (the same bits every time, whatever block.deterministic says; with
+ * tied_logits the output matrix's part of that gradient follows block.deterministic).  All else as in the call beside it.
  * Errors: as that call and t5_distill_loss_and_grad (top_k > vocab -> T5_ERR_SHAPE, > 256 -> T5_ERR_UNSUPPORTED). */
 typedef struct {
   int32_t top_k;

@@ -564,12 +564,12 @@ def t5_stack_top_logits(sc, tokens, weights, top_k, values=None, ids=None, works
     cs = _stack_cfg_struct(sc)
     _check_tensor(tokens, torch.int32, b.batch * b.seq, "tokens")
     ws = _stack_weights_struct(sc, weights)
-    nbytes = lib().t5_stack_top_logits_workspace_bytes(C.byref(cs), top_k)
+    nbytes = lib().t5_stack_top_logits_workspace_bytes(C.byref(cs), _i32(top_k))
     if nbytes:  # (0: the call below says what is wrong)
         values, ids = _top_outputs(b.batch, b.seq, top_k, dev, values, ids)
     workspace = _model_workspace(workspace, nbytes, dev)
-    _call(lib().t5_stack_top_logits, "t5_stack_top_logits", dev, C.byref(cs), tokens.data_ptr(), C.byref(ws), top_k,
-          _ptr(values), _ptr(ids), workspace.data_ptr(), workspace.numel())
+    _call(lib().t5_stack_top_logits, "t5_stack_top_logits", dev, C.byref(cs), tokens.data_ptr(), C.byref(ws),
+          _i32(top_k), _ptr(values), _ptr(ids), workspace.data_ptr(), workspace.numel())
     return values, ids
 
 
@@ -582,7 +582,7 @@ def t5_stack_distill_loss_and_grad(sc, tokens, targets, teacher_logits, teacher_
     n_tok = b.batch * b.seq
     _check_tensor(tokens, torch.int32, n_tok, "tokens")
     _check_on(dev, targets, torch.int32, n_tok, "targets")
-    opts = _DistillOpts(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev), temperature, soft_weight)
+    opts = _DistillOpts(_i32(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev)), temperature, soft_weight)
     ws = _stack_weights_struct(sc, weights)
     gs_ref = None
     if want_grads:
@@ -710,12 +710,12 @@ def t5_encdec_top_logits(ec, enc_tokens, dec_tokens, weights, top_k, values=None
     _check_tensor(enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
     _check_tensor(dec_tokens, torch.int32, d.batch * d.seq, "dec_tokens")
     ws = _encdec_weights_struct(ec, weights)
-    nbytes = lib().t5_encdec_top_logits_workspace_bytes(C.byref(cs), top_k)
+    nbytes = lib().t5_encdec_top_logits_workspace_bytes(C.byref(cs), _i32(top_k))
     if nbytes:  # (0: the call below says what is wrong)
         values, ids = _top_outputs(d.batch, d.seq, top_k, dev, values, ids)
     workspace = _model_workspace(workspace, nbytes, dev)
     _call(lib().t5_encdec_top_logits, "t5_encdec_top_logits", dev, C.byref(cs), enc_tokens.data_ptr(),
-          dec_tokens.data_ptr(), C.byref(ws), top_k, _ptr(values), _ptr(ids), workspace.data_ptr(), workspace.numel())
+          dec_tokens.data_ptr(), C.byref(ws), _i32(top_k), _ptr(values), _ptr(ids), workspace.data_ptr(), workspace.numel())
     return values, ids
 
 
@@ -729,7 +729,7 @@ def t5_encdec_distill_loss_and_grad(ec, enc_tokens, dec_tokens, targets, teacher
     _check_tensor(dec_tokens, torch.int32, n_tok, "dec_tokens")
     _check_on(dev, enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
     _check_on(dev, targets, torch.int32, n_tok, "targets")
-    opts = _DistillOpts(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev), temperature, soft_weight)
+    opts = _DistillOpts(_i32(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev)), temperature, soft_weight)
     ws = _encdec_weights_struct(ec, weights)
     gs_ref = None
     if want_grads:
@@ -856,6 +856,11 @@ def _elem_type(t, name):
     return T5_F32
 
 
+def _i32(v):
+    """A size for an int32 field: what does not fit is passed as the largest, which every call refuses."""
+    return v if -2 ** 31 <= v < 2 ** 31 else 2 ** 31 - 1
+
+
 def _check_on(device, t, dtype, numel, name):
     _check_tensor(t, dtype, numel, name)
     if t.device != device:
@@ -899,7 +904,7 @@ def t5_embed_fwd(tokens, table, scale=1.0, x=None):
         x = torch.empty(*tokens.shape, d, dtype=table.dtype, device=table.device)
     else:
         _check_on(table.device, x, table.dtype, n * d, "x")
-    cfg = _EmbedCfg(n, vocab, d, ty, scale)
+    cfg = _EmbedCfg(n, _i32(vocab), _i32(d), ty, scale)
     _call(lib().t5_embed_fwd, "t5_embed_fwd", table.device, C.byref(cfg), tokens.data_ptr(), table.data_ptr(), x.data_ptr())
     return x
 
@@ -910,11 +915,12 @@ def t5_embed_bwd(tokens, dx, vocab, scale=1.0, dtable=None, accumulate=False, wo
     n, d = tokens.numel(), dx.shape[-1]
     _check_tensor(dx, dx.dtype, n * d, "dx")
     _check_on(dx.device, tokens, torch.int32, n, "tokens")
-    if dtable is None:
-        dtable = (torch.zeros if accumulate else torch.empty)(vocab, d, dtype=torch.float32, device=dx.device)
+    if dtable is None:  # (a size that the call refuses is not worth an allocation)
+        rows = vocab if 0 < vocab <= 1 << 22 else 0
+        dtable = (torch.zeros if accumulate else torch.empty)(rows, d, dtype=torch.float32, device=dx.device)
     else:
         _check_on(dx.device, dtable, torch.float32, vocab * d, "dtable")
-    cfg = _EmbedCfg(n, vocab, d, ty, scale)
+    cfg = _EmbedCfg(n, _i32(vocab), _i32(d), ty, scale)
     if workspace is None:
         workspace = _byte_buffer(lib().t5_embed_bwd_workspace_bytes(C.byref(cfg)), dx.device)
     else:
@@ -930,15 +936,16 @@ def t5_top_logits(logits, top_k, values=None, ids=None):
     ty = _elem_type(logits, "logits")
     rows, vocab, ld = _check_rows(logits, "logits")
     dev = logits.device
+    k = top_k if 0 < top_k <= 256 else 0  # (a number that the call refuses is not worth an allocation)
     if values is None:
-        values = torch.empty(rows, top_k, dtype=torch.float32, device=dev)
+        values = torch.empty(rows, k, dtype=torch.float32, device=dev)
     else:
         _check_on(dev, values, torch.float32, rows * top_k, "values")
     if ids is None:
-        ids = torch.empty(rows, top_k, dtype=torch.int32, device=dev)
+        ids = torch.empty(rows, k, dtype=torch.int32, device=dev)
     else:
         _check_on(dev, ids, torch.int32, rows * top_k, "ids")
-    cfg = _TopCfg(rows, ld, vocab, top_k, ty)
+    cfg = _TopCfg(rows, ld, _i32(vocab), _i32(top_k), ty)
     _call(lib().t5_top_logits, "t5_top_logits", dev, C.byref(cfg), logits.data_ptr(), values.data_ptr(), ids.data_ptr())
     return values, ids
 
@@ -975,7 +982,7 @@ def t5_distill_loss_and_grad(logits, targets, teacher_logits, teacher_ids, tempe
     elif dlogits.device != dev or dlogits.dtype != logits.dtype or _check_rows(dlogits, "dlogits") != (rows, vocab, ld):
         raise ValueError(f"dlogits: need type, shape and row stride of logits, got {dlogits.dtype} {tuple(dlogits.shape)} "
                          f"with strides {dlogits.stride()} on {dlogits.device}")
-    cfg = _DistillCfg(rows, ld, vocab, k, ty, temperature, soft_weight, z_loss)
+    cfg = _DistillCfg(rows, ld, _i32(vocab), _i32(k), ty, temperature, soft_weight, z_loss)
     if workspace is None:
         workspace = _byte_buffer(lib().t5_distill_workspace_bytes(C.byref(cfg)), dev)
     else:

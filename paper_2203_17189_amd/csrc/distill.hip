@@ -273,7 +273,7 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
     if (NW > 1)
       for (int i = 1; i < NW; ++i) kl += red_kl[i];
     float r = a.z_loss * lse * lse;
-    if (a.soft > 0.f) r += a.soft * a.tau * a.tau * kl;
+    if (a.soft > 0.f) r += a.soft * (a.tau * (a.tau * kl));
     if (a.soft < 1.f) r += (1.f - a.soft) * (log_s1 - (x_t - m));
     a.row_loss[row] = r;
   };

@@ -308,7 +308,7 @@ __global__ __launch_bounds__(256) void embed_sort_merge_kernel(const u32x4* __re
 
 // ------------------------------------------------------------------------------------------------
 // Sums over the sorted positions, cut into tiles of `tile` positions however long the runs of equal ids are, so that
-// a padding id with half of all positions costs no more than any other.  G lanes take a tile and VEC columns each, eight
+// a padding id with half of all positions costs no more than any other.  G lanes take a tile and VEC columns each, eight or sixteen
 // rows in flight.  A run inside its tile is written to its row at once; the part of a run that reaches over an end
 // of the tile goes to partial[tile][slot], slot 0 if it is the tile's first run, else 1, and is joined afterwards.
 // ------------------------------------------------------------------------------------------------
@@ -323,6 +323,7 @@ struct SumArgs {
 
 template <typename T, int VEC, int G>
 __global__ __launch_bounds__(256) void embed_tile_sum_kernel(SumArgs a) {
+  constexpr int NB = G == 64 ? 16 : 8;  // rows in flight
   typedef typename Piece<T, VEC>::type P;
   typedef typename Piece<float, VEC>::vec F;
   uint32_t unit = blockIdx.x * (256 / G) + threadIdx.x / G;
@@ -338,30 +339,31 @@ __global__ __launch_bounds__(256) void embed_tile_sum_kernel(SumArgs a) {
   F acc{};
   auto flush = [&](bool part) {
     if (!q.on) return;
-    if (part) put_cols<VEC, F>(a.partial + ((size_t)t * 2 + (first ? 0 : 1)) * a.d + q.c, q, acc * a.scale, false);
-    else put_cols<VEC, F>(a.dE + (size_t)cur * a.d + q.c, q, acc * a.scale, a.accumulate);
+    float* o = part ? a.partial + ((size_t)t * 2 + (first ? 0 : 1)) * a.d : a.dE + (size_t)cur * a.d;
+    put_cols<VEC, F>(o + q.c, q, acc * a.scale, a.accumulate && !part);
   };
-  for (int i = t0; i < t1; i += 8) {
-    u32x2 s[8];
-    typename Piece<T, VEC>::vec v[8];
+  for (int i = t0; i < t1; i += NB) {
+    u32x2 s[NB];
+    typename Piece<T, VEC>::vec v[NB];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = a.sorted[min(i + j, t1 - 1)];
+    for (int j = 0; j < NB; ++j) s[j] = a.sorted[min(i + j, t1 - 1)];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const P*>(dx + (size_t)s[j].y * a.d);
+    for (int j = 0; j < NB; ++j) v[j] = *reinterpret_cast<const P*>(dx + (size_t)s[j].y * a.d);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (i + j >= t1) break;
-      if (s[j].x != cur) {
-        flush(first && from_before);
-        first = false;
-        cur = s[j].x;
-        acc = F{};
-      }
-      if constexpr (VEC == 1) {
-        acc += to_f32(v[j]);
-      } else {
+    for (int j = 0; j < NB; ++j) {
+      if (i + j < t1) {
+        if (s[j].x != cur) {
+          flush(first && from_before);
+          first = false;
+          cur = s[j].x;
+          acc = F{};
+        }
+        if constexpr (VEC == 1) {
+          acc += to_f32(v[j]);
+        } else {
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) acc[k] += to_f32(v[j][k]);
+          for (int k = 0; k < VEC; ++k) acc[k] += to_f32(v[j][k]);
+        }
       }
     }
   }
@@ -458,6 +460,17 @@ __device__ __forceinline__ F sum_listed(const T* dx, int d, const uint16_t* list
   return acc;
 }
 
+template <typename F>
+__device__ __forceinline__ F add_lanes(F s, int off) {  // the lane's and that of lane ^ off
+  if constexpr (sizeof(F) == 4) {
+    s += __shfl_xor(s, off, 64);
+  } else {
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(F) / 4); ++k) s[k] += __shfl_xor(s[k], off, 64);
+  }
+  return s;
+}
+
 template <typename T, int VEC>
 __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
   typedef typename Piece<float, VEC>::vec F;
@@ -468,6 +481,7 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
   __shared__ int found[8];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint64_t lower = (1ull << lane) - 1;
+  const int pieces = (min(a.split_cols, a.d) + VEC - 1) / VEC, width = pieces > 32 ? 64 : pieces > 16 ? 32 : pieces > 8 ? 16 : 8;
   uint32_t id[kOwnerTokens / 512];
 #pragma unroll
   for (int k = 0; k < kOwnerTokens / 512; ++k) id[k] = k * 512 + tid < a.n ? clamp_id(a.tok[k * 512 + tid], a.vocab) : ~0u;
@@ -528,9 +542,13 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
       if (lane == 0) many[atomicAdd(&n_many, 1u)] = v;
     } else if (first) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      for (int c = c_begin + lane * VEC; c < c_end; c += 64 * VEC) {
+      // `width` lanes a row; where that leaves lanes, each group of them takes a share of the list
+      const int groups = 64 / width, each = (m + groups - 1) / groups, l0 = lane / width * each, l1 = min(l0 + each, m);
+      for (int c = c_begin + lane % width * VEC; c < c_end; c += 64 * VEC) {
         const Cols q(c, a.d, VEC);
-        put(v, q, sum_listed<T, VEC, F>((const T*)a.dx + q.c, a.d, few[w], 0, m));
+        F s = sum_listed<T, VEC, F>((const T*)a.dx + q.c, a.d, few[w], l0, l1);
+        for (int off = width; off < 64; off <<= 1) s = add_lanes(s, off);
+        if (lane < width) put(v, q, s);
       }
     }
   }
@@ -558,15 +576,16 @@ __global__ __launch_bounds__(512) void embed_owner_sum_kernel(OwnerArgs a) {
       mine += __popcll(hit[k]);
     }
     __syncthreads();
-    const int each = (m + 7) / 8, l0 = w * each, l1 = min(l0 + each, m);
+    const int shares = 8 * (64 / width), share = (w * 64 + lane) / width, each = (m + shares - 1) / shares;
+    const int l0 = share * each, l1 = min(l0 + each, m);
     for (int c0 = c_begin; c0 < c_end; c0 += 64 * VEC) {
-      const Cols q(c0 + lane * VEC, c_end, VEC);  // (a part ends with the row, or with whole pieces)
+      const Cols q(c0 + lane % width * VEC, c_end, VEC);  // (a part ends with the row, or with whole pieces)
       red[w][lane] = sum_listed<T, VEC, F>((const T*)a.dx + q.c, a.d, list, l0, l1);
       __syncthreads();
-      if (w == 0 && q.on) {
-        F s = red[0][lane];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) s += red[j][lane];
+      if (tid < width && q.on) {
+        const F* part = &red[0][0] + tid;  // of share j: part[j * width]
+        F s = part[0];
+        for (int j = 1; j < shares && j * each < m; ++j) s += part[j * width];
         put(v, q, s);
       }
       __syncthreads();

@@ -25,7 +25,9 @@ def _tokens(n, vocab, kind, rng):
 CASES = [(1, 1, 1, "skewed"), (1, 2, 8, "one"), (3, 5, 3, "wild"), (64, 256, 64, "skewed"), (65, 257, 72, "two"),
          (777, 509, 67, "runs"), (2047, 128, 40, "one"), (2048, 300, 512, "wild"), (2049, 65536, 16, "skewed"),
          (5000, 65537, 24, "skewed"), (9001, 1000, 520, "two"), (9000, 3, 264, "runs"), (20000, 32128, 768, "skewed"),
-         (70001, 4000, 33, "runs"), (600000, 70000, 8, "skewed")]
+         (70001, 4000, 33, "runs"), (600000, 70000, 8, "skewed"),
+         (4096, 7, 65, "two"), (4097, 1, 20, "one"), (16384, 262144, 4, "wild"), (16385, 2, 100, "two"), (16000, 300000, 5, "skewed"),
+         (3000, 900, 1030, "two"), (300000, 40, 2, "runs")]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

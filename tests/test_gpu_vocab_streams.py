@@ -89,6 +89,8 @@ def test_refusals_of_the_wrappers():
     for f in (lambda: P.t5_top_logits(x, 17), lambda: P.t5_distill_loss_and_grad(x, None, t, ids, soft_weight=0.5),
               lambda: P.t5_distill_loss_and_grad(x, i32, t, ids, workspace=torch.empty(16, dtype=torch.uint8, device="cuda")),
               lambda: P.t5_embed_bwd(i32, x, 9, workspace=torch.empty(16, dtype=torch.uint8, device="cuda")),
-              lambda: P.t5_embed_fwd(i32, x, scale=float("nan"))):
+              lambda: P.t5_embed_fwd(i32, x, scale=float("nan")), lambda: P.t5_embed_bwd(i32, x, 2 ** 32 + 8),
+              lambda: P.t5_embed_bwd(i32, x, 0), lambda: P.t5_top_logits(x, 2 ** 32 + 2), lambda: P.t5_top_logits(x, 0),
+              lambda: P.t5_top_logits(x, -3)):
         with pytest.raises(P.T5Error):
             f()

@@ -53,6 +53,7 @@ def test_embed_nulls_empty_and_workspace():
     assert L.t5_embed_bwd(C.byref(c), D, D, D, 0, None, 1 << 40, None) == NULL
     need = L.t5_embed_bwd_workspace_bytes(C.byref(c))
     assert need > 0 and L.t5_embed_bwd(C.byref(c), D, D, D, 0, D, need - 1, None) == WORKSPACE
+    assert L.t5_embed_bwd(C.byref(c), D, D, D, 0, C.c_void_p(4096 + 128), 1 << 40, None) == WORKSPACE
     assert L.t5_embed_fwd(C.byref(e), None, None, None, None) == 0  # nothing to do
     assert L.t5_embed_bwd(C.byref(e), None, None, None, 1, None, 0, None) == 0
 
@@ -87,6 +88,7 @@ def test_top_and_distill_nulls_and_workspace():
         assert L.t5_distill_loss_and_grad(C.byref(d), *a, 1 << 40, None) == NULL, i
     need = L.t5_distill_workspace_bytes(C.byref(d))
     assert need > 0 and L.t5_distill_loss_and_grad(C.byref(d), D, D, D, D, D, D, D, D, need - 1, None) == WORKSPACE
+    assert L.t5_distill_loss_and_grad(C.byref(d), D, D, D, D, D, D, D, C.c_void_p(4096 + 8), 1 << 40, None) == WORKSPACE
 
 
 def test_wrappers_refuse_host_tensors_types_and_shapes():
