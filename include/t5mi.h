@@ -342,7 +342,7 @@ int t5_encdec_loss_and_grad(const t5_encdec_cfg* cfg, const int32_t* enc_tokens,
  * Token embedding with a scale:  x[t, :] = scale * table[tokens[t], :], rounded once.  tokens: device int32 [n_tokens],
  * ids clamped into [0, vocab) as in a stack; table [vocab, d_model] and x [n_tokens, d_model] of dtype.
  * Errors: NULL with n_tokens > 0 -> T5_ERR_NULL; n_tokens < 0, vocab or d_model < 1, scale not finite -> T5_ERR_SHAPE;
- * n_tokens > 2^24, vocab > 2^22, d_model > 2^16, unknown dtype -> T5_ERR_UNSUPPORTED.  n_tokens == 0 is a no-op. */
+ * n_tokens >= 2^24, vocab > 2^22, d_model > 2^16, unknown dtype -> T5_ERR_UNSUPPORTED.  n_tokens == 0 is a no-op. */
 typedef struct {
   int64_t n_tokens;
   int32_t vocab, d_model;
@@ -365,7 +365,7 @@ int t5_embed_bwd(const t5_embed_cfg* cfg, const int32_t* tokens, const void* dx,
  * (the logits themselves, exactly); ids: int32 [rows, top_k].  -0 and +0 are equal (and come back as +0); NaN counts as
  * larger than +inf and comes back as NaN.  Elements between vocab and ld are not read.  rows == 0 is a no-op.
  * Errors: NULL with rows > 0 -> T5_ERR_NULL; rows < 0, vocab < 2, ld < vocab, top_k < 1 or > vocab -> T5_ERR_SHAPE;
- * rows > 2^24, vocab > 2^22, ld > 2^32, top_k > 256, unknown dtype -> T5_ERR_UNSUPPORTED. */
+ * rows >= 2^24, vocab > 2^22, ld > 2^32, top_k > 256, unknown dtype -> T5_ERR_UNSUPPORTED. */
 typedef struct {
   int64_t rows, ld;
   int32_t vocab, top_k;

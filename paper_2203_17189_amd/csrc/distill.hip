@@ -16,6 +16,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSelfCount = 1024;  // rows up to which every workgroup counts the targets itself
+constexpr int kAhead = 16;        // loads in flight where one workgroup goes over all rows
 
 // Which exponentials a row needs: one (tau = 1, or only one of the two softmaxes has weight), two of which the second is
 // the square or fourth power of the first, or two.
@@ -45,8 +46,13 @@ __global__ __launch_bounds__(1024) void distill_count_kernel(const int32_t* __re
                                                              float* __restrict__ n_counted) {
   __shared__ int red[16];
   int c = 0;
-#pragma unroll 8
-  for (int r = threadIdx.x; r < (int)rows; r += 1024) c += targets[r] >= 0 && targets[r] < V ? 1 : 0;
+  for (int r0 = threadIdx.x; r0 < (int)rows; r0 += 1024 * kAhead) {
+    int t[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) t[j] = targets[min(r0 + j * 1024, (int)rows - 1)];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) c += r0 + j * 1024 < (int)rows && t[j] >= 0 && t[j] < V ? 1 : 0;
+  }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) c += __shfl_xor(c, off, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
@@ -330,10 +336,21 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float* __restr
                                                             int64_t rows, int V, float* __restrict__ loss) {
   __shared__ float red[16];
   float s = 0.f, n = 0.f;  // (whole numbers below 2^24: exact)
-#pragma unroll 8
-  for (int r = threadIdx.x; r < (int)rows; r += 1024) {
-    s += row_loss[r];
-    n += !targets || (targets[r] >= 0 && targets[r] < V) ? 1.f : 0.f;
+  for (int r0 = threadIdx.x; r0 < (int)rows; r0 += 1024 * kAhead) {
+    float l[kAhead];
+    int t[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int r = min(r0 + j * 1024, (int)rows - 1);
+      l[j] = row_loss[r];
+      t[j] = targets ? targets[r] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (r0 + j * 1024 < (int)rows) {
+        s += l[j];
+        n += t[j] >= 0 && t[j] < V ? 1.f : 0.f;
+      }
   }
   s = block_sum<16>(s, red);
   n = block_sum<16>(n, red);
@@ -347,7 +364,7 @@ constexpr int kPartPieces = 256 * kPartNV;
 // leave compute units without work.
 int row_parts(int64_t rows, int V, int type) {
   const int pieces = ceil_div(V, type == IN_BF16 ? 8 : 4);
-  return pieces <= 4096 || (pieces <= 16384 && rows >= 256) ? 1 : ceil_div(pieces, kPartPieces);
+  return pieces <= 4096 || (pieces <= 16384 && rows >= 128) ? 1 : ceil_div(pieces, kPartPieces);
 }
 
 template <typename T, int MODE, bool GRAD>
@@ -365,7 +382,6 @@ void rows_of_mode(const DistillArgs& a, const T* x, T* g, int64_t rows, hipStrea
   }
   // a row in a workgroup's registers, 16 pieces a thread at most; few rows: more threads for each
   if (pieces <= 256) go(distill_rows_kernel<T, 64, 4, MODE, WHOLE_ROW, GRAD>, 64);
-  else if (rows < 512 && pieces <= 4096) go(distill_rows_kernel<T, 1024, 4, MODE, WHOLE_ROW, GRAD>, 1024);
   else if (pieces <= 512) go(distill_rows_kernel<T, 128, 4, MODE, WHOLE_ROW, GRAD>, 128);
   else if (pieces <= 1024) go(distill_rows_kernel<T, 256, 4, MODE, WHOLE_ROW, GRAD>, 256);
   else if (pieces <= 2048) go(distill_rows_kernel<T, 256, 8, MODE, WHOLE_ROW, GRAD>, 256);

@@ -308,8 +308,9 @@ __global__ __launch_bounds__(256) void embed_sort_merge_kernel(const u32x4* __re
 
 // ------------------------------------------------------------------------------------------------
 // Sums over the sorted positions, cut into tiles of `tile` positions however long the runs of equal ids are, so that
-// a padding id with half of all positions costs no more than any other.  G lanes take a tile and VEC columns each, eight or sixteen
-// rows in flight.  A run inside its tile is written to its row at once; the part of a run that reaches over an end
+// a padding id with half of all positions costs no more than any other.  A wavefront takes a tile, VEC columns a lane and
+// sixteen rows in flight (16384 x 768, bf16: 40.7 us in all, 42.2 with eight).  Rows of fewer than 64 pieces leave lanes
+// idle; two or four tiles a wavefront, which no longer walks its runs together, cost more (32768 x 64: 27.0 us against 25.2).  A run inside its tile is written to its row at once; the part of a run that reaches over an end
 // of the tile goes to partial[tile][slot], slot 0 if it is the tile's first run, else 1, and is joined afterwards.
 // ------------------------------------------------------------------------------------------------
 struct SumArgs {
@@ -321,16 +322,15 @@ struct SumArgs {
   float scale;
 };
 
-template <typename T, int VEC, int G>
+template <typename T, int VEC>
 __global__ __launch_bounds__(256) void embed_tile_sum_kernel(SumArgs a) {
-  constexpr int NB = G == 64 ? 16 : 8;  // rows in flight
+  constexpr int NB = 16;  // rows in flight
   typedef typename Piece<T, VEC>::type P;
   typedef typename Piece<float, VEC>::vec F;
-  uint32_t unit = blockIdx.x * (256 / G) + threadIdx.x / G;
-  if (G == 64) unit = __builtin_amdgcn_readfirstlane(unit);
+  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int t = unit / a.slabs;
   if (t >= a.tiles) return;
-  const Cols q(((unit - t * a.slabs) * G + threadIdx.x % G) * VEC, a.d, VEC);
+  const Cols q(((unit - t * a.slabs) * 64 + threadIdx.x % 64) * VEC, a.d, VEC);
   const T* dx = (const T*)a.dx + q.c;
   const int t0 = t * a.tile, t1 = min(t0 + a.tile, a.n);
   uint32_t cur = a.sorted[t0].x;
@@ -643,16 +643,9 @@ size_t carve_bwd_ws(int64_t n, int vocab, int d, void* base, BwdWs* w) {
 
 template <typename T>
 void launch_tile_sum(const SumArgs& a, bool vec, hipStream_t st) {
-  SumArgs b = a;
-  auto go = [&](auto kern, int vec_n, int G) {
-    b.slabs = ceil_div(a.d, G * vec_n);
-    kern<<<(unsigned)ceil_div((int64_t)b.tiles * b.slabs, 256 / G), 256, 0, st>>>(b);
-  };
-  // 64 lanes a tile where they have columns to hold, else 32 or 16 (a wavefront then takes two or four tiles)
-  if (!vec) go(embed_tile_sum_kernel<T, 1, 16>, 1, 16);
-  else if (a.d > 128) go(embed_tile_sum_kernel<T, 4, 64>, 4, 64);
-  else if (a.d > 64) go(embed_tile_sum_kernel<T, 4, 32>, 4, 32);
-  else go(embed_tile_sum_kernel<T, 4, 16>, 4, 16);
+  const unsigned grid = (unsigned)ceil_div((int64_t)a.tiles * a.slabs, 4);
+  if (vec) embed_tile_sum_kernel<T, 4><<<grid, 256, 0, st>>>(a);
+  else embed_tile_sum_kernel<T, 1><<<grid, 256, 0, st>>>(a);
 }
 
 }  // namespace
@@ -737,14 +730,14 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
   }
   SumArgs a;
   a.sorted = sorted; a.dx = dx; a.dE = dE; a.partial = w.partial;
-  a.n = (int)n; a.d = d; a.tile = sum_tile(n, d); a.tiles = ceil_div(n, a.tile); a.slabs = 0; a.accumulate = accumulate;
+  a.n = (int)n; a.d = d; a.tile = sum_tile(n, d); a.tiles = ceil_div(n, a.tile); a.slabs = ceil_div(d, vec ? 256 : 64);
+  a.accumulate = accumulate;
   a.scale = scale;
   if (type == IN_BF16) launch_tile_sum<bf16>(a, vec, st);
   else launch_tile_sum<float>(a, vec, st);
   if (a.tiles > 1) {
     // most workgroups have nothing to do and cost 0.3 ns a wavefront: four pieces each where there are more than four
     // (32768 x 2048: 111.5 us in all with one piece, 109.3 with four; 16384 x 768, a seventh of it padding: 39.0 and 41.1)
-    a.slabs = ceil_div(d, vec ? 256 : 64);
     a.join = a.slabs > 4 ? 4 : 1;
     const dim3 grid((unsigned)a.tiles, (unsigned)ceil_div(a.slabs, a.join));
     if (vec) embed_join_kernel<4><<<grid, 512, 0, st>>>(a);

@@ -328,7 +328,7 @@ hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, 
     // wavefronts on one; else workgroups of four wavefronts, more of them at a time on rows of up to 16 KB
     if (V <= 1024 && K <= 32) go(top_logits_kernel<T, 64, 16, true>, 64, p);
     else if (V <= 4096 && K > pieces / 8) go(top_logits_kernel<T, 256, 16, true>, 256, p);
-    else if (rows < 512 && V >= 16384) go(top_logits_kernel<T, 1024, 16, false>, 1024, p);
+    else if (rows <= 256 && pieces > 4096) go(top_logits_kernel<T, 1024, 16, false>, 1024, p);
     else if (pieces <= 1024) go(top_logits_kernel<T, 256, 4, false>, 256, p);
     else go(top_logits_kernel<T, 256, 16, false>, 256, p);
   };

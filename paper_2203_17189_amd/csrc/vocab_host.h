@@ -12,7 +12,7 @@ int elem_type(int32_t dtype, int* ty) {
 
 int check_rows(int64_t rows, int32_t vocab, int64_t ld, int32_t top_k) {
   if (rows < 0 || vocab < 2 || ld < vocab || top_k < 1 || top_k > vocab) return T5_ERR_SHAPE;
-  if (rows > (1 << 24) || vocab > (1 << 22) || ld > ((int64_t)1 << 32) || top_k > kTopMost) return T5_ERR_UNSUPPORTED;
+  if (rows >= (1 << 24) || vocab > (1 << 22) || ld > ((int64_t)1 << 32) || top_k > kTopMost) return T5_ERR_UNSUPPORTED;
   return T5_OK;
 }
 

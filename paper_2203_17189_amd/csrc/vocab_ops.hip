@@ -8,7 +8,7 @@ namespace {
 int check_embed(const t5_embed_cfg* c, int* ty) {
   if (!c) return T5_ERR_NULL;
   if (c->n_tokens < 0 || c->vocab < 1 || c->d_model < 1 || !std::isfinite(c->scale)) return T5_ERR_SHAPE;
-  if (c->n_tokens > (1 << 24) || c->vocab > (1 << 22) || c->d_model > (1 << 16)) return T5_ERR_UNSUPPORTED;
+  if (c->n_tokens >= (1 << 24) || c->vocab > (1 << 22) || c->d_model > (1 << 16)) return T5_ERR_UNSUPPORTED;
   return elem_type(c->dtype, ty);
 }
 

@@ -24,10 +24,10 @@ def _distill(**kw):
 
 
 EMBED_BAD = [(dict(n_tokens=-1), SHAPE), (dict(vocab=0), SHAPE), (dict(d_model=0), SHAPE), (dict(scale=float("nan")), SHAPE),
-             (dict(scale=float("inf")), SHAPE), (dict(dtype=2), UNSUPPORTED), (dict(n_tokens=(1 << 24) + 1), UNSUPPORTED),
+             (dict(scale=float("inf")), SHAPE), (dict(dtype=2), UNSUPPORTED), (dict(n_tokens=1 << 24), UNSUPPORTED),
              (dict(vocab=(1 << 22) + 1), UNSUPPORTED), (dict(d_model=(1 << 16) + 1), UNSUPPORTED)]
 ROWS_BAD = [(dict(rows=-1), SHAPE), (dict(vocab=1), SHAPE), (dict(ld=15), SHAPE), (dict(top_k=0), SHAPE), (dict(top_k=17), SHAPE),
-            (dict(dtype=7), UNSUPPORTED), (dict(rows=(1 << 24) + 1), UNSUPPORTED), (dict(ld=1000, vocab=1000, top_k=257), UNSUPPORTED),
+            (dict(dtype=7), UNSUPPORTED), (dict(rows=1 << 24), UNSUPPORTED), (dict(ld=1000, vocab=1000, top_k=257), UNSUPPORTED),
             (dict(ld=1 << 23, vocab=(1 << 22) + 1), UNSUPPORTED), (dict(ld=(1 << 32) + 1), UNSUPPORTED)]
 nan, inf = float("nan"), float("inf")
 DISTILL_BAD = [(dict(temperature=v), SHAPE) for v in (0.0, -1.0, nan, inf, 1e-39)] + \
