@@ -213,3 +213,17 @@ def test_gradient_by_differences(rows, vocab):
     h = 5e-3 / np.sum(g * g)
     num = (f(x + h * g) - f(x - h * g)) / (2 * h)
     assert abs(num - np.sum(g * g)) <= 2e-3 * np.sum(g * g)
+
+
+def test_rows_beyond_32_bit_offsets():
+    """520 rows, 2^23 + 8 elements apart, the gradient over the logits."""
+    import paper_2203_17189_amd as P
+    rows, vocab, k = 520, 1000, 8
+    x, tgt, t, ids = make(rows, vocab, k, 4)
+    wide, tx = rows_with_gap(x, "bf16", (1 << 23) + 8, fill=7.0)
+    args = (ints(tgt), dev(t), ints(ids))
+    more = dict(temperature=2.0, soft_weight=0.5)
+    want = P.t5_distill_loss_and_grad(tx.contiguous(), *args, **more)
+    loss, row, g = P.t5_distill_loss_and_grad(tx, *args, dlogits=tx, **more)
+    assert torch.equal(loss, want[0]) and torch.equal(row, want[1]) and torch.equal(g.contiguous(), want[2])
+    assert bool((wide[:, vocab:] == 7.0).all())

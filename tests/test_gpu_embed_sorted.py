@@ -101,3 +101,42 @@ def test_infinities_and_nans_stay_in_their_rows():
     dx[1, 3], dx[3, 5], dx[4, 7] = np.nan, np.inf, -np.inf
     g = host(P.t5_embed_bwd(ints(tok), dev(dx), 6))
     assert np.array_equal(g, VO.embed_bwd(tok, dx, 6), equal_nan=True)
+
+
+@pytest.mark.parametrize("n", [100, 5000, 20000])
+def test_tables_beyond_32_bit_offsets(n):
+    """2^22 rows of 1032 columns: 4.3e9 elements, every form of the gradient."""
+    import paper_2203_17189_amd as P
+    vocab, d = 1 << 22, 1032
+    rng = np.random.default_rng(n)
+    tok = np.r_[0, vocab - 1, vocab - 1, vocab - 2, rng.integers(0, vocab, n - 4)]
+    tt = ints(tok).long()
+    table = torch.zeros(vocab, d, dtype=torch.bfloat16, device="cuda")
+    table[tt] = dev(rng.standard_normal((n, d)), "bf16")
+    assert torch.equal(P.t5_embed_fwd(ints(tok), table), table[tt])
+    del table
+    dx = dev(rng.standard_normal((n, d)), "bf16")
+    g = P.t5_embed_bwd(ints(tok), dx, vocab)
+    ids, at = np.unique(tok, return_inverse=True)
+    want, size = VO.embed_bwd(at, host(dx), len(ids)), VO.embed_bwd(at, np.abs(host(dx)), len(ids))
+    rows = g[ints(ids).long()]
+    assert np.all(np.abs(host(rows) - want) <= (np.bincount(at)[:, None] + 1) * U * size)
+    g[ints(ids).long()] = 0
+    assert not any(bool(part.any()) for part in g.split(1 << 18))
+
+
+def test_activations_beyond_32_bit_offsets():
+    import paper_2203_17189_amd as P
+    n, vocab, d = 70000, 4, 65536
+    rng = np.random.default_rng(3)
+    tok = rng.integers(0, vocab, n)
+    table = dev(rng.standard_normal((vocab, d)), "bf16")
+    x = P.t5_embed_fwd(ints(tok), table)
+    for r in (0, 1, 65535, 65536, n - 1):
+        assert torch.equal(x[r], table[int(tok[r])])
+    x[-100:] *= -3
+    g = P.t5_embed_bwd(ints(tok), x, vocab)
+    for c in (slice(0, 100), slice(d - 100, d)):
+        part = host(x[:, c])
+        want, size = VO.embed_bwd(tok, part, vocab), VO.embed_bwd(tok, np.abs(part), vocab)
+        assert np.all(np.abs(host(g[:, c]) - want) <= np.bincount(tok)[:, None] * U * size)

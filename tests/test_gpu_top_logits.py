@@ -96,3 +96,14 @@ def test_empty():
     import paper_2203_17189_amd as P
     v, i = P.t5_top_logits(torch.zeros(0, 10, device="cuda"), 3)
     assert v.shape == i.shape == (0, 3)
+
+
+def test_rows_beyond_32_bit_offsets():
+    """520 rows, 2^23 + 8 elements apart."""
+    import paper_2203_17189_amd as P
+    rng = np.random.default_rng(8)
+    _, x = rows_with_gap(rng.standard_normal((520, 1000)), "bf16", (1 << 23) + 8, fill=float("inf"))
+    values, ids = P.t5_top_logits(x, 20)
+    want = P.t5_top_logits(x.contiguous(), 20)
+    assert torch.equal(values, want[0]) and torch.equal(ids, want[1])
+    _check(x[-3:], 20, values[-3:], ids[-3:])
