@@ -228,10 +228,12 @@ __global__ __launch_bounds__(1024) void embed_sort_place_kernel(SortPass p) {
 // ------------------------------------------------------------------------------------------------
 // The same order in two launches, for n <= kMergeSort and id and position in 32 bits together: blocks of 1024 keys are
 // sorted by a workgroup each, then the place of a key is its place in its block plus the number of smaller keys in every
-// other block, found by bisection in LDS, which holds all keys.  768 columns, whole gradient: 5000 tokens 26.7 us against
-// 33.2 by digits, 16384 40.6 against 44.1; beyond that the keys do not fit beside a second workgroup in LDS.
+// other block, found by bisection in LDS, which holds all keys.  768 columns, whole gradient: 5000 tokens 26.3 us against
+// 33.2 by digits, 16384 39.8 against 44.1; beyond that the keys do not fit beside a second workgroup in LDS.
 // ------------------------------------------------------------------------------------------------
 constexpr int kMergeSort = 16384;
+// (the clearing workgroups hold those 64 KB too: with 256 threads they leave the chip half empty, 8192 x 768 31.1 us against 29.7)
+constexpr int kMergeThreads = 512;
 
 __global__ __launch_bounds__(1024) void embed_sort_block_kernel(const int32_t* __restrict__ tok, uint32_t* __restrict__ out,
                                                                 int n, int vocab, int pos_bits, int passes, int bits,
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(1024) void embed_sort_block_kernel(const int32_t* _
   out[i] = key;
 }
 
-__global__ __launch_bounds__(256) void embed_sort_merge_kernel(const u32x4* __restrict__ in, u32x2* __restrict__ out, int n,
+__global__ __launch_bounds__(kMergeThreads) void embed_sort_merge_kernel(const u32x4* __restrict__ in, u32x2* __restrict__ out, int n,
                                                                int pos_bits, Fill fill) {
   __shared__ uint32_t keys[kMergeSort];
   if ((int)blockIdx.x >= fill.first) {
@@ -294,9 +296,9 @@ __global__ __launch_bounds__(256) void embed_sort_merge_kernel(const u32x4* __re
     return;
   }
   const int tid = threadIdx.x, blocks = (n + 1023) / 1024;
-  for (int j = tid; j < blocks * 256; j += 256) reinterpret_cast<u32x4*>(keys)[j] = in[j];
+  for (int j = tid; j < blocks * 256; j += kMergeThreads) reinterpret_cast<u32x4*>(keys)[j] = in[j];
   __syncthreads();
-  const int i = blockIdx.x * 256 + tid;
+  const int i = blockIdx.x * kMergeThreads + tid;
   if (i >= n) return;
   const uint32_t mine = keys[i];
   uint32_t place = i & 1023;
@@ -736,8 +738,8 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
   if (s.pos_bits) {
     unsigned grid = blocks(s.blocks);
     embed_sort_block_kernel<<<grid, 1024, 0, st>>>(tokens, (uint32_t*)w.buf[1], (int)n, vocab, s.pos_bits, s.passes, s.bits_each, p.fill);
-    grid = blocks(ceil_div(n, 256));
-    embed_sort_merge_kernel<<<grid, 256, 0, st>>>((const u32x4*)w.buf[1], w.buf[0], (int)n, s.pos_bits, p.fill);
+    grid = blocks(ceil_div(n, kMergeThreads));
+    embed_sort_merge_kernel<<<grid, kMergeThreads, 0, st>>>((const u32x4*)w.buf[1], w.buf[0], (int)n, s.pos_bits, p.fill);
   }
   for (int q = 0; q < s.passes && !s.pos_bits; ++q) {
     p.tok = q == 0 ? tokens : nullptr;
