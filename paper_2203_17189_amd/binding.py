@@ -3,6 +3,7 @@ streams.  There is no CPU fallback: a missing library raises."""
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 import torch
@@ -582,7 +583,7 @@ def t5_stack_distill_loss_and_grad(sc, tokens, targets, teacher_logits, teacher_
     n_tok = b.batch * b.seq
     _check_tensor(tokens, torch.int32, n_tok, "tokens")
     _check_on(dev, targets, torch.int32, n_tok, "targets")
-    opts = _DistillOpts(_i32(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev)), temperature, soft_weight)
+    opts = _DistillOpts(_i32(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev)), float(temperature), float(soft_weight))
     ws = _stack_weights_struct(sc, weights)
     gs_ref = None
     if want_grads:
@@ -729,7 +730,7 @@ def t5_encdec_distill_loss_and_grad(ec, enc_tokens, dec_tokens, targets, teacher
     _check_tensor(dec_tokens, torch.int32, n_tok, "dec_tokens")
     _check_on(dev, enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
     _check_on(dev, targets, torch.int32, n_tok, "targets")
-    opts = _DistillOpts(_i32(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev)), temperature, soft_weight)
+    opts = _DistillOpts(_i32(_teacher_entries(n_tok, teacher_logits, teacher_ids, dev)), float(temperature), float(soft_weight))
     ws = _encdec_weights_struct(ec, weights)
     gs_ref = None
     if want_grads:
@@ -857,7 +858,8 @@ def _elem_type(t, name):
 
 
 def _i32(v):
-    """A size for an int32 field: what does not fit is passed as the largest, which every call refuses."""
+    """A whole number for an int32 field: what does not fit is passed as the largest, which every call refuses."""
+    v = operator.index(v)
     return v if -2 ** 31 <= v < 2 ** 31 else 2 ** 31 - 1
 
 
@@ -904,7 +906,7 @@ def t5_embed_fwd(tokens, table, scale=1.0, x=None):
         x = torch.empty(*tokens.shape, d, dtype=table.dtype, device=table.device)
     else:
         _check_on(table.device, x, table.dtype, n * d, "x")
-    cfg = _EmbedCfg(n, _i32(vocab), _i32(d), ty, scale)
+    cfg = _EmbedCfg(n, _i32(vocab), _i32(d), ty, float(scale))
     _call(lib().t5_embed_fwd, "t5_embed_fwd", table.device, C.byref(cfg), tokens.data_ptr(), table.data_ptr(), x.data_ptr())
     return x
 
@@ -920,7 +922,7 @@ def t5_embed_bwd(tokens, dx, vocab, scale=1.0, dtable=None, accumulate=False, wo
         dtable = (torch.zeros if accumulate else torch.empty)(rows, d, dtype=torch.float32, device=dx.device)
     else:
         _check_on(dx.device, dtable, torch.float32, vocab * d, "dtable")
-    cfg = _EmbedCfg(n, _i32(vocab), _i32(d), ty, scale)
+    cfg = _EmbedCfg(n, _i32(vocab), _i32(d), ty, float(scale))
     if workspace is None:
         workspace = _byte_buffer(lib().t5_embed_bwd_workspace_bytes(C.byref(cfg)), dx.device)
     else:
@@ -982,7 +984,7 @@ def t5_distill_loss_and_grad(logits, targets, teacher_logits, teacher_ids, tempe
     elif dlogits.device != dev or dlogits.dtype != logits.dtype or _check_rows(dlogits, "dlogits") != (rows, vocab, ld):
         raise ValueError(f"dlogits: need type, shape and row stride of logits, got {dlogits.dtype} {tuple(dlogits.shape)} "
                          f"with strides {dlogits.stride()} on {dlogits.device}")
-    cfg = _DistillCfg(rows, ld, _i32(vocab), _i32(k), ty, temperature, soft_weight, z_loss)
+    cfg = _DistillCfg(rows, ld, _i32(vocab), _i32(k), ty, float(temperature), float(soft_weight), float(z_loss))
     if workspace is None:
         workspace = _byte_buffer(lib().t5_distill_workspace_bytes(C.byref(cfg)), dev)
     else:

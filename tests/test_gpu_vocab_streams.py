@@ -16,7 +16,7 @@ def _inputs(seed, n, vocab, d, rows, lvocab, k, dtype):
                 t=dev(rng.standard_normal((rows, k))), ids=ints(rng.integers(-1, lvocab, (rows, k))))
 
 
-# forms of the gradient: no sort, by rank, by digits; forms of the rows: one wavefront, one workgroup, parts
+# forms of the gradient: no sort, blocks merged, by digits (twice); forms of the rows: one wavefront, one workgroup, parts
 SHAPES = [(500, 700, 40, 300, 700, 9), (3000, 700, 520, 20, 40000, 64), (17000, 300, 24, 5, 140000, 33), (70000, 40000, 8, 1100, 5000, 16)]
 
 
@@ -93,4 +93,22 @@ def test_refusals_of_the_wrappers():
               lambda: P.t5_embed_bwd(i32, x, 0), lambda: P.t5_top_logits(x, 2 ** 32 + 2), lambda: P.t5_top_logits(x, 0),
               lambda: P.t5_top_logits(x, -3)):
         with pytest.raises(P.T5Error):
+            f()
+
+
+def test_numbers_of_other_kinds():
+    """numpy's numbers are taken as Python's; a fraction is no size."""
+    import paper_2203_17189_amd as P
+    x = torch.arange(96.0, device="cuda").view(6, 16) / 50
+    i32 = torch.arange(6, dtype=torch.int32, device="cuda")
+    v, i = P.t5_top_logits(x, np.int64(3))
+    assert torch.equal(i, P.t5_top_logits(x, 3)[1])
+    two = np.float32(2.0)
+    a = P.t5_distill_loss_and_grad(x, i32, v, i, temperature=two, soft_weight=np.float64(0.5), z_loss=0)
+    b = P.t5_distill_loss_and_grad(x, i32, v, i, temperature=2.0, soft_weight=0.5)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    assert torch.equal(P.t5_embed_fwd(i32, x, scale=two), 2 * x)
+    assert torch.equal(P.t5_embed_bwd(i32, x, np.int32(9), scale=two), P.t5_embed_bwd(i32, x, 9, scale=2.0))
+    for f in (lambda: P.t5_top_logits(x, 2.5), lambda: P.t5_embed_bwd(i32, x, 9.5)):
+        with pytest.raises(TypeError):
             f()
