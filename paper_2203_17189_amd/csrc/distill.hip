@@ -6,9 +6,9 @@
 // Bound by bytes where the row stays in registers: every logit is read once and its gradient written once.  With two
 // softmaxes the exponentials (a quarter of the rate of other instructions) come close behind: exp(x - m) is the square or
 // the fourth power of exp((x - m) / tau) where tau is 2 or 4.
-// Measured on one MI355X, three sets of inputs in turn, loss and gradient: 16384 rows of 32128 in bf16, K = 64, 425 us (2.1 GB,
-// 5.0 TB/s; a copy's 5.2 come to 409); the loss alone, 4096 rows, 50 us (264 MB, 5.3 TB/s); 200 rows of 131071 in
-// float32, which are read twice, 70 us (315 MB, 4.5 TB/s); 48 rows of 509, 7.5 us, two launches.
+// Measured on one MI355X, three sets of inputs in turn, loss and gradient: 16384 rows of 32128 in bf16, K = 64, 414 us (2.1 GB,
+// 5.1 TB/s; a copy's 5.2 come to 409); the loss alone, 4096 rows, 50 us (264 MB, 5.3 TB/s); 200 rows of 131071 in
+// float32, which are read twice, 67 us (315 MB, 4.7 TB/s); 48 rows of 509, 7.5 us, two launches.
 #include "kernels.h"
 #include "vocab_rows.h"
 #include <algorithm>
@@ -84,8 +84,8 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   typedef typename RowVec<T>::type VT;
   __shared__ float red_m[NW], red_t[NW], red_a[NW], red_b[NW], red_w[NW], red_kl[NW];
   __shared__ int red_n[NW];
-  __shared__ int s_id[256];
-  __shared__ float s_p[256];
+  __shared__ alignas(16) int s_id[256];
+  __shared__ alignas(16) float s_p[256];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, V = a.V;
   // the parts of a row are neighbours: workgroups that start together read one stretch of memory, not one part of many
   // rows a power of two apart
@@ -325,8 +325,15 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
         const int p = v - sp.head;
         if (p < 0 || p >= sp.pieces * EPV ? part != 0 : p < first * EPV || p > last * EPV + EPV - 1) return;
       }
+      // all entries of this id, four at a time (600 x 2000, K = 256: 28 us, 75 one by one; 16384 x 32128, K = 64: 414 and 427)
       float ps = 0.f;
-      for (int k = 0; k < a.K; ++k) ps += s_id[k] == v ? s_p[k] : 0.f;
+#pragma unroll 4
+      for (int k = 0; k < a.K; k += 4) {  // (places from K on hold no id)
+        const u32x4 ids = *reinterpret_cast<const u32x4*>(s_id + k);
+        const f32x4 ps4 = *reinterpret_cast<const f32x4*>(s_p + k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ps += (int)ids[j] == v ? ps4[j] : 0.f;
+      }
       float r = grad(xv) - kp * ps;
       if (v == tgt) r -= h * inv_n;
       g[v] = from_f32<T>(r);
