@@ -18,7 +18,6 @@ namespace t5mi {
 
 namespace {
 
-constexpr int kCand = 2048;  // keys collected in LDS at most
 
 // -0 counts as +0, NaN as larger than everything else.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -56,7 +55,9 @@ __device__ __forceinline__ float piece_max<bf16>(u32x4 r) {
 
 template <int NT>
 struct TopShared {
-  static constexpr int kKeys = NT == 64 ? 1024 : kCand;
+  // keys collected at most: with 1024 and 2048 for one and two wavefronts, LDS holds fewer rows on a compute unit (16384 x 500,
+  // K = 16: 29.6 us against 22.5; 8192 x 8000, K = 64: 63.7 and 50.6)
+  static constexpr int kKeys = NT == 64 ? 256 : NT == 128 ? 512 : 2048;
   alignas(16) uint32_t best[256];
   alignas(16) uint64_t cand[kKeys];
   uint32_t places[NT];
@@ -82,7 +83,7 @@ template <int NT>
 __device__ __forceinline__ void keep_top(TopShared<NT>& s, int C, int K) {
   const int tid = threadIdx.x;
   constexpr int R = (TopShared<NT>::kKeys + NT - 1) / NT;
-  if (C > NT && C > 512) {
+  if (C > (NT < 1024 ? 2 * NT : NT)) {
     // the K-th largest, from its highest bit down; the keys below it are dropped
     uint64_t key[R];
 #pragma unroll
@@ -103,11 +104,12 @@ __device__ __forceinline__ void keep_top(TopShared<NT>& s, int C, int K) {
     __syncthreads();
     C = K;
   }
-  // each key's place is the number of larger ones; where keys are few, several threads count a part of the list each
+  // Each key's place is the number of larger ones; where keys are few, several threads count a part of the list each.
+  // (C <= 2 NT, and C <= 1024.)
   const int keys = C <= 64 ? 64 : C <= 128 ? 128 : C <= 256 ? 256 : C <= 512 ? 512 : 1024;  // threads a part, C and more (or 2 NT)
   const int parts = keys < NT ? NT / keys : 1, part = keys < NT ? tid / keys : 0, own = keys < NT ? tid % keys : tid;
   if (tid == 0 && C & 1) s.cand[C] = 0;  // (C < kKeys here)
-  const bool two = C > NT;  // (C <= 2 NT: with NT = 64 there are no more than 128 keys)
+  const bool two = C > NT;
   const uint64_t k0 = own < C ? s.cand[own] : 0, k1 = two && NT + tid < C ? s.cand[NT + tid] : 0;
   int place0 = 0, place1 = 0;
   __syncthreads();
@@ -150,7 +152,7 @@ __device__ __forceinline__ void keep_top(TopShared<NT>& s, int C, int K) {
 // NT threads a row, NP pieces of 16 bytes a thread in a chunk, or (ONE) of one element: rows too short to give every
 // thread a whole piece.
 template <typename T, int NT, int NP, bool ONE>
-__global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : 4) void top_logits_kernel(
+__global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : NP == 8 ? 8 : 4) void top_logits_kernel(
     const T* __restrict__ logits, int V, int64_t ld, int K, float* __restrict__ values, int32_t* __restrict__ ids) {
   constexpr int EPV = ONE ? 1 : RowSplit<T>::EPV;
   constexpr bool kAgain = NP > 4 && !ONE;  // pieces that matter are read again (from L2) instead of held
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : 4) void 
   const int own = ONE ? -1 : sp.single(tid, NT, V);
   const float xs = own >= 0 ? to_f32(x[own]) : -INFINITY;
   // twice K groups bound nearly as well as more, for fewer comparisons (8192 x 32128, K = 16: 96 us, with 256 groups 111)
-  const int groups = K <= 32 ? 64 : K <= 64 ? 128 : 256;
+  const int groups = K <= 32 ? 64 : K <= 96 ? 128 : 256;
   bool crowded = false;
   uint32_t level = 0;  // value of the bound
   for (int p0 = 0; p0 == 0 || p0 < pieces; p0 += NT * NP) {
@@ -185,7 +187,9 @@ __global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : 4) void 
       for (int i = 0; i < NP; ++i) top[i] = piece_max<T>(raw[i]);
     }
     const bool with_single = p0 == 0 && own >= 0;
-    if (p0 == 0) {
+    if (p0 == 0 && V <= 256 && 3 * K > V) {  // a large part of a short row: all of it is ranked
+      __syncthreads();
+    } else if (p0 == 0) {
       // the K-th largest of `groups` groups' largest values: the largest that at least K of them reach
       uint32_t g = with_single ? ordered(xs) : 0;
 #pragma unroll
@@ -328,14 +332,23 @@ hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, 
   auto go = [&](auto kern, int nt, auto* p) { kern<<<(unsigned)rows, nt, 0, st>>>(p, V, ld, K, values, ids); };
   auto of_type = [&](auto* p) {
     typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type T;
-    // short rows: a wavefront that reads elements one by one (16384 x 500, K = 16: 29.5 us, with four wavefronts 62.9), or
-    // a workgroup where pieces are too few to bound K well (16384 x 500, K = 100: 109 us, by pieces 328; 4096 x 4000: 43.6
-    // and 45.4).  Rows of more than 64 KB that leave compute units idle: sixteen wavefronts each (8 x 32128 in float32:
-    // 11.0 us, with four 16.2; 256 x 131072: 40.0 and 49.5; but 384 rows of them 62 and 59).  Else four wavefronts, and
-    // for rows of up to 16 KB fewer registers, so more of them at a time (8192 x 2048: 40.1 and 60.2).
+    // One element at a time where pieces are too few to bound K well (16384 x 500, K = 100: 109 us, by pieces 328; 4096 x 4000:
+    // 43.6 and 45.4).  Many rows: one wavefront each as long as its 64 groups bound K and 16 pieces a lane hold the row, two up
+    // to K = 96, so that more rows are on their way at a time (16384 x 500, K = 16: 22.5 us, 62.9 with four wavefronts;
+    // 8192 x 2048, K = 16: 19.6 and 42.5; 8192 x 8000, K = 32: 38.3 and 61.1, K = 64: 50.6 and 74.6; 8192 x 16000, K = 16:
+    // 57.5 and 73.8; but 8192 x 32128, K = 64, in chunks: 132 and 115).  Fewer than 512 rows: 4 wavefronts (400 x
+    // 8000, K = 64: 11.2 us, with two 13.4), or 16 on rows of more than 64 KB that leave compute units idle (8 x 32128 in
+    // float32: 11.0 us, with four 16.2; 256 x 131072: 40.0 and 49.5; but 384 rows of them 62 and 59).  Rows of up to
+    // 16 KB are one chunk of four pieces a lane (8192 x 8000, K = 120: 104 us, with sixteen 121).
+    const bool many = rows >= 512;
     if (V <= 1024 && K <= 32) go(top_logits_kernel<T, 64, 16, true>, 64, p);
+    else if (V <= 2048 && K > pieces / 8 && K <= 96 && many) go(top_logits_kernel<T, 128, 16, true>, 128, p);
     else if (V <= 4096 && K > pieces / 8) go(top_logits_kernel<T, 256, 16, true>, 256, p);
     else if (rows <= 256 && pieces > 4096) go(top_logits_kernel<T, 1024, 16, false>, 1024, p);
+    else if (pieces <= 512 && K <= 32 && many) go(top_logits_kernel<T, 64, 8, false>, 64, p);
+    else if (pieces <= 1024 && K <= 32 && many) go(top_logits_kernel<T, 64, 16, false>, 64, p);
+    else if (pieces <= 1024 && K <= 96 && many) go(top_logits_kernel<T, 128, 8, false>, 128, p);
+    else if (pieces <= 2048 && K <= 96 && many) go(top_logits_kernel<T, 128, 16, false>, 128, p);
     else if (pieces <= 1024) go(top_logits_kernel<T, 256, 4, false>, 256, p);
     else go(top_logits_kernel<T, 256, 16, false>, 256, p);
   };

@@ -66,7 +66,8 @@ def test_rows_with_a_longer_stride(vocab, ld, shift, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", ["random", "equal", "coarse", "stripes", "odd"])
-@pytest.mark.parametrize("rows,vocab,k", [(600, 100, 32), (600, 1024, 32), (600, 1025, 33), (700, 4096, 20), (700, 8200, 128), (513, 20000, 200), (300, 70000, 100)])
+@pytest.mark.parametrize("rows,vocab,k", [(600, 100, 32), (600, 1024, 32), (600, 1025, 33), (700, 4096, 20), (700, 8200, 128), (513, 20000, 200), (300, 70000, 100),
+                                          (600, 250, 200), (600, 300, 90), (600, 3000, 31), (550, 8000, 90), (550, 16000, 40), (520, 8000, 12)])
 def test_many_rows(rows, vocab, k, kind, dtype):
     """Rows enough for workgroups that share a compute unit; long rows of the few-rows kernel are above."""
     import paper_2203_17189_amd as P
@@ -90,6 +91,24 @@ def test_thousands_of_ties_next_to_the_bound():
             x[2, :] = -np.inf
             for k in (20, 21, 31, 100):
                 _check(dev(x, dtype), k, *P.t5_top_logits(dev(x, dtype), k))
+
+
+@pytest.mark.parametrize("vocab", [900, 4000, 8000, 16000])
+def test_ties_in_many_rows(vocab):
+    """The same, in the forms that give many rows a wavefront or two each."""
+    import paper_2203_17189_amd as P
+    for dtype in ("f32", "bf16"):
+        rng = np.random.default_rng(vocab)
+        x = np.where(rng.random((4, vocab)) < 0.7, 2.0, -1.0)
+        x[:, rng.permutation(vocab)[:20]] = 3.0 + np.arange(20) % 3
+        x[1] = np.where(np.arange(vocab) < vocab - 30, -np.inf, 0.0)
+        x[2, :] = -np.inf
+        x[3] = rng.integers(0, 40, vocab)
+        rows = dev(x, dtype)
+        for k in (20, 31, 60, 96):
+            v, i = P.t5_top_logits(rows.repeat(130, 1), k)
+            _check(rows, k, v[:4], i[:4])
+            assert torch.equal(i.view(130, 4, k), i[:4].expand(130, 4, k)) and torch.equal(v.view(130, 4, k), v[:4].expand(130, 4, k))
 
 
 def test_empty():
