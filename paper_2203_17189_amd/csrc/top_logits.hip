@@ -339,9 +339,12 @@ hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, 
     // 57.5 and 73.8; but 8192 x 32128, K = 64, in chunks: 132 and 115).  Fewer than 512 rows: 4 wavefronts (400 x
     // 8000, K = 64: 11.2 us, with two 13.4), or 16 on rows of more than 64 KB that leave compute units idle (8 x 32128 in
     // float32: 11.0 us, with four 16.2; 256 x 131072: 40.0 and 49.5; but 384 rows of them 62 and 59).  Rows of up to
-    // 16 KB are one chunk of four pieces a lane (8192 x 8000, K = 120: 104 us, with sixteen 121).
+    // 16 KB are one chunk of four pieces a lane (8192 x 8000, K = 120: 104 us, with sixteen 121); the shortest take as few loads as
+    // they have elements for (16384 x 64, K = 8: 16.4 and 18.9; 8192 x 500, K = 64: 25.3 and 28.5).
     const bool many = rows >= 512;
-    if (V <= 1024 && K <= 32) go(top_logits_kernel<T, 64, 16, true>, 64, p);
+    if (V <= 256 && K <= 32) go(top_logits_kernel<T, 64, 4, true>, 64, p);
+    else if (V <= 1024 && K <= 32) go(top_logits_kernel<T, 64, 16, true>, 64, p);
+    else if (V <= 1024 && K <= 96 && many) go(top_logits_kernel<T, 128, 8, true>, 128, p);
     else if (V <= 2048 && K > pieces / 8 && K <= 96 && many) go(top_logits_kernel<T, 128, 16, true>, 128, p);
     else if (V <= 4096 && K > pieces / 8) go(top_logits_kernel<T, 256, 16, true>, 256, p);
     else if (rows <= 256 && pieces > 4096) go(top_logits_kernel<T, 1024, 16, false>, 1024, p);

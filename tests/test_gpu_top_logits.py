@@ -67,7 +67,7 @@ def test_rows_with_a_longer_stride(vocab, ld, shift, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", ["random", "equal", "coarse", "stripes", "odd"])
 @pytest.mark.parametrize("rows,vocab,k", [(600, 100, 32), (600, 1024, 32), (600, 1025, 33), (700, 4096, 20), (700, 8200, 128), (513, 20000, 200), (300, 70000, 100),
-                                          (600, 250, 200), (600, 300, 90), (600, 3000, 31), (550, 8000, 90), (550, 16000, 40), (520, 8000, 12)])
+                                          (600, 250, 200), (600, 300, 90), (600, 3000, 31), (550, 8000, 90), (550, 16000, 40), (520, 8000, 12), (600, 200, 60), (700, 1030, 40)])
 def test_many_rows(rows, vocab, k, kind, dtype):
     """Rows enough for workgroups that share a compute unit; long rows of the few-rows kernel are above."""
     import paper_2203_17189_amd as P
