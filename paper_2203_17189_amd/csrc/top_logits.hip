@@ -3,12 +3,12 @@
 //
 // A logit and its id form one 64-bit key, (value ordered as an unsigned number) * 2^32 + (2^32 - 1 - id): keys of a row
 // differ, so "the K largest" has one answer.  A workgroup reads its row a chunk at a time into registers.  In the first
-// chunk the K-th largest of 64 to 256 groups' largest values is a lower bound of the row's K-th largest value, and few
+// chunk a value that the largest of K of 64 to 256 groups reach is a lower bound of the row's K-th largest value, and few
 // elements reach it: these are collected in LDS.  Later chunks add what exceeds the K-th largest key so far.  Rows laid
 // out against that (thousands of elements above the bound) are searched bit by bit instead.
-// Measured on one MI355X, random logits: 8192 rows of 32128 in bf16, K = 64, 110 us (4.8 TB/s; a copy's 5.2 come to 103);
+// Measured on one MI355X, random logits: 8192 rows of 32128 in bf16, K = 64, 105 us (5.0 TB/s; a copy's 5.2 come to 103);
 // 1023 rows of 100003 in float32, 13 elements between them, K = 100, 90 us (4.5 TB/s); 8 rows of 32128 in float32,
-// K = 16, 9.5 us: one pass of a workgroup each, from the loads to the ranking.
+// K = 16, 8.4 us: one pass of a workgroup each, from the loads to the ranking.
 #include "kernels.h"
 #include "vocab_rows.h"
 #include <algorithm>
@@ -17,7 +17,6 @@
 namespace t5mi {
 
 namespace {
-
 
 // -0 counts as +0, NaN as larger than everything else.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -165,7 +164,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : NP == 8 
   const int head = ONE ? 0 : sp.head, pieces = ONE ? V : sp.pieces, last = pieces - 1;
   const u32x4* body = reinterpret_cast<const u32x4*>(x + head);
   if (tid == 0) {
-    s.level = 0;
+    s.level = ~0u;
     s.count = 0;
   }
   const int own = ONE ? -1 : sp.single(tid, NT, V);
@@ -187,10 +186,8 @@ __global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : NP == 8 
       for (int i = 0; i < NP; ++i) top[i] = piece_max<T>(raw[i]);
     }
     const bool with_single = p0 == 0 && own >= 0;
-    if (p0 == 0 && V <= 256 && 3 * K > V) {  // a large part of a short row: all of it is ranked
-      __syncthreads();
-    } else if (p0 == 0) {
-      // the K-th largest of `groups` groups' largest values: the largest that at least K of them reach
+    if (p0 == 0) {
+      // a value that at least K of `groups` groups' largest values reach
       uint32_t g = with_single ? ordered(xs) : 0;
 #pragma unroll
       for (int i = 0; i < NP; ++i)
@@ -198,16 +195,20 @@ __global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : NP == 8 
       for (int off = 1; off < NT / groups; off <<= 1) g = max(g, (uint32_t)__shfl_xor(g, off, 64));
       if (NT <= groups || tid % (NT / groups) == 0) s.best[NT <= groups ? tid : tid / (NT / groups)] = g;
       __syncthreads();
+      // each wavefront's share of K among its 64 groups, bit by bit (K = 16: 16384 x 64 9.9 us, 16.4 by counting, for each group,
+      // the larger ones in LDS; 8 x 32128 in float32 8.0 and 9.5)
       if (tid < groups) {
+        constexpr bool kHalf = sizeof(T) == 2;
         const uint32_t mine = s.best[tid];
-        int level = 0;
-        const u32x4* four = reinterpret_cast<const u32x4*>(s.best);
+        const int need = (K * 64 + groups - 1) / groups;
+        uint32_t t = 0;
 #pragma unroll 4
-        for (int i = 0; i < groups / 4; ++i) {
-          const u32x4 o = four[i];
-          level += (o[0] >= mine) + (o[1] >= mine) + (o[2] >= mine) + (o[3] >= mine);
+        for (int bit = 31; bit >= (kHalf ? 16 : 0); --bit) {
+          const uint32_t probe = t | 1u << bit;
+          if (__popcll(__ballot(mine >= probe)) >= need) t = probe;
         }
-        if (level >= K) atomicMax(&s.level, mine);  // (0 where fewer groups than K hold elements)
+        if (kHalf) t |= t > 0xFF800000u ? 0xFFFFu : t >> 31 ? 0u : 0xFFFFu;  // the lower half of a bf16's order: NaN, +, -
+        if ((tid & 63) == 0) atomicMin(&s.level, t);  // (no element is less where some groups hold none)
       }
       __syncthreads();
     }
@@ -332,15 +333,17 @@ hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, 
   auto go = [&](auto kern, int nt, auto* p) { kern<<<(unsigned)rows, nt, 0, st>>>(p, V, ld, K, values, ids); };
   auto of_type = [&](auto* p) {
     typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type T;
-    // One element at a time where pieces are too few to bound K well (16384 x 500, K = 100: 109 us, by pieces 328; 4096 x 4000:
-    // 43.6 and 45.4).  Many rows: one wavefront each as long as its 64 groups bound K and 16 pieces a lane hold the row, two up
-    // to K = 96, so that more rows are on their way at a time (16384 x 500, K = 16: 22.5 us, 62.9 with four wavefronts;
+    // (Both sides of each choice as they were measured, with a slower bound: now 10 to 40% less for either.)  One element
+    // at a time where pieces are too few to bound K well (16384 x 500, K = 100: 109 us, by pieces 328; 4096 x 4000: 43.6 and
+    // 45.4).  Many rows: one wavefront each as long as its 64 groups bound K and 16 pieces a lane hold the row, two up to
+    // K = 96, so that more rows are on their way at a time (16384 x 500, K = 16: 22.5 us, 62.9 with four wavefronts;
     // 8192 x 2048, K = 16: 19.6 and 42.5; 8192 x 8000, K = 32: 38.3 and 61.1, K = 64: 50.6 and 74.6; 8192 x 16000, K = 16:
-    // 57.5 and 73.8; but 8192 x 32128, K = 64, in chunks: 132 and 115).  Fewer than 512 rows: 4 wavefronts (400 x
-    // 8000, K = 64: 11.2 us, with two 13.4), or 16 on rows of more than 64 KB that leave compute units idle (8 x 32128 in
-    // float32: 11.0 us, with four 16.2; 256 x 131072: 40.0 and 49.5; but 384 rows of them 62 and 59).  Rows of up to
-    // 16 KB are one chunk of four pieces a lane (8192 x 8000, K = 120: 104 us, with sixteen 121); the shortest take as few loads as
-    // they have elements for (16384 x 64, K = 8: 16.4 and 18.9; 8192 x 500, K = 64: 25.3 and 28.5).
+    // 57.5 and 73.8; but 8192 x 8000, K = 110: 123 and 79, and 8192 x 32128, K = 64, in chunks: 132 and 115).  Fewer than 512
+    // rows: 4 wavefronts (400 x 8000, K = 64: 11.2 us, with two 13.4), or 16 on rows of more than 64 KB that leave compute
+    // units idle (8 x 32128 in float32: 11.0 us, with four 16.2; 256 x 131072: 40.0 and 49.5; but 384 rows of them 62 and
+    // 59).  Rows of up to 16 KB are one chunk of four pieces a lane (8192 x 8000, K = 120: 104 us, with sixteen 121); the
+    // shortest take as few loads as they have elements for (16384 x 64, K = 8: 16.4 and 18.9; 8192 x 500, K = 64: 25.3 and
+    // 28.5).
     const bool many = rows >= 512;
     if (V <= 256 && K <= 32) go(top_logits_kernel<T, 64, 4, true>, 64, p);
     else if (V <= 1024 && K <= 32) go(top_logits_kernel<T, 64, 16, true>, 64, p);
