@@ -6,7 +6,7 @@
 // chunk a value that the largest of K of 64 to 256 groups reach is a lower bound of the row's K-th largest value, and few
 // elements reach it: these are collected in LDS.  Later chunks add what exceeds the K-th largest key so far.  Rows laid
 // out against that (thousands of elements above the bound) are searched bit by bit instead.
-// Measured on one MI355X, random logits: 8192 rows of 32128 in bf16, K = 64, 105 us (5.0 TB/s; a copy's 5.2 come to 103);
+// Measured on one MI355X, random logits: 8192 rows of 32128 in bf16, K = 64, 100 to 105 us (5.0 to 5.3 TB/s; a copy's 5.2 come to 103);
 // 1023 rows of 100003 in float32, 13 elements between them, K = 100, 90 us (4.5 TB/s); 8 rows of 32128 in float32,
 // K = 16, 8.4 us: one pass of a workgroup each, from the loads to the ranking.
 #include "kernels.h"
