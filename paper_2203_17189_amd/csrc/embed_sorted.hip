@@ -112,10 +112,10 @@ __device__ __forceinline__ void fill_zero(const Fill& f) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// Stable sort of (id, position) by id: least significant digit first, `bits` (at most 8) bits a pass, two launches a
-// pass.  Workgroup b owns keys [b * chunk, (b + 1) * chunk) of the pass's input, 1024 at a time.  (One launch less a pass,
-// each counting the next one's digits as it places its keys, costs more than it saves where an id is frequent: atomics on
-// few addresses, 36 -> 47 us with 30% padding among 40000.)
+// Stable sort of (id, position) by id: least significant digit first, `bits` bits a pass (at most 8, or at most 10 where
+// that saves a pass), two launches a pass.  Workgroup b owns keys [b * chunk, (b + 1) * chunk) of the pass's input, 1024
+// at a time.  (One launch less a pass, each counting the next one's digits as it places its keys, costs more than it
+// saves where an id is frequent: atomics on few addresses, 36 -> 47 us with 30% padding among 40000.)
 // ------------------------------------------------------------------------------------------------
 constexpr int kSortTile = 1024;
 constexpr int kSortBlocks = 256;  // at most; a workgroup then loops over its chunk
@@ -124,7 +124,7 @@ struct SortPass {
   const int32_t* tok;  // first pass: ids as given; else null
   const u32x2* in;     // (id, position), sorted by the lower digits
   u32x2* out;
-  uint32_t* hist;      // [blocks][256]
+  uint32_t* hist;      // [blocks][DIGITS]
   int32_t n, vocab, chunk, blocks, shift, bits;
   Fill fill;
 };
@@ -134,53 +134,62 @@ __device__ __forceinline__ u32x2 sort_load(const SortPass& p, int i) {
   return p.in[i];
 }
 
+template <int DIGITS>
 __global__ __launch_bounds__(1024) void embed_sort_count_kernel(SortPass p) {
-  __shared__ uint32_t cnt[256];
+  __shared__ uint32_t cnt[DIGITS];
   if ((int)blockIdx.x >= p.blocks) {
     fill_zero(p.fill);
     return;
   }
   const int tid = threadIdx.x;
-  if (tid < 256) cnt[tid] = 0;
+  if (tid < DIGITS) cnt[tid] = 0;
   __syncthreads();
   const int i0 = blockIdx.x * p.chunk, i1 = min(i0 + p.chunk, p.n);
   for (int i = i0 + tid; i < i1; i += 1024)
     atomicAdd(&cnt[(sort_load(p, i).x >> p.shift) & ((1u << p.bits) - 1)], 1u);  // whole numbers: the order does not matter
   __syncthreads();
-  if (tid < 256) p.hist[blockIdx.x * 256 + tid] = cnt[tid];
+  if (tid < DIGITS) p.hist[blockIdx.x * DIGITS + tid] = cnt[tid];
 }
 
 // base[d]: first place of digit d's keys of this workgroup = keys of smaller digits + keys of digit d of earlier
 // workgroups.  Then 1024 keys at a time: each wavefront ranks its 64 among equal digits with ballots, the sixteen
 // wavefronts' counts are joined, and every key goes to its place.
+template <int DIGITS>
 __global__ __launch_bounds__(1024) void embed_sort_place_kernel(SortPass p) {
-  __shared__ uint32_t cnt[16][256], base[256], all[4][256], before[4][256], wsum[4];
+  constexpr int kParts = 1024 / DIGITS;  // threads a digit
+  __shared__ uint16_t cnt[16][DIGITS];
+  __shared__ uint32_t base[DIGITS], all[kParts][DIGITS], before[kParts][DIGITS], wsum[DIGITS / 64];
   if ((int)blockIdx.x >= p.blocks) {
     fill_zero(p.fill);
     return;
   }
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, d4 = tid & 255, part = tid >> 8;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, own = tid % DIGITS, part = tid / DIGITS;
   const uint32_t mask = (1u << p.bits) - 1;
   const int i0 = blockIdx.x * p.chunk, i1 = min(i0 + p.chunk, p.n);
   u32x2 key = i0 + tid < i1 ? sort_load(p, i0 + tid) : u32x2{0, 0};
   uint32_t total = 0, mine = 0;
-  for (int b = part; b < p.blocks; b += 32) {  // a quarter of the workgroups' counts each, eight in flight
+  for (int b = part; b < p.blocks; b += 8 * kParts) {  // a share of the workgroups' counts each, eight in flight
     uint32_t c[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c[j] = b + 4 * j < p.blocks ? p.hist[(b + 4 * j) * 256 + d4] : 0;
+    for (int j = 0; j < 8; ++j) c[j] = b + kParts * j < p.blocks ? p.hist[(b + kParts * j) * DIGITS + own] : 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       total += c[j];
-      mine += b + 4 * j < (int)blockIdx.x ? c[j] : 0;
+      mine += b + kParts * j < (int)blockIdx.x ? c[j] : 0;
     }
   }
-  all[part][d4] = total;
-  before[part][d4] = mine;
+  all[part][own] = total;
+  before[part][own] = mine;
   __syncthreads();
   uint32_t incl = 0;
-  if (tid < 256) {
-    mine = before[0][tid] + before[1][tid] + before[2][tid] + before[3][tid];
-    incl = total = all[0][tid] + all[1][tid] + all[2][tid] + all[3][tid];
+  if (tid < DIGITS) {
+    total = mine = 0;
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) {
+      total += all[q][tid];
+      mine += before[q][tid];
+    }
+    incl = total;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
       const uint32_t o = __shfl_up(incl, off, 64);
@@ -189,7 +198,7 @@ __global__ __launch_bounds__(1024) void embed_sort_place_kernel(SortPass p) {
     if (lane == 63) wsum[w] = incl;
   }
   __syncthreads();
-  if (tid < 256) {
+  if (tid < DIGITS) {
     uint32_t at = incl - total + mine;
     for (int q = 0; q < w; ++q) at += wsum[q];
     base[tid] = at;
@@ -205,23 +214,23 @@ __global__ __launch_bounds__(1024) void embed_sort_place_kernel(SortPass p) {
     }
     const uint32_t below = (uint32_t)__popcll(same & ((1ull << lane) - 1));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) cnt[w][i * 64 + lane] = 0;
+    for (int i = 0; i < DIGITS / 64; ++i) cnt[w][i * 64 + lane] = 0;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (on && below == 0) cnt[w][d] = (uint32_t)__popcll(same);
+    if (on && below == 0) cnt[w][d] = (uint16_t)__popcll(same);
     __syncthreads();
-    if (tid < 256) {
-      uint32_t at = base[tid];
+    uint32_t here = 0;  // of digit tid among these 1024 keys
+    if (tid < DIGITS) {
 #pragma unroll
       for (int q = 0; q < 16; ++q) {
         const uint32_t c = cnt[q][tid];
-        cnt[q][tid] = at;
-        at += c;
+        cnt[q][tid] = (uint16_t)here;
+        here += c;
       }
-      base[tid] = at;
     }
     __syncthreads();
-    if (on) p.out[cnt[w][d] + below] = key;
+    if (on) p.out[base[d] + cnt[w][d] + below] = key;
     __syncthreads();
+    if (tid < DIGITS) base[tid] += here;
   }
 }
 
@@ -616,7 +625,7 @@ int owner_cols(int64_t n, int d) {
 bool owner_takes(int64_t n, int d) { return n <= kOwnerTokens && n * std::min(owner_cols(n, d), d) <= 1 << 19; }
 
 struct SortPlan {
-  int bits_each, passes, blocks, chunk;
+  int bits_each, passes, digits, blocks, chunk;
   int pos_bits;  // > 0: blocks and a merge
 };
 int bits_of(int64_t v) {  // of the numbers 0 .. v, at least 1
@@ -628,7 +637,10 @@ SortPlan sort_plan(int64_t n, int vocab) {
   SortPlan s;
   const int bits = bits_of(vocab - 1), pos_bits = bits_of(std::max<int64_t>(n - 1, 0));
   s.pos_bits = n <= kMergeSort && bits + pos_bits <= 32 ? pos_bits : 0;
-  s.passes = ceil_div(bits, 8);
+  // ten bits a pass where that saves one, as long as the workgroups' counts of 1024 digits are few (29103 x 149, 327 ids: 29.7 us
+  // against 34.0; 32768 x 128, 100000 ids: 38.2 and 39.3; but 200000 x 64: 78.5 and 67.8)
+  s.digits = n <= 65536 && ceil_div(bits, 10) < ceil_div(bits, 8) ? 1024 : 256;
+  s.passes = ceil_div(bits, s.pos_bits || s.digits == 256 ? 8 : 10);
   s.bits_each = ceil_div(bits, s.passes);
   s.chunk = std::max(1, ceil_div(n, (int64_t)kSortBlocks * kSortTile)) * kSortTile;
   s.blocks = ceil_div(n, s.chunk);
@@ -658,7 +670,7 @@ size_t carve_bwd_ws(int64_t n, int vocab, int d, void* base, BwdWs* w) {
   };
   w->buf[0] = (u32x2*)take((size_t)n * sizeof(u32x2));
   w->buf[1] = (u32x2*)take((size_t)std::max<int64_t>(n, 1024) * sizeof(u32x2));
-  w->hist = (uint32_t*)take(s.pos_bits ? 0 : (size_t)s.blocks * 256 * 4);
+  w->hist = (uint32_t*)take(s.pos_bits ? 0 : (size_t)s.blocks * s.digits * 4);
   w->partial = (float*)take((size_t)ceil_div(n, sum_tile(n, d)) * 2 * d * 4);
   return off;
 }
@@ -746,8 +758,13 @@ hipError_t launch_embed_sorted_bwd(const int32_t* tokens, const void* dx, int ty
     p.in = w.buf[(q + 1) & 1];
     p.out = w.buf[q & 1];
     p.shift = q * s.bits_each;
-    embed_sort_count_kernel<<<blocks(s.blocks), 1024, 0, st>>>(p);
-    embed_sort_place_kernel<<<blocks(s.blocks), 1024, 0, st>>>(p);
+    if (s.digits == 1024) {
+      embed_sort_count_kernel<1024><<<blocks(s.blocks), 1024, 0, st>>>(p);
+      embed_sort_place_kernel<1024><<<blocks(s.blocks), 1024, 0, st>>>(p);
+    } else {
+      embed_sort_count_kernel<256><<<blocks(s.blocks), 1024, 0, st>>>(p);
+      embed_sort_place_kernel<256><<<blocks(s.blocks), 1024, 0, st>>>(p);
+    }
     sorted = p.out;
   }
   SumArgs a;

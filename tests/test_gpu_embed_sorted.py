@@ -28,7 +28,8 @@ CASES = [(1, 1, 1, "skewed"), (1, 2, 8, "one"), (3, 5, 3, "wild"), (64, 256, 64,
          (70001, 4000, 33, "runs"), (600000, 70000, 8, "skewed"),
          (4096, 7, 65, "two"), (4097, 1, 20, "one"), (16384, 262144, 4, "wild"), (16385, 2, 100, "two"), (16000, 300000, 5, "skewed"),
          (3000, 900, 1030, "two"), (300000, 40, 2, "runs"),
-         (2000, 900, 1030, "two"), (900, 50, 4100, "runs"), (40, 300, 4500, "skewed"), (2048, 1, 260, "one")]
+         (2000, 900, 1030, "two"), (900, 50, 4100, "runs"), (40, 300, 4500, "skewed"), (2048, 1, 260, "one"),
+         (40000, 1000, 40, "runs"), (20000, 600, 33, "two"), (30000, 300000, 20, "wild"), (270000, 513, 4, "skewed")]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
