@@ -387,8 +387,8 @@ int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* value
  * or NULL: then the loss alone is computed.  Logits of -inf are allowed (their gradient is that of q = 0; an entry of
  * positive probability there makes the loss +inf); a row of nothing but -inf gives NaN.  Sums are float32.
  * Errors: as t5_top_logits; workspace small, or not 256-byte aligned -> T5_ERR_WORKSPACE; loss NULL, or targets NULL
- * with soft_weight != 1 -> T5_ERR_NULL; temperature <= 0 or not finite (nor its inverse), soft_weight outside [0, 1],
- * z_loss < 0 or not finite -> T5_ERR_SHAPE.  rows == 0 writes 0. */
+ * with soft_weight != 1 -> T5_ERR_NULL; temperature <= 0 or not finite, log2(e) / temperature not finite (below 4.24e-39),
+ * soft_weight outside [0, 1], z_loss < 0 or not finite -> T5_ERR_SHAPE.  rows == 0 writes 0. */
 typedef struct {
   int64_t rows, ld;
   int32_t vocab, top_k;

@@ -26,7 +26,8 @@ int check_distill(const t5_distill_cfg* c, int* ty) {
   if (!c) return T5_ERR_NULL;
   const int rc = check_rows(c->rows, c->vocab, c->ld, c->top_k);
   if (rc != T5_OK) return rc;
-  if (!(c->temperature > 0.f) || !std::isfinite(c->temperature) || !std::isfinite(1.f / c->temperature) ||
+  // (1.44 = log2(e): the kernels' exponentials are powers of two of (x - max) * log2(e) / T: 0 times an infinite factor would be NaN)
+  if (!(c->temperature > 0.f) || !std::isfinite(c->temperature) || !std::isfinite(1.4426950408889634f * (1.f / c->temperature)) ||
       !(c->soft_weight >= 0.f && c->soft_weight <= 1.f) || !(c->z_loss >= 0.f) || !std::isfinite(c->z_loss))
     return T5_ERR_SHAPE;
   return elem_type(c->dtype, ty);

@@ -1,0 +1,20 @@
+"""Further refusals and sizes of the vocabulary operators and of the models that call them; no device work."""
+import ctypes as C
+
+import pytest
+
+import paper_2203_17189_amd as P
+from paper_2203_17189_amd import binding as B
+from test_vocab_ops_cpu import D, SHAPE, _distill
+
+
+@pytest.mark.parametrize("t,ok", [(4e-39, False), (4.2e-39, False), (4.3e-39, True), (1e-37, True), (3e38, True)])
+def test_temperatures_whose_exponentials_overflow(t, ok):
+    """Exponentials are powers of two of log2(e) x / T: that factor has to be a number, not only 1 / T (below 2.9e-39 even
+    that is none)."""
+    L, d = P.lib(), _distill(temperature=t)
+    if ok:
+        assert L.t5_distill_workspace_bytes(C.byref(d)) > 0
+    else:
+        assert L.t5_distill_workspace_bytes(C.byref(d)) == 0
+        assert L.t5_distill_loss_and_grad(C.byref(d), D, D, D, D, D, D, D, D, 1 << 40, None) == SHAPE
