@@ -267,12 +267,13 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   const float log_s1 = logf(s1), log_st = logf(st);
   const float lse = m + log_s1;
   const float log_total = logf(total);
+  // T KL: differences of logits are not divided by a small T, behind which they may be no numbers (0.5 and the lowest logit)
   float kl = 0.f;
 #pragma unroll
   for (int q = 0; q < EK; ++q) {
     const float p = any ? wk[q] / total : 0.f;
     if (id[q] >= 0 && p != 0.f)
-      kl += p * (((t[q] - tm) * a.inv_tau - log_total) - ((xk[q] - m) * a.inv_tau - log_st));
+      kl += p * (((t[q] - tm) - (xk[q] - m)) + a.tau * (log_st - log_total));
     if (q * NT + tid < 256) {
       s_id[q * NT + tid] = id[q];
       s_p[q * NT + tid] = p;
@@ -285,7 +286,7 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
     if (NW > 1)
       for (int i = 1; i < NW; ++i) kl += red_kl[i];
     float r = a.z_loss * lse * lse;
-    if (a.soft > 0.f) r += a.soft * (a.tau * (a.tau * kl));
+    if (a.soft > 0.f) r += a.soft * (a.tau * kl);
     if (a.soft < 1.f) r += (1.f - a.soft) * (log_s1 - (x_t - m));
     a.row_loss[row] = r;
   };
