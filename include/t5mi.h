@@ -383,12 +383,15 @@ int t5_top_logits(const t5_top_logits_cfg* cfg, const void* logits, float* value
  * targets: device int32 [rows]; rows whose target is outside [0, vocab) carry no loss of any kind and get a zero
  * gradient, whatever their logits and entries hold (-1 for padding).  targets == NULL (soft_weight 1 only): every row counts.
  * loss: one float32, the mean over the rows that count (0 if there are none); row_loss: float32 [rows] (nullable);
- * dlogits: gradient of loss, rows ld elements apart, elements between vocab and ld left alone; it may be logits itself,
- * or NULL: then the loss alone is computed.  Logits of -inf are allowed (their gradient is that of q = 0; an entry of
- * positive probability there makes the loss +inf); a row of nothing but -inf gives NaN.  Sums are float32.
+ * dlogits: gradient of loss, rows dlogits_ld elements apart, elements between them left alone; it may be logits itself (rows
+ * as far apart) and otherwise shares no element with it, or NULL: then the loss alone is computed.  Rows are stored in
+ * pieces of 16 bytes where the addresses of dlogits and logits, and their strides, differ by multiples of 16 bytes, else by
+ * elements.  Logits of -inf are allowed (their gradient is that of q = 0; an entry of positive probability there makes the
+ * loss +inf); a row of nothing but -inf gives NaN.  Sums are float32.
  * Errors: as t5_top_logits; workspace small, or not 256-byte aligned -> T5_ERR_WORKSPACE; loss NULL, or targets NULL
  * with soft_weight != 1 -> T5_ERR_NULL; temperature <= 0 or not finite, log2(e) / temperature not finite (below 4.24e-39),
- * soft_weight outside [0, 1], z_loss < 0 or not finite -> T5_ERR_SHAPE.  rows == 0 writes 0. */
+ * soft_weight outside [0, 1], z_loss < 0 or not finite, dlogits_ld neither 0 nor >= vocab, or other than ld where dlogits is
+ * logits -> T5_ERR_SHAPE; dlogits_ld > 2^32 -> T5_ERR_UNSUPPORTED.  rows == 0 writes 0. */
 typedef struct {
   int64_t rows, ld;
   int32_t vocab, top_k;
@@ -396,6 +399,7 @@ typedef struct {
   float temperature;
   float soft_weight;
   float z_loss;
+  int64_t dlogits_ld; /* elements between rows of dlogits; 0: ld */
 } t5_distill_cfg;
 size_t t5_distill_workspace_bytes(const t5_distill_cfg* cfg);
 int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, const int32_t* targets,

@@ -89,7 +89,8 @@ class _TopCfg(C.Structure):
 
 
 class _DistillCfg(C.Structure):
-    _fields_ = _TopCfg._fields_ + [("temperature", C.c_float), ("soft_weight", C.c_float), ("z_loss", C.c_float)]
+    _fields_ = _TopCfg._fields_ + [("temperature", C.c_float), ("soft_weight", C.c_float), ("z_loss", C.c_float),
+                                 ("dlogits_ld", C.c_int64)]
 
 
 class _DistillOpts(C.Structure):
@@ -955,8 +956,9 @@ def t5_top_logits(logits, top_k, values=None, ids=None):
 def t5_distill_loss_and_grad(logits, targets, teacher_logits, teacher_ids, temperature=1.0, soft_weight=1.0, z_loss=0.0,
                              want_grads=True, loss=None, row_loss=None, dlogits=None, workspace=None):
     """Loss of logits [rows, vocab] (rows may have a longer stride) against a teacher's top logits and ids [rows, top_k] and
-    int32 targets [rows] (None: every row counts, soft targets alone).  dlogits may be the logits themselves; by default
-    it is a new tensor of the same strides.  Returns (loss of one float32, row losses float32, dlogits or None)."""
+    int32 targets [rows] (None: every row counts, soft targets alone).  dlogits may be the logits themselves, or have a row
+    stride of its own; by default it is a new tensor whose rows follow each other, or are less than 16 bytes apart where those
+    of the logits are no multiple of 16 bytes apart.  Returns (loss of one float32, row losses float32, dlogits or None)."""
     ty = _elem_type(logits, "logits")
     rows, vocab, ld = _check_rows(logits, "logits")
     dev = logits.device
@@ -975,16 +977,20 @@ def t5_distill_loss_and_grad(logits, targets, teacher_logits, teacher_ids, tempe
         row_loss = torch.empty(rows, dtype=torch.float32, device=dev)
     else:
         _check_on(dev, row_loss, torch.float32, rows, "row_loss")
+    out_ld = ld
     if not want_grads:
         dlogits = None
     elif dlogits is None:
-        dlogits = torch.empty(rows, ld, dtype=logits.dtype, device=dev)
-        if ld != vocab:
+        # (not the logits' stride, which may be a sequence of rows long; pieces of 16 bytes lie in both rows alike)
+        out_ld = vocab + (ld - vocab) % (16 // logits.element_size())
+        dlogits = torch.empty(rows, out_ld, dtype=logits.dtype, device=dev)
+        if out_ld != vocab:
             dlogits = dlogits[:, :vocab]
-    elif dlogits.device != dev or dlogits.dtype != logits.dtype or _check_rows(dlogits, "dlogits") != (rows, vocab, ld):
-        raise ValueError(f"dlogits: need type, shape and row stride of logits, got {dlogits.dtype} {tuple(dlogits.shape)} "
-                         f"with strides {dlogits.stride()} on {dlogits.device}")
-    cfg = _DistillCfg(rows, ld, _i32(vocab), _i32(k), ty, float(temperature), float(soft_weight), float(z_loss))
+    else:
+        *shape, out_ld = _check_rows(dlogits, "dlogits")
+        if dlogits.device != dev or dlogits.dtype != logits.dtype or shape != [rows, vocab]:
+            raise ValueError(f"dlogits: need type and shape of logits, got {dlogits.dtype} {tuple(dlogits.shape)} on {dlogits.device}")
+    cfg = _DistillCfg(rows, ld, _i32(vocab), _i32(k), ty, float(temperature), float(soft_weight), float(z_loss), out_ld)
     if workspace is None:
         workspace = _byte_buffer(lib().t5_distill_workspace_bytes(C.byref(cfg)), dev)
     else:

@@ -93,7 +93,7 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(DistillArgs a, const T
   const uint32_t row = blockIdx.x / parts;
   const int part = blockIdx.x - row * parts;
   const T* x = logits + row * a.ld;
-  T* g = GRAD ? out + row * a.ld : nullptr;
+  T* g = GRAD ? out + row * a.out_ld : nullptr;
   const RowSplit<T> sp(x, V);
   const u32x4* body = reinterpret_cast<const u32x4*>(x + sp.head);
   u32x4* gbody = GRAD ? reinterpret_cast<u32x4*>(g + sp.head) : nullptr;
@@ -438,7 +438,8 @@ hipError_t launch_distill_rows(const DistillArgs& args, const void* logits, void
   a.rows = rows;
   a.parts = row_parts(rows, a.V, type);
   if (rows * a.parts > INT32_MAX) return hipErrorInvalidValue;
-  a.apart = out && (((uintptr_t)out ^ (uintptr_t)logits) & 15) != 0;
+  const int64_t further = (a.out_ld - a.ld) * (type == IN_BF16 ? 2 : 4);
+  a.apart = out && ((((uintptr_t)out ^ (uintptr_t)logits) | further) & 15) != 0;
   if (type == IN_BF16) {
     if (out) rows_of_type<bf16, true>(a, (const bf16*)logits, (bf16*)out, mode, rows, st);
     else rows_of_type<bf16, false>(a, (const bf16*)logits, nullptr, mode, rows, st);

@@ -296,7 +296,7 @@ struct DistillArgs {
   const int32_t* all_targets;    // of the whole batch: the mean's divisor
   const float* n_counted;        // what launch_distill_count wrote
   float* row_loss;
-  int64_t ld, all_rows;
+  int64_t ld, out_ld, all_rows;  // elements between rows of the logits and of the gradient
   int32_t K, V;
   float tau, inv_tau, soft, z_loss;
   void* partial;  // distill_ws_bytes(rows, ...) bytes
@@ -307,7 +307,7 @@ struct DistillArgs {
 size_t distill_ws_bytes(int64_t rows, int V, int K, int type);
 // Number of the batch's rows that count (nothing where launch_distill_rows does without).
 hipError_t launch_distill_count(const int32_t* targets, int64_t rows, int V, float* n_counted, hipStream_t st);
-// Row losses and, with out (the logits themselves, or a buffer of the same row stride), the gradient of the mean.
+// Row losses and, with out (the logits themselves, or a buffer), the gradient of the mean.
 hipError_t launch_distill_rows(const DistillArgs& a, const void* logits, void* out, int type, int64_t rows, hipStream_t st);
 hipError_t launch_distill_mean(const float* row_loss, const int32_t* targets, int64_t rows, int V, float* loss, hipStream_t st);
 

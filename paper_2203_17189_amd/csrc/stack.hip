@@ -381,7 +381,7 @@ int head_logits(const Head& h, const Dims& D, int tc, const void* nf_c, hipStrea
 int head_distill_rows(const Head& h, const Dims& D, const int32_t* targets, int64_t t0, int tc, bool want_grads,
                       hipStream_t st) {
   DistillArgs a;
-  a.K = h.opts->top_k; a.V = h.V; a.ld = h.V;
+  a.K = h.opts->top_k; a.V = a.ld = a.out_ld = h.V;
   a.targets = targets + t0; a.teacher_logits = h.teacher_logits + t0 * a.K; a.teacher_ids = h.teacher_ids + t0 * a.K;
   a.all_targets = targets; a.all_rows = D.T; a.n_counted = h.n_valid; a.row_loss = h.loss_rows + t0; a.partial = h.distill_ws;
   a.tau = h.opts->temperature; a.inv_tau = 1.f / a.tau; a.soft = h.opts->soft_weight; a.z_loss = h.z_loss;
@@ -503,7 +503,7 @@ int check_opts(const t5_distill_opts* o, int64_t rows, int vocab, float z_loss) 
   if (!o) return T5_ERR_NULL;
   t5_distill_cfg c;
   c.rows = rows; c.ld = vocab; c.vocab = vocab; c.top_k = o->top_k; c.dtype = T5_F32;
-  c.temperature = o->temperature; c.soft_weight = o->soft_weight; c.z_loss = z_loss;
+  c.temperature = o->temperature; c.soft_weight = o->soft_weight; c.z_loss = z_loss; c.dlogits_ld = 0;
   int ty;
   return check_distill(&c, &ty);
 }

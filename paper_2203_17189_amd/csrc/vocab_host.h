@@ -30,6 +30,8 @@ int check_distill(const t5_distill_cfg* c, int* ty) {
   if (!(c->temperature > 0.f) || !std::isfinite(c->temperature) || !std::isfinite(1.4426950408889634f * (1.f / c->temperature)) ||
       !(c->soft_weight >= 0.f && c->soft_weight <= 1.f) || !(c->z_loss >= 0.f) || !std::isfinite(c->z_loss))
     return T5_ERR_SHAPE;
+  if (c->dlogits_ld != 0 && c->dlogits_ld < c->vocab) return T5_ERR_SHAPE;
+  if (c->dlogits_ld > ((int64_t)1 << 32)) return T5_ERR_UNSUPPORTED;
   return elem_type(c->dtype, ty);
 }
 

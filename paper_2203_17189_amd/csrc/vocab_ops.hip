@@ -86,6 +86,8 @@ int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, cons
   if (!loss || !workspace) return T5_ERR_NULL;
   if (cfg->rows > 0 && (!logits || !teacher_logits || !teacher_ids || (!targets && cfg->soft_weight != 1.f)))
     return T5_ERR_NULL;
+  const int64_t out_ld = cfg->dlogits_ld ? cfg->dlogits_ld : cfg->ld;
+  if (dlogits && dlogits == logits && out_ld != cfg->ld) return T5_ERR_SHAPE;  // rows over others still to be read
   DistillWs w;
   if (workspace_bytes < carve_distill(cfg, ty, workspace, &w) || ((uintptr_t)workspace & 255)) return T5_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
@@ -93,7 +95,7 @@ int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, cons
   a.targets = targets; a.teacher_logits = teacher_logits; a.teacher_ids = teacher_ids; a.n_counted = w.n_counted;
   a.all_targets = targets; a.all_rows = cfg->rows; a.partial = w.partial;
   a.row_loss = row_loss ? row_loss : w.row_loss;
-  a.ld = cfg->ld; a.K = cfg->top_k; a.V = cfg->vocab;
+  a.ld = cfg->ld; a.out_ld = out_ld; a.K = cfg->top_k; a.V = cfg->vocab;
   a.tau = cfg->temperature; a.inv_tau = 1.f / cfg->temperature; a.soft = cfg->soft_weight; a.z_loss = cfg->z_loss;
   if (dlogits) T5_STEP("distill_count", launch_distill_count(targets, cfg->rows, cfg->vocab, w.n_counted, st));
   T5_STEP("distill_rows", launch_distill_rows(a, logits, dlogits, ty, cfg->rows, st));

@@ -18,3 +18,16 @@ def test_temperatures_whose_exponentials_overflow(t, ok):
     else:
         assert L.t5_distill_workspace_bytes(C.byref(d)) == 0
         assert L.t5_distill_loss_and_grad(C.byref(d), D, D, D, D, D, D, D, D, 1 << 40, None) == SHAPE
+
+
+@pytest.mark.parametrize("out_ld,rc", [(-1, SHAPE), (15, SHAPE), ((1 << 32) + 1, 3)])
+def test_strides_of_the_gradient(out_ld, rc):
+    L, d = P.lib(), _distill(dlogits_ld=out_ld)
+    assert L.t5_distill_workspace_bytes(C.byref(d)) == 0
+    assert L.t5_distill_loss_and_grad(C.byref(d), D, D, D, D, D, D, D, D, 1 << 40, None) == rc
+
+
+def test_a_gradient_over_the_logits_keeps_their_stride():
+    L, d = P.lib(), _distill(dlogits_ld=17)
+    assert L.t5_distill_workspace_bytes(C.byref(d)) > 0
+    assert L.t5_distill_loss_and_grad(C.byref(d), D, D, D, D, D, D, D, D, 1 << 40, None) == SHAPE
