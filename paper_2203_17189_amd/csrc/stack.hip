@@ -29,6 +29,7 @@ struct Layers {
   float* d_rel_table = nullptr;
   // carved device memory
   void* xs = nullptr;
+  int x_slots = 1;  // buffers of xs: L + 1, or two in turn where no backward pass follows
   void* stash = nullptr;
   size_t stash_each = 0;
   float *diag = nullptr, *ddiag = nullptr;
@@ -43,7 +44,7 @@ struct Layers {
   const void** ptr_tab = nullptr;
 
   size_t xbytes() const { return (size_t)D.T * D.d * D.es; }
-  void* x_of(int l) const { return (char*)xs + (size_t)l * xbytes(); }
+  void* x_of(int l) const { return (char*)xs + (size_t)(l % x_slots) * xbytes(); }
   void* stash_of(int l) const { return (char*)stash + (remat ? 0 : (size_t)l * stash_each); }
 };
 
@@ -62,19 +63,19 @@ bool wgrads_grouped_ok(const Dims& D, int L, bool remat) {
   return true;
 }
 
-// forward_only: what layers_forward needs, with one stash for all layers
+// forward_only: what layers_forward needs, with one stash and two buffers of outputs for all layers
 void carve_layers(Carver& cv, Layers& s, bool forward_only = false) {
   const Dims& D = s.D;
+  s.x_slots = forward_only ? 2 : s.L + 1;
+  s.xs = cv.take((size_t)s.x_slots * s.xbytes());
   if (forward_only) {
     s.remat = true;
-    s.xs = cv.take((size_t)(s.L + 1) * s.xbytes());
     s.stash_each = carve_stash(D, nullptr, nullptr);
     s.stash = cv.take(s.stash_each);
     s.diag = cv.take<float>((size_t)D.H * (2 * D.S - 1) * 4);
     s.block_ws = cv.take(carve_fwd(D, nullptr, nullptr));
     return;
   }
-  s.xs = cv.take((size_t)(s.L + 1) * s.xbytes());
   s.stash_each = carve_stash(D, nullptr, nullptr);
   s.stash = cv.take(s.stash_each * (s.remat ? 1 : s.L));
   s.diag = cv.take<float>((size_t)D.H * (2 * D.S - 1) * 4);
@@ -301,10 +302,16 @@ void head_wgrad_gemm(const Head& h, const Dims& D, int tc, const void* nf_c, Gem
   e.aux0 = h.wg_partials;  // null unless carve_head took room for it
 }
 
+// The MFMA GEMMs want the contraction index contiguous in both operands.  logits = nf W contracts over
+// d_model: E [V, d] has it contiguous, Wout [d, V] is transposed once per step.  dnf = dlogits W^T
+// contracts over the vocabulary: Wout has it contiguous, E is transposed once per step.
+bool head_mfma(const Head& h, const Dims& D) { return D.ty == IN_BF16 && D.d % 64 == 0 && h.V % 64 == 0; }
+bool head_transposes(const Head& h, const Dims& D, bool want_grads) { return head_mfma(h, D) && (!h.tied || want_grads); }
+
 void carve_head(Carver& cv, Head& h, const Dims& D, bool forward_only = false) {
   h.nf = cv.take((size_t)D.T * D.d * D.es);
   h.logits = cv.take((size_t)h.chunk * h.V * D.es);
-  h.wout_t = cv.take((size_t)h.V * D.d * D.es);
+  if (!forward_only || head_transposes(h, D, false)) h.wout_t = cv.take((size_t)h.V * D.d * D.es);
   h.scale_s = cv.take((size_t)D.d * D.es);
   h.rf = cv.take<float>(D.T * 4);
   if (forward_only) return;
@@ -335,11 +342,6 @@ void carve_head(Carver& cv, Head& h, const Dims& D, bool forward_only = false) {
   }
 }
 
-// The MFMA GEMMs want the contraction index contiguous in both operands.  logits = nf W contracts over
-// d_model: E [V, d] has it contiguous, Wout [d, V] is transposed once per step.  dnf = dlogits W^T
-// contracts over the vocabulary: Wout has it contiguous, E is transposed once per step.
-bool head_mfma(const Head& h, const Dims& D) { return D.ty == IN_BF16 && D.d % 64 == 0 && h.V % 64 == 0; }
-
 // Final norm, and the output matrix as the GEMMs want it; *gf_out: the norm's scale as it was used.
 int head_norm(const Head& h, const Dims& D, float rms_eps, const void* x_last, bool want_grads, const void** gf_out,
               hipStream_t st) {
@@ -354,7 +356,7 @@ int head_norm(const Head& h, const Dims& D, float rms_eps, const void* x_last, b
   }
   T5_STEP("rmsnorm_fwd", launch_rmsnorm_fwd(x_last, ty, gf, h.nf, ty, h.rf, T, D.d, rms_eps, st));
   T5_SUB(end_dropout(D, h.drop_site_final, h.nf, ty, st));  // the logits (and dW) see the dropped norm output
-  if (head_mfma(h, D) && (!h.tied || want_grads)) {
+  if (head_transposes(h, D, want_grads)) {
     PackJobs pj;
     std::memset(&pj, 0, sizeof(pj));
     if (h.tied) pj.j[0] = PackJob{{h.embedding, nullptr, nullptr}, 1, V, D.d, 0, h.wout_t};   // -> [d, V]

@@ -1,9 +1,11 @@
 """Further refusals and sizes of the vocabulary operators and of the models that call them; no device work."""
 import ctypes as C
+from dataclasses import replace
 
 import pytest
 
 import paper_2203_17189_amd as P
+import synth_inputs as SI
 from paper_2203_17189_amd import binding as B
 from test_vocab_ops_cpu import D, SHAPE, _distill
 
@@ -31,3 +33,21 @@ def test_a_gradient_over_the_logits_keeps_their_stride():
     L, d = P.lib(), _distill(dlogits_ld=17)
     assert L.t5_distill_workspace_bytes(C.byref(d)) > 0
     assert L.t5_distill_loss_and_grad(C.byref(d), D, D, D, D, D, D, D, D, 1 << 40, None) == SHAPE
+
+
+def _stack(n_layers, tied=False):
+    sc = SI.StackConfig("m", SI.BlockConfig("m", 1, 2, 64, 128, 2, 64, 256, causal=True), n_layers=n_layers, vocab=1024, tied_logits=tied)
+    return P.lib().t5_stack_top_logits_workspace_bytes(C.byref(B._stack_cfg_struct(sc)), 8)
+
+
+def _pair(n_enc, n_dec, tied=False):
+    ec = replace(SI._encdec("m", 1, 2, 64, 32, 128, 2, 64, 256, n_enc, n_dec, 1024), tied_logits=tied)
+    return P.lib().t5_encdec_top_logits_workspace_bytes(C.byref(B._encdec_cfg_struct(ec)), 8)
+
+
+def test_a_teacher_needs_room_for_one_layer():
+    """However deep the teacher is; and for no copy of its output matrix where that is the embedding, which the logits' GEMM
+    reads as it lies."""
+    assert _stack(1) == _stack(2) == _stack(24) > 0
+    assert _pair(1, 1) == _pair(24, 1) == _pair(1, 24) == _pair(24, 24) > 0
+    assert _stack(2) - _stack(2, tied=True) == _pair(2, 2) - _pair(2, 2, tied=True) == 1024 * 128 * 2
