@@ -408,13 +408,14 @@ int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, cons
 
 /* The same inside whole models.  The teacher's side: forward pass of a stack and the top_k largest logits of every
  * position, values float32 and ids int32 [batch, seq, top_k] (decoder positions for the pair); the logits exist a chunk of
- * tokens at a time, the workspace holds one layer's activations however many there are.  The configuration's dropout applies as everywhere: a
- * teacher's has dropout_rate 0.
+ * tokens at a time, the workspace holds one layer's activations however many there are.  The configuration's dropout
+ * applies as everywhere: a teacher's has dropout_rate 0.
  * The student's side: t5_stack_loss_and_grad with the loss of t5_distill_loss_and_grad in place of the cross-entropy,
  * z_loss from the configuration, teacher_logits and teacher_ids [batch, seq, top_k].  The embedded tokens' gradient is
  * added to the embedding's as by t5_embed_bwd (the same bits every time, whatever block.deterministic says; with
  * tied_logits the output matrix's part of that gradient follows block.deterministic).  All else as in the call beside it.
- * Errors: as that call and t5_distill_loss_and_grad (top_k > vocab -> T5_ERR_SHAPE, > 256 -> T5_ERR_UNSUPPORTED). */
+ * Errors: as that call and t5_distill_loss_and_grad (top_k > vocab -> T5_ERR_SHAPE, > 256 -> T5_ERR_UNSUPPORTED; workspace
+ * small, or not 256-byte aligned -> T5_ERR_WORKSPACE). */
 typedef struct {
   int32_t top_k;
   float temperature;

@@ -566,6 +566,7 @@ int run_stack(StackPlan& p, const t5_stack_cfg* cfg, const int32_t* tokens, cons
                    grads ? grads->rel_table : nullptr, grads != nullptr);
   if (rc != T5_OK) return rc;
   if (workspace_bytes < carve_stack(p, nullptr)) return T5_ERR_WORKSPACE;
+  if (p.H.opts && !aligned256(workspace)) return T5_ERR_WORKSPACE;
   carve_stack(p, workspace);
   hipStream_t st = (hipStream_t)stream;
   const Dims& D = p.S.D;
@@ -626,6 +627,7 @@ int run_encdec(EncDecPlan& p, const t5_encdec_cfg* cfg, const int32_t* enc_token
                    grads ? grads->dec_cross : nullptr, grads ? grads->dec_rel_table : nullptr, grads != nullptr);
   if (rc != T5_OK) return rc;
   if (workspace_bytes < carve_encdec(p, nullptr)) return T5_ERR_WORKSPACE;
+  if (p.H.opts && !aligned256(workspace)) return T5_ERR_WORKSPACE;
   carve_encdec(p, workspace);
   hipStream_t st = (hipStream_t)stream;
   const Dims& E = p.E.D;
@@ -713,7 +715,7 @@ int t5_stack_top_logits(const t5_stack_cfg* cfg, const int32_t* tokens, const t5
   if (!w->embedding || !w->final_scale || (!p.H.tied && !w->logits_w)) return T5_ERR_NULL;
   rc = bind_layers(p.S, w->layers, nullptr, w->rel_table, nullptr, nullptr, nullptr, false);
   if (rc != T5_OK) return rc;
-  if (workspace_bytes < carve_stack(p, nullptr, true)) return T5_ERR_WORKSPACE;
+  if (workspace_bytes < carve_stack(p, nullptr, true) || !aligned256(workspace)) return T5_ERR_WORKSPACE;
   carve_stack(p, workspace, true);
   hipStream_t st = (hipStream_t)stream;
   const Dims& D = p.S.D;
@@ -780,7 +782,7 @@ int t5_encdec_top_logits(const t5_encdec_cfg* cfg, const int32_t* enc_tokens, co
   if (rc != T5_OK) return rc;
   rc = bind_layers(p.Dc, w->dec_layers, w->dec_cross, w->dec_rel_table, nullptr, nullptr, nullptr, false);
   if (rc != T5_OK) return rc;
-  if (workspace_bytes < carve_encdec(p, nullptr, true)) return T5_ERR_WORKSPACE;
+  if (workspace_bytes < carve_encdec(p, nullptr, true) || !aligned256(workspace)) return T5_ERR_WORKSPACE;
   carve_encdec(p, workspace, true);
   hipStream_t st = (hipStream_t)stream;
   p.H.embedding = w->embedding; p.H.final_scale = w->dec_final_scale; p.H.logits_w = w->logits_w;

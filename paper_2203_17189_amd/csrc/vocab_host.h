@@ -4,6 +4,8 @@
 
 namespace {
 
+bool aligned256(const void* workspace) { return ((uintptr_t)workspace & 255) == 0; }
+
 int elem_type(int32_t dtype, int* ty) {
   if (dtype != T5_F32 && dtype != T5_BF16) return T5_ERR_UNSUPPORTED;
   *ty = dtype == T5_BF16 ? IN_BF16 : IN_F32;

@@ -52,7 +52,7 @@ int t5_embed_bwd(const t5_embed_cfg* cfg, const int32_t* tokens, const void* dx,
   if (rc != T5_OK) return rc;
   if (cfg->n_tokens == 0 && accumulate) return T5_OK;
   if (!dtable || !workspace || (cfg->n_tokens > 0 && (!tokens || !dx))) return T5_ERR_NULL;
-  if (workspace_bytes < t5_embed_bwd_workspace_bytes(cfg) || ((uintptr_t)workspace & 255)) return T5_ERR_WORKSPACE;
+  if (workspace_bytes < t5_embed_bwd_workspace_bytes(cfg) || !aligned256(workspace)) return T5_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   T5_STEP("embed_bwd", launch_embed_sorted_bwd(tokens, dx, ty, dtable, cfg->n_tokens, cfg->d_model, cfg->vocab, cfg->scale,
                                                accumulate ? 1 : 0, workspace, st));
@@ -89,7 +89,7 @@ int t5_distill_loss_and_grad(const t5_distill_cfg* cfg, const void* logits, cons
   const int64_t out_ld = cfg->dlogits_ld ? cfg->dlogits_ld : cfg->ld;
   if (dlogits && dlogits == logits && out_ld != cfg->ld) return T5_ERR_SHAPE;  // rows over others still to be read
   DistillWs w;
-  if (workspace_bytes < carve_distill(cfg, ty, workspace, &w) || ((uintptr_t)workspace & 255)) return T5_ERR_WORKSPACE;
+  if (workspace_bytes < carve_distill(cfg, ty, workspace, &w) || !aligned256(workspace)) return T5_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   DistillArgs a;
   a.targets = targets; a.teacher_logits = teacher_logits; a.teacher_ids = teacher_ids; a.n_counted = w.n_counted;

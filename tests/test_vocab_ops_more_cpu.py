@@ -7,7 +7,7 @@ import pytest
 import paper_2203_17189_amd as P
 import synth_inputs as SI
 from paper_2203_17189_amd import binding as B
-from test_vocab_ops_cpu import D, SHAPE, _distill
+from test_vocab_ops_cpu import D, SHAPE, WORKSPACE, _distill
 
 
 @pytest.mark.parametrize("t,ok", [(4e-39, False), (4.2e-39, False), (4.3e-39, True), (1e-37, True), (3e38, True)])
@@ -51,3 +51,17 @@ def test_a_teacher_needs_room_for_one_layer():
     assert _stack(1) == _stack(2) == _stack(24) > 0
     assert _pair(1, 1) == _pair(24, 1) == _pair(1, 24) == _pair(24, 24) > 0
     assert _stack(2) - _stack(2, tied=True) == _pair(2, 2) - _pair(2, 2, tied=True) == 1024 * 128 * 2
+
+
+def test_model_workspaces_off_256_bytes():
+    L, odd, n = P.lib(), C.c_void_p(4096 + 128), 1 << 40
+    sc = SI.StackConfig("r", replace(SI.CONFIGS["c1_tiny_f32"], causal=True), n_layers=1, vocab=300)
+    ec = SI._encdec("r", 1, 2, 8, 8, 32, 2, 8, 48, 1, 1, 300)
+    cs, ce, o = B._stack_cfg_struct(sc), B._encdec_cfg_struct(ec), B._DistillOpts(8, 1.0, 0.5)
+    lw = (B._Weights * 1)(B._Weights(*[4096] * 10))
+    xw = (B._CrossWeights * 1)(B._CrossWeights(*[4096] * 5))
+    ws, we = B._StackWeights(4096, 4096, lw, 4096, 4096), B._EncDecWeights(4096, 4096, lw, 4096, 4096, lw, xw, 4096, 4096)
+    assert L.t5_stack_top_logits(C.byref(cs), D, C.byref(ws), 8, D, D, odd, n, None) == WORKSPACE
+    assert L.t5_encdec_top_logits(C.byref(ce), D, D, C.byref(we), 8, D, D, odd, n, None) == WORKSPACE
+    assert L.t5_stack_distill_loss_and_grad(C.byref(cs), C.byref(o), D, D, D, D, C.byref(ws), D, None, 0, odd, n, None) == WORKSPACE
+    assert L.t5_encdec_distill_loss_and_grad(C.byref(ce), C.byref(o), D, D, D, D, D, C.byref(we), D, None, 0, odd, n, None) == WORKSPACE
