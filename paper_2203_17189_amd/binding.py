@@ -551,6 +551,23 @@ def _model_workspace(workspace, nbytes, device):
     return workspace
 
 
+def _check_devices(device, tensors, name):
+    """Every tensor of a model's weights or gradients is on the device of its tokens."""
+    if isinstance(tensors, torch.Tensor):
+        if tensors.device != device:
+            raise ValueError(f"{name}: on {tensors.device}, other arguments on {device}")
+    elif tensors is not None:
+        for key, t in tensors.items() if isinstance(tensors, dict) else enumerate(tensors):
+            _check_devices(device, t, f"{name} {key}")
+
+
+def _loss_buffer(loss, device):
+    if loss is None:
+        return torch.zeros(1, dtype=torch.float32, device=device)
+    _check_on(device, loss, torch.float32, 1, "loss")
+    return loss
+
+
 def _teacher_entries(n_tok, teacher_logits, teacher_ids, device):
     """Entries per position of a teacher's top logits [..., top_k]."""
     k = teacher_ids.shape[-1]
@@ -566,6 +583,7 @@ def t5_stack_top_logits(sc, tokens, weights, top_k, values=None, ids=None, works
     cs = _stack_cfg_struct(sc)
     _check_tensor(tokens, torch.int32, b.batch * b.seq, "tokens")
     ws = _stack_weights_struct(sc, weights)
+    _check_devices(dev, weights, "weights")
     nbytes = lib().t5_stack_top_logits_workspace_bytes(C.byref(cs), _i32(top_k))
     if nbytes:  # (0: the call below says what is wrong)
         values, ids = _top_outputs(b.batch, b.seq, top_k, dev, values, ids)
@@ -593,8 +611,9 @@ def t5_stack_distill_loss_and_grad(sc, tokens, targets, teacher_logits, teacher_
         gs_ref = C.byref(_stack_grads_struct(sc, weights, grads))
     else:
         grads = None
-    if loss is None:
-        loss = torch.zeros(1, dtype=torch.float32, device=dev)
+    _check_devices(dev, weights, "weights")
+    _check_devices(dev, grads, "grads")
+    loss = _loss_buffer(loss, dev)
     workspace = _model_workspace(workspace, lib().t5_stack_distill_workspace_bytes(C.byref(cs), C.byref(opts)), dev)
     _call(lib().t5_stack_distill_loss_and_grad, "t5_stack_distill_loss_and_grad", dev, C.byref(cs), C.byref(opts),
           tokens.data_ptr(), targets.data_ptr(), teacher_logits.data_ptr(), teacher_ids.data_ptr(), C.byref(ws),
@@ -709,9 +728,10 @@ def t5_encdec_top_logits(ec, enc_tokens, dec_tokens, weights, top_k, values=None
     """t5_stack_top_logits for the encoder-decoder model: the largest logits of every decoder position."""
     e, d, dev = ec.enc_block, ec.dec_block, dec_tokens.device
     cs = _encdec_cfg_struct(ec)
-    _check_tensor(enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
     _check_tensor(dec_tokens, torch.int32, d.batch * d.seq, "dec_tokens")
+    _check_on(dev, enc_tokens, torch.int32, e.batch * e.seq, "enc_tokens")
     ws = _encdec_weights_struct(ec, weights)
+    _check_devices(dev, weights, "weights")
     nbytes = lib().t5_encdec_top_logits_workspace_bytes(C.byref(cs), _i32(top_k))
     if nbytes:  # (0: the call below says what is wrong)
         values, ids = _top_outputs(d.batch, d.seq, top_k, dev, values, ids)
@@ -740,8 +760,9 @@ def t5_encdec_distill_loss_and_grad(ec, enc_tokens, dec_tokens, targets, teacher
         gs_ref = C.byref(_encdec_grads_struct(ec, weights, grads))
     else:
         grads = None
-    if loss is None:
-        loss = torch.zeros(1, dtype=torch.float32, device=dev)
+    _check_devices(dev, weights, "weights")
+    _check_devices(dev, grads, "grads")
+    loss = _loss_buffer(loss, dev)
     workspace = _model_workspace(workspace, lib().t5_encdec_distill_workspace_bytes(C.byref(cs), C.byref(opts)), dev)
     _call(lib().t5_encdec_distill_loss_and_grad, "t5_encdec_distill_loss_and_grad", dev, C.byref(cs), C.byref(opts),
           enc_tokens.data_ptr(), dec_tokens.data_ptr(), targets.data_ptr(), teacher_logits.data_ptr(),

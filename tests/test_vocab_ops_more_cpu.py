@@ -3,6 +3,7 @@ import ctypes as C
 from dataclasses import replace
 
 import pytest
+import torch
 
 import paper_2203_17189_amd as P
 import synth_inputs as SI
@@ -65,3 +66,12 @@ def test_model_workspaces_off_256_bytes():
     assert L.t5_encdec_top_logits(C.byref(ce), D, D, C.byref(we), 8, D, D, odd, n, None) == WORKSPACE
     assert L.t5_stack_distill_loss_and_grad(C.byref(cs), C.byref(o), D, D, D, D, C.byref(ws), D, None, 0, odd, n, None) == WORKSPACE
     assert L.t5_encdec_distill_loss_and_grad(C.byref(ce), C.byref(o), D, D, D, D, D, C.byref(we), D, None, 0, odd, n, None) == WORKSPACE
+
+
+def test_tensors_of_a_model_on_another_device():
+    here, there = torch.zeros(2), torch.zeros(2, device="meta")
+    B._check_devices(here.device, None, "grads")
+    B._check_devices(here.device, dict(a=here, layers=[dict(b=here), dict(b=here, c=None)]), "weights")
+    for bad in (dict(a=there), dict(a=here, layers=[dict(b=here), dict(b=there)])):
+        with pytest.raises(ValueError):
+            B._check_devices(here.device, bad, "weights")
