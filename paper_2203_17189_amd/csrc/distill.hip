@@ -6,9 +6,10 @@
 // Bound by bytes where the row stays in registers: every logit is read once and its gradient written once.  With two
 // softmaxes the exponentials (a quarter of the rate of other instructions) come close behind: exp(x - m) is the square or
 // the fourth power of exp((x - m) / tau) where tau is 2 or 4.
-// Measured on one MI355X, three sets of inputs in turn, loss and gradient: 16384 rows of 32128 in bf16, K = 64, 414 us (2.1 GB,
-// 5.1 TB/s; a copy's 5.2 come to 409); the loss alone, 4096 rows, 50 us (264 MB, 5.3 TB/s); 200 rows of 131071 in
-// float32, which are read twice, 67 us (315 MB, 4.7 TB/s); 48 rows of 509, 7.5 us, two launches.
+// Measured on one MI355X, calls captured into a graph, three sets of inputs in turn, loss and gradient: 16384 rows of 32128 in
+// bf16, K = 64, 414 us (2.1 GB, 5.1 TB/s; a copy's 5.2 come to 409), 436 over the logits themselves; the loss alone, 4096 rows,
+// 50 us (264 MB, 5.3 TB/s); 200 rows of 131071 in float32, which are read twice, 67 us (315 MB, 4.7 TB/s); 48 rows of 509,
+// 7.5 us, two launches (16 us a call from Python).
 #include "kernels.h"
 #include "vocab_rows.h"
 #include <algorithm>
@@ -24,8 +25,9 @@ constexpr int kSelfCount = 1024;
 constexpr int kAhead = 16;        // loads in flight where one workgroup goes over all rows
 
 // Which exponentials a row needs: one (tau = 1, or only one of the two softmaxes has weight), two of which the second is
-// the square or fourth power of the first, or two.  (tau 2 against tau 1.5, bf16: 10240 x 2048 32.8 and 36.4 us, 300 x 131072
-// 66 and 76; no difference where bytes bind, in float32 or at 16384 x 32128.)
+// the square or fourth power of the first, or two.  (Against two, bf16: tau 2 10240 x 2048 30.0 and 32.5 us, 4096 x 8000 35.4 and
+// 39.9, 300 x 131072 64 and 74; tau 4 30.9 and 32.7, 36.7 and 41.6, 68 and 74; no difference where bytes bind, in float32 or
+// at 16384 x 32128.)
 enum { EXP_ONE = 0, EXP_SQUARE = 1, EXP_FOURTH = 2, EXP_TWO = 3 };
 
 bool distill_counts(const int32_t* targets, int64_t rows) { return targets && rows > kSelfCount; }
@@ -374,9 +376,13 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float* __restr
 constexpr int kPartNV = 8;
 constexpr int kPartPieces = 256 * kPartNV;
 
-// Workgroups that share a row: 1, or parts of 32 KB for rows that do not fit one workgroup's registers, or that would
-// leave compute units without work (bf16, 16 x 65536: 14.4 us in parts, 17 whole; 250 x 65536: 28.5 in parts, 23.4 whole).
-// 1000 rows of 262144: 311 us, with parts of 64 or 16 KB 321.
+// Workgroups that share a row: 1, or parts of 32 KB for rows that do not fit one workgroup's registers (more than 256 KB), and
+// for fewer than 128 rows of more than 64 KB, which would leave compute units without work.  Whole and in parts, T = 2, us:
+// bf16 16 x 65536 16.4 and 14.0, 64 x 40000 16.6 and 15.0, but float32 32 x 20000 11.2 and 12.8; 16 x 32000 12.7 and 14.0;
+// 128 x 65536 19.6 and 20.6, 1000 x 65536 77 and 94.  Rows of 128 to 256 KB leave a compute unit to one workgroup, and with
+// 128 of them and more the whole row is mostly ahead (1000 x 128256 146 and 166, 2048 x 100000 242 and 248, float32
+// 1000 x 50257 108 and 128), not always (300 x 131072 66 and 60, 500 x 70000 61 and 53) and not without a gradient (1000 x
+// 128256 73 and 59).  1000 rows of 262144: 311 us, with parts of 64 or 16 KB 321.
 int row_parts(int64_t rows, int V, int type) {
   const int pieces = ceil_div(V, type == IN_BF16 ? 8 : 4);
   return pieces <= 4096 || (pieces <= 16384 && rows >= 128) ? 1 : ceil_div(pieces, kPartPieces);
@@ -397,7 +403,8 @@ void rows_of_mode(const DistillArgs& a, const T* x, T* g, int64_t rows, hipStrea
   }
   // a row in a workgroup's registers, 16 pieces a thread at most; more workgroups at a time with fewer threads or fewer
   // registers each (bf16: 10240 x 500 28 us with 64 threads, 36 with 128; 10240 x 4096 53 with 128, 64 with 256; 8192 x 8000 68
-  // with 4 pieces, 86 with 8; 8192 x 16000 115 with 8, 141 with 16; 2048 x 65000 125 with 512 threads, 215 with 1024)
+  // with 4 pieces, 86 with 8; 8192 x 16000 115 with 8, 141 with 16; 2048 x 65000 125 with 512 threads, 215 with 1024).  With 1024
+  // threads a SIMD's registers are 128 for each, 7 to 10 fewer than the gradient wants: those are spilled.
   if (pieces <= 256) go(distill_rows_kernel<T, 64, 4, MODE, WHOLE_ROW, GRAD>, 64);
   else if (pieces <= 512) go(distill_rows_kernel<T, 128, 4, MODE, WHOLE_ROW, GRAD>, 128);
   else if (pieces <= 1024) go(distill_rows_kernel<T, 256, 4, MODE, WHOLE_ROW, GRAD>, 256);

@@ -5,7 +5,9 @@
 // positions of a row ascend), and every row of an id that occurs is written by the wavefronts that sum it.
 // Measured on one MI355X (a copy moves 5.2 TB/s there, a fill 6.9), three sets of inputs in turn, bf16: lookup of 16384 rows
 // of 768, 8.0 us (50 MB; a part of the table comes from the Infinity Cache); gradient of the same for 32128 rows, a
-// seventh of the tokens padding, 40 us (124 MB, 24 us at a copy's rate); 32768 x 2048, 112 us (397 MB, 77 us).
+// seventh of the tokens padding, 40 to 43 us (124 MB, 24 us at a copy's rate); 32768 x 2048, 113 us (397 MB, 77 us).  Added to a
+// gradient that is there, as the models do, for some 5900 and 10400 rows that occur: 37 us (61 MB, 12 us;
+// 13 in the sort, which has no clearing beside it, 19 in the sums, 6 in the join) and 97 us (304 MB, 59 us; 19, 76 and 7).
 #include "kernels.h"
 #include <algorithm>
 

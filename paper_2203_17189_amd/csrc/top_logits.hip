@@ -4,11 +4,15 @@
 // A logit and its id form one 64-bit key, (value ordered as an unsigned number) * 2^32 + (2^32 - 1 - id): keys of a row
 // differ, so "the K largest" has one answer.  A workgroup reads its row a chunk at a time into registers.  In the first
 // chunk a value that the largest of K of 64 to 256 groups reach is a lower bound of the row's K-th largest value, and few
-// elements reach it: these are collected in LDS.  Later chunks add what exceeds the K-th largest key so far.  Rows laid
-// out against that (thousands of elements above the bound) are searched bit by bit instead.
-// Measured on one MI355X, random logits: 8192 rows of 32128 in bf16, K = 64, 100 to 105 us (5.0 to 5.3 TB/s; a copy's 5.2 come to 103);
-// 1023 rows of 100003 in float32, 13 elements between them, K = 100, 90 us (4.5 TB/s); 8 rows of 32128 in float32,
-// K = 16, 8.4 us: one pass of a workgroup each, from the loads to the ranking.
+// elements reach it: these are collected in LDS.  Later chunks add what exceeds the K-th largest key so far.  A wavefront's 64
+// groups are asked for their share of K and the least share counts, so rows whose large values lie side by side are bounded
+// badly; with more keys at the bound than LDS holds (128 in the form of one wavefront, 512 in that of two, else 2048) a row is
+// read again: for its ties if these are what is too many, else once for each of a key's 64 bits.
+// Measured on one MI355X, independent logits, captured into a graph: 8192 rows of 32128 in bf16, K = 64, 100 to 105 us (5.0 to
+// 5.3 TB/s; a copy's 5.2 come to 103); 1023 rows of 100003 in float32, 13 elements between them, K = 100, 90 us (4.5 TB/s); 8 rows
+// of 32128 in float32, K = 16, 8.4 us: one pass of a workgroup each, from the loads to the ranking.  Bit by bit: 19.8 ms for the
+// first of these with all but 600 neighbouring logits at -inf, 5.9 ms for 8192 x 8000, K = 32, with 200 neighbours above the rest
+// (36.7 us without).
 #include "kernels.h"
 #include "vocab_rows.h"
 #include <algorithm>
@@ -55,7 +59,7 @@ __device__ __forceinline__ float piece_max<bf16>(u32x4 r) {
 template <int NT>
 struct TopShared {
   // keys collected at most: with 1024 and 2048 for one and two wavefronts, LDS holds fewer rows on a compute unit (16384 x 500,
-  // K = 16: 29.6 us against 22.5; 8192 x 8000, K = 64: 63.7 and 50.6)
+  // K = 16: 21.5 us against 17.3; 8192 x 8000, K = 64: 57.0 and 47.8)
   static constexpr int kKeys = NT == 64 ? 256 : NT == 128 ? 512 : 2048;
   alignas(16) uint32_t best[256];
   alignas(16) uint64_t cand[kKeys];
@@ -169,7 +173,8 @@ __global__ __launch_bounds__(NT, NT == 256 ? (NP > 4 && !ONE ? 5 : 6) : NP == 8 
   }
   const int own = ONE ? -1 : sp.single(tid, NT, V);
   const float xs = own >= 0 ? to_f32(x[own]) : -INFINITY;
-  // twice K groups bound nearly as well as more, for fewer comparisons (8192 x 32128, K = 16: 96 us, with 256 groups 111)
+  // twice K groups: fewer wavefronts to share K among than with 256 of them, which bound independent values no better (8192 x
+  // 32128, K = 16: 90 us with either; K = 64: 101 and 99)
   const int groups = K <= 32 ? 64 : K <= 96 ? 128 : 256;
   bool crowded = false;
   uint32_t level = 0;  // value of the bound
@@ -333,17 +338,17 @@ hipError_t launch_top_logits(const void* logits, int type, int64_t rows, int V, 
   auto go = [&](auto kern, int nt, auto* p) { kern<<<(unsigned)rows, nt, 0, st>>>(p, V, ld, K, values, ids); };
   auto of_type = [&](auto* p) {
     typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type T;
-    // (Both sides of each choice as they were measured, with a slower bound: now 10 to 40% less for either.)  One element
-    // at a time where pieces are too few to bound K well (16384 x 500, K = 100: 109 us, by pieces 328; 4096 x 4000: 43.6 and
-    // 45.4).  Many rows: one wavefront each as long as its 64 groups bound K and 16 pieces a lane hold the row, two up to
-    // K = 96, so that more rows are on their way at a time (16384 x 500, K = 16: 22.5 us, 62.9 with four wavefronts;
-    // 8192 x 2048, K = 16: 19.6 and 42.5; 8192 x 8000, K = 32: 38.3 and 61.1, K = 64: 50.6 and 74.6; 8192 x 16000, K = 16:
-    // 57.5 and 73.8; but 8192 x 8000, K = 110: 123 and 79, and 8192 x 32128, K = 64, in chunks: 132 and 115).  Fewer than 512
-    // rows: 4 wavefronts (400 x 8000, K = 64: 11.2 us, with two 13.4), or 16 on rows of more than 64 KB that leave compute
-    // units idle (8 x 32128 in float32: 11.0 us, with four 16.2; 256 x 131072: 40.0 and 49.5; but 384 rows of them 62 and
-    // 59).  Rows of up to 16 KB are one chunk of four pieces a lane (8192 x 8000, K = 120: 104 us, with sixteen 121); the
-    // shortest take as few loads as they have elements for (16384 x 64, K = 8: 16.4 and 18.9; 8192 x 500, K = 64: 25.3 and
-    // 28.5).
+    // (bf16 unless it says otherwise, us.)  One element at a time where pieces are too few to bound K well (16384 x 500,
+    // K = 100: 64, by pieces 275 and 306; 4096 x 4000: 31.0 and 34.0).  Many rows: one or two wavefronts each as long as 16
+    // pieces a lane hold the row and their 64 or 128 groups bound K, so that more rows are on their way at a time (with four
+    // wavefronts second: 16384 x 500, K = 16: 16.9 and 42.3; 8192 x 2048, K = 16: 15.9 and 28.7; 8192 x 8000, K = 64: 47.5 and 60.7;
+    // 8192 x 16000, K = 64: 71.7 and 82.7; 8192 x 32128, K = 64, which two wavefronts take in chunks: 123 and 101).  Of 513 to 1024
+    // pieces one wavefront gains nothing on two (8192 x 5000, K = 8: 21.9 and 22.4; 8192 x 8000, K = 32: 36.5 and 35.1; 600 x
+    // 8000, K = 16: 9.0 and 7.7).  Fewer than 512 rows: four wavefronts (400 x 8000, K = 64: 10.0, with two 12.6), or 16 on rows of
+    // more than 64 KB as long as each row has a compute unit (8 x 32128 in float32: 8.4, with four 10.5; 256 x 131072: 20.2 and
+    // 29.2; 300 rows of 36000: 21.3 and 18.0, of 131072 in float32 56.8 and 54.2, in bf16 29.9 and 32.7).  Rows of up to 16 KB are
+    // one chunk of four pieces a lane (8192 x 8000, K = 120: 84, with sixteen 103); the shortest take as few loads as they have
+    // elements for (16384 x 64, K = 8: 9.9 and 12.3; 8192 x 500, K = 64: 18.0 and 20.0).
     const bool many = rows >= 512;
     if (V <= 256 && K <= 32) go(top_logits_kernel<T, 64, 4, true>, 64, p);
     else if (V <= 1024 && K <= 32) go(top_logits_kernel<T, 64, 16, true>, 64, p);
