@@ -552,11 +552,12 @@ def _model_workspace(workspace, nbytes, device):
 
 
 def _check_devices(device, tensors, name):
-    """Every tensor of a model's weights or gradients is on the device of its tokens."""
+    """No tensor among a model's weights or gradients is on another GPU than its tokens.  (Those that the call reads are on a
+    GPU, as their own checks see to; whatever else the caller keeps beside them is of no interest.)"""
     if isinstance(tensors, torch.Tensor):
-        if tensors.device != device:
+        if tensors.device.type == device.type and tensors.device != device:
             raise ValueError(f"{name}: on {tensors.device}, other arguments on {device}")
-    elif tensors is not None:
+    elif isinstance(tensors, (dict, list, tuple)):
         for key, t in tensors.items() if isinstance(tensors, dict) else enumerate(tensors):
             _check_devices(device, t, f"{name} {key}")
 

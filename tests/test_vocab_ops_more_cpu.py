@@ -69,9 +69,11 @@ def test_model_workspaces_off_256_bytes():
 
 
 def test_tensors_of_a_model_on_another_device():
-    here, there = torch.zeros(2), torch.zeros(2, device="meta")
-    B._check_devices(here.device, None, "grads")
-    B._check_devices(here.device, dict(a=here, layers=[dict(b=here), dict(b=here, c=None)]), "weights")
-    for bad in (dict(a=there), dict(a=here, layers=[dict(b=here), dict(b=there)])):
+    t, other = torch.zeros(2), torch.device("cpu", 7)  # (two devices of one kind, as two GPUs are)
+    for tree in (t, dict(a=t), dict(layers=[dict(b=None), dict(b=t)])):
         with pytest.raises(ValueError):
-            B._check_devices(here.device, bad, "weights")
+            B._check_devices(other, tree, "weights")
+        B._check_devices(t.device, tree, "weights")
+    # what a caller keeps beside its weights: nothing, names, numbers, tensors on the host
+    B._check_devices(torch.device("cuda", 0), dict(name="model", step=3, note=None, host=t, more=(1, "x")), "weights")
+    B._check_devices(other, None, "grads")
