@@ -1,4 +1,4 @@
-// Host-side checker for the vocabulary operators of include/t5mi.h and the models that call them, as driver.cpp beside it
+// Host-side check of the vocabulary operators of include/t5mi.h and the models that call them, as driver.cpp beside it
 // (see tests/test_host_sanitizers_vocab.py).  Size queries and refusals over the whole range of every argument; and calls that
 // pass the checks, for the arithmetic of their launches: the runtime's stand-ins turn every launch away, so these end with
 // T5_ERR_DEVICE, and pointers are never followed.
