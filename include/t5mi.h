@@ -51,6 +51,9 @@ enum {
 };
 
 enum { T5_F32 = 0, T5_BF16 = 1 };
+/* 8-bit floating point (t5_quantize_fp8, t5_gemm_fp8): sign, exponent, fraction of 1, 4, 3 bits (largest value 448, no
+ * infinity) and of 1, 5, 2 bits (largest finite value 57344). */
+enum { T5_E4M3 = 2, T5_E5M2 = 3 };
 
 /* Feed-forward sublayer of a block (paper Sec. 4 names both T5 generations):
  *   T5_MLP_GEGLU_TANH  T5.1.1: (gelu_tanh(n2 Wi0) * (n2 Wi1)) Wo_ff
@@ -517,6 +520,99 @@ int adafactor_step_multi(const adafactor_tensor* tensors, int n_tensors, const a
  * 16-byte aligned, (m-contiguous case) M or N % 8 -> T5_ERR_UNSUPPORTED. */
 int t5_gemm_bf16(const void* A, const void* B, float* C, int M, int N, int K, int lda, int ldb, int ldc,
                  int a_kc, int b_kc, void* stream);
+
+/* Linear layers in 8 bits (the projections of paper Sec. 4's models, y = x W): the quantised matrix, and the product of two.
+ *
+ * A quantised matrix stands for  code[r, c] * 2^(scale[r', c / 128] - 127),  codes of T5_E4M3 or T5_E5M2, one byte of scale
+ * (the exponent of a power of two) for each block of 128 columns of one row (block_rows == 1, r' = r) or of 128 rows
+ * (block_rows == 128, r' = r / 128).  Rows of codes are a multiple of 16 bytes apart, rows of scales a multiple of 4; what
+ * lies between cols and the next multiple of 16, or of 4 scales, is read in whole pieces and has no effect.
+ *
+ * t5_quantize_fp8 makes one from x [rows, cols] of dtype, rows ld elements apart: q with rows t5_fp8_ld(cols) bytes apart
+ * and scale with rows t5_fp8_scale_ld(cols) bytes apart (the pieces' ends are written as zeros), and, read from x in the
+ * same pass, the transposed matrix: qt [cols] rows of t5_fp8_ld(rows) bytes, scale_t rows of t5_fp8_scale_ld(rows) bytes.
+ * With block_rows == 1 the transposed matrix has scales of its own, a block being 128 rows of one column of x (what the
+ * gradient of a weight reduces over); with block_rows == 128 its codes and scales are those of q.
+ * Per block, with b the largest finite |x| and M the largest finite value of q_dtype:  scale = the smallest power of two s
+ * with b / s <= M, not below 2^-127 (1 where b = 0);  code = x / s rounded to nearest, ties to even.  NaN becomes NaN;
+ * infinities become NaN in T5_E4M3 and stay infinities in T5_E5M2.  Either pair of outputs may be NULL.  rows == 0 is a no-op.
+ * Errors: rows < 0, cols < 1, ld < cols, block_rows neither 1 nor 128 -> T5_ERR_SHAPE; x NULL, no output, or one of a pair
+ * without the other -> T5_ERR_NULL; rows > 2^31 - 129, cols > 2^23, ld > 2^32, unknown types, q or qt not 16-byte aligned,
+ * scale or scale_t not 4-byte aligned -> T5_ERR_UNSUPPORTED. */
+typedef struct {
+  int64_t rows, cols, ld;
+  int32_t dtype;      /* T5_F32 or T5_BF16 */
+  int32_t q_dtype;    /* T5_E4M3 or T5_E5M2 */
+  int32_t block_rows; /* 1 or 128 */
+} t5_quantize_cfg;
+int64_t t5_fp8_ld(int64_t cols);       /* cols rounded up to a multiple of 16 */
+int64_t t5_fp8_scale_ld(int64_t cols); /* the number of blocks of 128, rounded up to a multiple of 4 */
+int t5_quantize_fp8(const t5_quantize_cfg* cfg, const void* x, void* q, uint8_t* scale, void* qt, uint8_t* scale_t,
+                    void* stream);
+
+/* C[m, n] (+)= sum over k of A[m, k] B[n, k], A [M, K] and B [N, K] quantised matrices, sums in float32.  With bfloat16 C
+ * each product is cut below 2^-13 of the largest of the eight consecutive ones it is added with (what the matrix unit does
+ * with codes), far below the result's own rounding; with float32 C products are whole, at half the rate, and an element of
+ * A or B below 2^-126 may count as zero.  Forward product: A = x, B = the weight with its input index along the row; gradient of x: A = dy,
+ * B = that weight transposed; gradient of the weight: A and B the transposed x and dy (t5_quantize_fp8 makes all of them).
+ * C: float32 or bfloat16 (c_dtype), rows ldc elements apart, elements between them left alone.  accumulate != 0 adds to C
+ * (float32 only).  Scale byte 255 is NaN.  Results do not depend on what else runs: the same bits every time.
+ * workspace: t5_gemm_fp8_workspace_bytes(cfg) bytes, 256-byte aligned (NULL where that is 0).  M == 0 is a no-op.
+ * Errors: M < 0, N or K < 1, lda or ldb < K, ldc < N, lsa or lsb less than the blocks of K, block rows neither 1 nor 128
+ * -> T5_ERR_SHAPE; NULL -> T5_ERR_NULL; accumulate with bfloat16, unknown types, lda or ldb no multiple of 16 or above 2^23,
+ * lsa or lsb no multiple of 4 or above 2^20, ldc > 2^32, M or N > 2^30, A or B not 16-byte, scales not 4-byte aligned, C not
+ * aligned to its elements -> T5_ERR_UNSUPPORTED; workspace small, or not 256-byte aligned -> T5_ERR_WORKSPACE. */
+typedef struct {
+  int32_t M, N, K;
+  int64_t lda, ldb, ldc; /* of A and B in bytes, of C in elements */
+  int64_t lsa, lsb;      /* bytes between rows of scales */
+  int32_t a_dtype, b_dtype;
+  int32_t a_block_rows, b_block_rows;
+  int32_t c_dtype;
+  int32_t accumulate;
+} t5_gemm_fp8_cfg;
+size_t t5_gemm_fp8_workspace_bytes(const t5_gemm_fp8_cfg* cfg);
+int t5_gemm_fp8(const t5_gemm_fp8_cfg* cfg, const void* A, const uint8_t* a_scale, const void* B, const uint8_t* b_scale,
+                void* C, void* workspace, size_t workspace_bytes, void* stream);
+
+/* AdamW for many tensors at once (an optimizer beside Adafactor; decoupled weight decay), float32 parameters updated in place:
+ *   g = grad_scale * grad;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2
+ *   param <- param (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * bf16_copy_out (nullable) receives the new parameters rounded to bf16.  Arithmetic is float32, factors are rounded once.
+ * state_bits == 32: m and v float32 [n].  state_bits == 8: m and v hold n codes of T5_E4M3 each, of m and of sqrt(v), and
+ * m_scale and v_scale one byte for each 128 consecutive elements, as in a quantised matrix; all zeros is the state before
+ * the first step.  The update uses m and v before they are rounded; each is then rounded at random, so that averages that
+ * move by less than a step of the format still move: with y = |value| / scale and t = y / (the type's step at y), the code
+ * is floor(t + u) steps, and of sqrt(v) > 0 at least the smallest code.  u is 16 bits: with mix32 as at t5_dropout_keep, i
+ * the tensor's place in the list and b, c the block and the place in the block of an element,
+ *   h = mix32(mix32(mix32(mix32(seed_lo ^ step) ^ i * 0x9E3779B9) ^ b ^ seed_hi) ^ c),
+ * u = (h mod 2^16) / 2^16 for m, (h div 2^16) / 2^16 for sqrt(v).  The same bits every time for the same arguments.
+ * A gradient that is not finite makes the element's parameter NaN and its states not finite (its neighbours' are as without
+ * it).  Tensors share no memory.  Every entry is checked before the first launch.
+ * Errors: NULL -> T5_ERR_NULL; n_tensors < 1, n < 1, step < 1, lr or weight_decay < 0 or not finite, beta1 or beta2 outside
+ * [0, 1), eps below 1e-30 or not finite, parameters of two
+ * entries that overlap -> T5_ERR_SHAPE; n_tensors > 65536, n > 2^36, state_bits neither
+ * 8 nor 32, unknown grad_dtype, a pointer not aligned to its elements -> T5_ERR_UNSUPPORTED. */
+typedef struct {
+  float* param;
+  const void* grad;    /* [n] of grad_dtype */
+  void* m;             /* [n] float32, or codes */
+  void* v;             /* [n] float32, or codes of sqrt(v) */
+  uint8_t* m_scale;    /* [(n + 127) / 128], state_bits == 8 only */
+  uint8_t* v_scale;
+  void* bf16_copy_out; /* nullable */
+  int64_t n;
+  int32_t grad_dtype;  /* T5_F32 or T5_BF16 */
+  int32_t state_bits;  /* 8 or 32 */
+  double weight_decay; /* 0.1, say; 0 for scales and tables */
+} adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int32_t step;             /* 1-based */
+  uint32_t seed_lo, seed_hi; /* of the random rounding of 8-bit states */
+  const float* grad_scale;  /* DEVICE pointer to one float32 (a clipping factor, 1 / loss scale), or NULL for 1 */
+} adamw_cfg;
+int adamw_step_multi(const adamw_tensor* tensors, int n_tensors, const adamw_cfg* cfg, void* stream);
 
 /* Opt-in overlap inside the backward passes.  The weight-gradient GEMMs are leaves of the backward's
  * dependency graph; after t5_wgrad_overlap_enable(1) every backward entry point launches them on a

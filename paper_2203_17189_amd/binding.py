@@ -13,7 +13,7 @@ _LIB = None
 
 WEIGHT_NAMES = ("ln1_scale", "wq", "wk", "wv", "wo", "rel_table", "ln2_scale", "wi0", "wi1", "wo_ff")
 CROSS_WEIGHT_NAMES = ("lnx_scale", "xq", "xk", "xv", "xo")
-T5_F32, T5_BF16 = 0, 1
+T5_F32, T5_BF16, T5_E4M3, T5_E5M2 = 0, 1, 2, 3
 MLP_KINDS = {"geglu_tanh": 0, "relu": 1, "geglu_erf": 2}
 
 
@@ -95,6 +95,26 @@ class _DistillCfg(C.Structure):
 
 class _DistillOpts(C.Structure):
     _fields_ = [("top_k", C.c_int32), ("temperature", C.c_float), ("soft_weight", C.c_float)]
+
+
+class _QuantizeCfg(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("dtype", C.c_int32), ("q_dtype", C.c_int32),
+                ("block_rows", C.c_int32)]
+
+
+class _GemmFp8Cfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("M", "N", "K")] + [(n, C.c_int64) for n in ("lda", "ldb", "ldc", "lsa", "lsb")] + \
+               [(n, C.c_int32) for n in ("a_dtype", "b_dtype", "a_block_rows", "b_block_rows", "c_dtype", "accumulate")]
+
+
+class _AdamTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "bf16_copy_out")] + \
+               [("n", C.c_int64), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32), ("weight_decay", C.c_double)]
+
+
+class _AdamCfg(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps")] + \
+               [("step", C.c_int32), ("seed_lo", C.c_uint32), ("seed_hi", C.c_uint32), ("grad_scale", C.c_void_p)]
 
 
 class _AfTensor(C.Structure):
@@ -204,6 +224,18 @@ def lib() -> C.CDLL:
     L.t5_distill_loss_and_grad.argtypes = [C.POINTER(_DistillCfg), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.t5_gemm_bf16.restype = i32
     L.t5_gemm_bf16.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, vp]
+    L.t5_fp8_ld.restype = i64
+    L.t5_fp8_ld.argtypes = [i64]
+    L.t5_fp8_scale_ld.restype = i64
+    L.t5_fp8_scale_ld.argtypes = [i64]
+    L.t5_quantize_fp8.restype = i32
+    L.t5_quantize_fp8.argtypes = [C.POINTER(_QuantizeCfg), vp, vp, vp, vp, vp, vp]
+    L.t5_gemm_fp8_workspace_bytes.restype = sz
+    L.t5_gemm_fp8_workspace_bytes.argtypes = [C.POINTER(_GemmFp8Cfg)]
+    L.t5_gemm_fp8.restype = i32
+    L.t5_gemm_fp8.argtypes = [C.POINTER(_GemmFp8Cfg), vp, vp, vp, vp, vp, vp, sz, vp]
+    L.adamw_step_multi.restype = i32
+    L.adamw_step_multi.argtypes = [C.POINTER(_AdamTensor), i32, C.POINTER(_AdamCfg), vp]
     L.t5_wgrad_overlap_enable.restype = i32
     L.t5_wgrad_overlap_enable.argtypes = [i32]
     L.t5_step_timing_enable.restype = None
@@ -1022,6 +1054,158 @@ def t5_distill_loss_and_grad(logits, targets, teacher_logits, teacher_ids, tempe
           teacher_logits.data_ptr(), teacher_ids.data_ptr(), loss.data_ptr(), row_loss.data_ptr(), addr(dlogits),
           workspace.data_ptr(), workspace.numel())
     return loss, row_loss, dlogits
+
+
+_FP8 = {torch.float8_e4m3fn: T5_E4M3, torch.float8_e5m2: T5_E5M2}
+_FP8_NAMES = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+_E8M0 = torch.float8_e8m0fnu
+
+
+def _fp8_pair(rows, cols, block_rows, q_dtype, device):
+    """Codes [rows, cols] and scales of a new quantised matrix, rows as far apart as t5_quantize_fp8 writes them."""
+    blocks = -(-cols // 128)
+    q = torch.empty(rows, -(-cols // 16) * 16, dtype=q_dtype, device=device)
+    s = torch.empty(-(-rows // block_rows), -(-blocks // 4) * 4, dtype=_E8M0, device=device)
+    return q if q.shape[1] == cols else q[:, :cols], s if s.shape[1] == blocks else s[:, :blocks]
+
+
+def _check_fp8_pair(q, scale, rows, cols, block_rows, q_dtype, device, name):
+    blocks = -(-cols // 128)
+    for t, dt, shape, ld, what in ((q, q_dtype, (rows, cols), -(-cols // 16) * 16, name),
+                                   (scale, _E8M0, (-(-rows // block_rows), blocks), -(-blocks // 4) * 4, name + "'s scale")):
+        if t is None or t.device != device or t.dtype != dt or tuple(t.shape) != shape or \
+                (shape[1] > 1 and t.stride(1) != 1) or (shape[0] > 1 and t.stride(0) != ld):
+            raise ValueError(f"{what}: need {dt} {shape} on {device} with rows {ld} apart, got " +
+                             ("nothing" if t is None else f"{t.dtype} {tuple(t.shape)}, strides {t.stride()} on {t.device}"))
+        room = t.untyped_storage().nbytes() - t.storage_offset()  # (rows are written in whole pieces, the last one too)
+        if shape[0] > 0 and room < shape[0] * ld:
+            raise ValueError(f"{what}: its last row has no room for the end of its last piece")
+
+
+def t5_quantize_fp8(x, q_dtype="e4m3", block_rows=1, rows=True, transposed=False, q=None, scale=None, qt=None, scale_t=None):
+    """Quantised matrix of x [rows, cols] (float32 or bfloat16; rows may have a longer stride), and with transposed=True the
+    transposed one: (q, scale, qt, scale_t), the pairs that are not asked for None.  q_dtype: "e4m3" or "e5m2" (or torch's
+    type).  A scale (float8_e8m0fnu) serves 128 columns of one row, or of 128 rows with block_rows=128; with block_rows=1 the
+    transposed matrix has scales of its own, for 128 rows of one column of x.  Outputs of the caller's own have rows as far
+    apart as the ones made here: codes a multiple of 16, scales a multiple of 4."""
+    ty = _elem_type(x, "x")
+    n, cols, ld = _check_rows(x, "x")
+    dev = x.device
+    dt = _FP8_NAMES.get(q_dtype, q_dtype)
+    if dt not in _FP8:
+        raise ValueError(f"q_dtype: need e4m3 or e5m2, got {q_dtype}")
+    block_rows = operator.index(block_rows)
+    br = block_rows if block_rows in (1, 128) else 1
+    if not rows:
+        q = scale = None
+    elif q is None and scale is None:
+        q, scale = _fp8_pair(n, cols, br, dt, dev)
+    else:
+        _check_fp8_pair(q, scale, n, cols, br, dt, dev, "q")
+    if not transposed:
+        qt = scale_t = None
+    elif qt is None and scale_t is None:
+        qt, scale_t = _fp8_pair(cols, n, br, dt, dev)
+    else:
+        _check_fp8_pair(qt, scale_t, cols, n, br, dt, dev, "qt")
+    addr = lambda t: None if t is None else t.data_ptr()
+    _call(lib().t5_quantize_fp8, "t5_quantize_fp8", dev, C.byref(_QuantizeCfg(n, cols, ld, ty, _FP8[dt], _i32(block_rows))),
+          x.data_ptr(), addr(q), addr(scale), addr(qt), addr(scale_t))
+    return q, scale, qt, scale_t
+
+
+def _fp8_operand(q, scale, name):
+    """(rows, K, bytes between rows, type, rows of a block, bytes between rows of scales) of a quantised matrix."""
+    if q.dtype not in _FP8 or scale.dtype != _E8M0:
+        raise ValueError(f"{name}: need float8_e4m3fn or float8_e5m2 codes with float8_e8m0fnu scales, got {q.dtype}, {scale.dtype}")
+    n, k, ld = _check_rows(q, name)
+    sn, sk, sld = _check_rows(scale, name + "'s scale")
+    if n == 1 and ld % 16:  # one row: what is behind it is no stride
+        ld = -(-k // 16) * 16
+    if sn <= 1 and sld % 4:
+        sld = -(-sk // 4) * 4
+    if sk != -(-k // 128) or sn not in (n, -(-n // 128)):
+        raise ValueError(f"{name}: codes {tuple(q.shape)} have scales [{n} or {-(-n // 128)}, {-(-k // 128)}], got {tuple(scale.shape)}")
+    for t, rows, cols, step, what in ((q, n, k, 16, name), (scale, sn, sk, 4, name + "'s scale")):
+        # rows are read in whole pieces: the last one's end has to be there
+        if rows > 0 and t.untyped_storage().nbytes() - t.storage_offset() < (rows - 1) * t.stride(0) + -(-cols // step) * step:
+            raise ValueError(f"{what}: its last row ends inside a piece of {step} bytes, and its memory with it")
+    return n, k, ld, _FP8[q.dtype], 1 if sn == n else 128, sld
+
+
+def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accumulate=False, workspace=None):
+    """C[m, n] = sum over k of A[m, k] B[n, k] of two quantised matrices as t5_quantize_fp8 makes them (one scale for each
+    128 columns of a row, or of 128 rows: by the scales' shape).  out: [M, N] float32 or bfloat16, rows may have a longer
+    stride; accumulate adds to it (float32).  Returns out."""
+    m, k, lda, ta, bra, lsa = _fp8_operand(a, a_scale, "a")
+    n, kb, ldb, tb, brb, lsb = _fp8_operand(b, b_scale, "b")
+    dev = a.device
+    if k != kb:
+        raise ValueError(f"a has {k} columns, b {kb}")
+    for t, what in ((a_scale, "a's scale"), (b, "b"), (b_scale, "b's scale")):
+        if t.device != dev:
+            raise ValueError(f"{what}: on {t.device}, other arguments on {dev}")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate: there is no out to add to")
+        out = torch.empty(m, n, dtype=out_dtype, device=dev)
+    tc = _elem_type(out, "out")
+    rows, cols, ldc = _check_rows(out, "out")
+    if (rows, cols) != (m, n) or out.device != dev:
+        raise ValueError(f"out: need [{m}, {n}] on {dev}, got {tuple(out.shape)} on {out.device}")
+    cfg = C.byref(_GemmFp8Cfg(_i32(m), _i32(n), _i32(k), lda, ldb, ldc, lsa, lsb, ta, tb, bra, brb, tc, int(bool(accumulate))))
+    L = lib()
+    nbytes = L.t5_gemm_fp8_workspace_bytes(cfg)
+    if workspace is not None:
+        _check_on(dev, workspace, torch.uint8, workspace.numel(), "workspace")
+    elif nbytes:
+        workspace = _byte_buffer(nbytes, dev)
+    _call(L.t5_gemm_fp8, "t5_gemm_fp8", dev, cfg, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
+          out.data_ptr(), None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel())
+    return out
+
+
+def _adam_entry(t, device):
+    p, g, m, v = t["param"], t["grad"], t["m"], t["v"]
+    n = p.numel()
+    bits = 32 if m.dtype == torch.float32 else 8
+    state = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    gt = _elem_type(g, "grad")
+    for x, dt, name in ((p, torch.float32, "param"), (g, g.dtype, "grad"), (m, state, "m"), (v, state, "v")):
+        if x.dtype != dt or x.numel() != n or x.device != device or not x.is_contiguous():
+            _check_on(device, x, dt, n, name)
+    ms = vs = None
+    if bits == 8:
+        ms, vs = t["m_scale"], t["v_scale"]
+        _check_on(device, ms, _E8M0, -(-n // 128), "m_scale")
+        _check_on(device, vs, _E8M0, -(-n // 128), "v_scale")
+        ms, vs = ms.data_ptr(), vs.data_ptr()
+    lp = t.get("bf16_copy_out")
+    if lp is not None:
+        _check_on(device, lp, torch.bfloat16, n, "bf16_copy_out")
+        lp = lp.data_ptr()
+    return p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs, lp, n, gt, bits, t.get("weight_decay", 0.0)
+
+
+def adamw_step_multi(tensors, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None):
+    """In-place AdamW update of several float32 tensors in one launch (of 40 tensors).  tensors: list of dicts with param,
+    grad (float32 or bfloat16), m, v and optionally weight_decay and bf16_copy_out.  States in 32 bits: m and v float32.  In
+    8 bits: m and v float8_e4m3fn, codes of m and of sqrt(v), with m_scale and v_scale float8_e8m0fnu, one for each 128
+    consecutive elements; zeros throughout before the first step (t.zero_() of a uint8 view).  seed: of their random rounding;
+    grad_scale: a float32 tensor of one element that multiplies every gradient, or None."""
+    dev = tensors[0]["param"].device if tensors else None
+    arr = (_AdamTensor * len(tensors))(*[_adam_entry(t, dev) for t in tensors])
+    if not tensors:
+        raise T5Error(2, "adamw_step_multi")
+    if not tensors[0]["param"].is_cuda:
+        raise ValueError(f"param: on {dev}")
+    if grad_scale is not None:
+        _check_on(dev, grad_scale, torch.float32, 1, "grad_scale")
+        grad_scale = grad_scale.data_ptr()
+    seed = operator.index(seed)
+    cfg = _AdamCfg(float(lr), float(beta1), float(beta2), float(eps), _i32(step), seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF,
+                   grad_scale)
+    _call(lib().adamw_step_multi, "adamw_step_multi", dev, arr, len(tensors), C.byref(cfg))
 
 
 def t5_gemm_bf16(a: torch.Tensor, b: torch.Tensor, a_kc: bool, b_kc: bool, out: torch.Tensor | None = None):

@@ -1,0 +1,242 @@
+// AdamW over many tensors in one launch, states in 32 bits or in 8 (see include/t5mi.h).
+//
+// One pass: parameter, gradient and states are read once and written once; nothing else moves.  A workgroup takes a chunk of
+// one tensor; which one it finds in the launch's list of first chunks.  The list travels as the kernel's argument (4 KB hold
+// kAdamTensors entries): no table in device memory, nothing to allocate, and a captured launch keeps it.
+#include "fp8.h"
+#include "kernels.h"
+#include <cmath>
+#include <cstring>
+
+namespace t5mi {
+namespace {
+
+constexpr int kChunk = 2048;  // elements: 8 for each of 256 threads
+
+enum { AW_8BIT = 1, AW_BF16_GRAD = 2, AW_VEC = 4 };
+struct AdamItem {
+  float* p;
+  const void* g;
+  void *m, *v;
+  uint8_t *ms, *vs;
+  bf16* lp;
+  int64_t n;
+  float keep;     // 1 - lr * weight_decay
+  uint32_t key;   // of the tensor's random bits
+  int32_t flags, pad;
+};
+struct AdamBatch {
+  int32_t count;
+  uint32_t seed_hi;
+  float b1, one_b1, b2, one_b2, root_factor, eps, step_size;
+  const float* grad_scale;
+  int32_t start[kAdamTensors + 1];
+  AdamItem it[kAdamTensors];
+};
+static_assert(sizeof(AdamBatch) <= 4096, "kernel arguments");
+
+// Up to 8 elements from p + i on (n of them exist), in 16-byte pieces where VEC and all 8 exist.
+template <bool VEC>
+__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
+  if (VEC && n >= 8) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[j + 4] = b[j]; }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : 0.f;
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load8(const bf16* p, int n, float (&v)[8]) {
+  if (VEC && n >= 8) {
+    const bf16x8 a = *reinterpret_cast<const bf16x8*>(p);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)a[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? (float)p[j] : 0.f;
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
+  if (VEC && n >= 8) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = v[j];
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(bf16* p, int n, const float (&v)[8]) {
+  if (VEC && n >= 8) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = (bf16)v[j];
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ u32x2 load_codes(const uint8_t* p, int n) {
+  if (VEC && n >= 8) return *reinterpret_cast<const u32x2*>(p);
+  u32x2 r = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < n) r[j >> 2] |= (uint32_t)p[j] << ((j & 3) * 8);
+  return r;
+}
+template <bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t* p, int n, u32x2 c) {
+  if (VEC && n >= 8) {
+    *reinterpret_cast<u32x2*>(p) = c;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = (uint8_t)(c[j >> 2] >> ((j & 3) * 8));
+  }
+}
+
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+__device__ __forceinline__ void decode8(u32x2 c, float s, float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[h], true);
+    v[h * 4] = lo[0] * s; v[h * 4 + 1] = lo[1] * s; v[h * 4 + 2] = hi[0] * s; v[h * 4 + 3] = hi[1] * s;
+  }
+}
+
+// |x| * inv in e4m3, a whole number of steps: floor(t + u) with u = bits / 2^16.  In the type's normal range a step is the
+// 20 low bits of the fraction, and adding u there and cutting them off is that floor; below, steps are 2^-9 wide.
+__device__ __forceinline__ float round_at_random(float x, float inv, uint32_t bits) {
+  const float y = fabsf(x) * inv;
+  const float normal = __uint_as_float((__float_as_uint(y) + (bits << 4)) & 0xFFF00000u);
+  const float small = floorf(fmaf(y, 512.f, (float)bits * (1.f / 65536.f))) * (1.f / 512.f);
+  return y < 0.015625f ? small : normal;  // (NaN: stays NaN, the quiet bit is one that is kept)
+}
+
+struct Step {
+  float b1, one_b1, b2, one_b2, root_factor, eps, step_size, keep;
+  __device__ __forceinline__ void moments(float g, float& m, float& v) const {
+    m = fmaf(b1, m, one_b1 * g);
+    v = fmaf(b2, v, one_b2 * g * g);
+  }
+  __device__ __forceinline__ float update(float p, float m, float root) const {
+    return fmaf(p, keep, -step_size * (m / fmaf(root, root_factor, eps)));
+  }
+};
+
+template <bool VEC, bool EIGHT>
+__device__ __forceinline__ void adam_chunk(const AdamItem& it, const Step& s, float gs, uint32_t seed_hi, int64_t i) {
+  const int64_t left = it.n - i;
+  const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
+  float p[8], g[8], m[8], v[8], root[8];
+  if (it.flags & AW_BF16_GRAD) load8<VEC>((const bf16*)it.g + i, n, g);
+  else load8<VEC>((const float*)it.g + i, n, g);
+  load8<VEC>(it.p + i, n, p);
+  const int64_t block = i >> 7;
+  if constexpr (EIGHT) {
+    const u32x2 cm = load_codes<VEC>((const uint8_t*)it.m + i, n), cv = load_codes<VEC>((const uint8_t*)it.v + i, n);
+    decode8(cm, n > 0 ? scale_value(it.ms[block]) : 0.f, m);
+    decode8(cv, n > 0 ? scale_value(it.vs[block]) : 0.f, root);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = root[j] * root[j];
+  } else {
+    load8<VEC>((const float*)it.m + i, n, m);
+    load8<VEC>((const float*)it.v + i, n, v);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    s.moments(g[j] * gs, m[j], v[j]);
+    root[j] = sqrtf(v[j]);
+    p[j] = s.update(p[j], m[j], root[j]);
+  }
+  store8<VEC>(it.p + i, n, p);
+  if (it.lp) store8<VEC>(it.lp + i, n, p);
+  if constexpr (EIGHT) {
+    uint32_t am = 0, ar = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= n) m[j] = root[j] = 0.f;
+      am = max(am, finite_bits(m[j]));
+      ar = max(ar, finite_bits(root[j]));
+    }
+    const int em = block_exponent<T5_E4M3>(max16(am)), er = block_exponent<T5_E4M3>(max16(ar));
+    const float im = block_inverse(em), ir = block_inverse(er);
+    const uint32_t row = mix32(it.key ^ (uint32_t)block ^ seed_hi);
+    const int c0 = (int)(i & 127);
+    float cm[8], cr[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t h = mix32(row ^ (uint32_t)(c0 + j));
+      cm[j] = copysignf(round_at_random(m[j], im, h & 0xFFFFu), m[j]);
+      const float r = round_at_random(root[j], ir, h >> 16);
+      cr[j] = root[j] > 0.f ? fmaxf(r, 1.f / 512.f) : r;
+      if (root[j] != root[j]) cr[j] = root[j];
+    }
+    store_codes<VEC>((uint8_t*)it.m + i, n, u32x2{pack_fp8x4<T5_E4M3>(cm[0], cm[1], cm[2], cm[3]), pack_fp8x4<T5_E4M3>(cm[4], cm[5], cm[6], cm[7])});
+    store_codes<VEC>((uint8_t*)it.v + i, n, u32x2{pack_fp8x4<T5_E4M3>(cr[0], cr[1], cr[2], cr[3]), pack_fp8x4<T5_E4M3>(cr[4], cr[5], cr[6], cr[7])});
+    if (n > 0 && c0 == 0) {
+      it.ms[block] = (uint8_t)(em + 127);
+      it.vs[block] = (uint8_t)(er + 127);
+    }
+  } else {
+    store8<VEC>((float*)it.m + i, n, m);
+    store8<VEC>((float*)it.v + i, n, v);
+  }
+}
+
+__global__ __launch_bounds__(256) void adamw_kernel(AdamBatch b) {
+  int t = 0;
+  while (t + 1 < b.count && (int)blockIdx.x >= b.start[t + 1]) ++t;
+  const AdamItem& it = b.it[t];
+  const int64_t i = (int64_t)((int)blockIdx.x - b.start[t]) * kChunk + threadIdx.x * 8;
+  const float gs = b.grad_scale ? *b.grad_scale : 1.f;
+  const Step s{b.b1, b.one_b1, b.b2, b.one_b2, b.root_factor, b.eps, b.step_size, it.keep};
+  if (it.flags & AW_8BIT) {
+    if (it.flags & AW_VEC) adam_chunk<true, true>(it, s, gs, b.seed_hi, i);
+    else adam_chunk<false, true>(it, s, gs, b.seed_hi, i);
+  } else {
+    if (it.flags & AW_VEC) adam_chunk<true, false>(it, s, gs, b.seed_hi, i);
+    else adam_chunk<false, false>(it, s, gs, b.seed_hi, i);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const adamw_tensor* t, int n, int first, const adamw_cfg& c, hipStream_t st) {
+  if (n < 1 || n > kAdamTensors) return hipErrorInvalidValue;
+  AdamBatch b;
+  std::memset(&b, 0, sizeof(b));
+  b.count = n;
+  b.seed_hi = c.seed_hi;
+  b.b1 = (float)c.beta1; b.one_b1 = (float)(1.0 - c.beta1);
+  b.b2 = (float)c.beta2; b.one_b2 = (float)(1.0 - c.beta2);
+  b.root_factor = (float)(1.0 / std::sqrt(1.0 - std::pow(c.beta2, (double)c.step)));
+  b.eps = (float)c.eps;
+  b.step_size = (float)(c.lr / (1.0 - std::pow(c.beta1, (double)c.step)));
+  b.grad_scale = c.grad_scale;
+  const uint32_t k0 = mix32(c.seed_lo ^ (uint32_t)c.step);
+  int64_t chunks = 0;
+  for (int i = 0; i < n; ++i) {
+    AdamItem& it = b.it[i];
+    it.p = t[i].param; it.g = t[i].grad; it.m = t[i].m; it.v = t[i].v;
+    it.ms = t[i].m_scale; it.vs = t[i].v_scale; it.lp = (bf16*)t[i].bf16_copy_out; it.n = t[i].n;
+    it.keep = (float)(1.0 - c.lr * t[i].weight_decay);
+    it.key = mix32(k0 ^ (uint32_t)(first + i) * 0x9E3779B9u);
+    const uintptr_t code_mask = t[i].state_bits == 8 ? 7 : 15;
+    const uintptr_t odd = ((uintptr_t)it.p & 15) | ((uintptr_t)it.g & 15) | ((uintptr_t)it.m & code_mask) |
+                          ((uintptr_t)it.v & code_mask) | ((uintptr_t)it.lp & 15);
+    it.flags = (t[i].state_bits == 8 ? AW_8BIT : 0) | (t[i].grad_dtype == T5_BF16 ? AW_BF16_GRAD : 0) | (odd == 0 ? AW_VEC : 0);
+    b.start[i] = (int32_t)chunks;
+    chunks += (t[i].n + kChunk - 1) / kChunk;
+    if (chunks > 0x7FFFFFFF) return hipErrorInvalidValue;
+  }
+  b.start[n] = (int32_t)chunks;
+  adamw_kernel<<<(unsigned)chunks, 256, 0, st>>>(b);
+  return hipGetLastError();
+}
+
+}  // namespace t5mi

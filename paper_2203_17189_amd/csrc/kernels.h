@@ -348,4 +348,16 @@ struct AfTensor {
 };
 hipError_t launch_adafactor_multi(const AfTensor* t, int n, const adafactor_cfg& c, void* ws, hipStream_t st);
 
+// ------------------------------------------------------------------ 8-bit training
+int64_t fp8_ld(int64_t cols);
+int64_t fp8_scale_ld(int64_t cols);
+hipError_t launch_quantize_fp8(const t5_quantize_cfg& c, const void* x, void* q, uint8_t* scale, void* qt, uint8_t* scale_t,
+                               hipStream_t st);
+size_t gemm_fp8_ws_bytes(const t5_gemm_fp8_cfg& c);
+hipError_t launch_gemm_fp8(const t5_gemm_fp8_cfg& c, const void* A, const uint8_t* sa, const void* B, const uint8_t* sb, void* C,
+                           void* ws, hipStream_t st);
+// One launch of up to kAdamTensors tensors; `first` is the place of t[0] in the caller's list.
+constexpr int kAdamTensors = 40;
+hipError_t launch_adamw(const adamw_tensor* t, int n, int first, const adamw_cfg& c, hipStream_t st);
+
 }  // namespace t5mi

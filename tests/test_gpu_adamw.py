@@ -1,0 +1,181 @@
+"""AdamW over many tensors on the GPU, states in 32 bits and in 8, against float64."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2203_17189_amd as P
+from oracle import fp8_oracle as O
+from fp8_util import DT, E8M0, U, codes, host
+
+pytestmark = pytest.mark.gpu
+HP = dict(lr=2e-3, beta1=0.9, beta2=0.99, eps=1e-8)
+
+
+def make(rng, n, bits, grad="f32", copy=False, decay=0.1, shift=0, zero_state=False):
+    def place(a, dt):
+        wide = torch.empty(n + shift, dtype=dt, device="cuda")
+        wide[shift:] = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda()
+        return wide[shift:]
+
+    size = np.repeat(np.exp(rng.standard_normal(-(-n // 128))), 128)[:n] * 1e-2
+    t = dict(param=place(rng.standard_normal(n) * 0.1, torch.float32), grad=place(rng.standard_normal(n) * size, DT[grad]),
+             weight_decay=decay, bf16_copy_out=torch.empty(n + shift, dtype=torch.bfloat16, device="cuda")[shift:] if copy else None)
+    m = 0.0 * size if zero_state else 0.3 * size * rng.standard_normal(n)
+    r = 0.0 * size if zero_state else size * rng.uniform(0.3, 2.0, n)
+    if bits == 32:
+        t["m"], t["v"] = place(m, torch.float32), place(r * r, torch.float32)
+        return t
+    for key, a in (("m", m), ("v", r)):
+        q, s = O.quantize(np.pad(a, (0, -n % 128)).reshape(-1, 128), "e4m3", 1)
+        if zero_state:
+            s[:] = 0
+        wide = torch.zeros(n + shift, dtype=torch.uint8, device="cuda")
+        wide[shift:] = torch.from_numpy(q.reshape(-1)[:n]).cuda()
+        t[key], t[key + "_scale"] = wide[shift:].view(torch.float8_e4m3fn), torch.from_numpy(s.reshape(-1)).cuda().view(E8M0)
+    return t
+
+
+def state(t):
+    """(m, sqrt(v) or v) in float64."""
+    if t["m"].dtype == torch.float32:
+        return host(t["m"]), host(t["v"])
+    n = t["m"].numel()
+    return tuple((O.code_values("e4m3")[codes(t[k])] * np.repeat(2.0 ** (codes(t[k + "_scale"]) - 127.0), 128)[:n]) for k in ("m", "v"))
+
+
+def step_and_check(tensors, step, seed=0, grad_scale=None, hp=HP):
+    before = [(host(t["param"]), host(t["grad"]), *state(t)) for t in tensors]
+    gs = None if grad_scale is None else torch.tensor([grad_scale], device="cuda")
+    P.adamw_step_multi(tensors, step=step, seed=seed, grad_scale=gs, **hp)
+    for i, (t, (p, g, m, v)) in enumerate(zip(tensors, before)):
+        eight = t["m"].dtype != torch.float32
+        g = g if gs is None else g * host(gs)[0]
+        if eight:
+            v = v * v
+        wp, wm, wv = O.adamw(p, g, m, v, step=step, weight_decay=t["weight_decay"], **hp)
+        # m: products and their sum are three roundings, factors one each; v: one more
+        bm = 6 * U * (np.abs(hp["beta1"] * m) + np.abs((1 - hp["beta1"]) * g)) + 1e-40
+        bv = 8 * U * wv + 1e-40
+        # the quotient: m and sqrt(v) as above, half the relative error of v, the factors, eps, the division and the product
+        upd = np.abs(wp - p * (1 - hp["lr"] * t["weight_decay"]))
+        root = np.sqrt(wv / (1 - hp["beta2"] ** step)) + hp["eps"]
+        bp = 2 * U * np.abs(p) + 16 * U * upd + hp["lr"] / (1 - hp["beta1"] ** step) * bm / root + U * np.abs(wp)
+        np.testing.assert_array_less(np.abs(host(t["param"]) - wp), bp + 1e-30)
+        if t["bf16_copy_out"] is not None:
+            assert torch.equal(t["bf16_copy_out"], t["param"].to(torch.bfloat16))
+        if not eight:
+            np.testing.assert_array_less(np.abs(host(t["m"]) - wm), bm)
+            np.testing.assert_array_less(np.abs(host(t["v"]) - wv), bv)
+            continue
+        um, ur = O.random_parts(p.size, i, step, seed)
+        for key, want, u, bound in (("m", wm, um, bm), ("v", np.sqrt(wv), ur, 5 * U * np.sqrt(wv))):
+            s, steps, width = O.steps_of(want)
+            edge = np.abs(want).reshape(-1)
+            got_s = codes(t[key + "_scale"])
+            # (a block whose largest value is within rounding of the type's largest may have either scale)
+            pad = np.pad(edge, (0, -len(edge) % 128)).reshape(-1, 128).max(1)
+            near = np.abs(pad / (2.0 ** (s - 127.0) * 448) - 1) < 1e-5
+            assert (got_s[~near] == s[~near]).all()
+            sure = np.repeat(~near, 128)[:p.size]
+            x = steps + u
+            k = np.floor(x)
+            if key == "v":
+                k = np.where(edge > 0, np.maximum(k, 1), k)
+            exact = np.copysign(k * width, want)
+            got = O.code_values("e4m3")[codes(t[key])] * np.repeat(2.0 ** (got_s - 127.0), 128)[:p.size]
+            slack = bound / width + 16 * U * (1 + x)  # where rounding of the value may move it past a whole number
+            clear = sure & (np.abs(x - np.round(x)) > slack)
+            assert (got[clear] == exact[clear]).all()
+            assert clear.mean() > 0.9
+            assert (np.abs(got - want)[sure] <= width[sure] * 1.001 + slack[sure] * width[sure]).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 7, 8, 127, 128, 129, 2048, 2049, 5000, 100003])
+def test_one_tensor(n, grad, bits):
+    step_and_check([make(np.random.default_rng(n), n, bits, grad, copy=True)], step=3, seed=0x123456789ABCDEF)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("shift", [1, 2, 3, 4])
+def test_alignments(shift, bits):
+    step_and_check([make(np.random.default_rng(shift), 3001, bits, g, copy=True, shift=shift) for g in ("f32", "bf16")], step=1)
+
+
+def test_long_list_of_both_kinds():
+    """More tensors than one launch takes; kinds, gradients and decays mixed; random bits by the place in the whole list."""
+    rng = np.random.default_rng(11)
+    ts = [make(rng, int(n), 8 if i % 3 else 32, "bf16" if i % 2 else "f32", copy=i % 5 == 0, decay=0.1 * (i % 4 == 0))
+          for i, n in enumerate(rng.integers(1, 9000, 97))]
+    step_and_check(ts, step=17, seed=5, grad_scale=0.37)
+
+
+def test_list_call_is_the_same_as_its_parts_in_32_bits():
+    rng = np.random.default_rng(12)
+    ts = [make(rng, n, 32) for n in (5, 4000, 129)]
+    one = [{k: (v.clone() if torch.is_tensor(v) else v) for k, v in t.items()} for t in ts]
+    P.adamw_step_multi(ts, step=2, **HP)
+    for t in one:
+        P.adamw_step_multi([t], step=2, **HP)
+    for a, b in zip(ts, one):
+        assert all(torch.equal(a[k], b[k]) for k in ("param", "m", "v"))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_from_zero_states(bits):
+    """First step: the update is lr times the gradient's sign (but for eps), whatever its size; zero gradients move nothing."""
+    t = make(np.random.default_rng(4), 1000, bits, decay=0.0, zero_state=True)
+    t["grad"][100:228] = 0.0
+    p = t["param"].clone()
+    step_and_check([t], step=1)
+    move = (t["param"] - p).cpu()
+    assert (move[100:228] == 0).all()
+    g = t["grad"].cpu()
+    on = g.abs() > 1e-4
+    np.testing.assert_allclose(move[on], -HP["lr"] * g.sign()[on], rtol=0.0, atol=HP["lr"] * 1e-3 + 2e-8)
+
+
+def test_states_in_8_bits_follow_slow_averages():
+    """sqrt(v) of a constant gradient from zero on: after 400 steps of beta2 = 0.99 its mean over many elements is that of
+    float64.  A step's rounding adds variance of at most width^2 / 4 to a root that forgets with 0.99^(1/2) a step; the mean
+    over 4096 independent elements is within six standard deviations, and sqrt of the mean square above the mean by less
+    than half the variance."""
+    n, g0 = 4096, 0.01
+    t = make(np.random.default_rng(6), n, 8, zero_state=True, decay=0.0)
+    t["grad"].fill_(g0)
+    for s in range(1, 401):
+        P.adamw_step_multi([t], step=s, seed=99, **{**HP, "lr": 0.0})
+    m, r = state(t)
+    want = g0 * np.sqrt(1 - 0.99 ** 400)
+    width = 2.0 ** -3  # of a step, relative, at most
+    var = (width ** 2 / 4) / (1 - 0.99) * 0.5  # relative variance of one element, an upper bound
+    assert abs(r.mean() / want - 1) <= 6 * np.sqrt(var / n) + 0.5 * var
+    assert abs(m.mean() / g0 - 1) <= 6 * np.sqrt((width ** 2 / 4) / (1 - 0.81) / n) + 1e-3
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_that_are_not_finite_stay_in_their_elements(bits):
+    t, clean = (make(np.random.default_rng(8), 600, bits) for _ in range(2))
+    for i, bad in ((3, float("inf")), (200, float("nan")), (599, -float("inf"))):
+        t["grad"][i] = bad
+        clean["grad"][i] = 0.0
+    for x in (t, clean):
+        P.adamw_step_multi([x], step=2, seed=1, **HP)
+    bad = [3, 200, 599]
+    ok = np.setdiff1d(np.arange(600), bad)
+    assert np.isnan(host(t["param"])[bad]).all()
+    assert np.isnan(state(t)[0][bad]).sum() >= 1 and not np.isfinite(state(t)[0][bad]).any() and not np.isfinite(state(t)[1][bad]).any()
+    np.testing.assert_array_equal(host(t["param"])[ok], host(clean["param"])[ok])
+
+
+def test_same_bits_every_time_and_others_for_another_step_or_seed():
+    make8 = lambda: make(np.random.default_rng(3), 5000, 8)  # noqa: E731
+    runs = []
+    for step, seed in ((5, 1), (5, 1), (6, 1), (5, 2), (5, 1 << 32)):
+        t = make8()
+        P.adamw_step_multi([t], step=step, seed=seed, **HP)
+        runs.append(codes(t["m"]))
+    assert (runs[0] == runs[1]).all()
+    for other in runs[2:]:
+        assert 0.2 < (other != runs[0]).mean() < 0.8
