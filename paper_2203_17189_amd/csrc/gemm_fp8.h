@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
+#include <utility>
 
 namespace t5mi {
 
@@ -34,6 +35,7 @@ struct Fp8Gemm {
   int64_t ldc;
   int out_bf16, accumulate;
   float* part;  // split > 1: slice s leaves its sums at part + s * M * N
+  int big;      // tiles of 256 x 256, else of 128 x 128
   int split, slice_tiles, tiles_m, tiles_n;
 };
 
@@ -51,17 +53,7 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 // Row r (128 bytes) holds the logical 16-byte piece c at place c ^ swz(r).
 __device__ __forceinline__ int fp8_swz(int row) { return (row ^ (row >> 3)) & 7; }
 
-// Piece c (lanes 0 .. 31) or c + 1 (32 .. 63) of row base + lane % 32.  Which values of k a lane half holds is the same for
-// both operands, and a row's scale is the same for all of them.
-__device__ __forceinline__ i32x4 fp8_piece(const char* tile, int base, int c, int lane) {
-  const int row = base + (lane & 31);
-  return *reinterpret_cast<const i32x4*>(tile + row * 128 + (((c + (lane >> 5)) ^ fp8_swz(row)) << 4));
-}
-// 32 values of k for k-step kk (64 values) of a tile.
-__device__ __forceinline__ i32x8 fp8_frag(const char* tile, int base, int kk, int lane) {
-  const i32x4 lo = fp8_piece(tile, base, kk * 4, lane), hi = fp8_piece(tile, base, kk * 4 + 2, lane);
-  return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-}
+typedef __attribute__((address_space(3))) const i32x4 lds_i32x4;
 
 // Eight codes as bfloat16, times 2^(byte - 127).
 template <int T>
@@ -103,41 +95,96 @@ __device__ __forceinline__ void fp8_place(const Fp8Gemm& g, int id, int& tm, int
   tn = t / h;
 }
 
-// F32: float32 C.
-template <int BM, int BN, int WM, int WN, int TA, int TB, bool F32>
+// Calls f(integral_constant<int, U>) for U = 0 .. N - 1.
+template <typename F, int... U>
+__device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, U...>) { (f(std::integral_constant<int, U>{}), ...); }
+
+// A wavefront's results to memory by way of its part of LDS, 32 rows at a time (rows m .. m + 32 MJ, columns n .. n + 32 NI;
+// of these the ones from m_own and n_own on and inside M x N).
+template <int NI> constexpr int fp8_store_bytes = 32 * (NI * 32 * 4 + 16);
+template <int NI, int MJ, typename T>
+__device__ __forceinline__ void fp8_store_tile(f32x16 (&acc)[NI][MJ], char* lds, T* C, int64_t ld, int m, int n, int m_own, int n_own,
+                                               int M, int N, bool add) {
+  constexpr int COLS = NI * 32, PITCH = COLS * (int)sizeof(T) + 16, EPV = 16 / sizeof(T), LPR = COLS / EPV;  // lanes of a row
+  const int lane = threadIdx.x & 63;
+  const bool vec = ((uintptr_t)(C + n) & 15) == 0 && (ld * (int64_t)sizeof(T)) % 16 == 0 && n >= n_own && n + COLS <= N;
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) {
+    char* to = lds + (lane & 31) * PITCH + (lane >> 5) * 4 * (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float a = acc[i][j][q * 4], b = acc[i][j][q * 4 + 1], c = acc[i][j][q * 4 + 2], d = acc[i][j][q * 4 + 3];
+        char* at = to + (i * 32 + q * 8) * (int)sizeof(T);
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(at) = u32x2{pack_bf16x2(a, b), pack_bf16x2(c, d)};
+        else *reinterpret_cast<f32x4*>(at) = f32x4{a, b, c, d};
+      }
+    const int mj = m + j * 32;
+    if (vec) {
+#pragma unroll
+      for (int k = 0; k < 32 * LPR / 64; ++k) {
+        const int row = (k * 64 + lane) / LPR, col = (lane % LPR) * EPV;
+        u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * PITCH + col * (int)sizeof(T));
+        if (mj + row < m_own || mj + row >= M) continue;
+        T* p = C + (int64_t)(mj + row) * ld + n + col;
+        if constexpr (sizeof(T) == 4)
+          if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + *reinterpret_cast<const f32x4*>(p));
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+      }
+    } else {
+      for (int row = 0; row < 32; ++row) {
+        if (mj + row < m_own || mj + row >= M) continue;
+        for (int col = lane; col < COLS; col += 64) {
+          if (n + col < n_own || n + col >= N) continue;
+          const T v = *reinterpret_cast<const T*>(lds + row * PITCH + col * (int)sizeof(T));
+          T* p = C + (int64_t)(mj + row) * ld + n + col;
+          if constexpr (sizeof(T) == 4) *p = add ? *p + v : v;
+          else *p = v;
+        }
+      }
+    }
+  }
+}
+
+// F32: float32 C.  AST: stages of A in LDS (of B: two).
+template <int BM, int BN, int WM, int WN, int TA, int TB, bool F32, int AST>
 __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
   constexpr int NW = WM * WN, MJ = BM / WM / 32, NI = BN / WN / 32;
-  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
+  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, B_AT = AST * A_BYTES;
   constexpr int A_DMA = BM / 8 / NW, B_DMA = BN / 8 / NW;
+  constexpr int KS = F32 ? 4 : 2;          // k-steps of a tile
+  constexpr int UN = AST == 3 ? 12 : 4;    // tiles of a turn: whole rounds of the stages, and of the words of scales
+  constexpr int WORDS = UN / 4;            // words of scales a lane holds for a turn, of each row
   extern __shared__ __align__(1024) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WM, wn = wave / WM;
   int tm, tn, ks;
   fp8_place(g, blockIdx.x, tm, tn, ks);
-  const int m0 = tm * BM, n0 = tn * BN;
+  // Tiles of 256 lie wholly in the matrices (M, N >= 256): the last one of a row or column begins early, and stores what is
+  // its own.  Rows are then a constant distance apart and the DMAs' row steps need no vector registers.
+  constexpr bool FIT = BM == 256;
+  const int m_own = tm * BM, n_own = tn * BN;
+  const int m0 = FIT ? min(m_own, g.M - BM) : m_own, n0 = FIT ? min(n_own, g.N - BN) : n_own;
   const int nk = (g.K + 127) >> 7, whole = g.K >> 7;
   const int t0 = ks * g.slice_tiles, t1 = min(t0 + g.slice_tiles, nk), tw = min(t1, whole);
 
   const uint8_t* pa = g.A + (int64_t)m0 * g.lda;
   const uint8_t* pb = g.B + (int64_t)n0 * g.ldb;
-  uint32_t a_off[A_DMA], b_off[B_DMA];
+  // DMA d of a wavefront fetches rows (wave + d * NW) * 8 + lane / 8.  FIT: from the first one's, d * NW * 8 rows on, and
+  // where that changes the swizzle (by 4, for NW == 4 and odd d) from the other half of the row.
+  static_assert(!FIT || NW == 4, "row steps");
+  auto dma_off = [&](int d, int64_t ld, int rows) __attribute__((always_inline)) {
+    const int row = (wave + d * NW) * 8 + (lane >> 3);
+    return (uint32_t)(FIT ? row : min(row, rows - 1)) * (uint32_t)ld + (((lane & 7) ^ fp8_swz(row)) << 4);
+  };
+  constexpr int A_OFF = FIT ? 2 : A_DMA, B_OFF = FIT ? 2 : B_DMA;
+  uint32_t a_off[A_OFF], b_off[B_OFF];
 #pragma unroll
-  for (int i = 0; i < A_DMA; ++i) {
-    const int row = (wave + i * NW) * 8 + (lane >> 3);
-    a_off[i] = (uint32_t)min(row, g.M - 1 - m0) * (uint32_t)g.lda + (((lane & 7) ^ fp8_swz(row)) << 4);
-  }
+  for (int d = 0; d < A_OFF; ++d) a_off[d] = dma_off(d, g.lda, g.M - m0);
 #pragma unroll
-  for (int i = 0; i < B_DMA; ++i) {
-    const int row = (wave + i * NW) * 8 + (lane >> 3);
-    b_off[i] = (uint32_t)min(row, g.N - 1 - n0) * (uint32_t)g.ldb + (((lane & 7) ^ fp8_swz(row)) << 4);
-  }
-  const uint8_t *ra[MJ], *rb[NI];
-#pragma unroll
-  for (int j = 0; j < MJ; ++j)
-    ra[j] = g.sa + (int64_t)(min(m0 + wm * (BM / WM) + j * 32 + (lane & 31), g.M - 1) >> g.sha) * g.lsa;
-#pragma unroll
-  for (int i = 0; i < NI; ++i)
-    rb[i] = g.sb + (int64_t)(min(n0 + wn * (BN / WN) + i * 32 + (lane & 31), g.N - 1) >> g.shb) * g.lsb;
+  for (int d = 0; d < B_OFF; ++d) b_off[d] = dma_off(d, g.ldb, g.N - n0);
+  const uint32_t a_step = (uint32_t)g.lda * (NW * 16), b_step = (uint32_t)g.ldb * (NW * 16);  // two DMAs' rows
 
   f32x16 acc[NI][MJ];
 #pragma unroll
@@ -146,80 +193,181 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
     for (int j = 0; j < MJ; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  int xa[MJ], xb[NI];
+
+  // Scales: the words of the current turn, and of the next one on their way.
+  int xa[WORDS][MJ], xb[WORDS][NI], ya[WORDS][MJ], yb[WORDS][NI];
   auto load_scales = [&](int t) __attribute__((always_inline)) {
+    const uint8_t *sa = g.sa + (int64_t)(m0 >> g.sha) * g.lsa, *sb = g.sb + (int64_t)(n0 >> g.shb) * g.lsb;
+    int row = lane & 31;
+    asm volatile("" : "+v"(row));  // addresses are formed here: kept over the loop they would take registers it needs
 #pragma unroll
-    for (int j = 0; j < MJ; ++j) xa[j] = *reinterpret_cast<const int*>(ra[j] + (t & ~3));
+    for (int j = 0; j < MJ; ++j) {
+      const uint32_t off = (uint32_t)((min(m0 + wm * (BM / WM) + j * 32 + row, g.M - 1) >> g.sha) - (m0 >> g.sha)) * (uint32_t)g.lsa;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) xb[i] = *reinterpret_cast<const int*>(rb[i] + (t & ~3));
-  };
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
-  auto dma = [&](int t, int st) __attribute__((always_inline)) {
-    const uint8_t *qa = pa + (int64_t)t * 128, *qb = pb + (int64_t)t * 128;
-#pragma unroll
-    for (int i = 0; i < A_DMA; ++i) dma_1k(lds0 + st * STAGE + (wave + i * NW) * 1024, qa, a_off[i]);
-#pragma unroll
-    for (int i = 0; i < B_DMA; ++i) dma_1k(lds0 + st * STAGE + A_BYTES + (wave + i * NW) * 1024, qb, b_off[i]);
-  };
-  auto compute = [&](int st, auto op_tag) __attribute__((always_inline)) {
-    constexpr int OP = decltype(op_tag)::value;
-    const char *sa = smem + st * STAGE, *sb = sa + A_BYTES;
-    if constexpr (F32) {
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        i32x4 ca[MJ], cb[NI];
-#pragma unroll
-        for (int j = 0; j < MJ; ++j) ca[j] = fp8_piece(sa, wm * (BM / WM) + j * 32, kk * 2, lane);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) cb[i] = fp8_piece(sb, wn * (BN / WN) + i * 32, kk * 2, lane);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          bf16x8 fa[MJ], fb[NI];
-#pragma unroll
-          for (int j = 0; j < MJ; ++j) fa[j] = widen8<TA>(ca[j][h * 2], ca[j][h * 2 + 1], scale_operand<OP>(xa[j]));
-#pragma unroll
-          for (int i = 0; i < NI; ++i) fb[i] = widen8<TB>(cb[i][h * 2], cb[i][h * 2 + 1], scale_operand<OP>(xb[i]));
-#pragma unroll
-          for (int i = 0; i < NI; ++i)
-#pragma unroll
-            for (int j = 0; j < MJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i], fa[j], acc[i][j], 0, 0, 0);
-        }
-      }
-      return;
+      for (int w = 0; w < WORDS; ++w) ya[w][j] = *reinterpret_cast<const int*>(sa + min(t + 4 * w, (nk - 1) & ~3) + off);
     }
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      i32x8 fa[MJ], fb[NI];
+    for (int i = 0; i < NI; ++i) {
+      const uint32_t off = (uint32_t)((min(n0 + wn * (BN / WN) + i * 32 + row, g.N - 1) >> g.shb) - (n0 >> g.shb)) * (uint32_t)g.lsb;
 #pragma unroll
-      for (int j = 0; j < MJ; ++j) fa[j] = fp8_frag(sa, wm * (BM / WM) + j * 32, kk, lane);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) fb[i] = fp8_frag(sb, wn * (BN / WN) + i * 32, kk, lane);
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < MJ; ++j) acc[i][j] = fp8_mfma<TA, TB, OP>(fb[i], fa[j], acc[i][j], xb[i], xa[j]);
+      for (int w = 0; w < WORDS; ++w) yb[w][i] = *reinterpret_cast<const int*>(sb + min(t + 4 * w, (nk - 1) & ~3) + off);
     }
   };
-  auto compute_at = [&](int t, int st) __attribute__((always_inline)) {
-    switch (t & 3) {
-      case 0: compute(st, std::integral_constant<int, 0>{}); break;
-      case 1: compute(st, std::integral_constant<int, 1>{}); break;
-      case 2: compute(st, std::integral_constant<int, 2>{}); break;
-      default: compute(st, std::integral_constant<int, 3>{}); break;
+  // The compiler counts its own loads only and would wait for every DMA behind them: made to wait where none is in flight.
+  auto settle_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+#pragma unroll
+      for (int j = 0; j < MJ; ++j) asm volatile("" : "+v"(ya[w][j]));
+#pragma unroll
+      for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(yb[w][i]));
+    }
+  };
+  auto next_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+#pragma unroll
+      for (int j = 0; j < MJ; ++j) xa[w][j] = ya[w][j];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) xb[w][i] = yb[w][i];
     }
   };
 
-  if (t0 < tw) dma(t0, 0);
-  for (int t = t0; t < tw; ++t) {
-    const int st = (t - t0) & 1;
-    if (t + 1 < tw) dma(t + 1, st ^ 1);
-    if ((t & 3) == 0) load_scales(t);
-    if (t + 1 < tw) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(A_DMA + B_DMA) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    compute_at(t, st);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+  auto dma_a = [&](int t, int st, int d0, int d1) __attribute__((always_inline)) {
+    const uint8_t* q = pa + (int64_t)min(t, tw - 1) * 128;
+#pragma unroll
+    for (int d = 0; d < A_DMA; ++d)
+      if (d >= d0 && d < d1)
+        dma_1k(lds0 + st * A_BYTES + (wave + d * NW) * 1024, FIT ? q + (uint64_t)a_step * (d / 2) : q, a_off[FIT ? d % 2 : d]);
+  };
+  auto dma_b = [&](int t, int st, int d0, int d1) __attribute__((always_inline)) {
+    const uint8_t* q = pb + (int64_t)min(t, tw - 1) * 128;
+#pragma unroll
+    for (int d = 0; d < B_DMA; ++d)
+      if (d >= d0 && d < d1)
+        dma_1k(lds0 + B_AT + st * B_BYTES + (wave + d * NW) * 1024, FIT ? q + (uint64_t)b_step * (d / 2) : q, b_off[FIT ? d % 2 : d]);
+  };
+
+  // Operands of a k-step, in two sets: codes (32 bytes a lane for the code instructions, 16 to be widened).
+  typedef std::conditional_t<F32, i32x4, i32x8> Frag;
+  Frag fa[2][MJ], fb[2][NI];
+  // Lane l of a fragment has row l % 32 of 32 rows, and of each 32 bytes of k the half l / 32: both operands alike, and a row's
+  // scale is the same for all of them.  The 16-byte piece c (even, plus the half) of rows 32 j ..: the swizzle is the lane's
+  // own, but for 4 (j odd), so that all addresses are one lane's with two bits turned and a constant added.
+  const uint32_t lane_at = (uint32_t)(lane & 31) * 128 + (((lane >> 5) ^ fp8_swz(lane & 31)) << 4);
+  const uint32_t a_lane = lds0 + wm * (BM / WM) * 128 + lane_at, b_lane = lds0 + B_AT + wn * (BN / WN) * 128 + lane_at;
+  static_assert((BM / WM) % 64 == 0 && (BN / WN) % 64 == 0, "swizzle of a wavefront's first row");
+  auto read = [&](uint32_t base, int j, int kk) __attribute__((always_inline)) {
+    auto piece = [&](int c) __attribute__((always_inline)) {
+      return *(lds_i32x4*)(uintptr_t)((base ^ (uint32_t)((c ^ ((j & 1) << 2)) << 4)) + j * 4096);
+    };
+    if constexpr (F32) return piece(kk * 2);
+    else {
+      const i32x4 lo = piece(kk * 4), hi = piece(kk * 4 + 2);
+      return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    }
+  };
+  auto first_reads = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < MJ; ++j) fa[0][j] = read(a_lane, j, 0);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) fb[0][i] = read(b_lane, i, 0);
+  };
+
+  // One k-step from set CUR, block U of the turn, in NI groups of matrix instructions.  Group i also issues its share of
+  // DMA (dma(i)) and reads its share of the next k-step's operands (A stage sa, B stage sb, k-step kk), in the order in
+  // which that step uses them, all before the last group, whose matrix instructions cover the reads' latency.
+  auto kstep = [&](auto cur_tag, auto u_tag, int sa, int sb, int kk, auto&& dma) __attribute__((always_inline)) {
+    constexpr int CUR = decltype(cur_tag)::value, U = decltype(u_tag)::value, OP = U & 3, W = U / 4;
+    constexpr int NLD = MJ + NI, GROUPS = NI > 1 ? NI - 1 : 1;
+    uint32_t la = a_lane, lb = b_lane;
+    asm volatile("" : "+v"(la), "+v"(lb));  // addresses are formed in the step that uses them, not kept for the whole loop
+    la += sa * A_BYTES;
+    lb += sb * B_BYTES;
+    auto reads = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+      for (int q = 0; q < NLD; ++q) {
+        if (q * GROUPS / NLD != i) continue;
+        if (q == 0) fb[CUR ^ 1][0] = read(lb, 0, kk);
+        else if (q <= MJ) fa[CUR ^ 1][q - 1] = read(la, q - 1, kk);
+        else fb[CUR ^ 1][q - MJ] = read(lb, q - MJ, kk);
+      }
+    };
+    if constexpr (F32) {
+      bf16x8 wa[2][MJ];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < MJ; ++j) wa[h][j] = widen8<TA>(fa[CUR][j][h * 2], fa[CUR][j][h * 2 + 1], scale_operand<OP>(xa[W][j]));
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        dma(i);
+        reads(i);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8 wb = widen8<TB>(fb[CUR][i][h * 2], fb[CUR][i][h * 2 + 1], scale_operand<OP>(xb[W][i]));
+#pragma unroll
+          for (int j = 0; j < MJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb, wa[h][j], acc[i][j], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        dma(i);
+        reads(i);
+#pragma unroll
+        for (int j = 0; j < MJ; ++j) acc[i][j] = fp8_mfma<TA, TB, OP>(fb[CUR][i], fa[CUR][j], acc[i][j], xb[W][i], xa[W][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  typedef std::integral_constant<int, 0> Zero;
+  typedef std::integral_constant<int, 1> One;
+  auto none = [](int) __attribute__((always_inline)) {};
+
+  if (t0 < tw) {
+    load_scales(t0);
+    dma_a(t0, 0, 0, A_DMA);
+    dma_b(t0, 0, 0, B_DMA);
+    settle_scales();
+    next_scales();
+    dma_a(t0 + 1, 1, 0, A_DMA);
+    dma_b(t0 + 1, 1, 0, B_DMA);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(A_DMA + B_DMA) : "memory");
+    first_reads();
+    // Tile t in A stage t % AST and B stage t % 2 (t from t0 on).  The barrier before its last k-step: this wavefront's reads
+    // of the tile are done and tile t + 1 has landed but for nothing; then the stages of tile t may be filled again.
+    // AST == 3: B of tile t + 2 in the last k-step, A of tile t + 2 in the first one (its stage was tile t - 1's).
+    // AST == 2: both in the last one.  In the last tile of a turn nothing younger than tile t + 1 is in flight at the barrier,
+    // and the next turn's scales arrive there.
+    for (int t = t0; t < tw; t += UN) {
+      const bool more = t + UN < tw;
+      unrolled([&](auto u_tag) __attribute__((always_inline)) {
+        constexpr int U = decltype(u_tag)::value, SA = U % AST, SB = U % 2, SA1 = (U + 1) % AST, SA2 = (U + 2) % AST;
+        constexpr bool LAST = U == UN - 1, EARLY_A = AST == 3 && !LAST;
+        if (t + U >= tw) return;
+        if (U == 0 && more) load_scales(t + UN);
+        kstep(Zero{}, u_tag, SA, SB, 1, [&](int i) __attribute__((always_inline)) {
+          if constexpr (EARLY_A) dma_a(t + U + 2, SA2, i * A_DMA / NI, (i + 1) * A_DMA / NI);
+        });
+        if constexpr (KS == 4) {
+          kstep(One{}, u_tag, SA, SB, 2, none);
+          kstep(Zero{}, u_tag, SA, SB, 3, none);
+        }
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(EARLY_A ? A_DMA : 0) : "memory");
+        if (LAST && more) settle_scales();
+        kstep(One{}, u_tag, SA1, SB ^ 1, 0, [&](int i) __attribute__((always_inline)) {
+          dma_b(t + U + 2, SB, i * B_DMA / NI, (i + 1) * B_DMA / NI);
+          if constexpr (!EARLY_A) dma_a(t + U + 2, SA2, i * A_DMA / NI, (i + 1) * A_DMA / NI);
+        });
+      }, std::make_integer_sequence<int, UN>{});
+      if (more) next_scales();
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what was requested past the end
   }
   if (t1 > tw) {  // the last tile of K, through registers: zeros past its end
+    __syncthreads();
     const int left = g.K - whole * 128;
     const uint8_t *qa = pa + (int64_t)whole * 128, *qb = pb + (int64_t)whole * 128;
     auto piece = [&](const uint8_t* base, uint32_t off, int row) __attribute__((always_inline)) {
@@ -235,56 +383,45 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
     };
 #pragma unroll
     for (int i = 0; i < A_DMA; ++i)
-      *reinterpret_cast<u32x4*>(smem + (wave + i * NW) * 1024 + lane * 16) = piece(qa, a_off[i], (wave + i * NW) * 8 + (lane >> 3));
+      *reinterpret_cast<u32x4*>(smem + (wave + i * NW) * 1024 + lane * 16) = piece(qa, dma_off(i, g.lda, g.M - m0), (wave + i * NW) * 8 + (lane >> 3));
 #pragma unroll
     for (int i = 0; i < B_DMA; ++i)
-      *reinterpret_cast<u32x4*>(smem + A_BYTES + (wave + i * NW) * 1024 + lane * 16) = piece(qb, b_off[i], (wave + i * NW) * 8 + (lane >> 3));
-    load_scales(whole);
+      *reinterpret_cast<u32x4*>(smem + B_AT + (wave + i * NW) * 1024 + lane * 16) = piece(qb, dma_off(i, g.ldb, g.N - n0), (wave + i * NW) * 8 + (lane >> 3));
+    load_scales(whole & ~3);
+    const int down = (whole & 3) * 8;  // the block's byte goes to the bottom of its word
+#pragma unroll
+    for (int j = 0; j < MJ; ++j) xa[0][j] = (int)((uint32_t)ya[0][j] >> down);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) xb[0][i] = (int)((uint32_t)yb[0][i] >> down);
     __syncthreads();
-    compute_at(whole, 0);
+    first_reads();
+    kstep(Zero{}, Zero{}, 0, 0, 1, none);
+    if constexpr (KS == 4) {
+      kstep(One{}, Zero{}, 0, 0, 2, none);
+      kstep(Zero{}, Zero{}, 0, 0, 3, none);
+    }
+    kstep(One{}, Zero{}, 0, 0, 0, none);
   }
 
-  // acc[i][j][r] is C[n0 + .. + (r / 4) * 8 + (lane / 32) * 4 + r % 4][m0 + .. + lane % 32] transposed: a lane holds runs of
-  // four columns of one row.
+  // acc[i][j][r] is C[m0 + .. + lane % 32][n0 + .. + (r / 4) * 8 + (lane / 32) * 4 + r % 4]: a lane holds runs of four columns
+  // of one row.  Stored from there, a store touches 32 rows in pieces of 16 or 32 bytes (16384 x 2048 x 768, bfloat16: 99 us;
+  // through LDS, in whole rows of a wavefront's tile: 45).  Each wavefront has a part of LDS of its own.
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   const bool part = g.split > 1;
-  float* pf = part ? g.part + (int64_t)ks * g.M * g.N : (float*)g.C;
-  const int64_t ld = part ? g.N : g.ldc;
-  const bool bf = !F32 && !part, add = F32 && !part && g.accumulate;
-  const bool vec = (ld & 3) == 0 && ((uintptr_t)pf & (bf ? 7 : 15)) == 0;
-#pragma unroll
-  for (int j = 0; j < MJ; ++j) {
-    const int m = m0 + wm * (BM / WM) + j * 32 + (lane & 31);
-    if (m >= g.M) continue;
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int n = n0 + wn * (BN / WN) + i * 32 + q * 8 + (lane >> 5) * 4;
-        float* p = pf + (int64_t)m * ld + n;
-        bf16* pl = (bf16*)pf + (int64_t)m * ld + n;
-        f32x4 v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
-        if (vec && n + 4 <= g.N) {
-          if (bf) *reinterpret_cast<u32x2*>(pl) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-          else {
-            if (add) v += *reinterpret_cast<const f32x4*>(p);
-            *reinterpret_cast<f32x4*>(p) = v;
-          }
-        } else {
-#pragma unroll
-          for (int w = 0; w < 4; ++w)
-            if (n + w < g.N) {
-              if (bf) pl[w] = (bf16)v[w];
-              else p[w] = add ? p[w] + v[w] : v[w];
-            }
-        }
-      }
+  if (F32 || part) {
+    float* c = part ? g.part + (int64_t)ks * g.M * g.N : (float*)g.C;
+    fp8_store_tile<NI, MJ>(acc, smem + wave * fp8_store_bytes<NI>, c, part ? g.N : g.ldc, m0 + wm * (BM / WM), n0 + wn * (BN / WN),
+                           m_own, n_own, g.M, g.N, F32 && !part && g.accumulate);
+  } else {
+    fp8_store_tile<NI, MJ>(acc, smem + wave * fp8_store_bytes<NI>, (bf16*)g.C, g.ldc, m0 + wm * (BM / WM), n0 + wn * (BN / WN),
+                           m_own, n_own, g.M, g.N, false);
   }
 }
 
-template <int BM, int BN, int WM, int WN, int TA, int TB, bool F32>
+template <int BM, int BN, int WM, int WN, int TA, int TB, bool F32, int AST>
 hipError_t launch_fp8_tiles(Fp8Gemm g, hipStream_t st) {
-  auto kern = gemm_fp8_kernel<BM, BN, WM, WN, TA, TB, F32>;
-  constexpr int lds = 2 * (BM + BN) * 128;
+  auto kern = gemm_fp8_kernel<BM, BN, WM, WN, TA, TB, F32, AST>;
+  constexpr int lds = std::max((AST * BM + 2 * BN) * 128, WM * WN * fp8_store_bytes<BN / WN / 32>);
   static std::atomic<bool> attr_set{false};  // once per instantiation; setting it twice is harmless
   if (!attr_set.load(std::memory_order_relaxed)) {
     const hipError_t err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -301,7 +438,9 @@ hipError_t launch_fp8_tiles(Fp8Gemm g, hipStream_t st) {
 
 template <int TA, int TB>
 hipError_t launch_fp8_types(const Fp8Gemm& g, hipStream_t st) {
-  return g.out_bf16 ? launch_fp8_tiles<128, 128, 2, 2, TA, TB, false>(g, st) : launch_fp8_tiles<128, 128, 2, 2, TA, TB, true>(g, st);
+  const bool big = g.big;
+  if (g.out_bf16) return big ? launch_fp8_tiles<256, 256, 2, 2, TA, TB, false, 3>(g, st) : launch_fp8_tiles<128, 128, 2, 2, TA, TB, false, 3>(g, st);
+  return big ? launch_fp8_tiles<256, 256, 2, 2, TA, TB, true, 2>(g, st) : launch_fp8_tiles<128, 128, 2, 2, TA, TB, true, 2>(g, st);
 }
 
 }  // namespace

@@ -46,6 +46,7 @@ hipError_t launch_gemm_fp8(const t5_gemm_fp8_cfg& c, const void* A, const uint8_
   g.C = C; g.ldc = c.ldc; g.out_bf16 = c.c_dtype == T5_BF16; g.accumulate = c.accumulate != 0;
   g.part = (float*)ws;
   g.split = plan_split(c, &g.slice_tiles);
+  g.big = (int64_t)ceil_div(c.M, 256) * ceil_div(c.N, 256) >= 128;
   hipError_t e;
   if (c.a_dtype == T5_E4M3) e = c.b_dtype == T5_E4M3 ? launch_gemm_fp8_44(g, st) : launch_gemm_fp8_45(g, st);
   else e = c.b_dtype == T5_E4M3 ? launch_gemm_fp8_54(g, st) : launch_gemm_fp8_55(g, st);

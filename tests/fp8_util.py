@@ -55,13 +55,13 @@ def product_bound(a, b, want, out):
     instructions adds them to an accumulator: at most 64 roundings of partial sums inside it and one of the accumulator, each
     at most u times the sum of the absolute products so far; slices and an addend are a few more.  bfloat16 results: seven of
     eight consecutive products lose what is below 2^-13 of the largest, each at most that much."""
-    a, b = np.abs(a), np.abs(b)
+    a, b, want = (torch.from_numpy(np.ascontiguousarray(x)).cuda().abs() for x in (a, b, want))
     k = a.shape[1]
-    bound = (k / 16 + 64 + 20) * U * (a @ b.T) + STORE[out] * np.abs(want) + 1e-30
+    bound = (k / 16 + 64 + 20) * U * (a @ b.T) + STORE[out] * want + 1e-30
     if out == "bf16":
         for g in range(0, k, 8):
-            big = np.zeros(want.shape)
+            big = torch.zeros_like(want)
             for j in range(g, min(g + 8, k)):
-                np.maximum(big, a[:, j, None] * b[None, :, j], out=big)
+                torch.maximum(big, a[:, j, None] * b[None, :, j], out=big)
             bound += 7 * 2.0 ** -13 * big
-    return bound
+    return bound.cpu().numpy()

@@ -13,7 +13,7 @@ def check(m, n, k, ta="e4m3", tb="e4m3", ra=1, rb=1, out="f32", seed=0, accumula
     rng = np.random.default_rng(seed + m * 7 + n * 3 + k)
     a, sa, va = operand(rng, m, k, ta, ra, **kw)
     b, sb, vb = operand(rng, n, k, tb, rb, **kw)
-    want = va @ vb.T
+    want = host(torch.from_numpy(va).cuda() @ torch.from_numpy(vb).cuda().T)
     wide = torch.full((m, ldc or n), 7.0, dtype=DT[out], device="cuda")
     c = wide[:, :n]
     if accumulate:
@@ -39,6 +39,22 @@ def test_sizes(m, n, k):
     for out in ("f32", "bf16"):
         check(m, n, k, out=out)
         check(m, n, k, rb=128, out=out)
+
+
+@pytest.mark.parametrize("m,n,k", [(2816, 3000, 128), (2816, 3000, 136), (3001, 2999, 300), (4097, 2049, 1000), (2600, 3333, 1537), (3000, 2900, 1664), (2900, 3100, 2000)])
+def test_many_tiles(m, n, k):
+    """Tiles of 256 x 256, the last ones of rows and columns reaching back; every number of k-tiles in a turn of the loop."""
+    for out in ("f32", "bf16"):
+        check(m, n, k, "e5m2", "e4m3", 1, 128, out=out)
+    check(m, n, k, "e4m3", "e5m2", 128, 1, out="f32", accumulate=True, ldc=n + 3)
+    check(m, n, k, "e4m3", "e4m3", 1, 1, out="bf16", ldc=n + 5)
+
+
+@pytest.mark.parametrize("tiles", range(1, 27))
+def test_number_of_k_tiles(tiles):
+    for m, n in ((2817, 2945), (130, 200)):
+        for out in ("f32", "bf16"):
+            check(m, n, 128 * tiles - 8 * (tiles % 3), out=out)
 
 
 @pytest.mark.parametrize("ta", ["e4m3", "e5m2"])
