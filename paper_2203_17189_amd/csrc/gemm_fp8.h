@@ -34,10 +34,20 @@ struct Fp8Gemm {
   void* C;
   int64_t ldc;
   int out_bf16, accumulate;
-  float* part;  // split > 1: slice s leaves its sums at part + s * M * N
-  int big;      // tiles of 256 x 256, else of 128 x 128
-  int split, slice_tiles, tiles_m, tiles_n;
+  // Output tiles (256 x 256 if big, else 128 x 128), numbered 0 .. tiles_m * tiles_n.  The first `shared` of them, in units of
+  // four k-tiles, are dealt out evenly to `workers` workgroups, in order; each of the others has a workgroup of its own.
+  int big, tiles_m, tiles_n, shared, workers;
+  float* part;  // what a worker adds up of a tile that others have parts of, a tile of float32: at place worker + tile
 };
+
+// Units of a tile; the worker that has unit u of the shared tiles; its first unit.
+__host__ __device__ inline int fp8_units(const Fp8Gemm& g) { return (g.K + 511) >> 9; }
+__host__ __device__ inline int fp8_worker(const Fp8Gemm& g, int64_t u) {
+  return (int)(((u + 1) * g.workers - 1) / ((int64_t)g.shared * fp8_units(g)));
+}
+__host__ __device__ inline int64_t fp8_first_unit(const Fp8Gemm& g, int w) {
+  return (int64_t)w * g.shared * fp8_units(g) / g.workers;
+}
 
 // One pair of types each (A's, B's number of exponent bits).
 hipError_t launch_gemm_fp8_44(const Fp8Gemm& g, hipStream_t st);
@@ -81,18 +91,17 @@ __device__ __forceinline__ f32x16 fp8_mfma(i32x8 b, i32x8 a, f32x16 c, int sb, i
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, TB == T5_E5M2, TA == T5_E5M2, OP, sb, OP, sa);
 }
 
-// Output tile and k-slice of a workgroup.  Consecutive ids go to the 8 XCDs in turn: each XCD takes a run of tiles, in
-// columns of 8 tile rows, and shares their operands through its own L2.
-__device__ __forceinline__ void fp8_place(const Fp8Gemm& g, int id, int& tm, int& tn, int& ks) {
-  const int total = g.tiles_m * g.tiles_n * g.split, per = total / 8, more = total % 8;
-  const int x = id % 8, at = id / 8;
-  int t = x * per + min(x, more) + at;
-  ks = t / (g.tiles_m * g.tiles_n);
-  t -= ks * (g.tiles_m * g.tiles_n);
-  const int grp = t / (8 * g.tiles_n), h = min(8, g.tiles_m - grp * 8);
-  t -= grp * 8 * g.tiles_n;
-  tm = grp * 8 + t % h;
+// Row and column of tile t: in columns of 8 tile rows, so that tiles that run at once share operands.
+__host__ __device__ inline void fp8_place(const Fp8Gemm& g, int t, int& tm, int& tn) {
+  const int group = t / (8 * g.tiles_n), rows = g.tiles_m - group * 8, h = rows < 8 ? rows : 8;
+  t -= group * 8 * g.tiles_n;
+  tm = group * 8 + t % h;
   tn = t / h;
+}
+// Consecutive workgroups go to the 8 XCDs in turn: each XCD takes a run of numbers, and shares their operands through its L2.
+__device__ __forceinline__ int fp8_by_xcd(int id, int total) {
+  const int x = id % 8;
+  return x * (total / 8) + min(x, total % 8) + id / 8;
 }
 
 // Calls f(integral_constant<int, U>) for U = 0 .. N - 1.
@@ -104,9 +113,8 @@ __device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, U...>
 template <int NI> constexpr int fp8_store_bytes = 32 * (NI * 32 * 4 + 16);
 template <int NI, int MJ, typename T>
 __device__ __forceinline__ void fp8_store_tile(f32x16 (&acc)[NI][MJ], char* lds, T* C, int64_t ld, int m, int n, int m_own, int n_own,
-                                               int M, int N, bool add) {
+                                               int M, int N, bool add, int lane) {
   constexpr int COLS = NI * 32, PITCH = COLS * (int)sizeof(T) + 16, EPV = 16 / sizeof(T), LPR = COLS / EPV;  // lanes of a row
-  const int lane = threadIdx.x & 63;
   const bool vec = ((uintptr_t)(C + n) & 15) == 0 && (ld * (int64_t)sizeof(T)) % 16 == 0 && n >= n_own && n + COLS <= N;
 #pragma unroll
   for (int j = 0; j < MJ; ++j) {
@@ -157,17 +165,33 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
   constexpr int UN = AST == 3 ? 12 : 4;    // tiles of a turn: whole rounds of the stages, and of the words of scales
   constexpr int WORDS = UN / 4;            // words of scales a lane holds for a turn, of each row
   extern __shared__ __align__(1024) char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nk = (g.K + 127) >> 7, whole = g.K >> 7, units = fp8_units(g);
+  const bool worker = (int)blockIdx.x < g.workers;
+  const int me = worker ? fp8_by_xcd(blockIdx.x, g.workers) : 0;
+  int64_t u = worker ? fp8_first_unit(g, me) : 0;
+  const int64_t u_end = worker ? fp8_first_unit(g, me + 1) : 0;
+  do {  // the parts of tiles that are this workgroup's
+  // (formed anew for each: what follows from them, kept over this loop, would take the registers of the inner one)
+  int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  asm volatile("" : "+v"(lane), "+s"(wave));
   const int wm = wave % WM, wn = wave / WM;
-  int tm, tn, ks;
-  fp8_place(g, blockIdx.x, tm, tn, ks);
+  int tile = g.shared + fp8_by_xcd((int)blockIdx.x - g.workers, (int)gridDim.x - g.workers), first = 0, last = units;
+  if (worker) {
+    if (u >= u_end) return;
+    tile = (int)(u / units);
+    first = (int)(u - (int64_t)tile * units);
+    last = (int)min((int64_t)units, first + (u_end - u));
+    u += last - first;
+  }
+  const int t0 = first * 4, t1 = min(last * 4, nk), tw = min(t1, whole);
+  const bool part = last - first < units;
+  int tm, tn;
+  fp8_place(g, tile, tm, tn);
   // Tiles of 256 lie wholly in the matrices (M, N >= 256): the last one of a row or column begins early, and stores what is
   // its own.  Rows are then a constant distance apart and the DMAs' row steps need no vector registers.
   constexpr bool FIT = BM == 256;
   const int m_own = tm * BM, n_own = tn * BN;
   const int m0 = FIT ? min(m_own, g.M - BM) : m_own, n0 = FIT ? min(n_own, g.N - BN) : n_own;
-  const int nk = (g.K + 127) >> 7, whole = g.K >> 7;
-  const int t0 = ks * g.slice_tiles, t1 = min(t0 + g.slice_tiles, nk), tw = min(t1, whole);
 
   const uint8_t* pa = g.A + (int64_t)m0 * g.lda;
   const uint8_t* pb = g.B + (int64_t)n0 * g.ldb;
@@ -407,19 +431,20 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
   // of one row.  Stored from there, a store touches 32 rows in pieces of 16 or 32 bytes (16384 x 2048 x 768, bfloat16: 99 us;
   // through LDS, in whole rows of a wavefront's tile: 45).  Each wavefront has a part of LDS of its own.
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  const bool part = g.split > 1;
-  if (F32 || part) {
-    float* c = part ? g.part + (int64_t)ks * g.M * g.N : (float*)g.C;
-    fp8_store_tile<NI, MJ>(acc, smem + wave * fp8_store_bytes<NI>, c, part ? g.N : g.ldc, m0 + wm * (BM / WM), n0 + wn * (BN / WN),
-                           m_own, n_own, g.M, g.N, F32 && !part && g.accumulate);
-  } else {
-    fp8_store_tile<NI, MJ>(acc, smem + wave * fp8_store_bytes<NI>, (bf16*)g.C, g.ldc, m0 + wm * (BM / WM), n0 + wn * (BN / WN),
-                           m_own, n_own, g.M, g.N, false);
-  }
+  const int mw = wm * (BM / WM), nw = wn * (BN / WN);
+  char* mine = smem + wave * fp8_store_bytes<NI>;
+  if (part)
+    fp8_store_tile<NI, MJ>(acc, mine, g.part + ((int64_t)me + tile) * (BM * BN), BN, mw, nw, 0, 0, BM, BN, false, lane);
+  else if constexpr (F32)
+    fp8_store_tile<NI, MJ>(acc, mine, (float*)g.C, g.ldc, m0 + mw, n0 + nw, m_own, n_own, g.M, g.N, g.accumulate != 0, lane);
+  else
+    fp8_store_tile<NI, MJ>(acc, mine, (bf16*)g.C, g.ldc, m0 + mw, n0 + nw, m_own, n_own, g.M, g.N, false, lane);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // LDS is free again
+  } while (worker);
 }
 
 template <int BM, int BN, int WM, int WN, int TA, int TB, bool F32, int AST>
-hipError_t launch_fp8_tiles(Fp8Gemm g, hipStream_t st) {
+hipError_t launch_fp8_tiles(const Fp8Gemm& g, hipStream_t st) {
   auto kern = gemm_fp8_kernel<BM, BN, WM, WN, TA, TB, F32, AST>;
   constexpr int lds = std::max((AST * BM + 2 * BN) * 128, WM * WN * fp8_store_bytes<BN / WN / 32>);
   static std::atomic<bool> attr_set{false};  // once per instantiation; setting it twice is harmless
@@ -428,9 +453,7 @@ hipError_t launch_fp8_tiles(Fp8Gemm g, hipStream_t st) {
     if (err != hipSuccess) return err;
     attr_set.store(true, std::memory_order_relaxed);
   }
-  g.tiles_m = ceil_div(g.M, BM);
-  g.tiles_n = ceil_div(g.N, BN);
-  const int64_t grid = (int64_t)g.tiles_m * g.tiles_n * g.split;
+  const int64_t grid = (int64_t)g.tiles_m * g.tiles_n - g.shared + g.workers;
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
   kern<<<(unsigned)grid, WM * WN * 64, lds, st>>>(g);
   return hipGetLastError();
