@@ -1116,21 +1116,26 @@ def t5_quantize_fp8(x, q_dtype="e4m3", block_rows=1, rows=True, transposed=False
 
 def _fp8_operand(q, scale, name):
     """(rows, K, bytes between rows, type, rows of a block, bytes between rows of scales) of a quantised matrix."""
-    if q.dtype not in _FP8 or scale.dtype != _E8M0:
+    ty = _FP8.get(q.dtype)
+    if ty is None or scale.dtype != _E8M0:
         raise ValueError(f"{name}: need float8_e4m3fn or float8_e5m2 codes with float8_e8m0fnu scales, got {q.dtype}, {scale.dtype}")
     n, k, ld = _check_rows(q, name)
-    sn, sk, sld = _check_rows(scale, name + "'s scale")
-    if n == 1 and ld % 16:  # one row: what is behind it is no stride
-        ld = -(-k // 16) * 16
-    if sn <= 1 and sld % 4:
-        sld = -(-sk // 4) * 4
-    if sk != -(-k // 128) or sn not in (n, -(-n // 128)):
+    sn, sk, sld = _check_rows(scale, name)
+    if sk != (k + 127) // 128 or sn != n and sn != (n + 127) // 128:
         raise ValueError(f"{name}: codes {tuple(q.shape)} have scales [{n} or {-(-n // 128)}, {-(-k // 128)}], got {tuple(scale.shape)}")
-    for t, rows, cols, step, what in ((q, n, k, 16, name), (scale, sn, sk, 4, name + "'s scale")):
-        # rows are read in whole pieces: the last one's end has to be there
-        if rows > 0 and t.untyped_storage().nbytes() - t.storage_offset() < (rows - 1) * t.stride(0) + -(-cols // step) * step:
-            raise ValueError(f"{what}: its last row ends inside a piece of {step} bytes, and its memory with it")
-    return n, k, ld, _FP8[q.dtype], 1 if sn == n else 128, sld
+    # rows are read in whole pieces: the end of the last one has to be there; one row may be of any length
+    if k % 16:
+        ld = _last_piece(q, n, k, ld, 16, name)
+    if sk % 4:
+        sld = _last_piece(scale, sn, sk, sld, 4, name + "'s scale")
+    return n, k, ld, ty, 1 if sn == n else 128, sld
+
+
+def _last_piece(t, rows, cols, ld, step, name):
+    whole = -(-cols // step) * step
+    if rows > 0 and t.untyped_storage().nbytes() - t.storage_offset() < (rows - 1) * ld + whole:
+        raise ValueError(f"{name}: its last row ends inside a piece of {step} bytes, and its memory with it")
+    return whole if rows <= 1 else ld
 
 
 def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accumulate=False, workspace=None):
@@ -1142,26 +1147,29 @@ def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accu
     dev = a.device
     if k != kb:
         raise ValueError(f"a has {k} columns, b {kb}")
-    for t, what in ((a_scale, "a's scale"), (b, "b"), (b_scale, "b's scale")):
-        if t.device != dev:
-            raise ValueError(f"{what}: on {t.device}, other arguments on {dev}")
+    if b.device != dev or a_scale.device != dev or b_scale.device != dev:
+        raise ValueError(f"a on {dev}, its scale on {a_scale.device}, b on {b.device}, its scale on {b_scale.device}")
     if out is None:
         if accumulate:
             raise ValueError("accumulate: there is no out to add to")
         out = torch.empty(m, n, dtype=out_dtype, device=dev)
-    tc = _elem_type(out, "out")
-    rows, cols, ldc = _check_rows(out, "out")
-    if (rows, cols) != (m, n) or out.device != dev:
-        raise ValueError(f"out: need [{m}, {n}] on {dev}, got {tuple(out.shape)} on {out.device}")
-    cfg = C.byref(_GemmFp8Cfg(_i32(m), _i32(n), _i32(k), lda, ldb, ldc, lsa, lsb, ta, tb, bra, brb, tc, int(bool(accumulate))))
+        ldc = n
+    else:
+        rows, cols, ldc = _check_rows(out, "out")
+        if (rows, cols) != (m, n) or out.device != dev:
+            raise ValueError(f"out: need [{m}, {n}] on {dev}, got {tuple(out.shape)} on {out.device}")
+    cfg = C.byref(_GemmFp8Cfg(_i32(m), _i32(n), _i32(k), lda, ldb, ldc, lsa, lsb, ta, tb, bra, brb, _elem_type(out, "out"),
+                              1 if accumulate else 0))
     L = lib()
-    nbytes = L.t5_gemm_fp8_workspace_bytes(cfg)
+    ws, nbytes = None, L.t5_gemm_fp8_workspace_bytes(cfg)
     if workspace is not None:
         _check_on(dev, workspace, torch.uint8, workspace.numel(), "workspace")
+        ws, nbytes = workspace.data_ptr(), workspace.numel()
     elif nbytes:
         workspace = _byte_buffer(nbytes, dev)
+        ws = workspace.data_ptr()
     _call(L.t5_gemm_fp8, "t5_gemm_fp8", dev, cfg, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
-          out.data_ptr(), None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel())
+          out.data_ptr(), ws, nbytes)
     return out
 
 

@@ -14,7 +14,7 @@ SOURCES = ["relpos.hip", "rmsnorm.hip", "gemm_simple.hip", "gemm_mfma.hip", "gem
            "gemm_mfma_resid.hip", "gemm_mfma_geglu_fwd.hip", "gemm_mfma_geglu_bwd.hip", "gemm_mfma_split.hip",
            "gemm_mfma_split_grouped.hip", "gemm_mfma_direct.hip", "gemm_f32.hip", "attn_simple.hip",
            "attn_mfma.hip", "attn_f32.hip", "adafactor.hip", "probe.hip", "embed_xent.hip", "embed_sorted.hip", "top_logits.hip", "distill.hip",
-           "quant_fp8.hip", "gemm_fp8.hip", "gemm_fp8_44.hip", "gemm_fp8_45.hip", "gemm_fp8_54.hip", "gemm_fp8_55.hip", "adamw.hip",
+           "quant_fp8.hip", "gemm_fp8.hip", "gemm_fp8_44.hip", "gemm_fp8_45.hip", "gemm_fp8_54.hip", "gemm_fp8_55.hip", "gemm_fp8_rows.hip", "adamw.hip",
            "block.hip", "stack.hip", "vocab_ops.hip", "fp8_ops.hip"]
 # -packed-fp32-ops is switched off: hand-written and compiler-made packed float32 math is avoided on
 # this target.

@@ -54,6 +54,9 @@ hipError_t launch_gemm_fp8_44(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_45(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_54(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_55(const Fp8Gemm& g, hipStream_t st);
+// M <= kFp8FewRows, without tiles (gemm_fp8_rows.hip).
+constexpr int kFp8FewRows = 64;
+hipError_t launch_gemm_fp8_rows(const Fp8Gemm& g, int ta, int tb, hipStream_t st);
 
 namespace {
 
@@ -65,23 +68,22 @@ __device__ __forceinline__ int fp8_swz(int row) { return (row ^ (row >> 3)) & 7;
 
 typedef __attribute__((address_space(3))) const i32x4 lds_i32x4;
 
-// Eight codes as bfloat16, times 2^(byte - 127).
+// Four codes, or eight, as bfloat16, times 2^(byte - 127).
 template <int T>
-__device__ __forceinline__ bf16x8 widen8(int lo, int hi, float scale) {
-  bf16x2 v[4];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int c = h ? hi : lo;
-    if constexpr (T == T5_E4M3) {
-      v[h * 2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false);
-      v[h * 2 + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true);
-    } else {
-      v[h * 2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, scale, false);
-      v[h * 2 + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, scale, true);
-    }
+__device__ __forceinline__ bf16x4 widen4(int c, float scale) {
+  bf16x2 lo, hi;
+  if constexpr (T == T5_E4M3) {
+    lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true);
+  } else {
+    lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, scale, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, scale, true);
   }
-  return bf16x8{v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
 }
+__device__ __forceinline__ bf16x8 both(bf16x4 lo, bf16x4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
+template <int T>
+__device__ __forceinline__ bf16x8 widen8(int lo, int hi, float scale) { return both(widen4<T>(lo, scale), widen4<T>(hi, scale)); }
 // The scale of block OP of a word as the conversion takes it: only the exponent counts there (0: 2^-127).
 template <int OP>
 __device__ __forceinline__ float scale_operand(int word) { return __uint_as_float((uint32_t)((word >> (8 * OP)) & 255) << 23); }
@@ -113,7 +115,7 @@ __device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, U...>
 template <int NI> constexpr int fp8_store_bytes = 32 * (NI * 32 * 4 + 16);
 template <int NI, int MJ, typename T>
 __device__ __forceinline__ void fp8_store_tile(f32x16 (&acc)[NI][MJ], char* lds, T* C, int64_t ld, int m, int n, int m_own, int n_own,
-                                               int M, int N, bool add, int lane) {
+                                               int M, int N, bool add, int lane, bool again) {
   constexpr int COLS = NI * 32, PITCH = COLS * (int)sizeof(T) + 16, EPV = 16 / sizeof(T), LPR = COLS / EPV;  // lanes of a row
   const bool vec = ((uintptr_t)(C + n) & 15) == 0 && (ld * (int64_t)sizeof(T)) % 16 == 0 && n >= n_own && n + COLS <= N;
 #pragma unroll
@@ -138,17 +140,28 @@ __device__ __forceinline__ void fp8_store_tile(f32x16 (&acc)[NI][MJ], char* lds,
         T* p = C + (int64_t)(mj + row) * ld + n + col;
         if constexpr (sizeof(T) == 4)
           if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + *reinterpret_cast<const f32x4*>(p));
-        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+        // (C is not read again here, parts are, soon: 4096 x 32128 x 768 147 us against 152, 3000 x 3000 x 1024 in parts 50 against 72)
+        if (again) *reinterpret_cast<u32x4*>(p) = v;
+        else __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
       }
     } else {
-      for (int row = 0; row < 32; ++row) {
-        if (mj + row < m_own || mj + row >= M) continue;
-        for (int col = lane; col < COLS; col += 64) {
-          if (n + col < n_own || n + col >= N) continue;
-          const T v = *reinterpret_cast<const T*>(lds + row * PITCH + col * (int)sizeof(T));
-          T* p = C + (int64_t)(mj + row) * ld + n + col;
-          if constexpr (sizeof(T) == 4) *p = add ? *p + v : v;
-          else *p = v;
+      // element by element, 64 neighbours a store
+      constexpr int AT_ONCE = 8;
+      for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
+#pragma unroll
+        for (int c = 0; c < COLS / 64; ++c) {
+          const int col = c * 64 + lane;
+          const bool on = n + col >= n_own && n + col < N;
+          T v[AT_ONCE];
+#pragma unroll
+          for (int r = 0; r < AT_ONCE; ++r) v[r] = *reinterpret_cast<const T*>(lds + (r0 + r) * PITCH + col * (int)sizeof(T));
+          T* p = C + (int64_t)(mj + r0) * ld + n + col;
+#pragma unroll
+          for (int r = 0; r < AT_ONCE; ++r)
+            if (on && mj + r0 + r >= m_own && mj + r0 + r < M) {
+              if constexpr (sizeof(T) == 4) p[r * ld] = add ? p[r * ld] + v[r] : v[r];
+              else p[r * ld] = v[r];
+            }
         }
       }
     }
@@ -161,7 +174,6 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
   constexpr int NW = WM * WN, MJ = BM / WM / 32, NI = BN / WN / 32;
   constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, B_AT = AST * A_BYTES;
   constexpr int A_DMA = BM / 8 / NW, B_DMA = BN / 8 / NW;
-  constexpr int KS = F32 ? 4 : 2;          // k-steps of a tile
   constexpr int UN = AST == 3 ? 12 : 4;    // tiles of a turn: whole rounds of the stages, and of the words of scales
   constexpr int WORDS = UN / 4;            // words of scales a lane holds for a turn, of each row
   extern __shared__ __align__(1024) char smem[];
@@ -303,6 +315,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
   // DMA (dma(i)) and reads its share of the next k-step's operands (A stage sa, B stage sb, k-step kk), in the order in
   // which that step uses them, all before the last group, whose matrix instructions cover the reads' latency.
   auto kstep = [&](auto cur_tag, auto u_tag, int sa, int sb, int kk, auto&& dma) __attribute__((always_inline)) {
+    if constexpr (!F32) {
     constexpr int CUR = decltype(cur_tag)::value, U = decltype(u_tag)::value, OP = U & 3, W = U / 4;
     constexpr int NLD = MJ + NI, GROUPS = NI > 1 ? NI - 1 : 1;
     uint32_t la = a_lane, lb = b_lane;
@@ -318,32 +331,63 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
         else fb[CUR ^ 1][q - MJ] = read(lb, q - MJ, kk);
       }
     };
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      dma(i);
+      reads(i);
+#pragma unroll
+      for (int j = 0; j < MJ; ++j) acc[i][j] = fp8_mfma<TA, TB, OP>(fb[CUR][i], fa[CUR][j], acc[i][j], xb[W][i], xa[W][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    }
+  };
+
+  // One k-step of float32 C.  Its matrix instructions wait for nothing: A's operands were widened in the step before, B's in
+  // the group before, and the codes of the step after the next one are read here (A stage sa, B stage sb, k-step kk), into
+  // the registers of this one's.  Two conversions stand behind each matrix instruction and are done while it runs (all of a
+  // step's in front of its first one: 32768 x 2048 x 5120 561 us, like this 513).  STEP: 0 .. 3 of the tile.
+  bf16x4 wa[F32 ? 2 : 1][MJ][4], wb[2][4];
+  auto widen_a = [&](int set, int j, int q, int word, auto op_tag) __attribute__((always_inline)) {
+    if constexpr (F32) wa[set][j][q] = widen4<TA>(fa[set][j][q], scale_operand<decltype(op_tag)::value>(word));
+  };
+  auto widen_b = [&](int to, int set, int i, int q, int word, auto op_tag) __attribute__((always_inline)) {
+    if constexpr (F32) wb[to][q] = widen4<TB>(fb[set][i][q], scale_operand<decltype(op_tag)::value>(word));
+  };
+  auto wide_step = [&](auto step_tag, auto u_tag, int sa, int sb, int kk, auto&& dma) __attribute__((always_inline)) {
     if constexpr (F32) {
-      bf16x8 wa[2][MJ];
+    constexpr int STEP = decltype(step_tag)::value, CUR = STEP & 1, NXT = CUR ^ 1, U = decltype(u_tag)::value;
+    constexpr int U1 = STEP == 3 ? U + 1 : U;  // the next step's block
+    typedef std::integral_constant<int, U & 3> Op;
+    typedef std::integral_constant<int, U1 & 3> Op1;
+    uint32_t la = a_lane, lb = b_lane;
+    asm volatile("" : "+v"(la), "+v"(lb));
+    la += sa * A_BYTES;
+    lb += sb * B_BYTES;
+    auto word_a = [&](int j) __attribute__((always_inline)) { return U1 < UN ? xa[U1 < UN ? U1 / 4 : 0][j] : ya[0][j]; };
+    auto word_b = [&](int i) __attribute__((always_inline)) { return U1 < UN ? xb[U1 < UN ? U1 / 4 : 0][i] : yb[0][i]; };
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      dma(i);
+      if (i < MJ) fa[CUR][i] = read(la, i, kk);
+      fb[CUR][i] = read(lb, i, kk);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < MJ; ++j) wa[h][j] = widen8<TA>(fa[CUR][j][h * 2], fa[CUR][j][h * 2 + 1], scale_operand<OP>(xa[W][j]));
+        for (int j = 0; j < MJ; ++j) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(both(wb[i & 1][h * 2], wb[i & 1][h * 2 + 1]),
+                                                               both(wa[CUR][j][h * 2], wa[CUR][j][h * 2 + 1]), acc[i][j], 0, 0, 0);
+          const int at = h * MJ + j;  // of 2 MJ places, 4 conversions of B and 4 of A in turn
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        dma(i);
-        reads(i);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const bf16x8 wb = widen8<TB>(fb[CUR][i][h * 2], fb[CUR][i][h * 2 + 1], scale_operand<OP>(xb[W][i]));
-#pragma unroll
-          for (int j = 0; j < MJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb, wa[h][j], acc[i][j], 0, 0, 0);
+          for (int q = 0; q < 4; ++q) {
+            if (q * 2 * MJ / 4 / 2 == at) {
+              if (i + 1 < NI) widen_b((i + 1) & 1, CUR, i + 1, q, xb[U / 4][i + 1 < NI ? i + 1 : 0], Op{});
+              else widen_b(0, NXT, 0, q, word_b(0), Op1{});
+            }
+            if (i < MJ && MJ + q * 2 * MJ / 4 / 2 == at) widen_a(NXT, i, q, word_a(i < MJ ? i : 0), Op1{});
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        dma(i);
-        reads(i);
-#pragma unroll
-        for (int j = 0; j < MJ; ++j) acc[i][j] = fp8_mfma<TA, TB, OP>(fb[CUR][i], fa[CUR][j], acc[i][j], xb[W][i], xa[W][j]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+    }
     }
   };
   typedef std::integral_constant<int, 0> Zero;
@@ -360,6 +404,18 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
     dma_b(t0 + 1, 1, 0, B_DMA);
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(A_DMA + B_DMA) : "memory");
     first_reads();
+    if constexpr (F32) {
+#pragma unroll
+      for (int j = 0; j < MJ; ++j) {
+        fa[1][j] = read(a_lane, j, 1);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) widen_a(0, j, q, xa[0][j], std::integral_constant<int, 0>{});
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fb[1][i] = read(b_lane, i, 1);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) widen_b(0, 0, 0, q, xb[0][0], std::integral_constant<int, 0>{});
+    }
     // Tile t in A stage t % AST and B stage t % 2 (t from t0 on).  The barrier before its last k-step: this wavefront's reads
     // of the tile are done and tile t + 1 has landed but for nothing; then the stages of tile t may be filled again.
     // AST == 3: B of tile t + 2 in the last k-step, A of tile t + 2 in the first one (its stage was tile t - 1's).
@@ -372,13 +428,23 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
         constexpr bool LAST = U == UN - 1, EARLY_A = AST == 3 && !LAST;
         if (t + U >= tw) return;
         if (U == 0 && more) load_scales(t + UN);
+        if constexpr (F32) {  // (reads are two steps ahead: the barrier stands before the third one)
+          static_assert(AST == 2, "stages");
+          wide_step(std::integral_constant<int, 0>{}, u_tag, SA, SB, 2, none);
+          wide_step(std::integral_constant<int, 1>{}, u_tag, SA, SB, 3, none);
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          if (LAST && more) settle_scales();
+          wide_step(std::integral_constant<int, 2>{}, u_tag, SA1, SB ^ 1, 0, [&](int i) __attribute__((always_inline)) {
+            dma_a(t + U + 2, SA2, i * A_DMA / NI, (i + 1) * A_DMA / NI);
+          });
+          wide_step(std::integral_constant<int, 3>{}, u_tag, SA1, SB ^ 1, 1, [&](int i) __attribute__((always_inline)) {
+            dma_b(t + U + 2, SB, i * B_DMA / NI, (i + 1) * B_DMA / NI);
+          });
+          return;
+        }
         kstep(Zero{}, u_tag, SA, SB, 1, [&](int i) __attribute__((always_inline)) {
           if constexpr (EARLY_A) dma_a(t + U + 2, SA2, i * A_DMA / NI, (i + 1) * A_DMA / NI);
         });
-        if constexpr (KS == 4) {
-          kstep(One{}, u_tag, SA, SB, 2, none);
-          kstep(Zero{}, u_tag, SA, SB, 3, none);
-        }
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(EARLY_A ? A_DMA : 0) : "memory");
         if (LAST && more) settle_scales();
         kstep(One{}, u_tag, SA1, SB ^ 1, 0, [&](int i) __attribute__((always_inline)) {
@@ -418,13 +484,33 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) xb[0][i] = (int)((uint32_t)yb[0][i] >> down);
     __syncthreads();
-    first_reads();
-    kstep(Zero{}, Zero{}, 0, 0, 1, none);
-    if constexpr (KS == 4) {
-      kstep(One{}, Zero{}, 0, 0, 2, none);
-      kstep(Zero{}, Zero{}, 0, 0, 3, none);
+    if constexpr (F32) {
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+        for (int j = 0; j < MJ; ++j) {
+          fa[0][j] = read(a_lane, j, kk);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) widen_a(0, j, q, xa[0][j], Zero{});
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          fb[0][i] = read(b_lane, i, kk);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) widen_b(0, 0, i, q, xb[0][i], Zero{});
+#pragma unroll
+          for (int j = 0; j < MJ; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(both(wb[0][h * 2], wb[0][h * 2 + 1]),
+                                                                   both(wa[0][j][h * 2], wa[0][j][h * 2 + 1]), acc[i][j], 0, 0, 0);
+        }
+      }
+    } else {
+      first_reads();
+      kstep(Zero{}, Zero{}, 0, 0, 1, none);
+      kstep(One{}, Zero{}, 0, 0, 0, none);
     }
-    kstep(One{}, Zero{}, 0, 0, 0, none);
   }
 
   // acc[i][j][r] is C[m0 + .. + lane % 32][n0 + .. + (r / 4) * 8 + (lane / 32) * 4 + r % 4]: a lane holds runs of four columns
@@ -434,11 +520,11 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
   const int mw = wm * (BM / WM), nw = wn * (BN / WN);
   char* mine = smem + wave * fp8_store_bytes<NI>;
   if (part)
-    fp8_store_tile<NI, MJ>(acc, mine, g.part + ((int64_t)me + tile) * (BM * BN), BN, mw, nw, 0, 0, BM, BN, false, lane);
+    fp8_store_tile<NI, MJ>(acc, mine, g.part + ((int64_t)me + tile) * (BM * BN), BN, mw, nw, 0, 0, BM, BN, false, lane, true);
   else if constexpr (F32)
-    fp8_store_tile<NI, MJ>(acc, mine, (float*)g.C, g.ldc, m0 + mw, n0 + nw, m_own, n_own, g.M, g.N, g.accumulate != 0, lane);
+    fp8_store_tile<NI, MJ>(acc, mine, (float*)g.C, g.ldc, m0 + mw, n0 + nw, m_own, n_own, g.M, g.N, g.accumulate != 0, lane, false);
   else
-    fp8_store_tile<NI, MJ>(acc, mine, (bf16*)g.C, g.ldc, m0 + mw, n0 + nw, m_own, n_own, g.M, g.N, false, lane);
+    fp8_store_tile<NI, MJ>(acc, mine, (bf16*)g.C, g.ldc, m0 + mw, n0 + nw, m_own, n_own, g.M, g.N, false, lane, false);
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // LDS is free again
   } while (worker);
 }

@@ -34,19 +34,49 @@ __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(Fp8Gemm g) {
   }
 }
 
+// Which tiles, and whether those of the last, partly filled round are shared out along k: whatever is estimated to be faster.
+// Estimates in us, fitted to the kernels of this file on shapes of 300 .. 32768 by 500 .. 32128 by 512 .. 32768.  A k-tile of
+// a full round (256 tiles of 256 x 256, one on each compute unit, or 512 of 128 x 128) takes the longer the more of the chip
+// is at work, as clocks follow power: `idle` where few tiles run, `busy` more in a full round.  A round has `ends` besides.
+// Sharing costs a launch and the parts' way to memory and back, 5 MB a us.  Both sides, shape and type of C:
+//   2048 x 2048 x 4096   bf16  128: 26 us, shared 36;   256: 51, shared 44        (taken: 128)
+//   4096 x 4096 x 4096   bf16  128: 73;                 256: 65                   (256)
+//   768 x 2048 x 16384   f32   128: 112, shared 65;     256: 279, shared 84       (128, shared)
+//   5120 x 2048 x 32768  bf16  128: 394, shared 372;    256: 353, shared 408      (256)
+//   5120 x 2048 x 32768  f32   128: 609, shared 565;    256: 590, shared 549      (256, shared)
+struct TileCost { double idle, busy, from, ends; };
+constexpr TileCost kTileCost[2][2] = {{{0.53, 0.55, 0.2, 2.5}, {1.1, 0.5, 0.4, 12.5}},   // bf16 C: tiles of 128, of 256
+                                      {{0.83, 0.92, 0.2, 5.0}, {2.05, 1.0, 0.5, 12.5}}};  // float32 C
 constexpr int kCus = 256;
 
+double round_cost(const TileCost& t, double fill, double nk) {
+  return nk * (t.idle + t.busy * std::max(0.0, fill - t.from) / (1.0 - t.from)) + t.ends;
+}
+
 void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
-  const int units = ceil_div(c.K, 512);
-  g->big = c.M >= 256 && c.N >= 256 && (int64_t)ceil_div(c.M, 256) * ceil_div(c.N, 256) * units >= 256;
-  const int B = g->big ? 256 : 128, slots = g->big ? kCus : 2 * kCus;
-  g->tiles_m = ceil_div(c.M, B);
-  g->tiles_n = ceil_div(c.N, B);
-  const int64_t tiles = (int64_t)g->tiles_m * g->tiles_n, rest = tiles % slots;
   g->shared = g->workers = 0;
-  if (rest > 0 && rest <= slots * 7 / 8 && units > 1) {
-    g->shared = (int)rest;
-    g->workers = (int)std::min<int64_t>(slots, rest * units);
+  if (c.M <= kFp8FewRows) return;
+  const int units = ceil_div(c.K, 512);
+  const double nk = c.K / 128.0;
+  double best = -1.0;
+  for (int big = 0; big < 2; ++big) {
+    if (big && (c.M < 256 || c.N < 256)) break;
+    const int B = big ? 256 : 128, slots = big ? kCus : 2 * kCus, tm = ceil_div(c.M, B), tn = ceil_div(c.N, B);
+    const TileCost& t = kTileCost[c.c_dtype == T5_F32][big];
+    const int64_t tiles = (int64_t)tm * tn, rest = tiles % slots;
+    const double full = (double)(tiles / slots) * round_cost(t, 1.0, nk), fill = (double)rest / slots;
+    const double alone = full + (rest ? round_cost(t, fill, nk) : 0.0);
+    const int64_t workers = std::min<int64_t>(slots, rest * units);
+    const double run = (double)workers / slots;
+    const double shared = full + round_cost(t, run, nk * rest / std::max<int64_t>(workers, 1)) + 6.0 +
+                          (double)(workers + rest) * B * B * 8 / 5e6;
+    const bool share = rest > 0 && workers > rest && shared < alone;
+    const double cost = share ? shared : alone;
+    if (best >= 0.0 && cost >= best) continue;
+    best = cost;
+    g->big = big; g->tiles_m = tm; g->tiles_n = tn;
+    g->shared = share ? (int)rest : 0;
+    g->workers = share ? (int)workers : 0;
   }
 }
 
@@ -55,8 +85,9 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
 size_t gemm_fp8_ws_bytes(const t5_gemm_fp8_cfg& c) {
   Fp8Gemm g;
   plan(c, &g);
+  if (g.workers <= g.shared) return 0;
   const size_t B = g.big ? 256 : 128;
-  return g.workers > g.shared ? ((size_t)g.workers + g.shared) * B * B * 4 : 0;
+  return ((size_t)g.workers + g.shared) * B * B * 4;
 }
 
 hipError_t launch_gemm_fp8(const t5_gemm_fp8_cfg& c, const void* A, const uint8_t* sa, const void* B, const uint8_t* sb, void* C,
@@ -69,6 +100,7 @@ hipError_t launch_gemm_fp8(const t5_gemm_fp8_cfg& c, const void* A, const uint8_
   g.M = c.M; g.N = c.N; g.K = c.K;
   g.C = C; g.ldc = c.ldc; g.out_bf16 = c.c_dtype == T5_BF16; g.accumulate = c.accumulate != 0;
   g.part = (float*)ws;
+  if (c.M <= kFp8FewRows) return launch_gemm_fp8_rows(g, c.a_dtype, c.b_dtype, st);
   hipError_t e;
   if (c.a_dtype == T5_E4M3) e = c.b_dtype == T5_E4M3 ? launch_gemm_fp8_44(g, st) : launch_gemm_fp8_45(g, st);
   else e = c.b_dtype == T5_E4M3 ? launch_gemm_fp8_54(g, st) : launch_gemm_fp8_55(g, st);

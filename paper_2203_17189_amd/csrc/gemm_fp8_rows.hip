@@ -1,0 +1,158 @@
+// Product of a few quantised rows (single tokens, short batches) with a quantised matrix.
+//
+// Bound by reading B once.  A workgroup has 16 rows of B; its wavefronts take the blocks of 128 k in turn, straight from
+// memory into the operands of a matrix instruction: no LDS, no barrier before the end, and every load of a wavefront's
+// blocks is under way at once.  The wavefronts' sums meet in LDS, in order.  A is read again by each workgroup, from L2.
+// The instructions are the ones of gemm_fp8.h, 16 x 16 wide: codes with scales for bfloat16 C, widened codes for float32.
+#include "gemm_fp8.h"
+
+namespace t5mi {
+namespace {
+
+// 32 bytes from p; of these the ones before `left` (16-byte pieces that begin there are in memory as wholes), zeros behind.
+__device__ __forceinline__ i32x8 load32(const uint8_t* p, int left) {
+  i32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    i32x4 q = {0, 0, 0, 0};
+    if (left > h * 16) q = *reinterpret_cast<const i32x4*>(p + h * 16);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int keep = left - h * 16 - w * 4;
+      v[h * 4 + w] = keep >= 4 ? q[w] : keep <= 0 ? 0 : (int)((uint32_t)q[w] & ((1u << (keep * 8)) - 1u));
+    }
+  }
+  return v;
+}
+__device__ __forceinline__ i32x8 load32(const uint8_t* p) {
+  const i32x4 a = *reinterpret_cast<const i32x4*>(p), b = *reinterpret_cast<const i32x4*>(p + 16);
+  return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+template <int MT, int NT> struct Block {
+  i32x8 b[NT], a[MT];
+  int sb[NT], sa[MT];
+};
+
+// MT, NT: tiles of 16 rows of A and of B.  NW wavefronts, IN blocks each under way at a time.
+template <int TA, int TB, bool F32, int MT, int NT, int NW, int IN>
+__global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
+  __shared__ f32x4 sums[NW][NT * MT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = blockIdx.x * (16 * NT), nk = (g.K + 127) >> 7;
+  const int k0 = (lane >> 4) * 32;
+  const uint8_t *pa[MT], *qa[MT], *pb[NT], *qb[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int rb = min(n0 + i * 16 + (lane & 15), g.N - 1);
+    pb[i] = g.B + (int64_t)rb * g.ldb + k0;
+    qb[i] = g.sb + (int64_t)(rb >> g.shb) * g.lsb;
+  }
+#pragma unroll
+  for (int j = 0; j < MT; ++j) {
+    const int ra = min(j * 16 + (lane & 15), g.M - 1);
+    pa[j] = g.A + (int64_t)ra * g.lda + k0;
+    qa[j] = g.sa + (int64_t)(ra >> g.sha) * g.lsa;
+  }
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto load = [&](Block<MT, NT>& x, int t) __attribute__((always_inline)) {
+    const int left = g.K - t * 128 - k0;
+    const bool whole = (t + 1) * 128 <= g.K;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      x.b[i] = whole ? load32(pb[i] + (int64_t)t * 128) : load32(pb[i] + (int64_t)t * 128, left);
+      x.sb[i] = qb[i][t];
+    }
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      x.a[j] = whole ? load32(pa[j] + (int64_t)t * 128) : load32(pa[j] + (int64_t)t * 128, left);
+      x.sa[j] = qa[j][t];
+    }
+  };
+  auto add = [&](const Block<MT, NT>& x) __attribute__((always_inline)) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        bf16x8 wb[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) wb[i] = widen8<TB>(x.b[i][s * 2], x.b[i][s * 2 + 1], scale_operand<0>(x.sb[i]));
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          const bf16x8 wa = widen8<TA>(x.a[j][s * 2], x.a[j][s * 2 + 1], scale_operand<0>(x.sa[j]));
+#pragma unroll
+          for (int i = 0; i < NT; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[i], wa, acc[i][j], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x.b[i], x.a[j], acc[i][j], TB == T5_E5M2, TA == T5_E5M2, 0, x.sb[i], 0, x.sa[j]);
+    }
+  };
+  int t = wave;
+  for (; t + (IN - 1) * NW < nk; t += IN * NW) {
+    Block<MT, NT> x[IN];
+#pragma unroll
+    for (int i = 0; i < IN; ++i) load(x[i], t + i * NW);
+#pragma unroll
+    for (int i = 0; i < IN; ++i) add(x[i]);
+  }
+  for (; t < nk; t += NW) {
+    Block<MT, NT> x;
+    load(x, t);
+    add(x);
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) sums[wave][i * MT + j][lane] = acc[i][j];
+  __syncthreads();
+  for (int at = threadIdx.x; at < NT * MT * 64; at += NW * 64) {
+    const int ij = at >> 6, l = at & 63;
+    f32x4 s = sums[0][ij][l];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) s += sums[w][ij][l];
+    const int m = ij % MT * 16 + (l & 15), n = n0 + ij / MT * 16 + (l >> 4) * 4;  // a lane holds four columns of a row
+    if (m >= g.M) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (n + i >= g.N) continue;
+      if constexpr (F32) {
+        float* p = (float*)g.C + (int64_t)m * g.ldc + n + i;
+        *p = g.accumulate ? *p + s[i] : s[i];
+      } else {
+        ((bf16*)g.C)[(int64_t)m * g.ldc + n + i] = (bf16)s[i];
+      }
+    }
+  }
+}
+
+template <int TA, int TB, bool F32>
+hipError_t launch(const Fp8Gemm& g, hipStream_t st) {
+  const unsigned grid = (unsigned)ceil_div(g.N, 16), half = (grid + 1) / 2;
+  if (g.M <= 16) {
+    if (g.K > 1024) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 8, 4><<<grid, 512, 0, st>>>(g);
+    else gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 4, 2><<<grid, 256, 0, st>>>(g);
+  } else if (g.M <= 32) {
+    gemm_fp8_rows_kernel<TA, TB, F32, 2, 2, 8, 2><<<half, 512, 0, st>>>(g);
+  } else {
+    gemm_fp8_rows_kernel<TA, TB, F32, 4, 2, 8, 1><<<half, 512, 0, st>>>(g);
+  }
+  return hipGetLastError();
+}
+template <int TA, int TB>
+hipError_t launch(const Fp8Gemm& g, hipStream_t st) { return g.out_bf16 ? launch<TA, TB, false>(g, st) : launch<TA, TB, true>(g, st); }
+
+}  // namespace
+
+hipError_t launch_gemm_fp8_rows(const Fp8Gemm& g, int ta, int tb, hipStream_t st) {
+  if (ta == T5_E4M3) return tb == T5_E4M3 ? launch<T5_E4M3, T5_E4M3>(g, st) : launch<T5_E4M3, T5_E5M2>(g, st);
+  return tb == T5_E4M3 ? launch<T5_E5M2, T5_E4M3>(g, st) : launch<T5_E5M2, T5_E5M2>(g, st);
+}
+
+}  // namespace t5mi
