@@ -5,6 +5,7 @@ from __future__ import annotations
 import ctypes as C
 import operator
 import os
+import struct
 
 import torch
 
@@ -939,9 +940,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (the tensors are there: CUDA is set up)
+
+
 def _call(fn, what, device, *args):
     """One library call on the current stream of the tensors' device."""
-    if device.index != torch.cuda.current_device():
+    if device.index != _current_device():
         with torch.cuda.device(device):
             rc = fn(*args, _raw_stream(device.index))
     else:
@@ -1173,26 +1177,27 @@ def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accu
     return out
 
 
-def _adam_entry(t, device):
-    p, g, m, v = t["param"], t["grad"], t["m"], t["v"]
-    n = p.numel()
-    bits = 32 if m.dtype == torch.float32 else 8
-    state = torch.float32 if bits == 32 else torch.float8_e4m3fn
-    gt = _elem_type(g, "grad")
-    for x, dt, name in ((p, torch.float32, "param"), (g, g.dtype, "grad"), (m, state, "m"), (v, state, "v")):
-        if x.dtype != dt or x.numel() != n or x.device != device or not x.is_contiguous():
-            _check_on(device, x, dt, n, name)
-    ms = vs = None
-    if bits == 8:
-        ms, vs = t["m_scale"], t["v_scale"]
-        _check_on(device, ms, _E8M0, -(-n // 128), "m_scale")
-        _check_on(device, vs, _E8M0, -(-n // 128), "v_scale")
-        ms, vs = ms.data_ptr(), vs.data_ptr()
-    lp = t.get("bf16_copy_out")
-    if lp is not None:
-        _check_on(device, lp, torch.bfloat16, n, "bf16_copy_out")
-        lp = lp.data_ptr()
-    return p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs, lp, n, gt, bits, t.get("weight_decay", 0.0)
+_ADAM_PACK = struct.Struct("7Qq2id")
+assert _ADAM_PACK.size == C.sizeof(_AdamTensor)
+
+
+def _adam_check(t, index):
+    """Says what is wrong with an entry of adamw_step_multi's list."""
+    device = torch.device("cuda", index)
+    n = t["param"].numel()
+    state = t["m"].dtype if t["m"].dtype == torch.float32 else torch.float8_e4m3fn
+    _elem_type(t["grad"], "grad")
+    for name, dt, size in (("param", torch.float32, n), ("grad", t["grad"].dtype, n), ("m", state, n), ("v", state, n)):
+        _check_on(device, t[name], dt, size, name)
+    if state != torch.float32:
+        _check_on(device, t["m_scale"], _E8M0, -(-n // 128), "m_scale")
+        _check_on(device, t["v_scale"], _E8M0, -(-n // 128), "v_scale")
+    if t.get("bf16_copy_out") is not None:
+        _check_on(device, t["bf16_copy_out"], torch.bfloat16, n, "bf16_copy_out")
+
+
+def _adam_fits(x, dtype, n, index):
+    return x.dtype is dtype and x.numel() == n and x.get_device() == index and x.is_contiguous()
 
 
 def adamw_step_multi(tensors, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None):
@@ -1201,19 +1206,41 @@ def adamw_step_multi(tensors, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, see
     8 bits: m and v float8_e4m3fn, codes of m and of sqrt(v), with m_scale and v_scale float8_e8m0fnu, one for each 128
     consecutive elements; zeros throughout before the first step (t.zero_() of a uint8 view).  seed: of their random rounding;
     grad_scale: a float32 tensor of one element that multiplies every gradient, or None."""
-    dev = tensors[0]["param"].device if tensors else None
-    arr = (_AdamTensor * len(tensors))(*[_adam_entry(t, dev) for t in tensors])
     if not tensors:
         raise T5Error(2, "adamw_step_multi")
-    if not tensors[0]["param"].is_cuda:
+    dev = tensors[0]["param"].device
+    if dev.type != "cuda":
         raise ValueError(f"param: on {dev}")
+    index, f32, e4m3 = dev.index, torch.float32, torch.float8_e4m3fn
+    arr = bytearray(_ADAM_PACK.size * len(tensors))
+    at, pack, fits = 0, _ADAM_PACK.pack_into, _adam_fits  # (2 us of a call are an entry: every name counts)
+    for t in tensors:
+        p, g, m, v, lp = t["param"], t["grad"], t["m"], t["v"], t.get("bf16_copy_out")
+        n = p.numel()
+        gt = g.dtype
+        state = m.dtype
+        good = (gt is f32 or gt is torch.bfloat16) and fits(p, f32, n, index) and fits(g, gt, n, index) and \
+            (state is f32 or state is e4m3) and fits(m, state, n, index) and fits(v, state, n, index) and \
+            (lp is None or fits(lp, torch.bfloat16, n, index))
+        if state is f32:
+            ms = vs = 0
+        elif good:
+            ms, vs = t["m_scale"], t["v_scale"]
+            good = fits(ms, _E8M0, (n + 127) // 128, index) and fits(vs, _E8M0, (n + 127) // 128, index)
+            ms, vs = ms.data_ptr(), vs.data_ptr()
+        if not good:
+            _adam_check(t, index)
+            raise ValueError("adamw_step_multi: an entry's tensors do not belong together")
+        pack(arr, at, p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs, 0 if lp is None else lp.data_ptr(), n,
+             T5_F32 if gt is f32 else T5_BF16, 32 if state is f32 else 8, t.get("weight_decay", 0.0))
+        at += _ADAM_PACK.size
     if grad_scale is not None:
-        _check_on(dev, grad_scale, torch.float32, 1, "grad_scale")
+        _check_on(dev, grad_scale, f32, 1, "grad_scale")
         grad_scale = grad_scale.data_ptr()
     seed = operator.index(seed)
     cfg = _AdamCfg(float(lr), float(beta1), float(beta2), float(eps), _i32(step), seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF,
                    grad_scale)
-    _call(lib().adamw_step_multi, "adamw_step_multi", dev, arr, len(tensors), C.byref(cfg))
+    _call(lib().adamw_step_multi, "adamw_step_multi", dev, (_AdamTensor * len(tensors)).from_buffer(arr), len(tensors), C.byref(cfg))
 
 
 def t5_gemm_bf16(a: torch.Tensor, b: torch.Tensor, a_kc: bool, b_kc: bool, out: torch.Tensor | None = None):

@@ -100,21 +100,34 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int n, u32x2 c) {
 }
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
-__device__ __forceinline__ void decode8(u32x2 c, float s, float (&v)[8]) {
+__device__ __forceinline__ void decode8(u32x2 c, float scale, float (&v)[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[h], true);
-    v[h * 4] = lo[0] * s; v[h * 4 + 1] = lo[1] * s; v[h * 4 + 2] = hi[0] * s; v[h * 4 + 3] = hi[1] * s;
+    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)c[h], scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)c[h], scale, true);
+    v[h * 4] = lo[0]; v[h * 4 + 1] = lo[1]; v[h * 4 + 2] = hi[0]; v[h * 4 + 3] = hi[1];
   }
 }
 
-// |x| * inv in e4m3, a whole number of steps: floor(t + u) with u = bits / 2^16.  In the type's normal range a step is the
-// 20 low bits of the fraction, and adding u there and cutting them off is that floor; below, steps are 2^-9 wide.
-__device__ __forceinline__ float round_at_random(float x, float inv, uint32_t bits) {
-  const float y = fabsf(x) * inv;
-  const float normal = __uint_as_float((__float_as_uint(y) + (bits << 4)) & 0xFFF00000u);
-  const float small = floorf(fmaf(y, 512.f, (float)bits * (1.f / 65536.f))) * (1.f / 512.f);
-  return y < 0.015625f ? small : normal;  // (NaN: stays NaN, the quiet bit is one that is kept)
+// Four codes of x / scale, each floor(t + u) steps: the conversion with a random word adds the word's top bits below the
+// type's last place, in its subnormal range too, and cuts off; u is `bits` / 2^16 where the word is bits << 16.
+__device__ __forceinline__ uint32_t round_at_random4(const float* x, const uint32_t* word, float scale) {
+  int r = __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(0, x[0], word[0], scale, 0);
+  r = __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(r, x[1], word[1], scale, 1);
+  r = __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(r, x[2], word[2], scale, 2);
+  return (uint32_t)__builtin_amdgcn_cvt_scalef32_sr_fp8_f32(r, x[3], word[3], scale, 3);
+}
+
+// Bits of the largest finite |x| of a thread's eight.
+__device__ __forceinline__ uint32_t largest8(const float (&x)[8]) {
+  uint32_t b = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) b = max(b, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+  if (b >= 0x7F800000u) {
+    b = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b = max(b, finite_bits(x[j]));
+  }
+  return b;
 }
 
 struct Step {
@@ -123,13 +136,14 @@ struct Step {
     m = fmaf(b1, m, one_b1 * g);
     v = fmaf(b2, v, one_b2 * g * g);
   }
+  // (v_sqrt_f32 and v_rcp_f32 are within one unit of the last place; the divisor is eps or more, 1e-30 at least)
   __device__ __forceinline__ float update(float p, float m, float root) const {
-    return fmaf(p, keep, -step_size * (m / fmaf(root, root_factor, eps)));
+    return fmaf(p, keep, -step_size * (m * __builtin_amdgcn_rcpf(fmaf(root, root_factor, eps))));
   }
 };
 
 template <bool VEC, bool EIGHT>
-__device__ __forceinline__ void adam_chunk(const AdamItem& it, const Step& s, float gs, uint32_t seed_hi, int64_t i) {
+__device__ __forceinline__ void adam_chunk(const AdamItem& it, const Step& s, const float* gs, uint32_t seed_hi, int64_t i) {
   const int64_t left = it.n - i;
   const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
   float p[8], g[8], m[8], v[8], root[8];
@@ -139,45 +153,50 @@ __device__ __forceinline__ void adam_chunk(const AdamItem& it, const Step& s, fl
   const int64_t block = i >> 7;
   if constexpr (EIGHT) {
     const u32x2 cm = load_codes<VEC>((const uint8_t*)it.m + i, n), cv = load_codes<VEC>((const uint8_t*)it.v + i, n);
-    decode8(cm, n > 0 ? scale_value(it.ms[block]) : 0.f, m);
-    decode8(cv, n > 0 ? scale_value(it.vs[block]) : 0.f, root);
+    decode8(cm, n > 0 ? scale_operand8(it.ms[block]) : 0.f, m);
+    decode8(cv, n > 0 ? scale_operand8(it.vs[block]) : 0.f, root);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = root[j] * root[j];
   } else {
     load8<VEC>((const float*)it.m + i, n, m);
     load8<VEC>((const float*)it.v + i, n, v);
   }
+  if (gs) {
+    const float f = *gs;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] *= f;
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    s.moments(g[j] * gs, m[j], v[j]);
-    root[j] = sqrtf(v[j]);
+    s.moments(g[j], m[j], v[j]);
+    root[j] = __builtin_amdgcn_sqrtf(v[j]);
     p[j] = s.update(p[j], m[j], root[j]);
   }
   store8<VEC>(it.p + i, n, p);
   if (it.lp) store8<VEC>(it.lp + i, n, p);
   if constexpr (EIGHT) {
-    uint32_t am = 0, ar = 0;
+    if (n < 8) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (j >= n) m[j] = root[j] = 0.f;
-      am = max(am, finite_bits(m[j]));
-      ar = max(ar, finite_bits(root[j]));
+      for (int j = 0; j < 8; ++j)
+        if (j >= n) m[j] = root[j] = 0.f;
     }
-    const int em = block_exponent<T5_E4M3>(max16(am)), er = block_exponent<T5_E4M3>(max16(ar));
-    const float im = block_inverse(em), ir = block_inverse(er);
-    const uint32_t row = mix32(it.key ^ (uint32_t)block ^ seed_hi);
+    const int em = block_exponent<T5_E4M3>(max16(largest8(m))), er = block_exponent<T5_E4M3>(max16(largest8(root)));
+    const float sm = scale_of(em), sr = scale_of(er), least = scale_value((uint32_t)(er + 127)) * (1.f / 512.f);
+    const uint32_t row = mix32(it.key ^ (uint32_t)block ^ seed_hi), pre = row ^ (row >> 16);
     const int c0 = (int)(i & 127);
-    float cm[8], cr[8];
+    uint32_t wm[8], wr[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint32_t h = mix32(row ^ (uint32_t)(c0 + j));
-      cm[j] = copysignf(round_at_random(m[j], im, h & 0xFFFFu), m[j]);
-      const float r = round_at_random(root[j], ir, h >> 16);
-      cr[j] = root[j] > 0.f ? fmaxf(r, 1.f / 512.f) : r;
-      if (root[j] != root[j]) cr[j] = root[j];
+      // mix32(row ^ column): the first step's x >> 16 holds none of the column's seven bits
+      uint32_t h = (pre ^ (uint32_t)(c0 + j)) * 0x7FEB352Du;
+      h = (h ^ (h >> 15)) * 0x846CA68Bu;
+      h ^= h >> 16;
+      wm[j] = h << 16;
+      wr[j] = h & 0xFFFF0000u;
+      root[j] = root[j] > 0.f ? fmaxf(root[j], least) : root[j];  // at least the smallest code
     }
-    store_codes<VEC>((uint8_t*)it.m + i, n, u32x2{pack_fp8x4<T5_E4M3>(cm[0], cm[1], cm[2], cm[3]), pack_fp8x4<T5_E4M3>(cm[4], cm[5], cm[6], cm[7])});
-    store_codes<VEC>((uint8_t*)it.v + i, n, u32x2{pack_fp8x4<T5_E4M3>(cr[0], cr[1], cr[2], cr[3]), pack_fp8x4<T5_E4M3>(cr[4], cr[5], cr[6], cr[7])});
+    store_codes<VEC>((uint8_t*)it.m + i, n, u32x2{round_at_random4(m, wm, sm), round_at_random4(m + 4, wm + 4, sm)});
+    store_codes<VEC>((uint8_t*)it.v + i, n, u32x2{round_at_random4(root, wr, sr), round_at_random4(root + 4, wr + 4, sr)});
     if (n > 0 && c0 == 0) {
       it.ms[block] = (uint8_t)(em + 127);
       it.vs[block] = (uint8_t)(er + 127);
@@ -193,7 +212,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamBatch b) {
   while (t + 1 < b.count && (int)blockIdx.x >= b.start[t + 1]) ++t;
   const AdamItem& it = b.it[t];
   const int64_t i = (int64_t)((int)blockIdx.x - b.start[t]) * kChunk + threadIdx.x * 8;
-  const float gs = b.grad_scale ? *b.grad_scale : 1.f;
+  const float* gs = b.grad_scale;
   const Step s{b.b1, b.one_b1, b.b2, b.one_b2, b.root_factor, b.eps, b.step_size, it.keep};
   if (it.flags & AW_8BIT) {
     if (it.flags & AW_VEC) adam_chunk<true, true>(it, s, gs, b.seed_hi, i);

@@ -36,6 +36,7 @@ struct Fp8Gemm {
   int out_bf16, accumulate;
   // Output tiles (256 x 256 if big, else 128 x 128), numbered 0 .. tiles_m * tiles_n.  The first `shared` of them, in units of
   // four k-tiles, are dealt out evenly to `workers` workgroups, in order; each of the others has a workgroup of its own.
+  int few;  // none of that: gemm_fp8_rows.hip
   int big, tiles_m, tiles_n, shared, workers;
   float* part;  // what a worker adds up of a tile that others have parts of, a tile of float32: at place worker + tile
 };
@@ -54,8 +55,7 @@ hipError_t launch_gemm_fp8_44(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_45(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_54(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_55(const Fp8Gemm& g, hipStream_t st);
-// M <= kFp8FewRows, without tiles (gemm_fp8_rows.hip).
-constexpr int kFp8FewRows = 64;
+// Without tiles, M <= 64 (gemm_fp8_rows.hip).
 hipError_t launch_gemm_fp8_rows(const Fp8Gemm& g, int ta, int tb, hipStream_t st);
 
 namespace {
@@ -84,9 +84,9 @@ __device__ __forceinline__ bf16x4 widen4(int c, float scale) {
 __device__ __forceinline__ bf16x8 both(bf16x4 lo, bf16x4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
 template <int T>
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi, float scale) { return both(widen4<T>(lo, scale), widen4<T>(hi, scale)); }
-// The scale of block OP of a word as the conversion takes it: only the exponent counts there (0: 2^-127).
+// The scale of block OP of a word.
 template <int OP>
-__device__ __forceinline__ float scale_operand(int word) { return __uint_as_float((uint32_t)((word >> (8 * OP)) & 255) << 23); }
+__device__ __forceinline__ float scale_operand(int word) { return scale_operand8((uint32_t)(word >> (8 * OP)) & 255u); }
 
 template <int TA, int TB, int OP>
 __device__ __forceinline__ f32x16 fp8_mfma(i32x8 b, i32x8 a, f32x16 c, int sb, int sa) {

@@ -53,9 +53,12 @@ double round_cost(const TileCost& t, double fill, double nk) {
   return nk * (t.idle + t.busy * std::max(0.0, fill - t.from) / (1.0 - t.from)) + t.ends;
 }
 
+bool few_rows(const t5_gemm_fp8_cfg& c) { return c.M <= 32 || (c.M <= 64 && (int64_t)c.N * c.K <= (16 << 20)); }
+
 void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
   g->shared = g->workers = 0;
-  if (c.M <= kFp8FewRows) return;
+  g->few = few_rows(c);
+  if (g->few) return;
   const int units = ceil_div(c.K, 512);
   const double nk = c.K / 128.0;
   double best = -1.0;
@@ -100,7 +103,7 @@ hipError_t launch_gemm_fp8(const t5_gemm_fp8_cfg& c, const void* A, const uint8_
   g.M = c.M; g.N = c.N; g.K = c.K;
   g.C = C; g.ldc = c.ldc; g.out_bf16 = c.c_dtype == T5_BF16; g.accumulate = c.accumulate != 0;
   g.part = (float*)ws;
-  if (c.M <= kFp8FewRows) return launch_gemm_fp8_rows(g, c.a_dtype, c.b_dtype, st);
+  if (g.few) return launch_gemm_fp8_rows(g, c.a_dtype, c.b_dtype, st);
   hipError_t e;
   if (c.a_dtype == T5_E4M3) e = c.b_dtype == T5_E4M3 ? launch_gemm_fp8_44(g, st) : launch_gemm_fp8_45(g, st);
   else e = c.b_dtype == T5_E4M3 ? launch_gemm_fp8_54(g, st) : launch_gemm_fp8_55(g, st);

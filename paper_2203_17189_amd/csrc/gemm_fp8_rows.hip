@@ -9,23 +9,24 @@
 namespace t5mi {
 namespace {
 
-// 32 bytes from p; of these the ones before `left` (16-byte pieces that begin there are in memory as wholes), zeros behind.
+// A lane's 32 bytes of a row's block of 128: 16 at p and 16 at p + 64, so that the four lanes of a row read 64 bytes in a
+// row with each load.  `left`: bytes of the matrix from p on; pieces that begin there are in memory as wholes, zeros behind.
 __device__ __forceinline__ i32x8 load32(const uint8_t* p, int left) {
   i32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     i32x4 q = {0, 0, 0, 0};
-    if (left > h * 16) q = *reinterpret_cast<const i32x4*>(p + h * 16);
+    if (left > h * 64) q = *reinterpret_cast<const i32x4*>(p + h * 64);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const int keep = left - h * 16 - w * 4;
+      const int keep = left - h * 64 - w * 4;
       v[h * 4 + w] = keep >= 4 ? q[w] : keep <= 0 ? 0 : (int)((uint32_t)q[w] & ((1u << (keep * 8)) - 1u));
     }
   }
   return v;
 }
 __device__ __forceinline__ i32x8 load32(const uint8_t* p) {
-  const i32x4 a = *reinterpret_cast<const i32x4*>(p), b = *reinterpret_cast<const i32x4*>(p + 16);
+  const i32x4 a = *reinterpret_cast<const i32x4*>(p), b = *reinterpret_cast<const i32x4*>(p + 64);
   return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
@@ -39,7 +40,7 @@ template <int TA, int TB, bool F32, int MT, int NT, int NW, int IN>
 __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
   __shared__ f32x4 sums[NW][NT * MT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = blockIdx.x * (16 * NT), nk = (g.K + 127) >> 7;
-  const int k0 = (lane >> 4) * 32;
+  const int k0 = (lane >> 4) * 16;
   const uint8_t *pa[MT], *qa[MT], *pb[NT], *qb[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
@@ -134,14 +135,20 @@ __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
 
 template <int TA, int TB, bool F32>
 hipError_t launch(const Fp8Gemm& g, hipStream_t st) {
-  const unsigned grid = (unsigned)ceil_div(g.N, 16), half = (grid + 1) / 2;
+  // Rows of B a workgroup: as many as leave at least two workgroups to a compute unit, as each reads A anew.
+  const int n16 = ceil_div(g.N, 16);
+  const int nt = n16 >= 2048 ? 4 : n16 >= 1024 ? 2 : 1;
+  const auto grid = [&](int rows) { return (unsigned)ceil_div(n16, rows); };
   if (g.M <= 16) {
-    if (g.K > 1024) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 8, 4><<<grid, 512, 0, st>>>(g);
-    else gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 4, 2><<<grid, 256, 0, st>>>(g);
+    if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 1, 4, 8, 2><<<grid(4), 512, 0, st>>>(g);
+    else if (nt == 2) gemm_fp8_rows_kernel<TA, TB, F32, 1, 2, 8, 2><<<grid(2), 512, 0, st>>>(g);
+    else if (g.K > 1024) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 8, 4><<<grid(1), 512, 0, st>>>(g);
+    else gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 4, 2><<<grid(1), 256, 0, st>>>(g);
   } else if (g.M <= 32) {
-    gemm_fp8_rows_kernel<TA, TB, F32, 2, 2, 8, 2><<<half, 512, 0, st>>>(g);
+    if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 2, 4, 8, 2><<<grid(4), 512, 0, st>>>(g);
+    else gemm_fp8_rows_kernel<TA, TB, F32, 2, 2, 8, 2><<<grid(2), 512, 0, st>>>(g);
   } else {
-    gemm_fp8_rows_kernel<TA, TB, F32, 4, 2, 8, 1><<<half, 512, 0, st>>>(g);
+    gemm_fp8_rows_kernel<TA, TB, F32, 4, 2, 8, 1><<<grid(2), 512, 0, st>>>(g);
   }
   return hipGetLastError();
 }
