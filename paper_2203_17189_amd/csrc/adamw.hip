@@ -11,7 +11,7 @@
 namespace t5mi {
 namespace {
 
-constexpr int kChunk = 2048;  // elements: 8 for each of 256 threads
+constexpr int kThreads = 256, kChunk = kThreads * 8;  // threads of a workgroup, 8 elements each
 
 enum { AW_8BIT = 1, AW_BF16_GRAD = 2, AW_VEC = 4 };
 struct AdamItem {
@@ -207,9 +207,10 @@ __device__ __forceinline__ void adam_chunk(const AdamItem& it, const Step& s, co
   }
 }
 
-__global__ __launch_bounds__(256) void adamw_kernel(AdamBatch b) {
-  int t = 0;
-  while (t + 1 < b.count && (int)blockIdx.x >= b.start[t + 1]) ++t;
+__global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b) {
+  // The tensor: how many start at or before this workgroup, but for the first (one load; in turn, each waits for the one before).
+  const int lane = threadIdx.x & 63;
+  const int t = __popcll(__ballot(lane < b.count - 1 && (int)blockIdx.x >= b.start[min(lane + 1, kAdamTensors)]));
   const AdamItem& it = b.it[t];
   const int64_t i = (int64_t)((int)blockIdx.x - b.start[t]) * kChunk + threadIdx.x * 8;
   const float* gs = b.grad_scale;
@@ -254,7 +255,7 @@ hipError_t launch_adamw(const adamw_tensor* t, int n, int first, const adamw_cfg
     if (chunks > 0x7FFFFFFF) return hipErrorInvalidValue;
   }
   b.start[n] = (int32_t)chunks;
-  adamw_kernel<<<(unsigned)chunks, 256, 0, st>>>(b);
+  adamw_kernel<<<(unsigned)chunks, kThreads, 0, st>>>(b);
   return hipGetLastError();
 }
 

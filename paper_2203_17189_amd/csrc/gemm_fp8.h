@@ -34,10 +34,10 @@ struct Fp8Gemm {
   void* C;
   int64_t ldc;
   int out_bf16, accumulate;
-  // Output tiles (256 x 256 if big, else 128 x 128), numbered 0 .. tiles_m * tiles_n.  The first `shared` of them, in units of
+  // Output tiles (of `tile` = 64, 128 or 256 rows and columns), numbered 0 .. tiles_m * tiles_n.  The first `shared` of them, in units of
   // four k-tiles, are dealt out evenly to `workers` workgroups, in order; each of the others has a workgroup of its own.
   int few;  // none of that: gemm_fp8_rows.hip
-  int big, tiles_m, tiles_n, shared, workers;
+  int tile, tiles_m, tiles_n, shared, workers;
   float* part;  // what a worker adds up of a tile that others have parts of, a tile of float32: at place worker + tile
 };
 
@@ -145,20 +145,20 @@ __device__ __forceinline__ void fp8_store_tile(f32x16 (&acc)[NI][MJ], char* lds,
         else __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
       }
     } else {
-      // element by element, 64 neighbours a store
-      constexpr int AT_ONCE = 8;
-      for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
+      // element by element, a row's neighbours side by side
+      constexpr int AT_ONCE = 8, WIDE = COLS < 64 ? COLS : 64, CHUNKS = COLS / WIDE;
+      for (int r0 = 0; r0 < 32; r0 += AT_ONCE * (64 / WIDE)) {
 #pragma unroll
-        for (int c = 0; c < COLS / 64; ++c) {
-          const int col = c * 64 + lane;
+        for (int c = 0; c < CHUNKS; ++c) {
+          const int col = c * WIDE + lane % WIDE, r1 = r0 + lane / WIDE * AT_ONCE;
           const bool on = n + col >= n_own && n + col < N;
           T v[AT_ONCE];
 #pragma unroll
-          for (int r = 0; r < AT_ONCE; ++r) v[r] = *reinterpret_cast<const T*>(lds + (r0 + r) * PITCH + col * (int)sizeof(T));
-          T* p = C + (int64_t)(mj + r0) * ld + n + col;
+          for (int r = 0; r < AT_ONCE; ++r) v[r] = *reinterpret_cast<const T*>(lds + (r1 + r) * PITCH + col * (int)sizeof(T));
+          T* p = C + (int64_t)(mj + r1) * ld + n + col;
 #pragma unroll
           for (int r = 0; r < AT_ONCE; ++r)
-            if (on && mj + r0 + r >= m_own && mj + r0 + r < M) {
+            if (on && mj + r1 + r >= m_own && mj + r1 + r < M) {
               if constexpr (sizeof(T) == 4) p[r * ld] = add ? p[r * ld] + v[r] : v[r];
               else p[r * ld] = v[r];
             }
@@ -292,8 +292,9 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
   // scale is the same for all of them.  The 16-byte piece c (even, plus the half) of rows 32 j ..: the swizzle is the lane's
   // own, but for 4 (j odd), so that all addresses are one lane's with two bits turned and a constant added.
   const uint32_t lane_at = (uint32_t)(lane & 31) * 128 + (((lane >> 5) ^ fp8_swz(lane & 31)) << 4);
-  const uint32_t a_lane = lds0 + wm * (BM / WM) * 128 + lane_at, b_lane = lds0 + B_AT + wn * (BN / WN) * 128 + lane_at;
-  static_assert((BM / WM) % 64 == 0 && (BN / WN) % 64 == 0, "swizzle of a wavefront's first row");
+  // (a wavefront that begins at an odd multiple of 32 rows has the odd swizzle first)
+  auto lane_from = [&](int row) __attribute__((always_inline)) { return (uint32_t)row * 128 + (lane_at ^ ((row & 32) << 1)); };
+  const uint32_t a_lane = lds0 + lane_from(wm * (BM / WM)), b_lane = lds0 + B_AT + lane_from(wn * (BN / WN));
   auto read = [&](uint32_t base, int j, int kk) __attribute__((always_inline)) {
     auto piece = [&](int c) __attribute__((always_inline)) {
       return *(lds_i32x4*)(uintptr_t)((base ^ (uint32_t)((c ^ ((j & 1) << 2)) << 4)) + j * 4096);
@@ -357,6 +358,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
     if constexpr (F32) {
     constexpr int STEP = decltype(step_tag)::value, CUR = STEP & 1, NXT = CUR ^ 1, U = decltype(u_tag)::value;
     constexpr int U1 = STEP == 3 ? U + 1 : U;  // the next step's block
+    constexpr int ODD = NI & STEP & 1;         // which of B's sets the first group has (a tile's four steps come out even)
     typedef std::integral_constant<int, U & 3> Op;
     typedef std::integral_constant<int, U1 & 3> Op1;
     uint32_t la = a_lane, lb = b_lane;
@@ -374,14 +376,14 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < MJ; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(both(wb[i & 1][h * 2], wb[i & 1][h * 2 + 1]),
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(both(wb[(i + ODD) & 1][h * 2], wb[(i + ODD) & 1][h * 2 + 1]),
                                                                both(wa[CUR][j][h * 2], wa[CUR][j][h * 2 + 1]), acc[i][j], 0, 0, 0);
           const int at = h * MJ + j;  // of 2 MJ places, 4 conversions of B and 4 of A in turn
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             if (q * 2 * MJ / 4 / 2 == at) {
-              if (i + 1 < NI) widen_b((i + 1) & 1, CUR, i + 1, q, xb[U / 4][i + 1 < NI ? i + 1 : 0], Op{});
-              else widen_b(0, NXT, 0, q, word_b(0), Op1{});
+              if (i + 1 < NI) widen_b((i + 1 + ODD) & 1, CUR, i + 1, q, xb[U / 4][i + 1 < NI ? i + 1 : 0], Op{});
+              else widen_b((NI + ODD) & 1, NXT, 0, q, word_b(0), Op1{});
             }
             if (i < MJ && MJ + q * 2 * MJ / 4 / 2 == at) widen_a(NXT, i, q, word_a(i < MJ ? i : 0), Op1{});
           }
@@ -547,9 +549,13 @@ hipError_t launch_fp8_tiles(const Fp8Gemm& g, hipStream_t st) {
 
 template <int TA, int TB>
 hipError_t launch_fp8_types(const Fp8Gemm& g, hipStream_t st) {
-  const bool big = g.big;
-  if (g.out_bf16) return big ? launch_fp8_tiles<256, 256, 2, 2, TA, TB, false, 3>(g, st) : launch_fp8_tiles<128, 128, 2, 2, TA, TB, false, 3>(g, st);
-  return big ? launch_fp8_tiles<256, 256, 2, 2, TA, TB, true, 2>(g, st) : launch_fp8_tiles<128, 128, 2, 2, TA, TB, true, 2>(g, st);
+  if (g.out_bf16)
+    return g.tile == 256   ? launch_fp8_tiles<256, 256, 2, 2, TA, TB, false, 3>(g, st)
+           : g.tile == 128 ? launch_fp8_tiles<128, 128, 2, 2, TA, TB, false, 3>(g, st)
+                           : launch_fp8_tiles<64, 64, 2, 2, TA, TB, false, 3>(g, st);
+  return g.tile == 256   ? launch_fp8_tiles<256, 256, 2, 2, TA, TB, true, 2>(g, st)
+         : g.tile == 128 ? launch_fp8_tiles<128, 128, 2, 2, TA, TB, true, 2>(g, st)
+                         : launch_fp8_tiles<64, 64, 2, 2, TA, TB, true, 2>(g, st);
 }
 
 }  // namespace

@@ -35,19 +35,22 @@ __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(Fp8Gemm g) {
 }
 
 // Which tiles, and whether those of the last, partly filled round are shared out along k: whatever is estimated to be faster.
-// Estimates in us, fitted to the kernels of this file on shapes of 300 .. 32768 by 500 .. 32128 by 512 .. 32768.  A k-tile of
-// a full round (256 tiles of 256 x 256, one on each compute unit, or 512 of 128 x 128) takes the longer the more of the chip
-// is at work, as clocks follow power: `idle` where few tiles run, `busy` more in a full round.  A round has `ends` besides.
-// Sharing costs a launch and the parts' way to memory and back, 5 MB a us.  Both sides, shape and type of C:
-//   2048 x 2048 x 4096   bf16  128: 26 us, shared 36;   256: 51, shared 44        (taken: 128)
-//   4096 x 4096 x 4096   bf16  128: 73;                 256: 65                   (256)
-//   768 x 2048 x 16384   f32   128: 112, shared 65;     256: 279, shared 84       (128, shared)
-//   5120 x 2048 x 32768  bf16  128: 394, shared 372;    256: 353, shared 408      (256)
-//   5120 x 2048 x 32768  f32   128: 609, shared 565;    256: 590, shared 549      (256, shared)
-struct TileCost { double idle, busy, from, ends; };
-constexpr TileCost kTileCost[2][2] = {{{0.53, 0.55, 0.2, 2.5}, {1.1, 0.5, 0.4, 12.5}},   // bf16 C: tiles of 128, of 256
-                                      {{0.83, 0.92, 0.2, 5.0}, {2.05, 1.0, 0.5, 12.5}}};  // float32 C
-constexpr int kCus = 256;
+// Estimates in us, fitted to the kernels of gemm_fp8.h on shapes of 64 .. 32768 by 300 .. 32128 by 512 .. 32768.  A k-tile of
+// a full round (`at_once` tiles: one, two or four workgroups on each of 256 compute units) takes the longer the more of the
+// chip is at work, as clocks follow power: `idle` where few tiles run, `busy` more in a full round, rising from a fill of
+// `from` on.  A round has `ends` besides.  Sharing costs a launch and the parts' way to memory and back, 5 MB a us.
+// Small tiles have more loads and conversions to a matrix instruction, large ones fewer workgroups and longer ends.  Measured,
+// M x N x K and type of C, us:                tiles of 64, shared      128, shared      256, shared
+//   300 x 500 x 1024      f32                  8.5    13.1            13.4    13.3        41      28
+//   2048 x 2048 x 2048    bf16                17.4    17.7            13.0    25.8        30      37
+//   768 x 2048 x 16384    f32                 85.5    92.3             114      65       279      84
+//   4096 x 4096 x 4096    bf16                                          73                65
+//   5120 x 2048 x 32768   bf16                                         394     372       353     408
+//   5120 x 2048 x 32768   f32                                          609     565       590     549
+struct TileCost { int tile, at_once; double idle, busy, from, ends; };
+constexpr TileCost kTileCost[2][3] = {
+    {{64, 1024, 0.39, 0.6, 0.25, 2.0}, {128, 512, 0.53, 0.55, 0.2, 2.5}, {256, 256, 1.1, 0.5, 0.4, 12.5}},   // bf16 C
+    {{64, 1024, 0.55, 0.85, 0.25, 2.0}, {128, 512, 0.83, 0.92, 0.2, 5.0}, {256, 256, 2.05, 1.0, 0.5, 12.5}}};  // float32 C
 
 double round_cost(const TileCost& t, double fill, double nk) {
   return nk * (t.idle + t.busy * std::max(0.0, fill - t.from) / (1.0 - t.from)) + t.ends;
@@ -62,10 +65,9 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
   const int units = ceil_div(c.K, 512);
   const double nk = c.K / 128.0;
   double best = -1.0;
-  for (int big = 0; big < 2; ++big) {
-    if (big && (c.M < 256 || c.N < 256)) break;
-    const int B = big ? 256 : 128, slots = big ? kCus : 2 * kCus, tm = ceil_div(c.M, B), tn = ceil_div(c.N, B);
-    const TileCost& t = kTileCost[c.c_dtype == T5_F32][big];
+  for (const TileCost& t : kTileCost[c.c_dtype == T5_F32]) {
+    const int B = t.tile, slots = t.at_once, tm = ceil_div(c.M, B), tn = ceil_div(c.N, B);
+    if (B == 256 && (c.M < 256 || c.N < 256)) break;
     const int64_t tiles = (int64_t)tm * tn, rest = tiles % slots;
     const double full = (double)(tiles / slots) * round_cost(t, 1.0, nk), fill = (double)rest / slots;
     const double alone = full + (rest ? round_cost(t, fill, nk) : 0.0);
@@ -77,7 +79,7 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
     const double cost = share ? shared : alone;
     if (best >= 0.0 && cost >= best) continue;
     best = cost;
-    g->big = big; g->tiles_m = tm; g->tiles_n = tn;
+    g->tile = B; g->tiles_m = tm; g->tiles_n = tn;
     g->shared = share ? (int)rest : 0;
     g->workers = share ? (int)workers : 0;
   }
@@ -89,7 +91,7 @@ size_t gemm_fp8_ws_bytes(const t5_gemm_fp8_cfg& c) {
   Fp8Gemm g;
   plan(c, &g);
   if (g.workers <= g.shared) return 0;
-  const size_t B = g.big ? 256 : 128;
+  const size_t B = g.tile;
   return ((size_t)g.workers + g.shared) * B * B * 4;
 }
 
@@ -108,8 +110,9 @@ hipError_t launch_gemm_fp8(const t5_gemm_fp8_cfg& c, const void* A, const uint8_
   if (c.a_dtype == T5_E4M3) e = c.b_dtype == T5_E4M3 ? launch_gemm_fp8_44(g, st) : launch_gemm_fp8_45(g, st);
   else e = c.b_dtype == T5_E4M3 ? launch_gemm_fp8_54(g, st) : launch_gemm_fp8_55(g, st);
   if (e != hipSuccess || g.workers <= g.shared) return e;
-  if (g.big) gemm_fp8_sum_kernel<256><<<(unsigned)g.shared * 16, 256, 0, st>>>(g);
-  else gemm_fp8_sum_kernel<128><<<(unsigned)g.shared * 8, 256, 0, st>>>(g);
+  if (g.tile == 256) gemm_fp8_sum_kernel<256><<<(unsigned)g.shared * 16, 256, 0, st>>>(g);
+  else if (g.tile == 128) gemm_fp8_sum_kernel<128><<<(unsigned)g.shared * 8, 256, 0, st>>>(g);
+  else gemm_fp8_sum_kernel<64><<<(unsigned)g.shared * 4, 256, 0, st>>>(g);
   return hipGetLastError();
 }
 
