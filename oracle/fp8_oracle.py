@@ -87,11 +87,11 @@ def _mix32(x):
     return x ^ (x >> np.uint64(16))
 
 
-def random_parts(n, index, step, seed):
-    """The two 16-bit fractions of each element, of m and of sqrt(v)."""
+def random_parts(n, index, step, seed, first=0):
+    """The two 16-bit fractions of n elements from `first` on, of m and of sqrt(v)."""
     lo, hi = seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF
     key = _mix32(int(_mix32(lo ^ step)) ^ ((index * 0x9E3779B9) & 0xFFFFFFFF))
-    i = np.arange(n, dtype=np.uint64)
+    i = np.arange(first, first + n, dtype=np.uint64)
     h = _mix32(_mix32(key ^ ((i >> np.uint64(7)) & np.uint64(0xFFFFFFFF)) ^ np.uint64(hi)) ^ (i & np.uint64(127)))
     return (h & np.uint64(0xFFFF)) / 65536.0, (h >> np.uint64(16)) / 65536.0
 
