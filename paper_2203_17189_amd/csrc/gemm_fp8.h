@@ -312,34 +312,34 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
     for (int i = 0; i < NI; ++i) fb[0][i] = read(b_lane, i, 0);
   };
 
-  // One k-step from set CUR, block U of the turn, in NI groups of matrix instructions.  Group i also issues its share of
-  // DMA (dma(i)) and reads its share of the next k-step's operands (A stage sa, B stage sb, k-step kk), in the order in
-  // which that step uses them, all before the last group, whose matrix instructions cover the reads' latency.
+  // One k-step from set CUR, block U of the turn.  Between its matrix instructions stand its share of DMA (dma(p, of) before
+  // number p of `of`) and the reads of the next k-step's operands (A stage sa, B stage sb, k-step kk), in the order in which
+  // that step uses them, all in the first three quarters, so that the last ones' latency is covered.  One at a time: a
+  // wavefront whose memory instruction finds the queue full issues nothing, and the four wavefronts run in step.
   auto kstep = [&](auto cur_tag, auto u_tag, int sa, int sb, int kk, auto&& dma) __attribute__((always_inline)) {
     if constexpr (!F32) {
     constexpr int CUR = decltype(cur_tag)::value, U = decltype(u_tag)::value, OP = U & 3, W = U / 4;
-    constexpr int NLD = MJ + NI, GROUPS = NI > 1 ? NI - 1 : 1;
+    constexpr int NLD = MJ + NI, ALL = NI * MJ, READS = ALL > 3 ? ALL * 3 / 4 : ALL;
     uint32_t la = a_lane, lb = b_lane;
     asm volatile("" : "+v"(la), "+v"(lb));  // addresses are formed in the step that uses them, not kept for the whole loop
     la += sa * A_BYTES;
     lb += sb * B_BYTES;
-    auto reads = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-      for (int q = 0; q < NLD; ++q) {
-        if (q * GROUPS / NLD != i) continue;
-        if (q == 0) fb[CUR ^ 1][0] = read(lb, 0, kk);
-        else if (q <= MJ) fa[CUR ^ 1][q - 1] = read(la, q - 1, kk);
-        else fb[CUR ^ 1][q - MJ] = read(lb, q - MJ, kk);
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < MJ; ++j) {
+        const int p = i * MJ + j;
+        dma(p, ALL);
+#pragma unroll
+        for (int q = 0; q < NLD; ++q) {
+          if (q * READS / NLD != p) continue;
+          if (q == 0) fb[CUR ^ 1][0] = read(lb, 0, kk);
+          else if (q <= MJ) fa[CUR ^ 1][q - 1] = read(la, q - 1, kk);
+          else fb[CUR ^ 1][q - MJ] = read(lb, q - MJ, kk);
+        }
+        acc[i][j] = fp8_mfma<TA, TB, OP>(fb[CUR][i], fa[CUR][j], acc[i][j], xb[W][i], xa[W][j]);
+        __builtin_amdgcn_sched_barrier(0);
       }
-    };
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      dma(i);
-      reads(i);
-#pragma unroll
-      for (int j = 0; j < MJ; ++j) acc[i][j] = fp8_mfma<TA, TB, OP>(fb[CUR][i], fa[CUR][j], acc[i][j], xb[W][i], xa[W][j]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
     }
   };
 
@@ -369,13 +369,13 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
     auto word_b = [&](int i) __attribute__((always_inline)) { return U1 < UN ? xb[U1 < UN ? U1 / 4 : 0][i] : yb[0][i]; };
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      dma(i);
       if (i < MJ) fa[CUR][i] = read(la, i, kk);
       fb[CUR][i] = read(lb, i, kk);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < MJ; ++j) {
+          dma((i * 2 + h) * MJ + j, NI * 2 * MJ);
           acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(both(wb[(i + ODD) & 1][h * 2], wb[(i + ODD) & 1][h * 2 + 1]),
                                                                both(wa[CUR][j][h * 2], wa[CUR][j][h * 2 + 1]), acc[i][j], 0, 0, 0);
           const int at = h * MJ + j;  // of 2 MJ places, 4 conversions of B and 4 of A in turn
@@ -394,7 +394,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
   };
   typedef std::integral_constant<int, 0> Zero;
   typedef std::integral_constant<int, 1> One;
-  auto none = [](int) __attribute__((always_inline)) {};
+  auto none = [](int, int) __attribute__((always_inline)) {};
 
   if (t0 < tw) {
     load_scales(t0);
@@ -436,22 +436,22 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_fp8_kernel(Fp8Gemm g) {
           wide_step(std::integral_constant<int, 1>{}, u_tag, SA, SB, 3, none);
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
           if (LAST && more) settle_scales();
-          wide_step(std::integral_constant<int, 2>{}, u_tag, SA1, SB ^ 1, 0, [&](int i) __attribute__((always_inline)) {
-            dma_a(t + U + 2, SA2, i * A_DMA / NI, (i + 1) * A_DMA / NI);
+          wide_step(std::integral_constant<int, 2>{}, u_tag, SA1, SB ^ 1, 0, [&](int p, int of) __attribute__((always_inline)) {
+            dma_a(t + U + 2, SA2, p * A_DMA / of, (p + 1) * A_DMA / of);
           });
-          wide_step(std::integral_constant<int, 3>{}, u_tag, SA1, SB ^ 1, 1, [&](int i) __attribute__((always_inline)) {
-            dma_b(t + U + 2, SB, i * B_DMA / NI, (i + 1) * B_DMA / NI);
+          wide_step(std::integral_constant<int, 3>{}, u_tag, SA1, SB ^ 1, 1, [&](int p, int of) __attribute__((always_inline)) {
+            dma_b(t + U + 2, SB, p * B_DMA / of, (p + 1) * B_DMA / of);
           });
           return;
         }
-        kstep(Zero{}, u_tag, SA, SB, 1, [&](int i) __attribute__((always_inline)) {
-          if constexpr (EARLY_A) dma_a(t + U + 2, SA2, i * A_DMA / NI, (i + 1) * A_DMA / NI);
+        kstep(Zero{}, u_tag, SA, SB, 1, [&](int p, int of) __attribute__((always_inline)) {
+          if constexpr (EARLY_A) dma_a(t + U + 2, SA2, p * A_DMA / of, (p + 1) * A_DMA / of);
         });
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(EARLY_A ? A_DMA : 0) : "memory");
         if (LAST && more) settle_scales();
-        kstep(One{}, u_tag, SA1, SB ^ 1, 0, [&](int i) __attribute__((always_inline)) {
-          dma_b(t + U + 2, SB, i * B_DMA / NI, (i + 1) * B_DMA / NI);
-          if constexpr (!EARLY_A) dma_a(t + U + 2, SA2, i * A_DMA / NI, (i + 1) * A_DMA / NI);
+        kstep(One{}, u_tag, SA1, SB ^ 1, 0, [&](int p, int of) __attribute__((always_inline)) {
+          dma_b(t + U + 2, SB, p * B_DMA / of, (p + 1) * B_DMA / of);
+          if constexpr (!EARLY_A) dma_a(t + U + 2, SA2, p * A_DMA / of, (p + 1) * A_DMA / of);
         });
       }, std::make_integer_sequence<int, UN>{});
       if (more) next_scales();

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(Fp8Gemm g) {
 // Estimates in us, fitted to the kernels of gemm_fp8.h on shapes of 64 .. 32768 by 300 .. 32128 by 512 .. 32768.  A k-tile of
 // a full round (`at_once` tiles: one, two or four workgroups on each of 256 compute units) takes the longer the more of the
 // chip is at work, as clocks follow power: `idle` where few tiles run, `busy` more in a full round, rising from a fill of
-// `from` on.  A round has `ends` besides.  Sharing costs a launch and the parts' way to memory and back, 5 MB a us.
+// `from` on.  A round has `ends` besides.  Sharing costs a launch and the parts' way to memory and back, 3.5 MB a us.
 // Small tiles have more loads and conversions to a matrix instruction, large ones fewer workgroups and longer ends.  Measured,
 // M x N x K and type of C, us:                tiles of 64, shared      128, shared      256, shared
 //   300 x 500 x 1024      f32                  8.5    13.1            13.4    13.3        41      28
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(Fp8Gemm g) {
 //   5120 x 2048 x 32768   f32                                          609     565       590     549
 struct TileCost { int tile, at_once; double idle, busy, from, ends; };
 constexpr TileCost kTileCost[2][3] = {
-    {{64, 1024, 0.39, 0.6, 0.25, 2.0}, {128, 512, 0.53, 0.55, 0.2, 2.5}, {256, 256, 1.1, 0.5, 0.4, 12.5}},   // bf16 C
+    {{64, 1024, 0.39, 0.6, 0.25, 2.0}, {128, 512, 0.53, 0.55, 0.2, 2.5}, {256, 256, 1.1, 0.6, 0.4, 12.5}},   // bf16 C
     {{64, 1024, 0.55, 0.85, 0.25, 2.0}, {128, 512, 0.83, 0.92, 0.2, 5.0}, {256, 256, 2.05, 1.0, 0.5, 12.5}}};  // float32 C
 
 double round_cost(const TileCost& t, double fill, double nk) {
@@ -74,7 +74,7 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
     const int64_t workers = std::min<int64_t>(slots, rest * units);
     const double run = (double)workers / slots;
     const double shared = full + round_cost(t, run, nk * rest / std::max<int64_t>(workers, 1)) + 6.0 +
-                          (double)(workers + rest) * B * B * 8 / 5e6;
+                          (double)(workers + rest) * B * B * 8 / 3.5e6;
     const bool share = rest > 0 && workers > rest && shared < alone;
     const double cost = share ? shared : alone;
     if (best >= 0.0 && cost >= best) continue;
