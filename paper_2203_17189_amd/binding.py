@@ -5,7 +5,6 @@ from __future__ import annotations
 import ctypes as C
 import operator
 import os
-import struct
 
 import torch
 
@@ -1177,8 +1176,21 @@ def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accu
     return out
 
 
-_ADAM_PACK = struct.Struct("7Qq2id")
-assert _ADAM_PACK.size == C.sizeof(_AdamTensor)
+_LISTS = None
+
+
+def _lists():
+    """The module that reads lists of tensors (csrc/torch_lists.cpp; built with the library).  Raises if it is not there."""
+    global _LISTS
+    if _LISTS is None:
+        try:
+            from . import _torch_lists
+        except ImportError:
+            from . import build as _build
+            _build.build_lists()
+            from . import _torch_lists
+        _LISTS = _torch_lists
+    return _LISTS
 
 
 def _adam_check(t, index):
@@ -1194,10 +1206,7 @@ def _adam_check(t, index):
         _check_on(device, t["v_scale"], _E8M0, -(-n // 128), "v_scale")
     if t.get("bf16_copy_out") is not None:
         _check_on(device, t["bf16_copy_out"], torch.bfloat16, n, "bf16_copy_out")
-
-
-def _adam_fits(x, dtype, n, index):
-    return x.dtype is dtype and x.numel() == n and x.get_device() == index and x.is_contiguous()
+    float(t.get("weight_decay", 0.0))
 
 
 def adamw_step_multi(tensors, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None):
@@ -1211,31 +1220,14 @@ def adamw_step_multi(tensors, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, see
     dev = tensors[0]["param"].device
     if dev.type != "cuda":
         raise ValueError(f"param: on {dev}")
-    index, f32, e4m3 = dev.index, torch.float32, torch.float8_e4m3fn
-    arr = bytearray(_ADAM_PACK.size * len(tensors))
-    at, pack, fits = 0, _ADAM_PACK.pack_into, _adam_fits  # (2 us of a call are an entry: every name counts)
-    for t in tensors:
-        p, g, m, v, lp = t["param"], t["grad"], t["m"], t["v"], t.get("bf16_copy_out")
-        n = p.numel()
-        gt = g.dtype
-        state = m.dtype
-        good = (gt is f32 or gt is torch.bfloat16) and fits(p, f32, n, index) and fits(g, gt, n, index) and \
-            (state is f32 or state is e4m3) and fits(m, state, n, index) and fits(v, state, n, index) and \
-            (lp is None or fits(lp, torch.bfloat16, n, index))
-        if state is f32:
-            ms = vs = 0
-        elif good:
-            ms, vs = t["m_scale"], t["v_scale"]
-            good = fits(ms, _E8M0, (n + 127) // 128, index) and fits(vs, _E8M0, (n + 127) // 128, index)
-            ms, vs = ms.data_ptr(), vs.data_ptr()
-        if not good:
-            _adam_check(t, index)
-            raise ValueError("adamw_step_multi: an entry's tensors do not belong together")
-        pack(arr, at, p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs, 0 if lp is None else lp.data_ptr(), n,
-             T5_F32 if gt is f32 else T5_BF16, 32 if state is f32 else 8, t.get("weight_decay", 0.0))
-        at += _ADAM_PACK.size
+    tensors = list(tensors)
+    arr = bytearray(C.sizeof(_AdamTensor) * len(tensors))
+    good = _lists().adamw_entries(tensors, dev.index, arr)
+    if good != len(tensors):
+        _adam_check(tensors[good], dev.index)
+        raise ValueError(f"adamw_step_multi: entry {good} is no dict of tensors")
     if grad_scale is not None:
-        _check_on(dev, grad_scale, f32, 1, "grad_scale")
+        _check_on(dev, grad_scale, torch.float32, 1, "grad_scale")
         grad_scale = grad_scale.data_ptr()
     seed = operator.index(seed)
     cfg = _AdamCfg(float(lr), float(beta1), float(beta2), float(eps), _i32(step), seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF,

@@ -55,7 +55,8 @@ hipError_t launch_gemm_fp8_44(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_45(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_54(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_55(const Fp8Gemm& g, hipStream_t st);
-// Without tiles, M <= 64 (gemm_fp8_rows.hip).
+// Without tiles, M <= 64 (gemm_fp8_rows.hip), and how many times 16 rows of B a workgroup has there.
+int fp8_rows_of_b(int M, int N);
 hipError_t launch_gemm_fp8_rows(const Fp8Gemm& g, int ta, int tb, hipStream_t st);
 
 namespace {
@@ -67,6 +68,8 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 __device__ __forceinline__ int fp8_swz(int row) { return (row ^ (row >> 3)) & 7; }
 
 typedef __attribute__((address_space(3))) const i32x4 lds_i32x4;
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 
 // Four codes, or eight, as bfloat16, times 2^(byte - 127).
 template <int T>
@@ -117,7 +120,8 @@ template <int NI, int MJ, typename T>
 __device__ __forceinline__ void fp8_store_tile(f32x16 (&acc)[NI][MJ], char* lds, T* C, int64_t ld, int m, int n, int m_own, int n_own,
                                                int M, int N, bool add, int lane, bool again) {
   constexpr int COLS = NI * 32, PITCH = COLS * (int)sizeof(T) + 16, EPV = 16 / sizeof(T), LPR = COLS / EPV;  // lanes of a row
-  const bool vec = ((uintptr_t)(C + n) & 15) == 0 && (ld * (int64_t)sizeof(T)) % 16 == 0 && n >= n_own && n + COLS <= N;
+  typedef std::conditional_t<sizeof(T) == 4, u32x4_at4, u32x4_at2> Piece;  // (rows of any alignment: the part takes whole pieces anywhere)
+  const bool inside = n >= n_own && n + COLS <= N;
 #pragma unroll
   for (int j = 0; j < MJ; ++j) {
     char* to = lds + (lane & 31) * PITCH + (lane >> 5) * 4 * (int)sizeof(T);
@@ -131,37 +135,24 @@ __device__ __forceinline__ void fp8_store_tile(f32x16 (&acc)[NI][MJ], char* lds,
         else *reinterpret_cast<f32x4*>(at) = f32x4{a, b, c, d};
       }
     const int mj = m + j * 32;
-    if (vec) {
 #pragma unroll
-      for (int k = 0; k < 32 * LPR / 64; ++k) {
-        const int row = (k * 64 + lane) / LPR, col = (lane % LPR) * EPV;
-        u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * PITCH + col * (int)sizeof(T));
-        if (mj + row < m_own || mj + row >= M) continue;
-        T* p = C + (int64_t)(mj + row) * ld + n + col;
+    for (int k = 0; k < 32 * LPR / 64; ++k) {
+      const int row = (k * 64 + lane) / LPR, col = (lane % LPR) * EPV;
+      u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * PITCH + col * (int)sizeof(T));
+      if (mj + row < m_own || mj + row >= M) continue;
+      T* p = C + (int64_t)(mj + row) * ld + n + col;
+      if (inside || (n + col >= n_own && n + col + EPV <= N)) {
         if constexpr (sizeof(T) == 4)
-          if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + *reinterpret_cast<const f32x4*>(p));
+          if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + __builtin_bit_cast(f32x4, (u32x4)*reinterpret_cast<const Piece*>(p)));
         // (C is not read again here, parts are, soon: 4096 x 32128 x 768 147 us against 152, 3000 x 3000 x 1024 in parts 50 against 72)
-        if (again) *reinterpret_cast<u32x4*>(p) = v;
-        else __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
-      }
-    } else {
-      // element by element, a row's neighbours side by side
-      constexpr int AT_ONCE = 8, WIDE = COLS < 64 ? COLS : 64, CHUNKS = COLS / WIDE;
-      for (int r0 = 0; r0 < 32; r0 += AT_ONCE * (64 / WIDE)) {
+        if (again) *reinterpret_cast<Piece*>(p) = v;
+        else __builtin_nontemporal_store(v, reinterpret_cast<Piece*>(p));
+      } else {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-          const int col = c * WIDE + lane % WIDE, r1 = r0 + lane / WIDE * AT_ONCE;
-          const bool on = n + col >= n_own && n + col < N;
-          T v[AT_ONCE];
-#pragma unroll
-          for (int r = 0; r < AT_ONCE; ++r) v[r] = *reinterpret_cast<const T*>(lds + (r1 + r) * PITCH + col * (int)sizeof(T));
-          T* p = C + (int64_t)(mj + r1) * ld + n + col;
-#pragma unroll
-          for (int r = 0; r < AT_ONCE; ++r)
-            if (on && mj + r1 + r >= m_own && mj + r1 + r < M) {
-              if constexpr (sizeof(T) == 4) p[r * ld] = add ? p[r * ld] + v[r] : v[r];
-              else p[r * ld] = v[r];
-            }
+        for (int i = 0; i < EPV; ++i) {
+          if (n + col + i < n_own || n + col + i >= N) continue;
+          if constexpr (sizeof(T) == 4) p[i] = add ? p[i] + __uint_as_float(v[i]) : __uint_as_float(v[i]);
+          else p[i] = __builtin_bit_cast(bf16, (uint16_t)(v[i >> 1] >> ((i & 1) * 16)));
         }
       }
     }

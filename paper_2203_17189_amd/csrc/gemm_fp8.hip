@@ -56,12 +56,17 @@ double round_cost(const TileCost& t, double fill, double nk) {
   return nk * (t.idle + t.busy * std::max(0.0, fill - t.from) / (1.0 - t.from)) + t.ends;
 }
 
-bool few_rows(const t5_gemm_fp8_cfg& c) { return c.M <= 32 || (c.M <= 64 && (int64_t)c.N * c.K <= (16 << 20)); }
+// Few rows, without tiles: a wavefront's blocks of k one after the other, or B's bytes and A's for each workgroup.
+//   16 x 2048 x 16384: 23 us, 16 x 8192 x 8192: 24, 32 x 2048 x 16384: 45, 64 x 8192 x 8192: 38 (in tiles 25, 29, 25, 29)
+double rows_cost(const t5_gemm_fp8_cfg& c) {
+  const int mt = c.M <= 16 ? 1 : c.M <= 32 ? 2 : 4, nt = fp8_rows_of_b(c.M, c.N);
+  const double chain = 3.0 + (mt == 1 ? 1.25 : mt == 2 ? 2.6 : 4.0) * ceil_div(ceil_div(c.K, 128), c.K > 1024 || nt > 1 ? 8 : 4);
+  return std::max(chain, 1.0 + (double)c.N * c.K * (1.0 + (double)mt / nt) / 5.8e6);
+}
 
 void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
   g->shared = g->workers = 0;
-  g->few = few_rows(c);
-  if (g->few) return;
+  g->few = 0;
   const int units = ceil_div(c.K, 512);
   const double nk = c.K / 128.0;
   double best = -1.0;
@@ -82,6 +87,10 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
     g->tile = B; g->tiles_m = tm; g->tiles_n = tn;
     g->shared = share ? (int)rest : 0;
     g->workers = share ? (int)workers : 0;
+  }
+  if (c.M <= 64 && rows_cost(c) <= best) {
+    g->few = 1;
+    g->shared = g->workers = 0;
   }
 }
 

@@ -135,20 +135,18 @@ __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
 
 template <int TA, int TB, bool F32>
 hipError_t launch(const Fp8Gemm& g, hipStream_t st) {
-  // Rows of B a workgroup: as many as leave at least two workgroups to a compute unit, as each reads A anew.
-  const int n16 = ceil_div(g.N, 16);
-  const int nt = n16 >= 2048 ? 4 : n16 >= 1024 ? 2 : 1;
-  const auto grid = [&](int rows) { return (unsigned)ceil_div(n16, rows); };
+  const int nt = fp8_rows_of_b(g.M, g.N);
+  const unsigned grid = (unsigned)ceil_div(g.N, 16 * nt);
   if (g.M <= 16) {
-    if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 1, 4, 8, 2><<<grid(4), 512, 0, st>>>(g);
-    else if (nt == 2) gemm_fp8_rows_kernel<TA, TB, F32, 1, 2, 8, 2><<<grid(2), 512, 0, st>>>(g);
-    else if (g.K > 1024) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 8, 4><<<grid(1), 512, 0, st>>>(g);
-    else gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 4, 2><<<grid(1), 256, 0, st>>>(g);
+    if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 1, 4, 8, 2><<<grid, 512, 0, st>>>(g);
+    else if (nt == 2) gemm_fp8_rows_kernel<TA, TB, F32, 1, 2, 8, 2><<<grid, 512, 0, st>>>(g);
+    else if (g.K > 1024) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 8, 4><<<grid, 512, 0, st>>>(g);
+    else gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 4, 2><<<grid, 256, 0, st>>>(g);
   } else if (g.M <= 32) {
-    if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 2, 4, 8, 2><<<grid(4), 512, 0, st>>>(g);
-    else gemm_fp8_rows_kernel<TA, TB, F32, 2, 2, 8, 2><<<grid(2), 512, 0, st>>>(g);
+    if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 2, 4, 8, 2><<<grid, 512, 0, st>>>(g);
+    else gemm_fp8_rows_kernel<TA, TB, F32, 2, 2, 8, 2><<<grid, 512, 0, st>>>(g);
   } else {
-    gemm_fp8_rows_kernel<TA, TB, F32, 4, 2, 8, 1><<<grid(2), 512, 0, st>>>(g);
+    gemm_fp8_rows_kernel<TA, TB, F32, 4, 2, 8, 1><<<grid, 512, 0, st>>>(g);
   }
   return hipGetLastError();
 }
@@ -156,6 +154,13 @@ template <int TA, int TB>
 hipError_t launch(const Fp8Gemm& g, hipStream_t st) { return g.out_bf16 ? launch<TA, TB, false>(g, st) : launch<TA, TB, true>(g, st); }
 
 }  // namespace
+
+// As many as leave two workgroups to a compute unit, as each reads A anew (32128 x 2048: 16 rows of A 20.9 us, like this 17.0).
+int fp8_rows_of_b(int M, int N) {
+  const int n16 = ceil_div(N, 16);
+  if (M > 32) return 2;
+  return n16 >= 2048 ? 4 : n16 >= 1024 || M > 16 ? 2 : 1;
+}
 
 hipError_t launch_gemm_fp8_rows(const Fp8Gemm& g, int ta, int tb, hipStream_t st) {
   if (ta == T5_E4M3) return tb == T5_E4M3 ? launch<T5_E4M3, T5_E4M3>(g, st) : launch<T5_E4M3, T5_E5M2>(g, st);

@@ -179,3 +179,30 @@ def test_same_bits_every_time_and_others_for_another_step_or_seed():
     assert (runs[0] == runs[1]).all()
     for other in runs[2:]:
         assert 0.2 < (other != runs[0]).mean() < 0.8
+
+
+def test_entries_that_do_not_belong_together_are_refused_before_anything_is_written():
+    good = lambda: make(np.random.default_rng(1), 300, 8, copy=True)  # noqa: E731
+    cut = lambda k: {k: lambda t: t[k][:-1]}  # noqa: E731
+    wrong = [cut("grad"), cut("m"), cut("v"), cut("m_scale"), cut("v_scale"), cut("bf16_copy_out"), {"grad": lambda t: t["grad"].half()},
+             {"param": lambda t: t["param"].double()}, {"m": lambda t: t["m"].view(torch.uint8)}, {"v": lambda t: t["v"].float()},
+             {"grad": lambda t: t["grad"].cpu()}, {"grad": lambda t: torch.zeros(600, device="cuda")[::2]}, {"m_scale": lambda t: t["m_scale"].view(torch.uint8)},
+             {"bf16_copy_out": lambda t: t["bf16_copy_out"].float()}, {"weight_decay": lambda t: "much"}, {"grad": lambda t: None}, {"m": lambda t: 3}]
+    for change in wrong:
+        ts = [good(), good(), good()]
+        (k, f), = change.items()
+        ts[1][k] = f(ts[1])
+        before = ts[0]["param"].clone()
+        with pytest.raises((ValueError, TypeError, AttributeError)):
+            P.adamw_step_multi(ts, step=1, **HP)
+        assert torch.equal(ts[0]["param"], before)
+    ts = [good(), good()]
+    del ts[1]["v"]
+    with pytest.raises(KeyError):
+        P.adamw_step_multi(ts, step=1, **HP)
+    t = good()
+    with pytest.raises(P.T5Error):  # the same tensor twice
+        P.adamw_step_multi([t, t], step=1, **HP)
+    with pytest.raises(P.T5Error):
+        P.adamw_step_multi([t], step=0, **HP)
+    P.adamw_step_multi((t,), step=1, **HP)  # a tuple is a list too
