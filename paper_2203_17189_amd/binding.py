@@ -1059,6 +1059,26 @@ def t5_distill_loss_and_grad(logits, targets, teacher_logits, teacher_ids, tempe
     return loss, row_loss, dlogits
 
 
+_LISTS = None
+
+
+def _lists():
+    """The native readers of tensors (csrc/torch_lists.cpp; built with the library) and the entry points that they call.  Raises if they are not there."""
+    global _LISTS
+    if _LISTS is None:
+        try:
+            from . import _torch_lists
+        except ImportError:
+            from . import build as _build
+            _build.build_lists()
+            from . import _torch_lists
+        L = lib()
+        addr = lambda fn: C.cast(fn, C.c_void_p).value
+        _LISTS = (_torch_lists.quantize_fp8, addr(L.t5_quantize_fp8), _torch_lists.gemm_fp8, addr(L.t5_gemm_fp8),
+                  addr(L.t5_gemm_fp8_workspace_bytes), _torch_lists.adamw_entries)
+    return _LISTS
+
+
 _FP8 = {torch.float8_e4m3fn: T5_E4M3, torch.float8_e5m2: T5_E5M2}
 _FP8_NAMES = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
 _E8M0 = torch.float8_e8m0fnu
@@ -1091,10 +1111,17 @@ def t5_quantize_fp8(x, q_dtype="e4m3", block_rows=1, rows=True, transposed=False
     type).  A scale (float8_e8m0fnu) serves 128 columns of one row, or of 128 rows with block_rows=128; with block_rows=1 the
     transposed matrix has scales of its own, for 128 rows of one column of x.  Outputs of the caller's own have rows as far
     apart as the ones made here: codes a multiple of 16, scales a multiple of 4."""
+    dt = _FP8_NAMES.get(q_dtype, q_dtype)
+    dev = x.device
+    if q is None and scale is None and qt is None and scale_t is None and dev.type == "cuda" and dev.index == _current_device() and dt in _FP8:
+        lists = _LISTS or _lists()  # (the ordinary call; what it does not take is checked below)
+        out = lists[0](lists[1], x, 1 if _FP8[dt] == T5_E5M2 else 0, block_rows, rows, transposed, _raw_stream(dev.index), dev.index)
+        if type(out) is tuple:
+            return out
+        if out:
+            raise T5Error(out, "t5_quantize_fp8")
     ty = _elem_type(x, "x")
     n, cols, ld = _check_rows(x, "x")
-    dev = x.device
-    dt = _FP8_NAMES.get(q_dtype, q_dtype)
     if dt not in _FP8:
         raise ValueError(f"q_dtype: need e4m3 or e5m2, got {q_dtype}")
     block_rows = operator.index(block_rows)
@@ -1145,9 +1172,16 @@ def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accu
     """C[m, n] = sum over k of A[m, k] B[n, k] of two quantised matrices as t5_quantize_fp8 makes them (one scale for each
     128 columns of a row, or of 128 rows: by the scales' shape).  out: [M, N] float32 or bfloat16, rows may have a longer
     stride; accumulate adds to it (float32).  Returns out."""
+    dev = a.device
+    if workspace is None and dev.type == "cuda" and dev.index == _current_device() and out_dtype in (torch.bfloat16, torch.float32):
+        lists = _LISTS or _lists()  # (the ordinary call; what it does not take is checked below)
+        made = lists[2](lists[3], lists[4], a, a_scale, b, b_scale, out, out_dtype is torch.float32, accumulate, _raw_stream(dev.index), dev.index)
+        if isinstance(made, torch.Tensor):
+            return made
+        if made:
+            raise T5Error(made, "t5_gemm_fp8")
     m, k, lda, ta, bra, lsa = _fp8_operand(a, a_scale, "a")
     n, kb, ldb, tb, brb, lsb = _fp8_operand(b, b_scale, "b")
-    dev = a.device
     if k != kb:
         raise ValueError(f"a has {k} columns, b {kb}")
     if b.device != dev or a_scale.device != dev or b_scale.device != dev:
@@ -1174,23 +1208,6 @@ def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accu
     _call(L.t5_gemm_fp8, "t5_gemm_fp8", dev, cfg, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
           out.data_ptr(), ws, nbytes)
     return out
-
-
-_LISTS = None
-
-
-def _lists():
-    """The module that reads lists of tensors (csrc/torch_lists.cpp; built with the library).  Raises if it is not there."""
-    global _LISTS
-    if _LISTS is None:
-        try:
-            from . import _torch_lists
-        except ImportError:
-            from . import build as _build
-            _build.build_lists()
-            from . import _torch_lists
-        _LISTS = _torch_lists
-    return _LISTS
 
 
 def _adam_check(t, index):
@@ -1222,7 +1239,7 @@ def adamw_step_multi(tensors, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, see
         raise ValueError(f"param: on {dev}")
     tensors = list(tensors)
     arr = bytearray(C.sizeof(_AdamTensor) * len(tensors))
-    good = _lists().adamw_entries(tensors, dev.index, arr)
+    good = (_LISTS or _lists())[5](tensors, dev.index, arr)
     if good != len(tensors):
         _adam_check(tensors[good], dev.index)
         raise ValueError(f"adamw_step_multi: entry {good} is no dict of tensors")

@@ -135,24 +135,41 @@ __device__ __forceinline__ void fp8_store_tile(f32x16 (&acc)[NI][MJ], char* lds,
         else *reinterpret_cast<f32x4*>(at) = f32x4{a, b, c, d};
       }
     const int mj = m + j * 32;
+    const auto piece = [&](int k, int& row, int& col) __attribute__((always_inline)) {
+      row = (k * 64 + lane) / LPR;
+      col = (lane % LPR) * EPV;
+      return *reinterpret_cast<const u32x4*>(lds + row * PITCH + col * (int)sizeof(T));
+    };
+    const auto put = [&](T* p, u32x4 v) __attribute__((always_inline)) {
+      if constexpr (sizeof(T) == 4)
+        if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + __builtin_bit_cast(f32x4, (u32x4)*reinterpret_cast<const Piece*>(p)));
+      // (C is not read again here, parts are, soon: 4096 x 32128 x 768 147 us against 152, 3000 x 3000 x 1024 in parts 50 against 72)
+      if (again) *reinterpret_cast<Piece*>(p) = v;
+      else __builtin_nontemporal_store(v, reinterpret_cast<Piece*>(p));
+    };
+    if (inside && mj >= m_own && mj + 32 <= M) {  // nothing to decide between a read and its store: they overlap
 #pragma unroll
-    for (int k = 0; k < 32 * LPR / 64; ++k) {
-      const int row = (k * 64 + lane) / LPR, col = (lane % LPR) * EPV;
-      u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * PITCH + col * (int)sizeof(T));
-      if (mj + row < m_own || mj + row >= M) continue;
-      T* p = C + (int64_t)(mj + row) * ld + n + col;
-      if (inside || (n + col >= n_own && n + col + EPV <= N)) {
-        if constexpr (sizeof(T) == 4)
-          if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + __builtin_bit_cast(f32x4, (u32x4)*reinterpret_cast<const Piece*>(p)));
-        // (C is not read again here, parts are, soon: 4096 x 32128 x 768 147 us against 152, 3000 x 3000 x 1024 in parts 50 against 72)
-        if (again) *reinterpret_cast<Piece*>(p) = v;
-        else __builtin_nontemporal_store(v, reinterpret_cast<Piece*>(p));
-      } else {
+      for (int k = 0; k < 32 * LPR / 64; ++k) {
+        int row, col;
+        const u32x4 v = piece(k, row, col);
+        put(C + (int64_t)(mj + row) * ld + n + col, v);
+      }
+    } else {
 #pragma unroll
-        for (int i = 0; i < EPV; ++i) {
-          if (n + col + i < n_own || n + col + i >= N) continue;
-          if constexpr (sizeof(T) == 4) p[i] = add ? p[i] + __uint_as_float(v[i]) : __uint_as_float(v[i]);
-          else p[i] = __builtin_bit_cast(bf16, (uint16_t)(v[i >> 1] >> ((i & 1) * 16)));
+      for (int k = 0; k < 32 * LPR / 64; ++k) {
+        int row, col;
+        const u32x4 v = piece(k, row, col);
+        if (mj + row < m_own || mj + row >= M) continue;
+        T* p = C + (int64_t)(mj + row) * ld + n + col;
+        if (n + col >= n_own && n + col + EPV <= N) {
+          put(p, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < EPV; ++i) {
+            if (n + col + i < n_own || n + col + i >= N) continue;
+            if constexpr (sizeof(T) == 4) p[i] = add ? p[i] + __uint_as_float(v[i]) : __uint_as_float(v[i]);
+            else p[i] = __builtin_bit_cast(bf16, (uint16_t)(v[i >> 1] >> ((i & 1) * 16)));
+          }
         }
       }
     }

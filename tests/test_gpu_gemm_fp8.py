@@ -130,3 +130,45 @@ def test_no_rows():
     b, sb, _ = operand(rng, 64, 256, "e4m3", 1)
     c = P.t5_gemm_fp8(b[:0], sb[:0], b, sb)
     assert c.shape == (0, 64)
+
+
+def test_refusals_that_need_tensors():
+    rng = np.random.default_rng(1)
+    a, sa, _ = operand(rng, 40, 300, "e4m3", 1)
+    b, sb, _ = operand(rng, 64, 300, "e5m2", 128)
+    f = P.t5_gemm_fp8
+    out = torch.zeros(40, 64, device="cuda")
+    u8, e8 = torch.uint8, torch.float8_e8m0fnu
+    tight = torch.zeros(40 * 304 - 4, dtype=u8, device="cuda").as_strided((40, 300), (304, 1)).view(torch.float8_e4m3fn)  # ends inside a piece
+    tight_s = torch.zeros(40 * 4 - 1, dtype=u8, device="cuda").as_strided((40, 3), (4, 1)).view(e8)
+    for args in ((a.view(u8), sa, b, sb), (a, sa.view(u8), b, sb), (a[:, :299], sa, b[:, :298], sb), (a, sa[:, :2], b, sb), (a, sa[:39], b, sb),
+                 (a, sa, b, sb[:0]), (a.cpu(), sa, b, sb), (a, sa.cpu(), b, sb), (a, sa, b, sb.cpu()), (a.t(), sa, b, sb), (a[0], sa, b, sb),
+                 (tight, sa, b, sb), (a, tight_s, b, sb)):
+        with pytest.raises(ValueError):
+            f(*args)
+    for kw in (dict(out=out[:39]), dict(out=out.t()), dict(out=out.half()), dict(out=out.cpu()), dict(accumulate=True),
+               dict(workspace=torch.zeros(8, device="cuda")), dict(out_dtype=torch.float16)):
+        with pytest.raises(ValueError):
+            f(a, sa, b, sb, **kw)
+    wide = torch.zeros(40, 312, dtype=u8, device="cuda").view(torch.float8_e4m3fn)[:, :300]  # rows 312 bytes apart
+    for args, kw in (((wide, sa, b, sb), {}), ((a, sa, b, sb), dict(out=out.bfloat16(), accumulate=True)),
+                     ((a.view(u8)[:, 1:257].view(torch.float8_e4m3fn), sa[:, :2], b[:, :256], sb[:, :2]), {})):
+        with pytest.raises(P.T5Error) as e:
+            f(*args, **kw)
+        assert e.value.status == 3
+    m, n, k = 300, 300, 40000
+    a, sa, _ = operand(rng, m, k, "e4m3", 1)
+    with pytest.raises(P.T5Error) as e:
+        f(a, sa, a, sa, workspace=torch.zeros(256, dtype=u8, device="cuda"))
+    assert e.value.status == 4
+
+
+def test_rows_of_few_bytes():
+    """One row may be of any length and end anywhere; a workspace of the caller's own."""
+    rng = np.random.default_rng(2)
+    for k in (1, 15, 16, 17, 127, 129, 500):
+        a, sa, va = operand(rng, 1, k, "e4m3", 1)
+        b, sb, vb = operand(rng, 9, k, "e4m3", 1)
+        c = P.t5_gemm_fp8(a, sa, b, sb, out_dtype=torch.float32, workspace=torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"))
+        assert (np.abs(host(c) - va @ vb.T) <= product_bound(va, vb, va @ vb.T, "f32")).all()
+        assert torch.equal(c, P.t5_gemm_fp8(a, sa, b, sb, out_dtype=torch.float32))

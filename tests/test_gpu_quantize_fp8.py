@@ -93,3 +93,21 @@ def test_no_rows():
     x = torch.empty(0, 64, device="cuda")
     q, s, qt, st = P.t5_quantize_fp8(x, transposed=True)
     assert q.shape == (0, 64) and s.shape == (0, 1) and qt.shape == (64, 0) and st.shape == (64, 0)
+
+
+def test_refusals_that_need_tensors():
+    x = torch.zeros(8, 200, device="cuda")
+    f = P.t5_quantize_fp8
+    for args, kw in (((x[0],), {}), ((x.half(),), {}), ((x.t(),), {}), ((x, "e3m4"), {}), ((x, torch.float32), {}),
+                     ((x,), dict(q=torch.zeros(8, 200, dtype=FP8["e4m3"], device="cuda"))), ((x,), dict(scale=torch.zeros(8, 2, dtype=torch.uint8, device="cuda").view(E8M0))),
+                     ((x,), dict(transposed=True, qt=torch.zeros(200, 8, dtype=FP8["e5m2"], device="cuda"), scale_t=None))):
+        with pytest.raises(ValueError):
+            f(*args, **kw)
+    good = f(x)
+    with pytest.raises(ValueError):  # rows that are no multiple of 16 bytes apart
+        f(x, q=torch.zeros(8, 200, dtype=torch.uint8, device="cuda").view(FP8["e4m3"]), scale=good[1])
+    for rows in (0, 2, 64, 129):
+        with pytest.raises(P.T5Error):
+            f(x, block_rows=rows)
+    with pytest.raises(P.T5Error):
+        f(x, rows=False)
