@@ -4,7 +4,8 @@
  * decoder layer with cross-attention): forward, backward, relative-position
  * buckets and the Adafactor update of its weights; of whole stacks of such
  * layers with embedding, final norm, logits and loss (one stack, or the
- * encoder-decoder pair); and of the dropout mask generator they share.
+ * encoder-decoder pair); of the dropout mask generator they share; and of
+ * linear layers trained in 8 bits, with AdamW.
  *
  * The paper (Sec. 4, "Example models") ships T5.1.1 and a decoder-only model as
  * its reference architectures and Sec. 2.3 describes them as ordinary layer
