@@ -538,7 +538,8 @@ int t5_gemm_bf16(const void* A, const void* B, float* C, int M, int N, int K, in
  * with b / s <= M, not below 2^-127 (1 where b = 0);  code = x / s rounded to nearest, ties to even.  NaN becomes NaN;
  * infinities become NaN in T5_E4M3 and stay infinities in T5_E5M2.  Either pair of outputs may be NULL.  rows == 0 is a no-op.
  * Errors: rows < 0, cols < 1, ld < cols, block_rows neither 1 nor 128 -> T5_ERR_SHAPE; x NULL, no output, or one of a pair
- * without the other -> T5_ERR_NULL; rows > 2^31 - 129, cols > 2^23, ld > 2^32, unknown types, q or qt not 16-byte aligned,
+ * without the other -> T5_ERR_NULL; rows > 2^31 - 129, cols > 2^23, ld > 2^32, 2^23 or more tiles of 128 x 128 (rows alone,
+ * block_rows == 1: rows * t5_fp8_scale_ld(cols) from 2^29 on), unknown types, q or qt not 16-byte aligned,
  * scale or scale_t not 4-byte aligned -> T5_ERR_UNSUPPORTED. */
 typedef struct {
   int64_t rows, cols, ld;
@@ -589,10 +590,11 @@ int t5_gemm_fp8(const t5_gemm_fp8_cfg* cfg, const void* A, const uint8_t* a_scal
  *   h = mix32(mix32(mix32(mix32(seed_lo ^ step) ^ i * 0x9E3779B9) ^ b ^ seed_hi) ^ c),
  * u = (h mod 2^16) / 2^16 for m, (h div 2^16) / 2^16 for sqrt(v).  The same bits every time for the same arguments.
  * A gradient that is not finite makes the element's parameter NaN and its states not finite (its neighbours' are as without
- * it).  Tensors share no memory.  Every entry is checked before the first launch.
+ * it).  Tensors share no memory.  Every entry is checked before the first launch.  step, lr and the other numbers are those
+ * of the call: captured into a graph, it repeats them (grad_scale is read each time).
  * Errors: NULL -> T5_ERR_NULL; n_tensors < 1, n < 1, step < 1, lr or weight_decay < 0 or not finite, beta1 or beta2 outside
  * [0, 1), eps below 1e-30 or not finite, parameters of two
- * entries that overlap -> T5_ERR_SHAPE; n_tensors > 65536, n > 2^36, state_bits neither
+ * entries that overlap -> T5_ERR_SHAPE; n_tensors > 65536, n > 2^34, state_bits neither
  * 8 nor 32, unknown grad_dtype, a pointer not aligned to its elements -> T5_ERR_UNSUPPORTED. */
 typedef struct {
   float* param;

@@ -1232,12 +1232,12 @@ def adamw_step_multi(tensors, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, see
     8 bits: m and v float8_e4m3fn, codes of m and of sqrt(v), with m_scale and v_scale float8_e8m0fnu, one for each 128
     consecutive elements; zeros throughout before the first step (t.zero_() of a uint8 view).  seed: of their random rounding;
     grad_scale: a float32 tensor of one element that multiplies every gradient, or None."""
-    if not tensors:
+    tensors = list(tensors)
+    if not tensors or not 0 < operator.index(step) < 2 ** 31:
         raise T5Error(2, "adamw_step_multi")
     dev = tensors[0]["param"].device
     if dev.type != "cuda":
         raise ValueError(f"param: on {dev}")
-    tensors = list(tensors)
     arr = bytearray(C.sizeof(_AdamTensor) * len(tensors))
     good = (_LISTS or _lists())[5](tensors, dev.index, arr)
     if good != len(tensors):
@@ -1247,7 +1247,7 @@ def adamw_step_multi(tensors, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, see
         _check_on(dev, grad_scale, torch.float32, 1, "grad_scale")
         grad_scale = grad_scale.data_ptr()
     seed = operator.index(seed)
-    cfg = _AdamCfg(float(lr), float(beta1), float(beta2), float(eps), _i32(step), seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF,
+    cfg = _AdamCfg(float(lr), float(beta1), float(beta2), float(eps), operator.index(step), seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF,
                    grad_scale)
     _call(lib().adamw_step_multi, "adamw_step_multi", dev, (_AdamTensor * len(tensors)).from_buffer(arr), len(tensors), C.byref(cfg))
 

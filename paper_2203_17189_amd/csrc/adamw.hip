@@ -252,7 +252,7 @@ hipError_t launch_adamw(const adamw_tensor* t, int n, int first, const adamw_cfg
     it.flags = (t[i].state_bits == 8 ? AW_8BIT : 0) | (t[i].grad_dtype == T5_BF16 ? AW_BF16_GRAD : 0) | (odd == 0 ? AW_VEC : 0);
     b.start[i] = (int32_t)chunks;
     chunks += (t[i].n + kChunk - 1) / kChunk;
-    if (chunks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (chunks >= (1 << 24)) return hipErrorInvalidValue;
   }
   b.start[n] = (int32_t)chunks;
   adamw_kernel<<<(unsigned)chunks, kThreads, 0, st>>>(b);

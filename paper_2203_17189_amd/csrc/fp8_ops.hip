@@ -5,7 +5,8 @@
 
 namespace {
 
-constexpr int kAdamMaxListed = 1 << 16;  // tensors one adamw_step_multi call may list
+constexpr int kAdamMaxListed = 1 << 16;           // tensors one adamw_step_multi call may list
+constexpr int64_t kAdamMost = (int64_t)1 << 34;   // elements of a tensor, and of a launch
 
 bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 bool fp8_type(int32_t t) { return t == T5_E4M3 || t == T5_E5M2; }
@@ -31,7 +32,7 @@ bool positive(double x) { return x >= 0.0 && std::isfinite(x); }
 
 int check_adam_tensor(const adamw_tensor& t) {
   if (t.n < 1 || !positive(t.weight_decay)) return T5_ERR_SHAPE;
-  if (t.n > ((int64_t)1 << 36) || (t.state_bits != 8 && t.state_bits != 32) || (t.grad_dtype != T5_F32 && t.grad_dtype != T5_BF16))
+  if (t.n > kAdamMost || (t.state_bits != 8 && t.state_bits != 32) || (t.grad_dtype != T5_F32 && t.grad_dtype != T5_BF16))
     return T5_ERR_UNSUPPORTED;
   if (!t.param || !t.grad || !t.m || !t.v || (t.state_bits == 8 && (!t.m_scale || !t.v_scale))) return T5_ERR_NULL;
   const uintptr_t state = t.state_bits == 8 ? 1 : 4;
@@ -67,6 +68,9 @@ int t5_quantize_fp8(const t5_quantize_cfg* cfg, const void* x, void* q, uint8_t*
   if (cfg->rows < 0 || cfg->cols < 1 || cfg->ld < cfg->cols || !block_rows_ok(cfg->block_rows)) return T5_ERR_SHAPE;
   if (cfg->rows > ((int64_t)1 << 31) - 129 || cfg->cols > (1 << 23) || cfg->ld > ((int64_t)1 << 32) ||
       (cfg->dtype != T5_F32 && cfg->dtype != T5_BF16) || !fp8_type(cfg->q_dtype))
+    return T5_ERR_UNSUPPORTED;
+  // (threads of a launch are numbered with 32 bits: 256 for 32 blocks of a row, 512 for a tile)
+  if (qt || cfg->block_rows == 128 ? blocks_of(cfg->rows) * blocks_of(cfg->cols) >= (1 << 23) : cfg->rows * fp8_scale_ld(cfg->cols) >= (1 << 29))
     return T5_ERR_UNSUPPORTED;
   if (cfg->rows == 0) return T5_OK;
   if (!x || (!q && !qt) || !q != !scale || !qt != !scale_t) return T5_ERR_NULL;
@@ -114,8 +118,14 @@ int adamw_step_multi(const adamw_tensor* tensors, int n_tensors, const adamw_cfg
   const int rc = check_disjoint(tensors, n_tensors);
   if (rc != T5_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
-  for (int i = 0; i < n_tensors; i += kAdamTensors)
-    T5_STEP("adamw", launch_adamw(tensors + i, std::min(kAdamTensors, n_tensors - i), i, *cfg, st));
+  for (int i = 0; i < n_tensors;) {
+    int m = 0;
+    int64_t elements = 0;  // (threads of a launch are numbered with 32 bits, each has 8 elements)
+    do elements += tensors[i + m++].n;
+    while (m < kAdamTensors && i + m < n_tensors && elements + tensors[i + m].n <= kAdamMost);
+    T5_STEP("adamw", launch_adamw(tensors + i, m, i, *cfg, st));
+    i += m;
+  }
   return T5_OK;
 }
 

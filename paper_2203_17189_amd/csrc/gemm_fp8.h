@@ -41,6 +41,9 @@ struct Fp8Gemm {
   float* part;  // what a worker adds up of a tile that others have parts of, a tile of float32: at place worker + tile
 };
 
+// Workgroups of 256 threads in one launch, whose threads are numbered with 32 bits (of 512: half of that).
+constexpr int64_t kMostWorkgroups = (1 << 24) - 1;
+
 // Units of a tile; the worker that has unit u of the shared tiles; its first unit.
 __host__ __device__ inline int fp8_units(const Fp8Gemm& g) { return (g.K + 511) >> 9; }
 __host__ __device__ inline int fp8_worker(const Fp8Gemm& g, int64_t u) {
@@ -543,14 +546,17 @@ template <int BM, int BN, int WM, int WN, int TA, int TB, bool F32, int AST>
 hipError_t launch_fp8_tiles(const Fp8Gemm& g, hipStream_t st) {
   auto kern = gemm_fp8_kernel<BM, BN, WM, WN, TA, TB, F32, AST>;
   constexpr int lds = std::max((AST * BM + 2 * BN) * 128, WM * WN * fp8_store_bytes<BN / WN / 32>);
-  static std::atomic<bool> attr_set{false};  // once per instantiation; setting it twice is harmless
-  if (!attr_set.load(std::memory_order_relaxed)) {
-    const hipError_t err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  static std::atomic<uint64_t> attr_set{0};  // once per instantiation and device; setting it twice is harmless
+  int device = 0;
+  hipError_t err = hipGetDevice(&device);
+  if (err != hipSuccess) return err;
+  if (!(attr_set.load(std::memory_order_relaxed) >> (device & 63) & 1)) {
+    err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (err != hipSuccess) return err;
-    attr_set.store(true, std::memory_order_relaxed);
+    attr_set.fetch_or((uint64_t)1 << (device & 63), std::memory_order_relaxed);
   }
   const int64_t grid = (int64_t)g.tiles_m * g.tiles_n - g.shared + g.workers;
-  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (grid > kMostWorkgroups) return hipErrorInvalidValue;
   kern<<<(unsigned)grid, WM * WN * 64, lds, st>>>(g);
   return hipGetLastError();
 }

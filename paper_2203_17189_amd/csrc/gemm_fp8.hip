@@ -74,6 +74,7 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
     const int B = t.tile, slots = t.at_once, tm = ceil_div(c.M, B), tn = ceil_div(c.N, B);
     if (B == 256 && (c.M < 256 || c.N < 256)) break;
     const int64_t tiles = (int64_t)tm * tn, rest = tiles % slots;
+    if (tiles + slots > kMostWorkgroups && (B == 64 || (B == 128 && c.M >= 256 && c.N >= 256))) continue;  // larger ones are fewer
     const double full = (double)(tiles / slots) * round_cost(t, 1.0, nk), fill = (double)rest / slots;
     const double alone = full + (rest ? round_cost(t, fill, nk) : 0.0);
     const int64_t workers = std::min<int64_t>(slots, rest * units);
@@ -88,7 +89,7 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
     g->shared = share ? (int)rest : 0;
     g->workers = share ? (int)workers : 0;
   }
-  if (c.M <= 64 && rows_cost(c) <= best) {
+  if (c.M <= 64 && rows_cost(c) <= best && ceil_div(c.N, 16 * fp8_rows_of_b(c.M, c.N)) <= kMostWorkgroups / 2) {
     g->few = 1;
     g->shared = g->workers = 0;
   }

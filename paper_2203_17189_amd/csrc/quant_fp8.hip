@@ -263,11 +263,9 @@ template <typename T, int Q, bool VEC>
 hipError_t launch(const QuantArgs& a, int square, hipStream_t st) {
   if (!square && !a.qt) {
     const int64_t units = a.rows * a.kbp, grid = (units + 16 * kUnits - 1) / (16 * kUnits);
-    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
     quant_rows_kernel<T, Q, VEC><<<(unsigned)grid, 256, 0, st>>>(a);
   } else {
     const int64_t grid = (a.rows + kBlock - 1) / kBlock * a.kb;
-    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
     if (square) quant_tile_kernel<T, Q, VEC, true><<<(unsigned)grid, 512, 0, st>>>(a);
     else quant_tile_kernel<T, Q, VEC, false><<<(unsigned)grid, 512, 0, st>>>(a);
   }

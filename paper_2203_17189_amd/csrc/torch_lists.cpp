@@ -3,6 +3,7 @@
 // t5_quantize_fp8 and t5_gemm_fp8, of which the checks were half (9.3 us and 8.1, of a launch of 3.5).  Whatever is not in
 // order is left to binding.py, which says what it is.
 #include <ATen/Functions.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <climits>
 #include <cstdint>
@@ -70,22 +71,21 @@ PyObject* adamw_entries(PyObject*, PyObject* args) {
   int index;
   Py_buffer to;
   if (!PyArg_ParseTuple(args, "O!iw*", &PyList_Type, &list, &index, &to)) return nullptr;
+  struct Release {  // however the function is left
+    Py_buffer* b;
+    ~Release() { PyBuffer_Release(b); }
+  } release{&to};
+  HANDLE_TH_ERRORS
   Py_ssize_t i = 0;
   const Py_ssize_t n = PyList_GET_SIZE(list);
-  PyObject* result = nullptr;
-  try {
-    if (to.len == n * (Py_ssize_t)sizeof(adamw_tensor))
-      for (; i < n; ++i) {
-        PyObject* entry = PyList_GET_ITEM(list, i);
-        if (!PyDict_Check(entry) || !read_entry(entry, index, static_cast<adamw_tensor*>(to.buf) + i)) break;
-      }
-    PyErr_Clear();
-    result = PyLong_FromSsize_t(i);
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-  }
-  PyBuffer_Release(&to);
-  return result;
+  if (to.len == n * (Py_ssize_t)sizeof(adamw_tensor))
+    for (; i < n; ++i) {
+      PyObject* entry = PyList_GET_ITEM(list, i);
+      if (!PyDict_Check(entry) || !read_entry(entry, index, static_cast<adamw_tensor*>(to.buf) + i)) break;
+    }
+  PyErr_Clear();
+  return PyLong_FromSsize_t(i);
+  END_HANDLE_TH_ERRORS
 }
 
 typedef int (*QuantizeFn)(const t5_quantize_cfg*, const void*, void*, uint8_t*, void*, uint8_t*, void*);
@@ -141,35 +141,32 @@ PyObject* quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
     PyErr_Clear();
     Py_RETURN_NONE;
   }
-  try {
-    const at::ScalarType type = e5m2 ? at::kFloat8_e5m2 : at::kFloat8_e4m3fn;
-    at::Tensor out[4];
-    auto make = [&](int64_t n, int64_t cols, at::Tensor* q, at::Tensor* s) {
-      const int64_t blocks = (cols + 127) / 128, ld = (cols + 15) / 16 * 16, lds = (blocks + 3) / 4 * 4;
-      *q = at::empty({n, ld}, x->options().dtype(type));
-      *s = at::empty({(n + block_rows - 1) / block_rows, lds}, x->options().dtype(at::kFloat8_e8m0fnu));
-    };
-    const bool straight = PyObject_IsTrue(args[4]) == 1, turned = PyObject_IsTrue(args[5]) == 1;
-    if (straight) make(r.n, r.cols, &out[0], &out[1]);
-    if (turned) make(r.cols, r.n, &out[2], &out[3]);
-    const t5_quantize_cfg cfg = {r.n, r.cols, r.ld, x->scalar_type() == at::kFloat ? T5_F32 : T5_BF16, e5m2 ? T5_E5M2 : T5_E4M3, (int32_t)block_rows};
-    const int rc = ((QuantizeFn)PyLong_AsVoidPtr(args[0]))(&cfg, x->data_ptr(), straight ? out[0].data_ptr() : nullptr, straight ? (uint8_t*)out[1].data_ptr() : nullptr,
-                                                           turned ? out[2].data_ptr() : nullptr, turned ? (uint8_t*)out[3].data_ptr() : nullptr, PyLong_AsVoidPtr(args[6]));
-    if (rc != T5_OK) return PyLong_FromLong(rc);
-    PyObject* result = PyTuple_New(4);
-    if (!result) return nullptr;
-    const int64_t cols[4] = {r.cols, (r.cols + 127) / 128, r.n, (r.n + 127) / 128};
-    for (int i = 0; i < 4; ++i) {
-      PyObject* o = Py_None;
-      if (out[i].defined()) o = THPVariable_Wrap(out[i].size(1) == cols[i] ? out[i] : out[i].narrow(1, 0, cols[i]));
-      else Py_INCREF(o);
-      PyTuple_SET_ITEM(result, i, o);
-    }
-    return result;
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
+  HANDLE_TH_ERRORS
+  const at::ScalarType type = e5m2 ? at::kFloat8_e5m2 : at::kFloat8_e4m3fn;
+  at::Tensor out[4];
+  auto make = [&](int64_t n, int64_t cols, at::Tensor* q, at::Tensor* s) {
+    const int64_t blocks = (cols + 127) / 128, ld = (cols + 15) / 16 * 16, lds = (blocks + 3) / 4 * 4;
+    *q = at::empty({n, ld}, x->options().dtype(type));
+    *s = at::empty({(n + block_rows - 1) / block_rows, lds}, x->options().dtype(at::kFloat8_e8m0fnu));
+  };
+  const bool straight = PyObject_IsTrue(args[4]) == 1, turned = PyObject_IsTrue(args[5]) == 1;
+  if (straight) make(r.n, r.cols, &out[0], &out[1]);
+  if (turned) make(r.cols, r.n, &out[2], &out[3]);
+  const t5_quantize_cfg cfg = {r.n, r.cols, r.ld, x->scalar_type() == at::kFloat ? T5_F32 : T5_BF16, e5m2 ? T5_E5M2 : T5_E4M3, (int32_t)block_rows};
+  const int rc = ((QuantizeFn)PyLong_AsVoidPtr(args[0]))(&cfg, x->data_ptr(), straight ? out[0].data_ptr() : nullptr, straight ? (uint8_t*)out[1].data_ptr() : nullptr,
+                                                         turned ? out[2].data_ptr() : nullptr, turned ? (uint8_t*)out[3].data_ptr() : nullptr, PyLong_AsVoidPtr(args[6]));
+  if (rc != T5_OK) return PyLong_FromLong(rc);
+  PyObject* result = PyTuple_New(4);
+  if (!result) return nullptr;
+  const int64_t cols[4] = {r.cols, (r.cols + 127) / 128, r.n, (r.n + 127) / 128};
+  for (int i = 0; i < 4; ++i) {
+    PyObject* o = Py_None;
+    if (out[i].defined()) o = THPVariable_Wrap(out[i].size(1) == cols[i] ? out[i] : out[i].narrow(1, 0, cols[i]));
+    else Py_INCREF(o);
+    PyTuple_SET_ITEM(result, i, o);
   }
+  return result;
+  END_HANDLE_TH_ERRORS
 }
 
 // gemm_fp8(entry point, its size query, a, a_scale, b, b_scale, out or None, float32, accumulate, stream, device) -> out, a status, or None
@@ -184,36 +181,33 @@ PyObject* gemm_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
     Py_RETURN_NONE;
   bool f32 = PyObject_IsTrue(args[7]) == 1;
   const bool add = PyObject_IsTrue(args[8]) == 1;
-  try {
-    at::Tensor out;
-    Rows c = {a.q.n, b.q.n, b.q.n};
-    if (args[6] == Py_None) {
-      if (add) Py_RETURN_NONE;
-      out = at::empty({a.q.n, b.q.n}, t[0]->options().dtype(f32 ? at::kFloat : at::kBFloat16));
-    } else {
-      const at::Tensor* given = tensor_on(args[6], index);
-      if (!given || !rows_of(*given, &c) || c.n != a.q.n || c.cols != b.q.n || (given->scalar_type() != at::kFloat && given->scalar_type() != at::kBFloat16))
-        Py_RETURN_NONE;
-      out = *given;
-      f32 = out.scalar_type() == at::kFloat;
-    }
-    const t5_gemm_fp8_cfg cfg = {(int32_t)a.q.n, (int32_t)b.q.n, (int32_t)a.q.cols, a.q.ld, b.q.ld, c.ld, a.s.ld, b.s.ld, a.type, b.type,
-                                 a.block_rows, b.block_rows, f32 ? T5_F32 : T5_BF16, add ? 1 : 0};
-    const size_t bytes = ((GemmBytesFn)PyLong_AsVoidPtr(args[1]))(&cfg);
-    at::Tensor workspace;
-    if (bytes) workspace = at::empty({(int64_t)bytes}, t[0]->options().dtype(at::kByte));
-    const int rc = ((GemmFn)PyLong_AsVoidPtr(args[0]))(&cfg, t[0]->data_ptr(), (const uint8_t*)t[1]->data_ptr(), t[2]->data_ptr(), (const uint8_t*)t[3]->data_ptr(),
-                                                       out.data_ptr(), bytes ? workspace.data_ptr() : nullptr, bytes, PyLong_AsVoidPtr(args[9]));
-    if (rc != T5_OK) return PyLong_FromLong(rc);
-    if (args[6] != Py_None) {
-      Py_INCREF(args[6]);
-      return args[6];
-    }
-    return THPVariable_Wrap(out);
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
+  HANDLE_TH_ERRORS
+  at::Tensor out;
+  Rows c = {a.q.n, b.q.n, b.q.n};
+  if (args[6] == Py_None) {
+    if (add) Py_RETURN_NONE;
+    out = at::empty({a.q.n, b.q.n}, t[0]->options().dtype(f32 ? at::kFloat : at::kBFloat16));
+  } else {
+    const at::Tensor* given = tensor_on(args[6], index);
+    if (!given || !rows_of(*given, &c) || c.n != a.q.n || c.cols != b.q.n || (given->scalar_type() != at::kFloat && given->scalar_type() != at::kBFloat16))
+      Py_RETURN_NONE;
+    out = *given;
+    f32 = out.scalar_type() == at::kFloat;
   }
+  const t5_gemm_fp8_cfg cfg = {(int32_t)a.q.n, (int32_t)b.q.n, (int32_t)a.q.cols, a.q.ld, b.q.ld, c.ld, a.s.ld, b.s.ld, a.type, b.type,
+                               a.block_rows, b.block_rows, f32 ? T5_F32 : T5_BF16, add ? 1 : 0};
+  const size_t bytes = ((GemmBytesFn)PyLong_AsVoidPtr(args[1]))(&cfg);
+  at::Tensor workspace;
+  if (bytes) workspace = at::empty({(int64_t)bytes}, t[0]->options().dtype(at::kByte));
+  const int rc = ((GemmFn)PyLong_AsVoidPtr(args[0]))(&cfg, t[0]->data_ptr(), (const uint8_t*)t[1]->data_ptr(), t[2]->data_ptr(), (const uint8_t*)t[3]->data_ptr(),
+                                                     out.data_ptr(), bytes ? workspace.data_ptr() : nullptr, bytes, PyLong_AsVoidPtr(args[9]));
+  if (rc != T5_OK) return PyLong_FromLong(rc);
+  if (args[6] != Py_None) {
+    Py_INCREF(args[6]);
+    return args[6];
+  }
+  return THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
 }
 
 PyMethodDef methods[] = {{"adamw_entries", adamw_entries, METH_VARARGS, nullptr},

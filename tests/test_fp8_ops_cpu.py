@@ -33,6 +33,7 @@ def _adam(**kw):
 @pytest.mark.parametrize("kw,rc", [(dict(rows=-1), SHAPE), (dict(cols=0), SHAPE), (dict(ld=129), SHAPE), (dict(block_rows=0), SHAPE),
                                    (dict(block_rows=64), SHAPE), (dict(rows=(1 << 31) - 128), UNSUPPORTED),
                                    (dict(cols=(1 << 23) + 1, ld=1 << 24), UNSUPPORTED), (dict(ld=(1 << 32) + 1), UNSUPPORTED),
+                                   (dict(rows=1 << 30, cols=1, ld=1), UNSUPPORTED),
                                    (dict(dtype=2), UNSUPPORTED), (dict(q_dtype=1), UNSUPPORTED), (dict(q_dtype=4), UNSUPPORTED)], ids=str)
 def test_quantize_refusals(kw, rc):
     assert P.lib().t5_quantize_fp8(C.byref(_quant(**kw)), D, D, D, D, D, None) == rc
@@ -51,6 +52,8 @@ def test_quantize_nulls_and_alignment():
     assert f(c, D, D, odd, D, D, None) == UNSUPPORTED and f(c, D, D, D, D, odd, None) == UNSUPPORTED
     assert f(c, C.c_void_p(4097), D, D, D, D, None) == UNSUPPORTED
     assert f(C.byref(_quant(rows=0)), None, None, None, None, None, None) == 0
+    many = C.byref(_quant(rows=1 << 29, cols=1, ld=1))  # threads of one launch
+    assert f(many, D, D, D, None, None, None) == UNSUPPORTED
     assert [L.t5_fp8_ld(n) for n in (1, 16, 17, 128)] == [16, 16, 32, 128]
     assert [L.t5_fp8_scale_ld(n) for n in (1, 128, 512, 513)] == [4, 4, 4, 8]
 
@@ -94,7 +97,7 @@ def test_adamw_refusals(kw, rc):
     assert P.lib().adamw_step_multi(t, 1, C.byref(_adam(**kw)), None) == rc
 
 
-@pytest.mark.parametrize("kw,rc", [(dict(n=0), SHAPE), (dict(weight_decay=-0.1), SHAPE), (dict(weight_decay=inf), SHAPE), (dict(n=(1 << 36) + 1), UNSUPPORTED),
+@pytest.mark.parametrize("kw,rc", [(dict(n=0), SHAPE), (dict(weight_decay=-0.1), SHAPE), (dict(weight_decay=inf), SHAPE), (dict(n=(1 << 34) + 1), UNSUPPORTED),
                                    (dict(state_bits=16), UNSUPPORTED), (dict(grad_dtype=2), UNSUPPORTED), (dict(param=None), NULL), (dict(grad=None), NULL),
                                    (dict(m=None), NULL), (dict(v=None), NULL), (dict(m_scale=None), NULL), (dict(v_scale=None), NULL),
                                    (dict(param=4098), UNSUPPORTED), (dict(grad=4098), UNSUPPORTED), (dict(grad=4097, grad_dtype=1), UNSUPPORTED),
@@ -135,6 +138,9 @@ def test_binding_refuses_what_it_can_see():
         P.t5_gemm_fp8(x, s, q, s)
     with pytest.raises(P.T5Error):
         P.adamw_step_multi([], step=1, lr=1e-3)
+    for step in (0, -3, 1 << 31, 1 << 40):
+        with pytest.raises(P.T5Error):
+            P.adamw_step_multi([{}], step=step, lr=1e-3)
     z = torch.zeros(8)
     with pytest.raises(ValueError):
         P.adamw_step_multi([dict(param=z, grad=z, m=z, v=z)], step=1, lr=1e-3)

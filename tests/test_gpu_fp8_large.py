@@ -90,3 +90,24 @@ def test_adamw_beyond_4_g_elements():
         k = np.maximum(np.floor(x), 1) if key == "v" else np.floor(x)
         got = O.code_values("e4m3")[codes(t[key][first:])] * np.repeat(2.0 ** (codes(t[key + "_scale"][first // 128:]) - 127.0), 128)[:n - first]
         assert (got[clear] == np.copysign(k * width, want)[clear]).all() and clear.mean() > 0.9
+
+
+def test_hundreds_of_millions_of_rows():
+    """As many rows as the arguments allow: workgroups of a launch are counted in 24 bits."""
+    need(128)
+    rows = 1 << 30
+    a = torch.full((rows, 16), 0x38, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    sa = torch.full((rows // 128, 4), 127, dtype=torch.uint8, device="cuda").view(E8M0)[:, :1]
+    b = torch.full((3, 16), 0x40, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    sb = torch.full((1, 4), 128, dtype=torch.uint8, device="cuda").view(E8M0)[:, :1]
+    a.view(torch.uint8)[-1, 3] = 0x40
+    c = P.t5_gemm_fp8(a, sa, b, sb)
+    assert (c[:-1] == 64).all() and (c[-1] == 68).all()
+    del c
+    c = P.t5_gemm_fp8(b, sb, a, sa)  # the few rows against them
+    assert (c[:, :-1] == 64).all() and (c[:, -1] == 68).all()
+    del c, a, sa
+    x = torch.ones((1 << 26) - 7, 5, dtype=torch.bfloat16, device="cuda")
+    x[-1] = 2.0
+    q, s, _, _ = P.t5_quantize_fp8(x)
+    assert (q.view(torch.uint8) == 0x78).all() and (s.view(torch.uint8)[:-1] == 119).all() and s.view(torch.uint8)[-1, 0] == 120

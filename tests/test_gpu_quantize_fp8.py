@@ -61,8 +61,10 @@ def test_special_values(fmt, block_rows):
     a[7, 5], a[7, 200], a[8, 300], a[9, 301] = np.inf, -np.inf, np.nan, -np.nan
     a[10, 384:] = np.inf
     a[128:, 384:] = 0.0
-    x = matrix(a, "f32")
-    check(x, fmt, block_rows, P.t5_quantize_fp8(x, fmt, block_rows, transposed=True))
+    for dtype in ("f32", "bf16"):
+        x = matrix(a, dtype)
+        check(x, fmt, block_rows, P.t5_quantize_fp8(x, fmt, block_rows, transposed=True))
+        check(x, fmt, block_rows, P.t5_quantize_fp8(x, fmt, block_rows), (True, False))
 
 
 def test_every_tie_and_neighbour():
