@@ -56,12 +56,15 @@ double round_cost(const TileCost& t, double fill, double nk) {
   return nk * (t.idle + t.busy * std::max(0.0, fill - t.from) / (1.0 - t.from)) + t.ends;
 }
 
-// Few rows, without tiles: a wavefront's blocks of k one after the other, or B's bytes and A's for each workgroup.
-//   16 x 2048 x 16384: 23 us, 16 x 8192 x 8192: 24, 32 x 2048 x 16384: 45, 64 x 8192 x 8192: 38 (in tiles 25, 29, 25, 29)
+// Few rows, without tiles: what a compute unit takes in (37 bytes a ns; widening on top of it), or B's bytes once and A's from
+// L2 for each workgroup, and the launch.  Measured, us, bfloat16, and in tiles:
+//   16 x 2048 x 2048: 3.8, 6.5     16 x 2048 x 16384: 16.6, 22.9     16 x 16384 x 2048: 7.0, 9.4     16 x 8192 x 8192: 20.9, 20.4
+//   32 x 2048 x 2048: 4.7, 6.5     32 x 2048 x 16384: 25.2, 23.2     48 x 5120 x 2048: 10.5, 6.8     64 x 2048 x 2048: 6.3, 6.7
 double rows_cost(const t5_gemm_fp8_cfg& c) {
-  const int mt = c.M <= 16 ? 1 : c.M <= 32 ? 2 : 4, nt = fp8_rows_of_b(c.M, c.N);
-  const double chain = 3.0 + (mt == 1 ? 1.25 : mt == 2 ? 2.6 : 4.0) * ceil_div(ceil_div(c.K, 128), c.K > 1024 || nt > 1 ? 8 : 4);
-  return std::max(chain, 1.0 + (double)c.N * c.K * (1.0 + (double)mt / nt) / 5.8e6);
+  const int64_t rb = 16 * fp8_rows_of_b(c.M, c.N), wgs = (c.N + rb - 1) / rb, k = c.K;
+  const int64_t ra = c.M <= 16 ? c.M : c.M <= 32 ? 32 : 64;
+  const double unit = (double)((wgs + 255) / 256 * (rb + ra) * k) / 37e3 * (c.c_dtype == T5_F32 ? 1.1 : 1.0);
+  return 2.0 + std::max(unit, (double)(c.N * k + wgs * ra * k / 8) / 6e6);
 }
 
 void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {

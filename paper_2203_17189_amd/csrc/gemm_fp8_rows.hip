@@ -1,8 +1,8 @@
 // Product of a few quantised rows (single tokens, short batches) with a quantised matrix.
 //
 // Bound by reading B once.  A workgroup has 16 rows of B; its wavefronts take the blocks of 128 k in turn, straight from
-// memory into the operands of a matrix instruction: no LDS, no barrier before the end, and every load of a wavefront's
-// blocks is under way at once.  The wavefronts' sums meet in LDS, in order.  A is read again by each workgroup, from L2.
+// memory into the operands of a matrix instruction: no LDS, no barrier before the end, and the loads of IN blocks of a
+// wavefront are under way at once.  The wavefronts' sums meet in LDS, in order.  A is read again by each workgroup, from L2.
 // The instructions are the ones of gemm_fp8.h, 16 x 16 wide: codes with scales for bfloat16 C, widened codes for float32.
 #include "gemm_fp8.h"
 
@@ -11,7 +11,7 @@ namespace {
 
 // A lane's 32 bytes of a row's block of 128: 16 at p and 16 at p + 64, so that the four lanes of a row read 64 bytes in a
 // row with each load.  `left`: bytes of the matrix from p on; pieces that begin there are in memory as wholes, zeros behind.
-__device__ __forceinline__ i32x8 load32(const uint8_t* p, int left) {
+__device__ __forceinline__ i32x8 load32_part(const uint8_t* p, int left) {
   i32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -25,9 +25,17 @@ __device__ __forceinline__ i32x8 load32(const uint8_t* p, int left) {
   }
   return v;
 }
-__device__ __forceinline__ i32x8 load32(const uint8_t* p) {
-  const i32x4 a = *reinterpret_cast<const i32x4*>(p), b = *reinterpret_cast<const i32x4*>(p + 64);
-  return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+// The same of a whole block, lanes with `odd` the second piece first: sixteen rows a multiple of 128 bytes apart would ask
+// for one half of each line together, which the L1 serves slowly (16 x 2048 x 16384: 23.3 us, like this 17.3).
+__device__ __forceinline__ i32x8 load32(const uint8_t* p, bool odd) {
+  const i32x4 a = *reinterpret_cast<const i32x4*>(p + (odd ? 64 : 0)), b = *reinterpret_cast<const i32x4*>(p + (odd ? 0 : 64));
+  i32x8 v;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    v[w] = odd ? b[w] : a[w];
+    v[4 + w] = odd ? a[w] : b[w];
+  }
+  return v;
 }
 
 template <int MT, int NT> struct Block {
@@ -39,19 +47,22 @@ template <int MT, int NT> struct Block {
 template <int TA, int TB, bool F32, int MT, int NT, int NW, int IN>
 __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
   __shared__ f32x4 sums[NW][NT * MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = blockIdx.x * (16 * NT), nk = (g.K + 127) >> 7;
-  const int k0 = (lane >> 4) * 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n0 = blockIdx.x * (16 * NT), nk = (g.K + 127) >> 7, k0 = (lane >> 4) * 16;
+  bool odd_a[MT], odd_b[NT];
   const uint8_t *pa[MT], *qa[MT], *pb[NT], *qb[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int rb = min(n0 + i * 16 + (lane & 15), g.N - 1);
     pb[i] = g.B + (int64_t)rb * g.ldb + k0;
+    odd_b[i] = rb & 1;
     qb[i] = g.sb + (int64_t)(rb >> g.shb) * g.lsb;
   }
 #pragma unroll
   for (int j = 0; j < MT; ++j) {
     const int ra = min(j * 16 + (lane & 15), g.M - 1);
     pa[j] = g.A + (int64_t)ra * g.lda + k0;
+    odd_a[j] = ra & 1;
     qa[j] = g.sa + (int64_t)(ra >> g.sha) * g.lsa;
   }
   f32x4 acc[NT][MT];
@@ -64,12 +75,12 @@ __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
     const bool whole = (t + 1) * 128 <= g.K;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      x.b[i] = whole ? load32(pb[i] + (int64_t)t * 128) : load32(pb[i] + (int64_t)t * 128, left);
+      x.b[i] = whole ? load32(pb[i] + (int64_t)t * 128, odd_b[i]) : load32_part(pb[i] + (int64_t)t * 128, left);
       x.sb[i] = qb[i][t];
     }
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
-      x.a[j] = whole ? load32(pa[j] + (int64_t)t * 128) : load32(pa[j] + (int64_t)t * 128, left);
+      x.a[j] = whole ? load32(pa[j] + (int64_t)t * 128, odd_a[j]) : load32_part(pa[j] + (int64_t)t * 128, left);
       x.sa[j] = qa[j][t];
     }
   };
@@ -95,18 +106,14 @@ __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
           acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x.b[i], x.a[j], acc[i][j], TB == T5_E5M2, TA == T5_E5M2, 0, x.sb[i], 0, x.sa[j]);
     }
   };
-  int t = wave;
-  for (; t + (IN - 1) * NW < nk; t += IN * NW) {
+  for (int t = wave; t < nk; t += IN * NW) {  // (the last blocks, too, are all loaded first: 1 x 5120 x 2048 5.4 us, like this 4.4)
     Block<MT, NT> x[IN];
 #pragma unroll
-    for (int i = 0; i < IN; ++i) load(x[i], t + i * NW);
+    for (int i = 0; i < IN; ++i)
+      if (t + i * NW < nk) load(x[i], t + i * NW);
 #pragma unroll
-    for (int i = 0; i < IN; ++i) add(x[i]);
-  }
-  for (; t < nk; t += NW) {
-    Block<MT, NT> x;
-    load(x, t);
-    add(x);
+    for (int i = 0; i < IN; ++i)
+      if (t + i * NW < nk) add(x[i]);
   }
 #pragma unroll
   for (int i = 0; i < NT; ++i)
@@ -137,16 +144,17 @@ template <int TA, int TB, bool F32>
 hipError_t launch(const Fp8Gemm& g, hipStream_t st) {
   const int nt = fp8_rows_of_b(g.M, g.N);
   const unsigned grid = (unsigned)ceil_div(g.N, 16 * nt);
+  // Sixteen wavefronts where each still has several blocks (1 x 2048 x 16384: with eight 15.6 us, 12.0).
   if (g.M <= 16) {
     if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 1, 4, 8, 2><<<grid, 512, 0, st>>>(g);
     else if (nt == 2) gemm_fp8_rows_kernel<TA, TB, F32, 1, 2, 8, 2><<<grid, 512, 0, st>>>(g);
+    else if (g.K > 4096) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 16, 4><<<grid, 1024, 0, st>>>(g);
     else if (g.K > 1024) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 8, 4><<<grid, 512, 0, st>>>(g);
     else gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 4, 2><<<grid, 256, 0, st>>>(g);
   } else if (g.M <= 32) {
-    if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 2, 4, 8, 2><<<grid, 512, 0, st>>>(g);
-    else gemm_fp8_rows_kernel<TA, TB, F32, 2, 2, 8, 2><<<grid, 512, 0, st>>>(g);
+    gemm_fp8_rows_kernel<TA, TB, F32, 2, 1, 8, 4><<<grid, 512, 0, st>>>(g);
   } else {
-    gemm_fp8_rows_kernel<TA, TB, F32, 4, 2, 8, 1><<<grid, 512, 0, st>>>(g);
+    gemm_fp8_rows_kernel<TA, TB, F32, 4, 1, 8, 2><<<grid, 512, 0, st>>>(g);
   }
   return hipGetLastError();
 }
@@ -155,11 +163,11 @@ hipError_t launch(const Fp8Gemm& g, hipStream_t st) { return g.out_bf16 ? launch
 
 }  // namespace
 
-// As many as leave two workgroups to a compute unit, as each reads A anew (32128 x 2048: 16 rows of A 20.9 us, like this 17.0).
+// As many as leave two workgroups to a compute unit, as each reads A anew (16 rows of A, 32128 x 2048: with one 18.2 us, like
+// this 15.1; 16384 x 2048: 8.9, 7.0).  More rows of A take the registers for one (32 x 2048 x 2048: with two 5.4 us, 4.5).
 int fp8_rows_of_b(int M, int N) {
   const int n16 = ceil_div(N, 16);
-  if (M > 32) return 2;
-  return n16 >= 2048 ? 4 : n16 >= 1024 || M > 16 ? 2 : 1;
+  return M > 16 ? 1 : n16 >= 2048 ? 4 : n16 >= 1024 ? 2 : 1;
 }
 
 hipError_t launch_gemm_fp8_rows(const Fp8Gemm& g, int ta, int tb, hipStream_t st) {

@@ -72,6 +72,22 @@ def test_accumulate_and_long_reductions(m, n, k):
     check(m, n, k, out="bf16")
 
 
+@pytest.mark.parametrize("m", [1, 2, 15, 16, 17, 32, 33, 50, 64])
+@pytest.mark.parametrize("n,k", [(129, 1030), (700, 2100), (97, 4096), (64, 4100), (200, 5000), (33, 16200), (48, 16384)])
+def test_few_rows_and_long_reductions(m, n, k):
+    """Every number of blocks left over, ends inside a block, rows a multiple of 128 bytes apart and others."""
+    check(m, n, k, "e4m3", "e5m2")
+    check(m, n, k, "e5m2", "e4m3", 1, 128, out="bf16")
+    check(m, n, k, accumulate=True, ld=-(-k // 16) * 16 + 16)
+
+
+@pytest.mark.parametrize("m,n", [(1, 16390), (9, 16384), (16, 32770), (20, 9000)])
+def test_few_rows_of_a_wide_matrix(m, n):
+    for k in (100, 768, 1100):
+        for out in ("f32", "bf16"):
+            check(m, n, k, out=out)
+
+
 @pytest.mark.parametrize("m,n", [(4, 67), (150, 135)])
 @pytest.mark.parametrize("ldc", [0, 1, 3, 8])
 def test_strides(m, n, ldc):
