@@ -36,7 +36,7 @@ struct Fp8Gemm {
   int out_bf16, accumulate;
   // Output tiles (of `tile` = 64, 128 or 256 rows and columns), numbered 0 .. tiles_m * tiles_n.  The first `shared` of them, in units of
   // four k-tiles, are dealt out evenly to `workers` workgroups, in order; each of the others has a workgroup of its own.
-  int few;  // none of that: gemm_fp8_rows.hip
+  int few;  // not 0: none of that, but gemm_fp8_rows.hip with so many times 16 rows of A a workgroup
   int tile, tiles_m, tiles_n, shared, workers;
   float* part;  // what a worker adds up of a tile that others have parts of, a tile of float32: at place worker + tile
 };

@@ -56,15 +56,18 @@ double round_cost(const TileCost& t, double fill, double nk) {
   return nk * (t.idle + t.busy * std::max(0.0, fill - t.from) / (1.0 - t.from)) + t.ends;
 }
 
-// Few rows, without tiles: what a compute unit takes in (37 bytes a ns; widening on top of it), or B's bytes once and A's from
-// L2 for each workgroup, and the launch.  Measured, us, bfloat16, and in tiles:
+// Without tiles, mt * 16 rows of A a workgroup: what a compute unit takes in (37 bytes a ns; widening on top of it), or B's
+// bytes once and what comes again from L2 for each workgroup, and the launch.  Measured, us, bfloat16, and in tiles:
 //   16 x 2048 x 2048: 3.8, 6.5     16 x 2048 x 16384: 16.6, 22.9     16 x 16384 x 2048: 7.0, 9.4     16 x 8192 x 8192: 20.9, 20.4
-//   32 x 2048 x 2048: 4.7, 6.5     32 x 2048 x 16384: 25.2, 23.2     48 x 5120 x 2048: 10.5, 6.8     64 x 2048 x 2048: 6.3, 6.7
-double rows_cost(const t5_gemm_fp8_cfg& c) {
-  const int64_t rb = 16 * fp8_rows_of_b(c.M, c.N), wgs = (c.N + rb - 1) / rb, k = c.K;
-  const int64_t ra = c.M <= 16 ? c.M : c.M <= 32 ? 32 : 64;
-  const double unit = (double)((wgs + 255) / 256 * (rb + ra) * k) / 37e3 * (c.c_dtype == T5_F32 ? 1.1 : 1.0);
-  return 2.0 + std::max(unit, (double)(c.N * k + wgs * ra * k / 8) / 6e6);
+//   32 x 2048 x 5120: 7.2, 12.6    64 x 2048 x 5120: 9.3, 12.9       189 x 128 x 2944: 4.4, 8.4       333 x 509 x 1001: 4.7, 5.8
+double rows_cost(const t5_gemm_fp8_cfg& c, int mt) {
+  const int64_t rb = 16 * fp8_rows_of_b(c.M, c.N), ra = std::min(c.M, 16 * mt), k = c.K;
+  const int64_t tm = ceil_div(c.M, 16 * mt), wgs = (c.N + rb - 1) / rb * tm;
+  const int64_t taken = rb + (c.M <= 16 ? ra : 16 * mt);  // rows behind a single token's are the same line
+  const bool f32 = c.c_dtype == T5_F32;
+  const int64_t rounds = (wgs + 255) / 256;  // ends and beginnings of workgroups with many registers do not overlap
+  const double unit = (double)(rounds * taken * k) / 37e3 * (f32 ? 1.1 : 1.0) + (mt > 1 ? (double)(rounds - 1) * (f32 ? 1.0 : 0.5) : 0.0);
+  return 2.0 + std::max(unit, (double)(c.N * k + (c.N * (tm - 1) + wgs * ra) * k / 8) / 6e6);
 }
 
 void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
@@ -92,8 +95,14 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
     g->shared = share ? (int)rest : 0;
     g->workers = share ? (int)workers : 0;
   }
-  if (c.M <= 64 && rows_cost(c) <= best && ceil_div(c.N, 16 * fp8_rows_of_b(c.M, c.N)) <= kMostWorkgroups / 2) {
-    g->few = 1;
+  for (int mt = 1; mt <= 4; mt *= 2) {
+    if (mt > 1 && c.M <= 8 * mt) break;
+    const int64_t wgs = (int64_t)ceil_div(c.N, 16 * fp8_rows_of_b(c.M, c.N)) * ceil_div(c.M, 16 * mt);
+    if (wgs > (c.M <= 16 ? kMostWorkgroups / 2 : 4096)) continue;
+    const double cost = rows_cost(c, mt);
+    if (cost > best) continue;
+    best = cost;
+    g->few = mt;
     g->shared = g->workers = 0;
   }
 }

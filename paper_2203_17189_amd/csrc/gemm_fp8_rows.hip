@@ -1,6 +1,6 @@
-// Product of a few quantised rows (single tokens, short batches) with a quantised matrix.
+// Product of a few quantised rows (single tokens, short batches) with a quantised matrix, and small products.
 //
-// Bound by reading B once.  A workgroup has 16 rows of B; its wavefronts take the blocks of 128 k in turn, straight from
+// Bound by reading B once.  A workgroup has 16 rows of B (and 16 to 64 of A); its wavefronts take the blocks of 128 k in turn, straight from
 // memory into the operands of a matrix instruction: no LDS, no barrier before the end, and the loads of IN blocks of a
 // wavefront are under way at once.  The wavefronts' sums meet in LDS, in order.  A is read again by each workgroup, from L2.
 // The instructions are the ones of gemm_fp8.h, 16 x 16 wide: codes with scales for bfloat16 C, widened codes for float32.
@@ -25,8 +25,8 @@ __device__ __forceinline__ i32x8 load32_part(const uint8_t* p, int left) {
   }
   return v;
 }
-// The same of a whole block, lanes with `odd` the second piece first: sixteen rows a multiple of 128 bytes apart would ask
-// for one half of each line together, which the L1 serves slowly (16 x 2048 x 16384: 23.3 us, like this 17.3).
+// The same of a whole block, lanes with `odd` the second piece first, so that even rows ask for one half of a line and odd
+// ones for the other: sixteen rows a multiple of 128 bytes apart would ask for the same half together, which the L1 serves slowly (16 x 2048 x 16384: 23.3 us, like this 17.3).
 __device__ __forceinline__ i32x8 load32(const uint8_t* p, bool odd) {
   const i32x4 a = *reinterpret_cast<const i32x4*>(p + (odd ? 64 : 0)), b = *reinterpret_cast<const i32x4*>(p + (odd ? 0 : 64));
   i32x8 v;
@@ -48,21 +48,21 @@ template <int TA, int TB, bool F32, int MT, int NT, int NW, int IN>
 __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
   __shared__ f32x4 sums[NW][NT * MT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n0 = blockIdx.x * (16 * NT), nk = (g.K + 127) >> 7, k0 = (lane >> 4) * 16;
+  const int n0 = blockIdx.x * (16 * NT), m0 = blockIdx.y * (16 * MT), nk = (g.K + 127) >> 7, k0 = (lane >> 4) * 16;
   bool odd_a[MT], odd_b[NT];
   const uint8_t *pa[MT], *qa[MT], *pb[NT], *qb[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int rb = min(n0 + i * 16 + (lane & 15), g.N - 1);
     pb[i] = g.B + (int64_t)rb * g.ldb + k0;
-    odd_b[i] = rb & 1;
+    odd_b[i] = ((uintptr_t)pb[i] >> 6 ^ rb) & 1;
     qb[i] = g.sb + (int64_t)(rb >> g.shb) * g.lsb;
   }
 #pragma unroll
   for (int j = 0; j < MT; ++j) {
-    const int ra = min(j * 16 + (lane & 15), g.M - 1);
+    const int ra = min(m0 + j * 16 + (lane & 15), g.M - 1);
     pa[j] = g.A + (int64_t)ra * g.lda + k0;
-    odd_a[j] = ra & 1;
+    odd_a[j] = ((uintptr_t)pa[j] >> 6 ^ ra) & 1;
     qa[j] = g.sa + (int64_t)(ra >> g.sha) * g.lsa;
   }
   f32x4 acc[NT][MT];
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
     f32x4 s = sums[0][ij][l];
 #pragma unroll
     for (int w = 1; w < NW; ++w) s += sums[w][ij][l];
-    const int m = ij % MT * 16 + (l & 15), n = n0 + ij / MT * 16 + (l >> 4) * 4;  // a lane holds four columns of a row
+    const int m = m0 + ij % MT * 16 + (l & 15), n = n0 + ij / MT * 16 + (l >> 4) * 4;  // a lane holds four columns of a row
     if (m >= g.M) continue;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -143,15 +143,15 @@ __global__ __launch_bounds__(NW * 64) void gemm_fp8_rows_kernel(Fp8Gemm g) {
 template <int TA, int TB, bool F32>
 hipError_t launch(const Fp8Gemm& g, hipStream_t st) {
   const int nt = fp8_rows_of_b(g.M, g.N);
-  const unsigned grid = (unsigned)ceil_div(g.N, 16 * nt);
+  const dim3 grid((unsigned)ceil_div(g.N, 16 * nt), (unsigned)ceil_div(g.M, 16 * g.few));
   // Sixteen wavefronts where each still has several blocks (1 x 2048 x 16384: with eight 15.6 us, 12.0).
-  if (g.M <= 16) {
+  if (g.few == 1) {
     if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 1, 4, 8, 2><<<grid, 512, 0, st>>>(g);
     else if (nt == 2) gemm_fp8_rows_kernel<TA, TB, F32, 1, 2, 8, 2><<<grid, 512, 0, st>>>(g);
     else if (g.K > 4096) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 16, 4><<<grid, 1024, 0, st>>>(g);
     else if (g.K > 1024) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 8, 4><<<grid, 512, 0, st>>>(g);
     else gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 4, 2><<<grid, 256, 0, st>>>(g);
-  } else if (g.M <= 32) {
+  } else if (g.few == 2) {
     gemm_fp8_rows_kernel<TA, TB, F32, 2, 1, 8, 4><<<grid, 512, 0, st>>>(g);
   } else {
     gemm_fp8_rows_kernel<TA, TB, F32, 4, 1, 8, 2><<<grid, 512, 0, st>>>(g);
@@ -164,7 +164,7 @@ hipError_t launch(const Fp8Gemm& g, hipStream_t st) { return g.out_bf16 ? launch
 }  // namespace
 
 // As many as leave two workgroups to a compute unit, as each reads A anew (16 rows of A, 32128 x 2048: with one 18.2 us, like
-// this 15.1; 16384 x 2048: 8.9, 7.0).  More rows of A take the registers for one (32 x 2048 x 2048: with two 5.4 us, 4.5).
+// this 15.1; 16384 x 2048: 8.9, 7.0).  More rows of A leave the registers for one (32 x 2048 x 2048: with two 5.4 us, 4.5).
 int fp8_rows_of_b(int M, int N) {
   const int n16 = ceil_div(N, 16);
   return M > 16 ? 1 : n16 >= 2048 ? 4 : n16 >= 1024 ? 2 : 1;

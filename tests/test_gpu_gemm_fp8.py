@@ -81,6 +81,15 @@ def test_few_rows_and_long_reductions(m, n, k):
     check(m, n, k, accumulate=True, ld=-(-k // 16) * 16 + 16)
 
 
+@pytest.mark.parametrize("m,n,k", [(189, 128, 2944), (200, 130, 6000), (97, 257, 16390), (130, 40, 900), (400, 33, 3100), (1000, 17, 1030), (90, 1000, 2050),
+                                   (70, 700, 4200)])
+def test_small_products(m, n, k):
+    """Workgroups of 16 to 64 rows by 16 columns in both directions."""
+    check(m, n, k, "e4m3", "e5m2", 128, 1, out="bf16", ldc=n + 1)
+    check(m, n, k, "e5m2", "e4m3", 1, 128)
+    check(m, n, k, accumulate=True, ld=-(-k // 16) * 16 + 64)
+
+
 @pytest.mark.parametrize("m,n", [(1, 16390), (9, 16384), (16, 32770), (20, 9000)])
 def test_few_rows_of_a_wide_matrix(m, n):
     for k in (100, 768, 1100):
