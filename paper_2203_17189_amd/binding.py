@@ -276,7 +276,14 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _strided(t):
+    """Whether a tensor has strides (sparse and nested ones raise errors of torch's own when asked for theirs)."""
+    return t.layout is torch.strided and not t.is_nested
+
+
 def _check_tensor(t, dtype, numel, name):
+    if not _strided(t):
+        raise ValueError(f"{name}: need a strided tensor, got layout {t.layout}{', nested' if t.is_nested else ''}")
     if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or t.numel() != numel:
         raise ValueError(f"{name}: need a contiguous cuda tensor of {dtype} with {numel} elements, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -926,6 +933,8 @@ def _check_on(device, t, dtype, numel, name):
 
 def _check_rows(t, name):
     """Rows of a matrix whose elements are contiguous; (rows, columns, row stride)."""
+    if not _strided(t):
+        raise ValueError(f"{name}: need a strided tensor, got layout {t.layout}{', nested' if t.is_nested else ''}")
     if t.is_cuda and t.dim() == 2 and t.is_contiguous():
         return t.shape[0], t.shape[1], t.shape[1]
     if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):

@@ -15,12 +15,17 @@ namespace {
 PyObject* names[8];  // of an entry's fields, made once
 enum { PARAM, GRAD, M, V, M_SCALE, V_SCALE, COPY, DECAY };
 
+// Whether a tensor is rows of memory on CUDA device `index`: sparse and nested ones have no strides, and say so by a C++ exception.
+bool plain_on(const at::Tensor& t, int index) {
+  return t.defined() && t.is_cuda() && t.get_device() == index && t.layout() == at::kStrided && !t.is_nested();
+}
+
 // The tensor under a name: contiguous, of n elements (n < 0: any number) on CUDA device `index`; nullptr if it is not.
 const at::Tensor* field(PyObject* entry, int name, int64_t n, int index) {
   PyObject* o = PyDict_GetItem(entry, names[name]);  // (borrowed)
   if (!o || o == Py_None || !THPVariable_Check(o)) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
-  if (!t.defined() || !t.is_cuda() || t.get_device() != index || !t.is_contiguous() || (n >= 0 && t.numel() != n)) return nullptr;
+  if (!plain_on(t, index) || !t.is_contiguous() || (n >= 0 && t.numel() != n)) return nullptr;
   return &t;
 }
 bool absent(PyObject* entry, int name) {
@@ -95,7 +100,7 @@ typedef size_t (*GemmBytesFn)(const t5_gemm_fp8_cfg*);
 const at::Tensor* tensor_on(PyObject* o, int index) {
   if (!THPVariable_Check(o)) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
-  return t.defined() && t.is_cuda() && t.get_device() == index ? &t : nullptr;
+  return plain_on(t, index) ? &t : nullptr;
 }
 
 struct Rows { int64_t n, cols, ld; };
@@ -131,6 +136,7 @@ bool fits32(int64_t v) { return v <= INT32_MAX; }
 
 // quantize_fp8(entry point, x, e5m2, block_rows, rows, transposed, stream, device) -> (q, scale, qt, scale_t), a status, or None
 PyObject* quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  HANDLE_TH_ERRORS  // (around everything that asks torch for something: an exception that left a C function would end the process)
   if (count != 8) Py_RETURN_NONE;
   const int index = (int)PyLong_AsLong(args[7]);
   const at::Tensor* x = tensor_on(args[1], index);
@@ -141,7 +147,6 @@ PyObject* quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
     PyErr_Clear();
     Py_RETURN_NONE;
   }
-  HANDLE_TH_ERRORS
   const at::ScalarType type = e5m2 ? at::kFloat8_e5m2 : at::kFloat8_e4m3fn;
   at::Tensor out[4];
   auto make = [&](int64_t n, int64_t cols, at::Tensor* q, at::Tensor* s) {
@@ -171,6 +176,7 @@ PyObject* quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
 
 // gemm_fp8(entry point, its size query, a, a_scale, b, b_scale, out or None, float32, accumulate, stream, device) -> out, a status, or None
 PyObject* gemm_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
   if (count != 11) Py_RETURN_NONE;
   const int index = (int)PyLong_AsLong(args[10]);
   const at::Tensor* t[4];
@@ -181,7 +187,6 @@ PyObject* gemm_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
     Py_RETURN_NONE;
   bool f32 = PyObject_IsTrue(args[7]) == 1;
   const bool add = PyObject_IsTrue(args[8]) == 1;
-  HANDLE_TH_ERRORS
   at::Tensor out;
   Rows c = {a.q.n, b.q.n, b.q.n};
   if (args[6] == Py_None) {
