@@ -7,6 +7,14 @@ namespace t5mi {
 
 constexpr int kBlock = 128;
 
+// Whether the quantiser reads its matrix in whole pieces of 16 bytes, and whether it reads the eight elements from column c
+// (a multiple of 8) of a row as such: those past the row's end too (and drops them) where another row follows.  Rows of four float32 would take in the
+// next row with it, and of a last one more than its columns; longer ones end at most four elements into a row of more.
+inline bool quant_in_pieces(const void* x, int64_t ld, int size) {
+  return ((uintptr_t)x & 15) == 0 && ld * size % 16 == 0 && ld >= 8;
+}
+__host__ __device__ __forceinline__ bool quant_whole_piece(int c, int cols, bool more) { return c + 8 <= cols || (more && c < cols); }
+
 // Exponent of the largest finite value 1.75 * 2^top of a type.
 template <int Q> constexpr int fp8_top = Q == T5_E4M3 ? 8 : 15;
 

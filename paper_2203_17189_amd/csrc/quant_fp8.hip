@@ -50,7 +50,7 @@ template <> struct Eight<float> {
 // the matrix too, and may be read (and is dropped).
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const T* row, int c, int cols, bool more, uint32_t (&v)[Eight<T>::W]) {
-  if (VEC && (c + 8 <= cols || (more && c < cols))) {
+  if (VEC && quant_whole_piece(c, cols, more)) {
 #pragma unroll
     for (int h = 0; h < Eight<T>::W / 4; ++h) {
       const u32x4 p = *reinterpret_cast<const u32x4*>(row + c + h * 4);
@@ -285,8 +285,7 @@ hipError_t launch(const QuantArgs& a, int square, hipStream_t st) {
 }
 template <typename T, int Q>
 hipError_t launch(const QuantArgs& a, int square, hipStream_t st) {
-  const bool vec = ((uintptr_t)a.x & 15) == 0 && (a.ld * (int64_t)sizeof(T)) % 16 == 0;
-  return vec ? launch<T, Q, true>(a, square, st) : launch<T, Q, false>(a, square, st);
+  return quant_in_pieces(a.x, a.ld, sizeof(T)) ? launch<T, Q, true>(a, square, st) : launch<T, Q, false>(a, square, st);
 }
 
 }  // namespace
