@@ -590,7 +590,9 @@ int t5_gemm_fp8(const t5_gemm_fp8_cfg* cfg, const void* A, const uint8_t* a_scal
  *   h = mix32(mix32(mix32(mix32(seed_lo ^ step) ^ i * 0x9E3779B9) ^ b ^ seed_hi) ^ c),
  * u = (h mod 2^16) / 2^16 for m, (h div 2^16) / 2^16 for sqrt(v).  The same bits every time for the same arguments.
  * A gradient that is not finite makes the element's parameter NaN and its states not finite (its neighbours' are as without
- * it).  Tensors share no memory.  Every entry is checked before the first launch.  step, lr and the other numbers are those
+ * it).  States in 8 bits follow finite gradients (times grad_scale) up to 2^125, as roots of second moments are formed and
+ * held without their squares; states in 32 bits hold v as the float32 it is, zero below 2^-150 and infinite from 2^128 on.
+ * Tensors share no memory.  Every entry is checked before the first launch.  step, lr and the other numbers are those
  * of the call: captured into a graph, it repeats them (grad_scale is read each time).
  * Errors: NULL -> T5_ERR_NULL; n_tensors < 1, n < 1, step < 1, lr or weight_decay < 0 or not finite, beta1 or beta2 outside
  * [0, 1), eps below 1e-30 or not finite, parameters of two

@@ -28,7 +28,7 @@ struct AdamItem {
 struct AdamBatch {
   int32_t count;
   uint32_t seed_hi;
-  float b1, one_b1, b2, one_b2, root_factor, eps, step_size;
+  float b1, one_b1, b2, one_b2, root_b2, root_one_b2, root_factor, eps, step_size;
   const float* grad_scale;
   int32_t start[kAdamTensors + 1];
   AdamItem it[kAdamTensors];
@@ -130,11 +130,30 @@ __device__ __forceinline__ uint32_t largest8(const float (&x)[8]) {
   return b;
 }
 
+// v_sqrt_f32 takes subnormal numbers as zero: those, and what else is small, are scaled.
+__device__ __forceinline__ float root_of(float v) {
+  const bool small = v < 0x1p-96f;
+  const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p32f : v);
+  return small ? r * 0x1p-16f : r;
+}
+// sqrt(x^2 + y^2) where the squares may leave float32, by the power of two of the larger.
+__device__ __forceinline__ float root_of_squares(float x, float y) {
+  const int e = __builtin_amdgcn_frexp_expf(fmaxf(fabsf(x), fabsf(y)));
+  x = ldexpf(x, -e);
+  y = ldexpf(y, -e);
+  return ldexpf(__builtin_amdgcn_sqrtf(fmaf(x, x, y * y)), e);
+}
+
 struct Step {
-  float b1, one_b1, b2, one_b2, root_factor, eps, step_size, keep;
+  float b1, one_b1, b2, one_b2, root_b2, root_one_b2, root_factor, eps, step_size, keep;
   __device__ __forceinline__ void moments(float g, float& m, float& v) const {
     m = fmaf(b1, m, one_b1 * g);
     v = fmaf(b2, v, one_b2 * g * g);
+  }
+  // Whether the root cannot be had from the sum v = b2 r^2 + one_b2 g^2: it, or what counts of its parts, is below float32's
+  // normal range, or it is above.  (Zeros of both are ordinary: tables have many.)
+  __device__ __forceinline__ bool far(float v, float r, float g) const {
+    return !(v >= 0x1p-96f && v < __builtin_inff()) && (r != 0.f || g != 0.f);
   }
   // (v_sqrt_f32 and v_rcp_f32 are within one unit of the last place; the divisor is eps or more, 1e-30 at least)
   __device__ __forceinline__ float update(float p, float m, float root) const {
@@ -166,12 +185,31 @@ __device__ __forceinline__ void adam_chunk(const AdamItem& it, const Step& s, co
 #pragma unroll
     for (int j = 0; j < 8; ++j) g[j] *= f;
   }
+  if constexpr (EIGHT) {
+    // The root is held, over all of float32's range; its square has half of that range.
+    float r[8];
+    bool far = false;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    s.moments(g[j], m[j], v[j]);
-    root[j] = __builtin_amdgcn_sqrtf(v[j]);
-    p[j] = s.update(p[j], m[j], root[j]);
+    for (int j = 0; j < 8; ++j) {
+      r[j] = root[j];
+      s.moments(g[j], m[j], v[j]);
+      root[j] = __builtin_amdgcn_sqrtf(v[j]);
+      far |= s.far(v[j], r[j], g[j]);
+    }
+    if (far) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (s.far(v[j], r[j], g[j])) root[j] = root_of_squares(s.root_b2 * r[j], s.root_one_b2 * g[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      s.moments(g[j], m[j], v[j]);
+      root[j] = root_of(v[j]);
+    }
   }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) p[j] = s.update(p[j], m[j], root[j]);
   store8<VEC>(it.p + i, n, p);
   if (it.lp) store8<VEC>(it.lp + i, n, p);
   if constexpr (EIGHT) {
@@ -214,7 +252,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b) {
   const AdamItem& it = b.it[t];
   const int64_t i = (int64_t)((int)blockIdx.x - b.start[t]) * kChunk + threadIdx.x * 8;
   const float* gs = b.grad_scale;
-  const Step s{b.b1, b.one_b1, b.b2, b.one_b2, b.root_factor, b.eps, b.step_size, it.keep};
+  const Step s{b.b1, b.one_b1, b.b2, b.one_b2, b.root_b2, b.root_one_b2, b.root_factor, b.eps, b.step_size, it.keep};
   if (it.flags & AW_8BIT) {
     if (it.flags & AW_VEC) adam_chunk<true, true>(it, s, gs, b.seed_hi, i);
     else adam_chunk<false, true>(it, s, gs, b.seed_hi, i);
@@ -234,6 +272,7 @@ hipError_t launch_adamw(const adamw_tensor* t, int n, int first, const adamw_cfg
   b.seed_hi = c.seed_hi;
   b.b1 = (float)c.beta1; b.one_b1 = (float)(1.0 - c.beta1);
   b.b2 = (float)c.beta2; b.one_b2 = (float)(1.0 - c.beta2);
+  b.root_b2 = (float)std::sqrt(c.beta2); b.root_one_b2 = (float)std::sqrt(1.0 - c.beta2);
   b.root_factor = (float)(1.0 / std::sqrt(1.0 - std::pow(c.beta2, (double)c.step)));
   b.eps = (float)c.eps;
   b.step_size = (float)(c.lr / (1.0 - std::pow(c.beta1, (double)c.step)));
