@@ -574,6 +574,20 @@ typedef struct {
   int32_t accumulate;
 } t5_gemm_fp8_cfg;
 size_t t5_gemm_fp8_workspace_bytes(const t5_gemm_fp8_cfg* cfg);
+/* Which kernel a product runs on (a pure host-side query, usable without a GPU): a bit mask, or -1 for an invalid
+ * configuration.  Sizes and c_dtype decide, by estimated time. */
+enum {
+  T5_FP8_PATH_TILE64 = 1,   /* output tiles of 64 x 64 */
+  T5_FP8_PATH_TILE128 = 2,
+  T5_FP8_PATH_TILE256 = 4,
+  T5_FP8_PATH_SHARED = 8,   /* some tiles' k is divided, their parts meet in the workspace */
+  T5_FP8_PATH_ROWS = 16,    /* no tiles: 16 rows of A and 16 of B a workgroup, or with these bits more of them */
+  T5_FP8_PATH_ROWS_A32 = 32,
+  T5_FP8_PATH_ROWS_A64 = 64,
+  T5_FP8_PATH_ROWS_B32 = 128,
+  T5_FP8_PATH_ROWS_B64 = 256
+};
+int t5_gemm_fp8_kernel_path(const t5_gemm_fp8_cfg* cfg);
 int t5_gemm_fp8(const t5_gemm_fp8_cfg* cfg, const void* A, const uint8_t* a_scale, const void* B, const uint8_t* b_scale,
                 void* C, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -232,6 +232,8 @@ def lib() -> C.CDLL:
     L.t5_quantize_fp8.argtypes = [C.POINTER(_QuantizeCfg), vp, vp, vp, vp, vp, vp]
     L.t5_gemm_fp8_workspace_bytes.restype = sz
     L.t5_gemm_fp8_workspace_bytes.argtypes = [C.POINTER(_GemmFp8Cfg)]
+    L.t5_gemm_fp8_kernel_path.restype = i32
+    L.t5_gemm_fp8_kernel_path.argtypes = [C.POINTER(_GemmFp8Cfg)]
     L.t5_gemm_fp8.restype = i32
     L.t5_gemm_fp8.argtypes = [C.POINTER(_GemmFp8Cfg), vp, vp, vp, vp, vp, vp, sz, vp]
     L.adamw_step_multi.restype = i32
@@ -1217,6 +1219,16 @@ def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accu
     _call(L.t5_gemm_fp8, "t5_gemm_fp8", dev, cfg, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
           out.data_ptr(), ws, nbytes)
     return out
+
+
+FP8_PATH_TILE64, FP8_PATH_TILE128, FP8_PATH_TILE256, FP8_PATH_SHARED, FP8_PATH_ROWS = 1, 2, 4, 8, 16
+FP8_PATH_ROWS_A32, FP8_PATH_ROWS_A64, FP8_PATH_ROWS_B32, FP8_PATH_ROWS_B64 = 32, 64, 128, 256
+
+
+def t5_gemm_fp8_kernel_path(m, n, k, out_dtype=torch.bfloat16) -> int:
+    """Bit mask of the kernel that a product of [m, k] and [n, k] runs on (host-side query; -1: invalid sizes or type)."""
+    ld, lds, ty = -(-k // 16) * 16, -(-k // 512) * 4, {torch.bfloat16: T5_BF16, torch.float32: T5_F32}.get(out_dtype, -1)
+    return int(lib().t5_gemm_fp8_kernel_path(C.byref(_GemmFp8Cfg(m, n, k, ld, ld, n, lds, lds, T5_E4M3, T5_E4M3, 1, 1, ty, 0))))
 
 
 def _adam_check(t, index):

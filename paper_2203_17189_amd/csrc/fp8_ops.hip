@@ -85,6 +85,10 @@ size_t t5_gemm_fp8_workspace_bytes(const t5_gemm_fp8_cfg* cfg) {
   return check_gemm(cfg) == T5_OK && cfg->M > 0 ? gemm_fp8_ws_bytes(*cfg) : 0;
 }
 
+int t5_gemm_fp8_kernel_path(const t5_gemm_fp8_cfg* cfg) {
+  return check_gemm(cfg) != T5_OK ? -1 : cfg->M > 0 ? gemm_fp8_path(*cfg) : 0;
+}
+
 int t5_gemm_fp8(const t5_gemm_fp8_cfg* cfg, const void* A, const uint8_t* a_scale, const void* B, const uint8_t* b_scale,
                 void* C, void* workspace, size_t workspace_bytes, void* stream) {
   const int rc = check_gemm(cfg);

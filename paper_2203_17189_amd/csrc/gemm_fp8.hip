@@ -117,6 +117,18 @@ size_t gemm_fp8_ws_bytes(const t5_gemm_fp8_cfg& c) {
   return ((size_t)g.workers + g.shared) * B * B * 4;
 }
 
+int gemm_fp8_path(const t5_gemm_fp8_cfg& c) {
+  Fp8Gemm g;
+  plan(c, &g);
+  if (g.few) {
+    const int nt = fp8_rows_of_b(c.M, c.N);
+    return T5_FP8_PATH_ROWS | (g.few == 2 ? T5_FP8_PATH_ROWS_A32 : g.few == 4 ? T5_FP8_PATH_ROWS_A64 : 0) |
+           (nt == 2 ? T5_FP8_PATH_ROWS_B32 : nt == 4 ? T5_FP8_PATH_ROWS_B64 : 0);
+  }
+  return (g.tile == 64 ? T5_FP8_PATH_TILE64 : g.tile == 128 ? T5_FP8_PATH_TILE128 : T5_FP8_PATH_TILE256) |
+         (g.workers > g.shared ? T5_FP8_PATH_SHARED : 0);
+}
+
 hipError_t launch_gemm_fp8(const t5_gemm_fp8_cfg& c, const void* A, const uint8_t* sa, const void* B, const uint8_t* sb, void* C,
                            void* ws, hipStream_t st) {
   Fp8Gemm g;

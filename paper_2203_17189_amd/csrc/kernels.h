@@ -354,6 +354,7 @@ int64_t fp8_scale_ld(int64_t cols);
 hipError_t launch_quantize_fp8(const t5_quantize_cfg& c, const void* x, void* q, uint8_t* scale, void* qt, uint8_t* scale_t,
                                hipStream_t st);
 size_t gemm_fp8_ws_bytes(const t5_gemm_fp8_cfg& c);
+int gemm_fp8_path(const t5_gemm_fp8_cfg& c);  // T5_FP8_PATH_* bits
 hipError_t launch_gemm_fp8(const t5_gemm_fp8_cfg& c, const void* A, const uint8_t* sa, const void* B, const uint8_t* sb, void* C,
                            void* ws, hipStream_t st);
 // One launch of up to kAdamTensors tensors; `first` is the place of t[0] in the caller's list.

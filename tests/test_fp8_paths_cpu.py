@@ -1,0 +1,33 @@
+"""Which kernels the tests of the 8-bit product reach (tests/fp8_paths.py), on the CPU: a changed choice of kernels that leaves
+one of them without a test fails here."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2203_17189_amd as P
+from paper_2203_17189_amd import binding as B
+from fp8_paths import IDS, LAYERS, REACHED, SHAPES, SHARED, layer_products, path
+
+
+@pytest.mark.parametrize("m,n,k,out,want", SHAPES, ids=IDS)
+def test_shapes_run_on_the_kernels_they_are_listed_for(m, n, k, out, want):
+    assert path(m, n, k, out) == want
+    need = P.lib().t5_gemm_fp8_workspace_bytes(C.byref(B._GemmFp8Cfg(m, n, k, -(-k // 16) * 16, -(-k // 16) * 16, n, -(-k // 512) * 4,
+                                                                     -(-k // 512) * 4, 2, 2, 1, 1, 0 if out == "f32" else 1, 0)))
+    assert (need > 0) == bool(want & SHARED)
+
+
+def test_every_kernel_is_listed():
+    assert {(s[4], s[3]) for s in SHAPES} == set(REACHED)
+
+
+@pytest.mark.parametrize("tokens,d_in,d_out,which,tile", LAYERS)
+def test_layers_have_products_in_parts(tokens, d_in, d_out, which, tile):
+    assert path(*layer_products(tokens, d_in, d_out)[which]) == tile | SHARED
+
+
+def test_query():
+    assert P.t5_gemm_fp8_kernel_path(0, 5, 5) == 0
+    assert P.t5_gemm_fp8_kernel_path(-1, 5, 5) == P.t5_gemm_fp8_kernel_path(5, 0, 5) == P.t5_gemm_fp8_kernel_path(5, 5, 5, torch.float16) == -1
+    assert P.lib().t5_gemm_fp8_kernel_path(None) == -1
