@@ -584,8 +584,7 @@ enum {
   T5_FP8_PATH_ROWS = 16,    /* no tiles: 16 rows of A and 16 of B a workgroup, or with these bits more of them */
   T5_FP8_PATH_ROWS_A32 = 32,
   T5_FP8_PATH_ROWS_A64 = 64,
-  T5_FP8_PATH_ROWS_B32 = 128,
-  T5_FP8_PATH_ROWS_B64 = 256
+  T5_FP8_PATH_ROWS_B32 = 128
 };
 int t5_gemm_fp8_kernel_path(const t5_gemm_fp8_cfg* cfg);
 int t5_gemm_fp8(const t5_gemm_fp8_cfg* cfg, const void* A, const uint8_t* a_scale, const void* B, const uint8_t* b_scale,

@@ -1222,7 +1222,7 @@ def t5_gemm_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, accu
 
 
 FP8_PATH_TILE64, FP8_PATH_TILE128, FP8_PATH_TILE256, FP8_PATH_SHARED, FP8_PATH_ROWS = 1, 2, 4, 8, 16
-FP8_PATH_ROWS_A32, FP8_PATH_ROWS_A64, FP8_PATH_ROWS_B32, FP8_PATH_ROWS_B64 = 32, 64, 128, 256
+FP8_PATH_ROWS_A32, FP8_PATH_ROWS_A64, FP8_PATH_ROWS_B32 = 32, 64, 128
 
 
 def t5_gemm_fp8_kernel_path(m, n, k, out_dtype=torch.bfloat16) -> int:

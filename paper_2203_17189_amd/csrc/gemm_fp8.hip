@@ -56,16 +56,30 @@ double round_cost(const TileCost& t, double fill, double nk) {
   return nk * (t.idle + t.busy * std::max(0.0, fill - t.from) / (1.0 - t.from)) + t.ends;
 }
 
-// Without tiles, mt * 16 rows of A a workgroup: what a compute unit takes in (37 bytes a ns; widening on top of it), or B's
-// bytes once and what comes again from L2 for each workgroup, and the launch.  Measured, us, bfloat16, and in tiles:
-//   16 x 2048 x 2048: 3.8, 6.5     16 x 2048 x 16384: 16.6, 22.9     16 x 16384 x 2048: 7.0, 9.4     16 x 8192 x 8192: 20.9, 20.4
+// Against few rows of A, B comes from memory (a model's weights pass through the caches between two calls): a k-tile then takes
+// longer than the same of operands that many tiles share, and of more than 16 parts of a tile the sum waits for each.  Fitted
+// to 1 .. 16 rows against 512 .. 131072 by 384 .. 16384.
+constexpr TileCost kFewRowsCost[2] = {{64, 1024, 0.76, 0.71, 0.25, 2.5}, {64, 1024, 0.94, 0.64, 0.2, 2.8}};  // bf16 C, float32 C
+
+// Without tiles, mt * 16 rows of A a workgroup.  Up to 16 rows: a compute unit takes in 18.2 bytes of B a ns, workgroup after
+// workgroup.  Measured, B from memory, us (no tiles, tiles of 64):
+//   M x N x K               bfloat16         float32                             bfloat16         float32
+//   1 x  9216 x 2048       9.6   14.3      10.3   16.8      1 x 50257 x  768   15.3   12.7      16.2   13.5
+//   1 x 16384 x 5120      19.9   32.2      20.4   38.6      1 x 50257 x 2048   27.8   23.3      28.9   26.5
+//   1 x 32128 x  768       9.4    8.6      10.0   10.5     16 x 50257 x 2048   30.1   24.6      32.0   29.0
+//   1 x 32128 x 2048      16.8   16.6      18.1   21.7      1 x 65536 x 2048   33.6   28.3      32.3   30.3
+//  16 x 32128 x 2048      18.1   17.6      19.6   22.8      1 x 131072 x 768   31.1   23.4      33.2   26.2
+//   1 x 32128 x 5120      36.0   38.2      37.3   49.2      1 x 131072 x 5120   136    119       142    135
+// More rows: what a compute unit takes in (37 bytes a ns; widening on top of it), or B's bytes once and what comes again from
+// L2 for each workgroup, and the launch.  Measured, us, bfloat16, and in tiles:
 //   32 x 2048 x 5120: 7.2, 12.6    64 x 2048 x 5120: 9.3, 12.9       189 x 128 x 2944: 4.4, 8.4       333 x 509 x 1001: 4.7, 5.8
 double rows_cost(const t5_gemm_fp8_cfg& c, int mt) {
   const int64_t rb = 16 * fp8_rows_of_b(c.M, c.N), ra = std::min(c.M, 16 * mt), k = c.K;
   const int64_t tm = ceil_div(c.M, 16 * mt), wgs = (c.N + rb - 1) / rb * tm;
-  const int64_t taken = rb + (c.M <= 16 ? ra : 16 * mt);  // rows behind a single token's are the same line
+  const int64_t taken = rb + 16 * mt;
   const bool f32 = c.c_dtype == T5_F32;
   const int64_t rounds = (wgs + 255) / 256;  // ends and beginnings of workgroups with many registers do not overlap
+  if (c.M <= 16) return 2.0 + (double)rounds * (0.5 + ((double)rb + c.M / 8.0) * (double)k / 18.2e3) * (f32 ? 1.0 : 0.95);
   const double unit = (double)(rounds * taken * k) / 37e3 * (f32 ? 1.1 : 1.0) + (mt > 1 ? (double)(rounds - 1) * (f32 ? 1.0 : 0.5) : 0.0);
   return 2.0 + std::max(unit, (double)(c.N * k + (c.N * (tm - 1) + wgs * ra) * k / 8) / 6e6);
 }
@@ -76,7 +90,9 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
   const int units = ceil_div(c.K, 512);
   const double nk = c.K / 128.0;
   double best = -1.0;
-  for (const TileCost& t : kTileCost[c.c_dtype == T5_F32]) {
+  for (const TileCost& many : kTileCost[c.c_dtype == T5_F32]) {
+    if (c.M <= 16 && best >= 0.0) break;  // larger tiles only where these would be too many
+    const TileCost& t = c.M <= 16 && many.tile == 64 ? kFewRowsCost[c.c_dtype == T5_F32] : many;
     const int B = t.tile, slots = t.at_once, tm = ceil_div(c.M, B), tn = ceil_div(c.N, B);
     if (B == 256 && (c.M < 256 || c.N < 256)) break;
     const int64_t tiles = (int64_t)tm * tn, rest = tiles % slots;
@@ -85,8 +101,8 @@ void plan(const t5_gemm_fp8_cfg& c, Fp8Gemm* g) {
     const double alone = full + (rest ? round_cost(t, fill, nk) : 0.0);
     const int64_t workers = std::min<int64_t>(slots, rest * units);
     const double run = (double)workers / slots;
-    const double shared = full + round_cost(t, run, nk * rest / std::max<int64_t>(workers, 1)) + 6.0 +
-                          (double)(workers + rest) * B * B * 8 / 3.5e6;
+    double shared = full + round_cost(t, run, nk * rest / std::max<int64_t>(workers, 1)) + 6.0 + (double)(workers + rest) * B * B * 8 / 3.5e6;
+    if (c.M <= 16 && rest > 0) shared += 0.25 * std::max(0.0, (double)workers / (double)rest - 16.0);
     const bool share = rest > 0 && workers > rest && shared < alone;
     const double cost = share ? shared : alone;
     if (best >= 0.0 && cost >= best) continue;
@@ -123,7 +139,7 @@ int gemm_fp8_path(const t5_gemm_fp8_cfg& c) {
   if (g.few) {
     const int nt = fp8_rows_of_b(c.M, c.N);
     return T5_FP8_PATH_ROWS | (g.few == 2 ? T5_FP8_PATH_ROWS_A32 : g.few == 4 ? T5_FP8_PATH_ROWS_A64 : 0) |
-           (nt == 2 ? T5_FP8_PATH_ROWS_B32 : nt == 4 ? T5_FP8_PATH_ROWS_B64 : 0);
+           (nt == 2 ? T5_FP8_PATH_ROWS_B32 : 0);
   }
   return (g.tile == 64 ? T5_FP8_PATH_TILE64 : g.tile == 128 ? T5_FP8_PATH_TILE128 : T5_FP8_PATH_TILE256) |
          (g.workers > g.shared ? T5_FP8_PATH_SHARED : 0);

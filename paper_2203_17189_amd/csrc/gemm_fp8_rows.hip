@@ -146,8 +146,7 @@ hipError_t launch(const Fp8Gemm& g, hipStream_t st) {
   const dim3 grid((unsigned)ceil_div(g.N, 16 * nt), (unsigned)ceil_div(g.M, 16 * g.few));
   // Sixteen wavefronts where each still has several blocks (1 x 2048 x 16384: with eight 15.6 us, 12.0).
   if (g.few == 1) {
-    if (nt == 4) gemm_fp8_rows_kernel<TA, TB, F32, 1, 4, 8, 2><<<grid, 512, 0, st>>>(g);
-    else if (nt == 2) gemm_fp8_rows_kernel<TA, TB, F32, 1, 2, 8, 2><<<grid, 512, 0, st>>>(g);
+    if (nt == 2) gemm_fp8_rows_kernel<TA, TB, F32, 1, 2, 8, 2><<<grid, 512, 0, st>>>(g);
     else if (g.K > 4096) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 16, 4><<<grid, 1024, 0, st>>>(g);
     else if (g.K > 1024) gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 8, 4><<<grid, 512, 0, st>>>(g);
     else gemm_fp8_rows_kernel<TA, TB, F32, 1, 1, 4, 2><<<grid, 256, 0, st>>>(g);
@@ -163,11 +162,11 @@ hipError_t launch(const Fp8Gemm& g, hipStream_t st) { return g.out_bf16 ? launch
 
 }  // namespace
 
-// As many as leave two workgroups to a compute unit, as each reads A anew (16 rows of A, 32128 x 2048: with one 18.2 us, like
-// this 15.1; 16384 x 2048: 8.9, 7.0).  More rows of A leave the registers for one (32 x 2048 x 2048: with two 5.4 us, 4.5).
+// Two where that leaves two workgroups to a compute unit, as each reads A anew (one row of A, float32, B from memory: 32128 x
+// 2048 with one 21.5 us, with two 18.1, with four 20.2; 16384 x 5120 27.3, 20.4, 23.2; 50257 x 768 14.6, 16.2, 20.7).  More rows of A leave the registers for one (32 x 2048 x 2048: with two 5.4 us, 4.5).
 int fp8_rows_of_b(int M, int N) {
   const int n16 = ceil_div(N, 16);
-  return M > 16 ? 1 : n16 >= 2048 ? 4 : n16 >= 1024 ? 2 : 1;
+  return M > 16 ? 1 : n16 >= 1024 ? 2 : 1;
 }
 
 hipError_t launch_gemm_fp8_rows(const Fp8Gemm& g, int ta, int tb, hipStream_t st) {
