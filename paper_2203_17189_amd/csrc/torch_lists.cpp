@@ -132,6 +132,15 @@ bool operand_of(const at::Tensor& q, const at::Tensor& s, Operand* o) {
   o->block_rows = o->s.n == o->q.n ? 1 : 128;
   return o->s.cols == (o->q.cols + 127) / 128 && (o->s.n == o->q.n || o->s.n == squares);
 }
+// A flag; an object that is neither true nor false (a tensor of several elements, say) leaves its error in *wrong.
+bool flag(PyObject* o, bool* wrong) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) {
+    PyErr_Clear();
+    *wrong = true;
+  }
+  return v == 1;
+}
 bool fits32(int64_t v) { return v <= INT32_MAX; }
 
 // quantize_fp8(entry point, x, e5m2, block_rows, rows, transposed, stream, device) -> (q, scale, qt, scale_t), a status, or None
@@ -147,6 +156,9 @@ PyObject* quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
     PyErr_Clear();
     Py_RETURN_NONE;
   }
+  bool wrong = false;
+  const bool straight = flag(args[4], &wrong), turned = flag(args[5], &wrong);
+  if (wrong) Py_RETURN_NONE;
   const at::ScalarType type = e5m2 ? at::kFloat8_e5m2 : at::kFloat8_e4m3fn;
   at::Tensor out[4];
   auto make = [&](int64_t n, int64_t cols, at::Tensor* q, at::Tensor* s) {
@@ -154,7 +166,6 @@ PyObject* quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
     *q = at::empty({n, ld}, x->options().dtype(type));
     *s = at::empty({(n + block_rows - 1) / block_rows, lds}, x->options().dtype(at::kFloat8_e8m0fnu));
   };
-  const bool straight = PyObject_IsTrue(args[4]) == 1, turned = PyObject_IsTrue(args[5]) == 1;
   if (straight) make(r.n, r.cols, &out[0], &out[1]);
   if (turned) make(r.cols, r.n, &out[2], &out[3]);
   const t5_quantize_cfg cfg = {r.n, r.cols, r.ld, x->scalar_type() == at::kFloat ? T5_F32 : T5_BF16, e5m2 ? T5_E5M2 : T5_E4M3, (int32_t)block_rows};
@@ -185,8 +196,9 @@ PyObject* gemm_fp8(PyObject*, PyObject* const* args, Py_ssize_t count) {
   Operand a, b;
   if (!operand_of(*t[0], *t[1], &a) || !operand_of(*t[2], *t[3], &b) || a.q.cols != b.q.cols || !fits32(a.q.n) || !fits32(b.q.n) || !fits32(a.q.cols))
     Py_RETURN_NONE;
-  bool f32 = PyObject_IsTrue(args[7]) == 1;
-  const bool add = PyObject_IsTrue(args[8]) == 1;
+  bool wrong = false, f32 = flag(args[7], &wrong);
+  const bool add = flag(args[8], &wrong);
+  if (wrong) Py_RETURN_NONE;
   at::Tensor out;
   Rows c = {a.q.n, b.q.n, b.q.n};
   if (args[6] == Py_None) {

@@ -49,6 +49,17 @@ for place, f in places.items():
             print(type(r).__name__ if not isinstance(r, int) else r, len(calls), flush=True)
         except Exception as e:
             print(type(e).__name__, len(calls), flush=True)
+unclear = torch.zeros(2, dtype=torch.bool)  # neither true nor false
+flags = {"rows": lambda: L.quantize_fp8(at(quant), x, 0, 1, unclear, True, 0, -1), "transposed": lambda: L.quantize_fp8(at(quant), x, 0, 1, True, unclear, 0, -1),
+         "block_rows": lambda: L.quantize_fp8(at(quant), x, 0, 1.5, True, True, 0, -1), "float32": lambda: L.gemm_fp8(at(gemm), at(size), codes, scales, codes, scales, None, unclear, False, 0, -1),
+         "accumulate": lambda: L.gemm_fp8(at(gemm), at(size), codes, scales, codes, scales, torch.zeros(4, 4), True, unclear, 0, -1)}
+for name, f in flags.items():
+    print("flag", name, end=" ", flush=True)
+    calls.clear()
+    try:
+        print(type(f()).__name__, len(calls), flush=True)
+    except Exception as e:
+        print(type(e).__name__, len(calls), flush=True)
 """
 
 
@@ -69,12 +80,17 @@ def module(tmp_path_factory):
     return tmp, out
 
 
-@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
-def test_no_argument_ends_the_process(module):
+@pytest.fixture(scope="module")
+def answers(module):
     r = subprocess.run([sys.executable, str(module[0] / "program.py"), str(module[1])], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, (r.returncode, r.stdout.splitlines()[-1:], r.stderr[-2000:])  # (its last line names the call)
-    got = {tuple(line.split()[:2]): line.split()[2:] for line in r.stdout.splitlines()}
-    assert len(got) == 8 * 16
+    return {tuple(line.split()[:2]): line.split()[2:] for line in r.stdout.splitlines()}
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_no_argument_ends_the_process(answers):
+    got = answers
+    assert len(got) == 8 * 16 + 5
     assert got["quantize", "strided"] == ["tuple", "1"] and got["out", "none"] == ["Tensor", "1"]
     assert got["param", "strided"] == got["grad", "strided"] == ["1", "0"]  # entries read
     # what has no strides, or has the wrong ones, is left to the checks of the binding: no entry point was called for it
@@ -84,3 +100,9 @@ def test_no_argument_ends_the_process(module):
             assert got[place, name] == ["NoneType", "0"] or (place, name) == ("out", "none"), (place, name, got[place, name])
         for place in ("param", "grad"):
             assert got[place, name] == ["0", "0"], (place, name, got[place, name])
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_flags_that_are_neither_true_nor_false_call_nothing(answers):
+    for name in ("rows", "transposed", "block_rows", "float32", "accumulate"):
+        assert answers["flag", name] == ["NoneType", "0"], (name, answers["flag", name])
