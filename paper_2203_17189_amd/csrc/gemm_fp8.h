@@ -59,7 +59,7 @@ hipError_t launch_gemm_fp8_44(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_45(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_54(const Fp8Gemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_55(const Fp8Gemm& g, hipStream_t st);
-// Without tiles, M <= 64 (gemm_fp8_rows.hip), and how many times 16 rows of B a workgroup has there.
+// Without tiles (gemm_fp8_rows.hip): few rows of A, or a small product.  How many times 16 rows of B a workgroup has there.
 int fp8_rows_of_b(int M, int N);
 hipError_t launch_gemm_fp8_rows(const Fp8Gemm& g, int ta, int tb, hipStream_t st);
 

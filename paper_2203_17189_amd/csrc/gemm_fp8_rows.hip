@@ -1,7 +1,7 @@
 // Product of a few quantised rows (single tokens, short batches) with a quantised matrix, and small products.
 //
-// Bound by reading B once.  A workgroup has 16 rows of B (and 16 to 64 of A); its wavefronts take the blocks of 128 k in turn, straight from
-// memory into the operands of a matrix instruction: no LDS, no barrier before the end, and the loads of IN blocks of a
+// Bound by reading B once.  A workgroup has 16 rows of B, or 32, and 16 to 64 of A (16 to 64 by 16, or 16 by 32); its
+// wavefronts take the blocks of 128 k in turn, straight from memory into the operands of a matrix instruction: no LDS, no barrier before the end, and the loads of IN blocks of a
 // wavefront are under way at once.  The wavefronts' sums meet in LDS, in order.  A is read again by each workgroup, from L2.
 // The instructions are the ones of gemm_fp8.h, 16 x 16 wide: codes with scales for bfloat16 C, widened codes for float32.
 #include "gemm_fp8.h"
