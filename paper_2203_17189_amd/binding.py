@@ -1228,7 +1228,7 @@ FP8_PATH_ROWS_A32, FP8_PATH_ROWS_A64, FP8_PATH_ROWS_B32 = 32, 64, 128
 def t5_gemm_fp8_kernel_path(m, n, k, out_dtype=torch.bfloat16) -> int:
     """Bit mask of the kernel that a product of [m, k] and [n, k] runs on (host-side query; -1: invalid sizes or type)."""
     ld, lds, ty = -(-k // 16) * 16, -(-k // 512) * 4, {torch.bfloat16: T5_BF16, torch.float32: T5_F32}.get(out_dtype, -1)
-    return int(lib().t5_gemm_fp8_kernel_path(C.byref(_GemmFp8Cfg(m, n, k, ld, ld, n, lds, lds, T5_E4M3, T5_E4M3, 1, 1, ty, 0))))
+    return int(lib().t5_gemm_fp8_kernel_path(C.byref(_GemmFp8Cfg(_i32(m), _i32(n), _i32(k), ld, ld, n, lds, lds, T5_E4M3, T5_E4M3, 1, 1, ty, 0))))
 
 
 def _adam_check(t, index):

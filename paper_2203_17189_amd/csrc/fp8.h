@@ -8,8 +8,9 @@ namespace t5mi {
 constexpr int kBlock = 128;
 
 // Whether the quantiser reads its matrix in whole pieces of 16 bytes, and whether it reads the eight elements from column c
-// (a multiple of 8) of a row as such: those past the row's end too (and drops them) where another row follows.  Rows of four float32 would take in the
-// next row with it, and of a last one more than its columns; longer ones end at most four elements into a row of more.
+// (a multiple of 8) of a row as such: those past the row's end too (and drops them) where another row follows.  Rows of four
+// float32 would take in the next row with it, and of a last one more than its columns; longer ones end at most four elements
+// into a row of more.
 inline bool quant_in_pieces(const void* x, int64_t ld, int size) {
   return ((uintptr_t)x & 15) == 0 && ld * size % 16 == 0 && ld >= 8;
 }

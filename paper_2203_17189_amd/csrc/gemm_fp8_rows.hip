@@ -1,8 +1,8 @@
 // Product of a few quantised rows (single tokens, short batches) with a quantised matrix, and small products.
 //
 // Bound by reading B once.  A workgroup has 16 rows of B, or 32, and 16 to 64 of A (16 to 64 by 16, or 16 by 32); its
-// wavefronts take the blocks of 128 k in turn, straight from memory into the operands of a matrix instruction: no LDS, no barrier before the end, and the loads of IN blocks of a
-// wavefront are under way at once.  The wavefronts' sums meet in LDS, in order.  A is read again by each workgroup, from L2.
+// wavefronts take the blocks of 128 k in turn, straight from memory into the operands of a matrix instruction: no LDS, no
+// barrier before the end, and the loads of IN blocks of a wavefront are under way at once.  The wavefronts' sums meet in LDS, in order.  A is read again by each workgroup, from L2.
 // The instructions are the ones of gemm_fp8.h, 16 x 16 wide: codes with scales for bfloat16 C, widened codes for float32.
 #include "gemm_fp8.h"
 
@@ -163,7 +163,8 @@ hipError_t launch(const Fp8Gemm& g, hipStream_t st) { return g.out_bf16 ? launch
 }  // namespace
 
 // Two where that leaves two workgroups to a compute unit, as each reads A anew (one row of A, float32, B from memory: 32128 x
-// 2048 with one 21.5 us, with two 18.1, with four 20.2; 16384 x 5120 27.3, 20.4, 23.2; 50257 x 768 14.6, 16.2, 20.7).  More rows of A leave the registers for one (32 x 2048 x 2048: with two 5.4 us, 4.5).
+// 2048 with one 21.5 us, with two 18.1, with four 20.2; 16384 x 5120 27.3, 20.4, 23.2; 50257 x 768 14.6, 16.2, 20.7).
+// More rows of A leave the registers for one (32 x 2048 x 2048: with two 5.4 us, 4.5).
 int fp8_rows_of_b(int M, int N) {
   const int n16 = ceil_div(N, 16);
   return M > 16 ? 1 : n16 >= 1024 ? 2 : 1;

@@ -31,3 +31,5 @@ def test_query():
     assert P.t5_gemm_fp8_kernel_path(0, 5, 5) == 0
     assert P.t5_gemm_fp8_kernel_path(-1, 5, 5) == P.t5_gemm_fp8_kernel_path(5, 0, 5) == P.t5_gemm_fp8_kernel_path(5, 5, 5, torch.float16) == -1
     assert P.lib().t5_gemm_fp8_kernel_path(None) == -1
+    for sizes in (((1 << 32) + 1, 5, 5), (5, (1 << 32) + 5, 5), (5, 5, (1 << 32) + 5)):  # what 32 bits would cut off
+        assert P.t5_gemm_fp8_kernel_path(*sizes) == -1
